@@ -49,7 +49,8 @@ def listed():
 
 
 def _log_int(rng, lo, hi):
-    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    n = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    return n + (n == 3072)
 
 
 def draw(rng):
