@@ -95,6 +95,12 @@ typedef enum {
   CEP_GEMM_TCGEN05_1CTA = 2    /* tcgen05 with one CTA per 128x256 tile (comparison variant)    */
 } cep_gemm_impl;
 
+/* Element type of a plain (unquantised) tensor. */
+typedef enum {
+  CEP_ELEM_BF16 = 0,
+  CEP_ELEM_FP32 = 1
+} cep_elem;
+
 #define CEP_MAX_CHUNKS_PER_INVOCATION 32   /* a batch is launched early when it holds this many */
 #define CEP_ROW_ALIGN 128                  /* expert groups start on multiples of the GEMM tile */
 
@@ -220,6 +226,39 @@ CEP_API int ffn_set_addend(cep_plan* plan, const void* addend);
  */
 CEP_API int moe_route(const float* logits, int32_t n_tokens, int32_t n_experts_global, int32_t top_k,
                       int32_t* topk_ids, float* topk_weights, void* stream);
+
+/* Types, sizes and row strides (in elements) of moe_norm. */
+typedef struct {
+  int32_t n_tokens;            /* T >= 0; 0 does nothing                                        */
+  int32_t hidden;              /* H, 1..32768; any value (see below for the fast ones)          */
+  int32_t dtype;               /* cep_dtype of codes / scales; CEP_BF16: neither is written     */
+  int32_t x_elem;              /* cep_elem of x                                                 */
+  int32_t residual_elem;       /* cep_elem of residual and residual_out                         */
+  int32_t weight_elem;         /* cep_elem of weight                                            */
+  int64_t x_stride, residual_stride, residual_out_stride, y_stride;   /* >= hidden              */
+  float eps;                   /* finite, >= 0                                                  */
+} cep_norm_desc;
+
+/*
+ * The step in front of the layer: adds the residual stream, takes the root-mean-square norm and writes the
+ * activations in the format a plan of `dtype` takes.  Needs no plan.  Per row, in fp32 with one rounding per output:
+ *   h = x + residual;   y = h / sqrt(mean(h*h) + eps) * weight
+ *   x             [device] [T, H]
+ *   residual      [device] [T, H] or NULL (h = x)
+ *   weight        [device] [H] or NULL (all ones)
+ *   residual_out  [device] out [T, H], h rounded to residual_elem, or NULL; may be `residual` itself
+ *   y             [device] out bf16 [T, H] or NULL (for the router and the shared expert); may be x itself
+ *   codes         [device] out e4m3 [T, H] dense         (CEP_FP8_E4M3_BLOCK128, CEP_MXFP4_E4M3; else NULL)
+ *   scales        [device] out fp32 [T, ceil(H/128)], the block's largest magnitude / 448, 1 for a block of zeros
+ *                 (CEP_FP8_E4M3_BLOCK128); or uint8 ue8m0 [T, ceil(H/32)], the smallest power of two that brings the
+ *                 block's largest magnitude to <= 448 (CEP_MXFP4_E4M3).  The last block of a row may be short.
+ * codes are taken from the unrounded y.  A row that holds a NaN or an infinity comes out as NaN (infinite h) or all
+ * NaN codes; a sum of squares beyond the fp32 range counts as infinite.  Other than the two exact aliases named above,
+ * outputs may not overlap inputs.  Rows that all start on 16-byte boundaries with H a multiple of 8 take the wide path.
+ * Enqueued on `stream`.
+ */
+CEP_API int moe_norm(const cep_norm_desc* desc, const void* x, const void* residual, const void* weight,
+                     void* residual_out, void* y, void* codes, void* scales, void* stream);
 
 /*
  * A replica's routed tokens have arrived (Section 3.2: per-replica completion signal).

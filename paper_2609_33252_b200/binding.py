@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(HERE, "libcascade_ffn.so")
 
 CEP_BF16, CEP_FP8_E4M3_BLOCK128, CEP_MXFP4_E4M3 = 0, 1, 2
 DTYPE_OF = {"bf16": CEP_BF16, "fp8": CEP_FP8_E4M3_BLOCK128, "mxfp4": CEP_MXFP4_E4M3}   # workload dtype names
+CEP_ELEM_BF16, CEP_ELEM_FP32 = 0, 1
 CEP_MODE_SYNC, CEP_MODE_ASYNC, CEP_MODE_STREAMFFN = 0, 1, 2
 CEP_GEMM_TCGEN05, CEP_GEMM_SIMT, CEP_GEMM_TCGEN05_1CTA = 0, 1, 2
 STATUS_NAMES = {0: "CEP_OK", -1: "CEP_ERR_ARG", -2: "CEP_ERR_STATE", -3: "CEP_ERR_WORKSPACE",
@@ -25,7 +26,7 @@ EXPORTS = ["moe_plan_workspace_bytes", "moe_packed_weight_bytes", "moe_plan", "m
            "ffn_begin", "ffn_submit_chunk", "ffn_flush", "combine", "ffn_status", "ffn_num_invocations",
            "ffn_query", "ffn_debug_export", "cep_kernel_launches", "moe_plan_destroy", "cep_last_error",
            "cep_debug_decode_tile", "cep_debug_schedule", "layout_indices_noalloc", "cep_debug_wait_timeout", "ffn_set_addend", "moe_route", "cep_debug_check_guards", "ffn_wait_invocation",
-           "ffn_set_active_streams", "cep_calibrate", "ffn_query_call", "cep_calibrate_routed"]
+           "ffn_set_active_streams", "cep_calibrate", "ffn_query_call", "cep_calibrate_routed", "moe_norm"]
 
 
 class CepConfig(ctypes.Structure):
@@ -36,6 +37,13 @@ class CepConfig(ctypes.Structure):
                 ("threshold_pairs", ctypes.c_int64), ("gemm_impl", ctypes.c_int32),
                 ("debug_checks", ctypes.c_int32), ("profile_kernels", ctypes.c_int32),
                 ("defer_while_busy", ctypes.c_int32), ("gather_a", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("hidden", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("x_elem", ctypes.c_int32), ("residual_elem", ctypes.c_int32), ("weight_elem", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+                ("residual_out_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("eps", ctypes.c_float)]
 
 
 class InvocationInfo(ctypes.Structure):
@@ -113,6 +121,7 @@ def load_library(build_if_missing: bool = True):
                                          ctypes.POINTER(ProfilePoint), ctypes.POINTER(Calibration)]),
         "cep_calibrate_routed": (ctypes.c_int, [vp, ctypes.c_float, vp, i32, i32, vp, vp, vp, vp, vp,
                                                 ctypes.POINTER(ProfilePoint), ctypes.POINTER(Calibration)]),
+        "moe_norm": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "layout_indices_noalloc": (ctypes.c_int, [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -183,6 +192,47 @@ def moe_route(logits, top_k: int, topk_ids, topk_weights, stream=None):
     n_tokens, n_experts_global = logits.shape
     _check(lib().moe_route(logits.data_ptr(), n_tokens, n_experts_global, top_k, topk_ids.data_ptr(),
                            topk_weights.data_ptr(), _stream_handle(stream)))
+
+
+def _rows(t, name, n_tokens, hidden, dtypes):
+    """Row stride of a [T,H] CUDA tensor whose rows are contiguous; raises for anything the call cannot take."""
+    if t.dtype not in dtypes:
+        raise CepError(-1, "%s has dtype %s" % (name, t.dtype))
+    if t.dim() != 2 or t.shape[0] != n_tokens or t.shape[1] != hidden or (hidden > 1 and t.stride(1) != 1) or not t.is_cuda:
+        raise CepError(-1, "%s must be a [%d, %d] CUDA tensor with contiguous rows" % (name, n_tokens, hidden))
+    return t.stride(0) if n_tokens > 1 else hidden
+
+
+def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None, y=None, codes=None, scales=None,
+             dtype: int = CEP_BF16, stream=None):
+    """Residual addition, root-mean-square norm and the expert layer's activation format in one pass (see the header).
+
+    x [T,H] bf16 or fp32; residual / residual_out [T,H] bf16 or fp32 (one type); weight [H] bf16 or fp32; y bf16 [T,H];
+    codes float8_e4m3fn [T,H] and scales fp32 [T,ceil(H/128)] (CEP_FP8_E4M3_BLOCK128) or uint8 [T,ceil(H/32)]
+    (CEP_MXFP4_E4M3).  Rows of x, residual, residual_out and y may be strided."""
+    import torch
+    f32, plain = torch.float32, (torch.bfloat16, torch.float32)
+    T, H = x.shape
+    xs = _rows(x, "x", T, H, plain)
+    rs = os_ = ys = H
+    if residual is not None:
+        rs = _rows(residual, "residual", T, H, plain)
+    if residual_out is not None:
+        os_ = _rows(residual_out, "residual_out", T, H, plain if residual is None else (residual.dtype,))
+    if y is not None:
+        ys = _rows(y, "y", T, H, (torch.bfloat16,))
+    if weight is not None and (weight.dtype not in plain or weight.shape != (H,) or not weight.is_contiguous() or not weight.is_cuda):
+        raise CepError(-1, "weight must be a contiguous CUDA tensor of [%d] bf16 or fp32" % H)
+    if codes is not None and (codes.dtype not in (torch.float8_e4m3fn, torch.uint8) or codes.shape != (T, H) or not codes.is_contiguous()):
+        raise CepError(-1, "codes must be a contiguous [%d, %d] float8_e4m3fn tensor" % (T, H))
+    if scales is not None:
+        block, want = (32, torch.uint8) if dtype == CEP_MXFP4_E4M3 else (128, f32)
+        if scales.dtype != want or scales.shape != (T, (H + block - 1) // block) or not scales.is_contiguous():
+            raise CepError(-1, "scales must be a contiguous [%d, %d] %s tensor" % (T, (H + block - 1) // block, want))
+    desc = NormDesc(T, H, dtype, x.dtype == f32, residual is not None and residual.dtype == f32,
+                    weight is not None and weight.dtype == f32, xs, rs, os_, ys, eps)
+    _check(lib().moe_norm(ctypes.byref(desc), x.data_ptr(), _dptr(residual), _dptr(weight), _dptr(residual_out), _dptr(y),
+                          _dptr(codes), _dptr(scales), _stream_handle(stream)))
 
 
 def ffn_submit_chunk(plan, chunk_id: int, token_offset: int, n_tokens: int, tokens, token_scales, topk_ids,

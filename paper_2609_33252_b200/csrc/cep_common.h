@@ -21,6 +21,11 @@ __host__ __device__ inline size_t sf_atom_offset(long long row, int kb32, int k1
 }
 __host__ __device__ inline bool dtype_is_bytes(int dtype) { return dtype != CEP_BF16; }   // one-byte activation codes
 
+constexpr int kNormMaxHidden = 32768;           // moe_norm keeps a row in registers or shared memory
+
+// Sets the calling thread's plan-less error string (cep_last_error(NULL)) and returns `code`.
+int record_error(int code, const char* fmt, ...);
+
 // Device status word layout (int32 each).
 enum StatusWord { kStBadRouting = 0, kStTimeout = 1, kStBoundsViolation = 2, kStDetail = 3, kStWords = 8 };
 

@@ -316,6 +316,11 @@ int launch_invocation(cep_plan* p) {
 
 }  // namespace
 
+int cep::record_error(int code, const char* fmt, ...) {
+  va_list ap; va_start(ap, fmt); vsnprintf(g_error, sizeof g_error, fmt, ap); va_end(ap);
+  return code;
+}
+
 extern "C" {
 
 const char* cep_last_error(const cep_plan* plan) { return plan ? plan->err : g_error; }
