@@ -261,6 +261,58 @@ CEP_API int moe_norm(const cep_norm_desc* desc, const void* x, const void* resid
                      void* residual_out, void* y, void* codes, void* scales, void* stream);
 
 /*
+ * A projection shared by all requests of a batch with one low-rank adapter per request beside it:
+ *   y[t] = W x[t] + scale_a * B_a (A_a x[t]),   a = adapter_ids[t];   -1: no adapter, y[t] = W x[t]
+ * bf16 operands, fp32 accumulation; A_a x[t] is carried in fp32 and enters the accumulator of W x[t] as two bf16 terms
+ * (2^-17 relative), so y is rounded once.  Without adapters and with CEP_ELEM_FP32 it is the router's logits (moe_route).
+ */
+typedef struct cep_lora_plan cep_lora_plan;
+
+typedef struct {
+  int32_t in_features;         /* K; multiple of 8                                              */
+  int32_t out_features;        /* N >= 1                                                        */
+  int32_t max_tokens;          /* upper bound on tokens per call                                */
+  int32_t max_adapters;        /* slots of the adapter bank, 0..4096; 0: no adapters            */
+  int32_t max_rank;            /* largest rank, 1..256; 0 without adapters                      */
+  int32_t out_elem;            /* cep_elem of y                                                 */
+} cep_lora_config;
+
+/* Bytes of device workspace, and of the bank that holds the packed adapters (0 without adapters).  [host] out. */
+CEP_API int lora_plan_workspace_bytes(const cep_lora_config* cfg, size_t* bytes);
+CEP_API int lora_bank_bytes(const cep_lora_config* cfg, size_t* bytes);
+
+/*
+ * `weight` [device] bf16 [N, K], rows weight_stride elements apart (a multiple of 8), 16-byte aligned; `bank` and
+ * `workspace` [device], 256-byte aligned.  All three stay owned by the caller and must outlive the plan.  Must be called
+ * with the target device current; clears the counters and the bank's slots on `stream`.  A plan is not thread-safe.  Its
+ * calls may go to different streams: each waits for the plan's previous work (inside a stream capture the caller orders).
+ */
+CEP_API int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_stride, void* bank, size_t bank_bytes,
+                      void* workspace, size_t workspace_bytes, void* stream, cep_lora_plan** out);
+
+/*
+ * Puts an adapter into a slot (replacing what was there; rank 0 empties it): down = A [device] bf16 [rank, K], up = B
+ * [device] bf16 [N, rank], rows down_stride / up_stride elements apart.  Copied on `stream`; both may be freed once that
+ * stream has completed.  Errors: CEP_ERR_CAPACITY for a slot or rank beyond the plan's.
+ */
+CEP_API int lora_load_adapter(cep_lora_plan* plan, int32_t slot, int32_t rank, float scale, const void* down,
+                              int64_t down_stride, const void* up, int64_t up_stride, void* stream);
+
+/*
+ *   x            [device] bf16 [T, K], rows x_stride elements apart (a multiple of 8), 16-byte aligned
+ *   adapter_ids  [device] int32 [T] slot of each token in any order, -1 for none; NULL: no token has an adapter
+ *   y            [device] out [T, N] of out_elem, rows y_stride elements apart; may not overlap x
+ * An id that names no loaded adapter counts as -1 and is reported by lora_status.  Enqueued on `stream`.
+ */
+CEP_API int lora_project(cep_lora_plan* plan, const void* x, int64_t x_stride, int32_t n_tokens, const int32_t* adapter_ids,
+                         void* y, int64_t y_stride, void* stream);
+
+/* Waits for the plan's work and returns what its kernels reported since the last call of this function: CEP_OK,
+ * CEP_ERR_BAD_ROUTING (an id without a loaded adapter) or CEP_ERR_DEVICE_TIMEOUT.  Off the hot path. */
+CEP_API int lora_status(cep_lora_plan* plan);
+CEP_API int lora_plan_destroy(cep_lora_plan* plan);
+
+/*
  * A replica's routed tokens have arrived (Section 3.2: per-replica completion signal).
  *   chunk_id       0..n_chunks_expected-1, each exactly once, any order
  *   token_offset   first token (row of `out`) this chunk covers

@@ -26,7 +26,9 @@ EXPORTS = ["moe_plan_workspace_bytes", "moe_packed_weight_bytes", "moe_plan", "m
            "ffn_begin", "ffn_submit_chunk", "ffn_flush", "combine", "ffn_status", "ffn_num_invocations",
            "ffn_query", "ffn_debug_export", "cep_kernel_launches", "moe_plan_destroy", "cep_last_error",
            "cep_debug_decode_tile", "cep_debug_schedule", "layout_indices_noalloc", "cep_debug_wait_timeout", "ffn_set_addend", "moe_route", "cep_debug_check_guards", "ffn_wait_invocation",
-           "ffn_set_active_streams", "cep_calibrate", "ffn_query_call", "cep_calibrate_routed", "moe_norm"]
+           "ffn_set_active_streams", "cep_calibrate", "ffn_query_call", "cep_calibrate_routed", "moe_norm",
+           "lora_plan_workspace_bytes", "lora_bank_bytes", "lora_plan", "lora_load_adapter", "lora_project", "lora_status",
+           "lora_plan_destroy"]
 
 
 class CepConfig(ctypes.Structure):
@@ -44,6 +46,11 @@ class NormDesc(ctypes.Structure):
                 ("x_elem", ctypes.c_int32), ("residual_elem", ctypes.c_int32), ("weight_elem", ctypes.c_int32),
                 ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
                 ("residual_out_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("eps", ctypes.c_float)]
+
+
+class LoraConfig(ctypes.Structure):
+    _fields_ = [("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+                ("max_adapters", ctypes.c_int32), ("max_rank", ctypes.c_int32), ("out_elem", ctypes.c_int32)]
 
 
 class InvocationInfo(ctypes.Structure):
@@ -122,6 +129,13 @@ def load_library(build_if_missing: bool = True):
         "cep_calibrate_routed": (ctypes.c_int, [vp, ctypes.c_float, vp, i32, i32, vp, vp, vp, vp, vp,
                                                 ctypes.POINTER(ProfilePoint), ctypes.POINTER(Calibration)]),
         "moe_norm": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "lora_plan_workspace_bytes": (ctypes.c_int, [vp, ctypes.POINTER(sz)]),
+        "lora_bank_bytes": (ctypes.c_int, [vp, ctypes.POINTER(sz)]),
+        "lora_plan": (ctypes.c_int, [vp, vp, i64, vp, sz, vp, sz, vp, ctypes.POINTER(vp)]),
+        "lora_load_adapter": (ctypes.c_int, [vp, i32, i32, ctypes.c_float, vp, i64, vp, i64, vp]),
+        "lora_project": (ctypes.c_int, [vp, vp, i64, i32, vp, vp, i64, vp]),
+        "lora_status": (ctypes.c_int, [vp]),
+        "lora_plan_destroy": (ctypes.c_int, [vp]),
         "layout_indices_noalloc": (ctypes.c_int, [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -233,6 +247,45 @@ def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None
                     weight is not None and weight.dtype == f32, xs, rs, os_, ys, eps)
     _check(lib().moe_norm(ctypes.byref(desc), x.data_ptr(), _dptr(residual), _dptr(weight), _dptr(residual_out), _dptr(y),
                           _dptr(codes), _dptr(scales), _stream_handle(stream)))
+
+
+def lora_plan_workspace_bytes(cfg: LoraConfig) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().lora_plan_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def lora_bank_bytes(cfg: LoraConfig) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().lora_bank_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def lora_plan(cfg: LoraConfig, weight, bank, workspace, stream=None) -> int:
+    """weight: bf16 [N,K] CUDA tensor; bank, workspace: torch uint8 CUDA tensors.  Returns the plan handle."""
+    h = ctypes.c_void_p()
+    _check(lib().lora_plan(ctypes.byref(cfg), weight.data_ptr(), weight.stride(0) if weight.shape[0] > 1 else weight.shape[1], _dptr(bank), 0 if bank is None else bank.numel(),
+                           workspace.data_ptr(), workspace.numel(), _stream_handle(stream), ctypes.byref(h)))
+    return h.value
+
+
+def lora_load_adapter(plan, slot: int, rank: int, scale: float, down, up, stream=None):
+    _check(lib().lora_load_adapter(plan, slot, rank, scale, _dptr(down), 0 if down is None else down.stride(0), _dptr(up),
+                                   0 if up is None else up.stride(0), _stream_handle(stream)))
+
+
+def lora_project(plan, x, adapter_ids, y, stream=None):
+    T = x.shape[0]                                        # (the stride of a single row means nothing)
+    _check(lib().lora_project(plan, x.data_ptr(), x.stride(0) if T > 1 else x.shape[1], T, _dptr(adapter_ids), y.data_ptr(),
+                              y.stride(0) if T > 1 else y.shape[1], _stream_handle(stream)))
+
+
+def lora_status(plan) -> int:
+    return lib().lora_status(plan)
+
+
+def lora_plan_destroy(plan):
+    _check(lib().lora_plan_destroy(plan))
 
 
 def ffn_submit_chunk(plan, chunk_id: int, token_offset: int, n_tokens: int, tokens, token_scales, topk_ids,
@@ -423,6 +476,72 @@ class MoELayer:
     def close(self):
         if getattr(self, "plan", None):
             moe_plan_destroy(self.plan)
+            self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class LoRAProjection:
+    """A projection shared by all requests with one low-rank adapter per request beside it: owns the torch-allocated
+    workspace and adapter bank of one plan, and keeps the weight alive.
+
+    weight bf16 [N,K] (the layout of a linear layer's weight), used in place.  ``load_adapter`` fills a slot; ``run``
+    takes the slot of every token.  max_adapters = 0 gives the plain projection (with out_elem=CEP_ELEM_FP32 the
+    router's logits).
+    """
+
+    def __init__(self, weight, max_tokens, max_adapters=0, max_rank=0, out_elem=CEP_ELEM_BF16, stream=None):
+        import torch
+        if not weight.is_cuda or weight.dtype != torch.bfloat16 or weight.dim() != 2 or weight.stride(1) != 1:
+            raise CepError(-1, "weight must be a bf16 CUDA tensor [out, in] with contiguous rows")
+        self.weight = weight
+        self.out_dtype = torch.float32 if out_elem == CEP_ELEM_FP32 else torch.bfloat16
+        self.cfg = LoraConfig(weight.shape[1], weight.shape[0], max_tokens, max_adapters, max_rank, out_elem)
+        self.workspace = torch.empty(lora_plan_workspace_bytes(self.cfg), dtype=torch.uint8, device=weight.device)
+        nb = lora_bank_bytes(self.cfg)
+        self.bank = torch.empty(nb, dtype=torch.uint8, device=weight.device) if nb else None
+        self.plan = lora_plan(self.cfg, weight, self.bank, self.workspace, stream)
+
+    def load_adapter(self, slot, down, up, scale=1.0, stream=None):
+        """down = A [rank, in], up = B [out, rank], bf16, rows may be strided; replaces what the slot held."""
+        import torch
+        rank = down.shape[0]
+        for t, name, shape in ((down, "down", (rank, self.cfg.in_features)), (up, "up", (self.cfg.out_features, rank))):
+            if t.dtype != torch.bfloat16 or not t.is_cuda or tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1):
+                raise CepError(-1, "%s must be a bf16 CUDA tensor [%d, %d] with contiguous rows" % ((name,) + shape))
+        lora_load_adapter(self.plan, slot, rank, scale, down, up, stream)
+
+    def drop_adapter(self, slot, stream=None):
+        """Empties a slot: its id then names no adapter."""
+        lora_load_adapter(self.plan, slot, 0, 0.0, None, None, stream)
+
+    def run(self, x, adapter_ids=None, out=None, stream=None):
+        """x bf16 [T,in], adapter_ids int32 [T] (-1: none) or None; returns out [T,out] (allocated if not given)."""
+        import torch
+        c = self.cfg
+        T = x.shape[0]
+        if x.dtype != torch.bfloat16 or not x.is_cuda or x.dim() != 2 or x.shape[1] != c.in_features or x.stride(1) != 1:
+            raise CepError(-1, "x must be a bf16 CUDA tensor [T, %d] with contiguous rows" % c.in_features)
+        if adapter_ids is not None and (adapter_ids.dtype != torch.int32 or adapter_ids.shape != (T,) or
+                                        not adapter_ids.is_contiguous() or not adapter_ids.is_cuda):
+            raise CepError(-1, "adapter_ids must be a contiguous int32 CUDA tensor [%d]" % T)
+        if out is None:
+            out = torch.empty((T, c.out_features), dtype=self.out_dtype, device=x.device)
+        elif out.dtype != self.out_dtype or out.shape != (T, c.out_features) or not out.is_cuda or (c.out_features > 1 and out.stride(1) != 1):
+            raise CepError(-1, "out must be a %s CUDA tensor [%d, %d] with contiguous rows" % (self.out_dtype, T, c.out_features))
+        lora_project(self.plan, x, adapter_ids, out, stream)
+        return out
+
+    def status(self) -> int:
+        return lora_status(self.plan)
+
+    def close(self):
+        if getattr(self, "plan", None):
+            lora_plan_destroy(self.plan)
             self.plan = None
 
     def __del__(self):

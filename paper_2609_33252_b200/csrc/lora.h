@@ -1,0 +1,65 @@
+// Internal interface of the projection with per-request low-rank adapters (lora.cu: plan and C ABI; lora_shrink.cu: the
+// down projection x A^T; lora_project.cu: the shared projection with the up projection inside its accumulator).
+#pragma once
+#include "cep_common.h"
+#include "gemm_tcgen05.h"
+
+namespace cep {
+
+constexpr int kLoraChunk = 16;               // ranks per K step of the up projection (one bf16 MMA)
+constexpr int kLoraMaxRank = 256;
+constexpr int kLoraMaxAdapters = 4096;
+constexpr int kShrinkRows = 64;              // tokens per block of the down projection
+constexpr int kSplitCtas = 148;              // a call's K-split blocks never exceed this (sizes the partial sums)
+constexpr int kSmallTok = 128;               // tokens per tile of the small kernel (fp32 outputs: 64)
+constexpr int kLargeTok = 256;               // tokens per tile of the large kernel
+
+// One adapter's place in the bank, read by the kernels.
+struct LoraBank {
+  const int32_t* rank;                       // [slots], 0: nothing loaded
+  const float* scale;                        // [slots]
+  const uint16_t* down;                      // bf16 [slots][rank_pad][K]; rows at or beyond the rank are not read
+  const uint16_t* up;                        // bf16 [slots][rank_pad/16][N][16]; ranks beyond the adapter's are zero
+  int slots, rank_pad;
+};
+
+// What the down projection leaves for the projection kernel.
+struct LoraStep {
+  const int32_t* ids;                        // [T] usable adapter slot of each token, -1: none
+  const int32_t* n_jobs;                     // [token tiles] distinct adapters of a tile
+  const int32_t* jobs;                       // [token tiles][tile tokens] their slots, in order of first appearance
+  const float* s;                            // [parts][T][rank_pad] scale * x A^T, one partial sum per K part
+  int parts;
+};
+
+cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const uint16_t* up, int64_t up_stride, int rank, float scale, int slot,
+                             int K, int N, const LoraBank& bank, cudaStream_t s);
+cudaError_t lora_shrink_setup();             // once per plan, with its device current
+// token_tile: tokens per tile of the projection kernel that follows (its job lists are made here).
+cudaError_t launch_lora_shrink(const uint16_t* x, int64_t x_stride, int T, int K, const int32_t* ids, const LoraBank& bank, int parts,
+                               int token_tile, int32_t* out_ids, int32_t* n_jobs, int32_t* jobs, float* s_out, int32_t* tile_counter,
+                               int32_t* status, cudaStream_t s);
+
+struct ProjectArgs {
+  int T, K, N;
+  int out_f32;
+  void* y; int64_t y_stride;
+  const LoraBank* bank;                      // nullptr: no adapters in this call
+  LoraStep step;
+  float* partial;                            // [kSplitCtas][kSmallTok][128]
+  int32_t* split_counters;                   // [kSplitCtas], zero between calls
+  int32_t* tile_counter;
+  int32_t* status;
+};
+// Tensor maps are encoded per call for x and once for the weight and the up bank.
+int make_tile_map(GemmTensorMap* out, const void* base, long long cols, long long rows, long long row_stride, long long depth,
+                  long long depth_stride, int box_cols, int box_rows, int swizzle_bytes);
+cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,
+                                 cudaStream_t s);
+cudaError_t launch_project_large(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,
+                                 int n_sms, cudaStream_t s);
+bool project_is_small(int T, int N);
+int project_small_tile(int out_f32);                // tokens per tile of the small kernel
+int project_small_tokens(int T, int out_f32);       // token columns of its MMA: T rounded up to 16, at most the tile's
+
+}  // namespace cep
