@@ -14,9 +14,9 @@ struct cep_lora_plan {
   GemmTensorMap tm_w, tm_up;
   LoraBank bank;
   uint8_t* ws;
-  int32_t* status; int32_t* tile_counter; int32_t* split_counters;
+  int32_t* status; int32_t* tile_counter;
   int32_t* ids; int32_t* n_jobs; int32_t* jobs;
-  float* s; float* partial;
+  float* s;
   // The plan's last enqueued work.  Work on another stream waits for it: the workspace and the bank are shared.
   cudaEvent_t last; cudaStream_t last_stream; bool have_last;
 };
@@ -46,7 +46,7 @@ int shrink_parts(int T, int K) {
   return std::max(1, std::min(std::min(8, 296 / tiles), steps / 2));
 }
 
-struct Carve { size_t status, tile_counter, split_counters, ids, n_jobs, jobs, s, partial, total; };
+struct Carve { size_t status, tile_counter, ids, n_jobs, jobs, s, total; };
 Carve carve(const cep_lora_config& c) {
   Carve w{};
   size_t o = 0;
@@ -54,7 +54,6 @@ Carve carve(const cep_lora_config& c) {
   const size_t T = c.max_tokens;
   take(w.status, kStWords * 4);
   take(w.tile_counter, 4);
-  take(w.split_counters, kSplitCtas * 4);
   if (c.max_adapters) {
     take(w.ids, T * 4);
     take(w.n_jobs, (T / 64 + 1) * 4);
@@ -63,7 +62,6 @@ Carve carve(const cep_lora_config& c) {
     const size_t rows = std::min<size_t>(8 * T, std::max<size_t>(296 * kShrinkRows, T));
     take(w.s, rows * rank_pad_of(c) * 4);
   }
-  take(w.partial, (size_t)kSplitCtas * kSmallTok * 128 * 4);
   w.total = o;
   return w;
 }
@@ -141,9 +139,9 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
   p->cfg = *cfg; p->weight = weight; p->weight_stride = weight_stride;
   p->ws = static_cast<uint8_t*>(workspace);
   auto ints = [&](size_t off) { return reinterpret_cast<int32_t*>(p->ws + off); };
-  p->status = ints(w.status); p->tile_counter = ints(w.tile_counter); p->split_counters = ints(w.split_counters);
+  p->status = ints(w.status); p->tile_counter = ints(w.tile_counter);
   p->ids = ints(w.ids); p->n_jobs = ints(w.n_jobs); p->jobs = ints(w.jobs);
-  p->s = reinterpret_cast<float*>(p->ws + w.s); p->partial = reinterpret_cast<float*>(p->ws + w.partial);
+  p->s = reinterpret_cast<float*>(p->ws + w.s);
   uint8_t* bk = static_cast<uint8_t*>(bank);
   p->bank = LoraBank{reinterpret_cast<int32_t*>(bk + b.rank), reinterpret_cast<float*>(bk + b.scale), reinterpret_cast<uint16_t*>(bk + b.down),
                      reinterpret_cast<uint16_t*>(bk + b.up), cfg->max_adapters, rank_pad_of(*cfg)};
@@ -167,7 +165,7 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
                       (long long)cfg->out_features * kLoraChunk * 2, kLoraChunk, 128, 32);
   if (m) { lora_plan_destroy(p); return record_error(CEP_ERR_CUDA, "lora: cuTensorMapEncodeTiled failed (%d)", m); }
   // the status word and the counters start at zero, every slot of the bank empty
-  e = cudaMemsetAsync(p->ws, 0, w.split_counters + kSplitCtas * 4, st);
+  e = cudaMemsetAsync(p->ws, 0, w.tile_counter + 4, st);
   if (e == cudaSuccess && b.total) e = cudaMemsetAsync(bk, 0, b.down, st);
   if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaMemsetAsync", e);
   rc = leave(p, st, false);
@@ -222,7 +220,7 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
   if (rc) return rc;
   ProjectArgs a{};
   a.T = n_tokens; a.K = c.in_features; a.N = c.out_features; a.out_f32 = f32;
-  a.y = y; a.y_stride = y_stride; a.partial = p->partial; a.split_counters = p->split_counters; a.tile_counter = p->tile_counter; a.status = p->status;
+  a.y = y; a.y_stride = y_stride; a.tile_counter = p->tile_counter; a.status = p->status;
   cudaError_t e = cudaSuccess;
   if (adapter_ids) {
     const int parts = shrink_parts(n_tokens, c.in_features);
@@ -241,11 +239,7 @@ int lora_status(cep_lora_plan* p) {
   int32_t st[kStWords] = {};
   cudaError_t e = p->have_last ? cudaEventSynchronize(p->last) : cudaSuccess;
   if (e == cudaSuccess) e = cudaMemcpy(st, p->status, sizeof st, cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess && st[kStTimeout]) {               // a call that gave up leaves its counters behind
-    e = cudaMemset(p->ws, 0, carve(p->cfg).split_counters + kSplitCtas * 4);
-  } else if (e == cudaSuccess && st[kStBadRouting]) {
-    e = cudaMemset(p->status, 0, sizeof st);
-  }
+  if (e == cudaSuccess && (st[kStTimeout] || st[kStBadRouting])) e = cudaMemset(p->status, 0, sizeof st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: reading the status failed: %s", cudaGetErrorString(e));
   if (st[kStTimeout]) return record_error(CEP_ERR_DEVICE_TIMEOUT, "lora: a bounded wait inside a kernel expired");
   if (st[kStBadRouting]) return record_error(CEP_ERR_BAD_ROUTING, "lora: an adapter id named no loaded adapter");

@@ -10,7 +10,7 @@ constexpr int kLoraChunk = 16;               // ranks per K step of the up proje
 constexpr int kLoraMaxRank = 256;
 constexpr int kLoraMaxAdapters = 4096;
 constexpr int kShrinkRows = 64;              // tokens per block of the down projection
-constexpr int kSplitCtas = 148;              // a call's K-split blocks never exceed this (sizes the partial sums)
+constexpr int kSms = 148;                    // K is split while the tiles are fewer than this
 constexpr int kSmallTok = 128;               // tokens per tile of the small kernel (fp32 outputs: 64)
 constexpr int kLargeTok = 256;               // tokens per tile of the large kernel
 
@@ -46,8 +46,6 @@ struct ProjectArgs {
   void* y; int64_t y_stride;
   const LoraBank* bank;                      // nullptr: no adapters in this call
   LoraStep step;
-  float* partial;                            // [kSplitCtas][kSmallTok][128]
-  int32_t* split_counters;                   // [kSplitCtas], zero between calls
   int32_t* tile_counter;
   int32_t* status;
 };

@@ -13,8 +13,9 @@
 //
 // Two kernels, both warp-specialised, TMA-fed, fp32 accumulators in tensor memory, every wait bounded (status word):
 //   large   CTA pairs on 256 tokens x 256 columns, tokens on the MMA's M side, persistent with a tile counter
-//   small   the weight on the M side (128 columns of y), up to 128 tokens on the N side, K split over several CTAs so that
-//           the weight streams through as many SMs as there are; partial sums are added in split order by the last CTA
+//   small   the weight on the M side (128 columns of y), up to 128 tokens on the N side, K split over the CTAs of a cluster so
+//           that the weight streams through as many SMs as there are; the CTAs exchange partial sums through shared memory,
+//           each adds a share of the tokens in split order
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -37,6 +38,11 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
                  "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 // K-major operand with rows of 32 bytes (16 ranks), 32-byte swizzle, 8-row groups 256 bytes apart
 __device__ __forceinline__ uint64_t make_smem_desc_32b(uint32_t saddr) {
@@ -97,13 +103,17 @@ struct LoraArgs {                                      // bank == nullptr on the
 // ------------------------------------------------------------------ small kernel
 constexpr int kSmallThreads = 192;
 constexpr int kSmallMaxStages = 12;
+constexpr int kMaxSplits = 8;                          // CTAs of a portable cluster
 constexpr int kSBufs = 2;
 constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
-constexpr int kSmallRing = 144 * 1024;                 // ring + s tiles; leaves room for a block of the down projection on the SM
+#ifndef CEP_LORA_SMALL_RING
+#define CEP_LORA_SMALL_RING (200 * 1024)
+#endif
+constexpr int kSmallRing = CEP_LORA_SMALL_RING;       // ring + s tiles
 struct __align__(8) SmallBarriers {
   uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], sfull[kSBufs], sempty[kSBufs], acc_full;
   uint32_t tmem_base;
-  int abort_flag, last;
+  int abort_flag;
 };
 static_assert(sizeof(SmallBarriers) <= 512, "barrier block");
 
@@ -113,8 +123,7 @@ template <typename OT>
 __global__ void __launch_bounds__(kSmallThreads, 1)
 project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
                      const __grid_constant__ CUtensorMap tm_up, int T, int N, int num_kb, int tok, int npad, int stages, int n_acc, const LoraArgs la,
-                     OT* __restrict__ y, int64_t y_stride, float* __restrict__ partial, int32_t* __restrict__ counters,
-                     int32_t* __restrict__ status) {
+                     OT* __restrict__ y, int64_t y_stride, int vec_ok, int32_t* __restrict__ status) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const int x_stage = npad * kKBytes, stage_bytes = kWStage + x_stage;
@@ -270,8 +279,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     const int n = n0 + lane_grp * 32 + lane;
     const int cols = min(tok, T - t0);                 // token columns that exist
     const uint32_t taddr = tmem + ((uint32_t)(lane_grp * 32) << 16);
-    const int tile = blockIdx.z * gridDim.x + blockIdx.x;
-    float* mine = partial + ((size_t)tile * splits + split) * (kSmallTok * 128);
+    float* mine = reinterpret_cast<float*>(smem);      // [token][128] partial sums, in the ring: every load has been consumed
     if (all) {
       tc_fence_after();
       for (int c = 0; c < cols; c += 16) {
@@ -295,41 +303,40 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (c + i < cols) __stcg(mine + (c + i) * 128 + lane_grp * 32 + lane, __uint_as_float(d[i]));
+            if (c + i < cols) mine[(c + i) * 128 + lane_grp * 32 + lane] = __uint_as_float(d[i]);
         }
       }
     }
-    if (splits > 1) {
-      // the CTA that arrives last adds the partial sums in split order; a CTA that gave up does not arrive, so the tile
-      // is then left unwritten and the status word says so
-      __threadfence();
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (tid == 0) {
-        bars->last = 0;
-        if (*abort_flag == 0) bars->last = atomicAdd(counters + tile, 1) == splits - 1;
-      }
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (bars->last) {
-        __threadfence();
-        if (tid == 0) counters[tile] = 0;
-        const float* first = partial + (size_t)tile * splits * (kSmallTok * 128) + lane_grp * 32 + lane;
-        for (int c = 0; c < cols; c += 4) {
-          float v[4];
+  }
+  if (splits > 1) {
+    // (a CTA that gave up still takes both barriers; its sums are then meaningless and the status word says so)
+    cluster_sync_all();
+    const int cols = min(tok, T - t0);
+    const int c0 = cols * split / splits, c1 = cols * (split + 1) / splits;
+    const uint32_t base = smem_u32(smem);
+    // four columns of y per lane, a token per warp
+    for (int c = c0 + warp; c < c1; c += kSmallThreads / 32) {
+      float4 v[kMaxSplits];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = c + i < cols ? __ldcg(first + (c + i) * 128) : 0.f;
-          for (int s = 1; s < splits; ++s) {
+      for (int s = 0; s < kMaxSplits; ++s)
+        if (s < splits) v[s] = ld_cluster_f4(mapa(base + (uint32_t)((c * 128 + lane * 4) * 4), (uint32_t)s));
+      float4 o = v[0];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (c + i < cols) v[i] += __ldcg(first + (size_t)s * (kSmallTok * 128) + (c + i) * 128);
-          }
-          if (n < N) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (c + i < cols) put_out(y + (size_t)(t0 + c + i) * y_stride + n, v[i]);
-          }
-        }
+      for (int s = 1; s < kMaxSplits; ++s)
+        if (s < splits) { o.x += v[s].x; o.y += v[s].y; o.z += v[s].z; o.w += v[s].w; }
+      OT* row = y + (size_t)(t0 + c) * y_stride + n0 + lane * 4;
+      const int left = N - n0 - lane * 4;
+      if (left >= 4 && vec_ok) {
+        if (sizeof(OT) == 2) *reinterpret_cast<uint2*>(row) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+        else *reinterpret_cast<float4*>(row) = o;
+      } else {
+        if (left > 0) put_out(row, o.x);
+        if (left > 1) put_out(row + 1, o.y);
+        if (left > 2) put_out(row + 2, o.z);
+        if (left > 3) put_out(row + 3, o.w);
       }
     }
+    cluster_sync_all();                                // no CTA leaves while another reads its sums
   }
   tc_fence_before();
   __syncthreads();
@@ -661,7 +668,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
 // ------------------------------------------------------------------ host side
 constexpr int kMaxDevices = 64;
 int g_large_clusters[kMaxDevices];                     // co-resident CTA pairs + 1 (0: not set up)
-bool g_small_ready[kMaxDevices];
+int g_small_clusters[kMaxDevices][kMaxSplits + 1];     // co-resident clusters by size; [0]: set up
 
 cudaError_t device_slot(int* dev) {
   cudaError_t e = cudaGetDevice(dev);
@@ -711,18 +718,39 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   int dev = 0;
   cudaError_t e = device_slot(&dev);
   if (e != cudaSuccess) return e;
-  if (!g_small_ready[dev]) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.blockDim = dim3(kSmallThreads, 1, 1); cfg.stream = s; cfg.attrs = attr;
+  int* clusters = g_small_clusters[dev];
+  if (clusters[0] == 0) {
     e = cudaFuncSetAttribute(project_small_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(project_small_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
     if (e != cudaSuccess) return e;
-    g_small_ready[dev] = true;
+    for (int c = 1; c <= kMaxSplits; ++c) {
+      attr[0].val.clusterDim.y = (unsigned)c;
+      cfg.gridDim = dim3(kSms, c, 1); cfg.dynamicSmemBytes = kSmallRing + 2048; cfg.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&clusters[c], project_small_kernel<__nv_bfloat16>, &cfg);
+      if (e != cudaSuccess) return e;
+    }
+    clusters[0] = 1;
   }
   const int npad = project_small_tokens(a.T, a.out_f32), tok = project_small_tile(a.out_f32);
   const int n_tiles = (a.N + 127) / 128, t_tiles = (a.T + tok - 1) / tok, num_kb = (a.K + 63) / 64;
   const long long tiles = (long long)n_tiles * t_tiles;
-  int splits = tiles >= kSplitCtas ? 1 : (int)(kSplitCtas / tiles);
-  if (splits > num_kb) splits = num_kb;
-  if (splits > 32) splits = 32;                        // the last CTA reads every partial sum
+  // The cluster size with the least work for the busiest SM, in K steps: a cluster needs that many free SMs in one GPC,
+  // so fewer SMs are usable for some sizes.  kExchange: what the exchange of partial sums costs (2 us).
+  constexpr long long kExchange = 6;
+  int splits = 1;
+  long long best = 1ll << 60;
+  for (int c = 1; c <= kMaxSplits && c <= num_kb; ++c) {
+    if (clusters[c] < 1) continue;
+    const long long cost = (tiles + clusters[c] - 1) / clusters[c] * ((num_kb + c - 1) / c) + (c > 1 ? kExchange : 0);
+    if (cost < best) { best = cost; splits = c; }
+  }
   const int steps = num_kb / splits;                   // K steps a CTA has at least
   int n_acc = a.out_f32 ? (steps + kSlabSteps - 1) / kSlabSteps : 1;
   if (n_acc > 512 / npad) n_acc = 512 / npad;
@@ -731,22 +759,20 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   int stages = (kSmallRing - kSBufs * npad * kKBytes) / stage;
   if (stages > kSmallMaxStages) stages = kSmallMaxStages;
   const size_t smem = 1024 + (size_t)stages * stage + kSBufs * npad * kKBytes + 512;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(n_tiles, splits, t_tiles); cfg.blockDim = dim3(kSmallThreads, 1, 1);
-  cfg.dynamicSmemBytes = smem; cfg.stream = s; cfg.attrs = attr;
-  cfg.numAttrs = a.bank ? 1 : 0;                       // only ever overlaps this call's own down projection
+  const size_t elt = a.out_f32 ? 4 : 2;
+  const int vec_ok = reinterpret_cast<uintptr_t>(a.y) % (4 * elt) == 0 && a.y_stride % 4 == 0;
+  attr[0].val.clusterDim.y = (unsigned)splits;
+  cfg.gridDim = dim3(n_tiles, splits, t_tiles); cfg.dynamicSmemBytes = smem;
+  cfg.numAttrs = a.bank ? 2 : 1;                       // only ever overlaps this call's own down projection
   const CUtensorMap& w = reinterpret_cast<const CUtensorMap&>(tm_w);
   const CUtensorMap& x = reinterpret_cast<const CUtensorMap&>(tm_x);
   const CUtensorMap& u = reinterpret_cast<const CUtensorMap&>(tm_up);
   const LoraArgs la = lora_args(a);
   if (a.out_f32)
-    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, num_kb, tok, npad, stages, n_acc, la, (float*)a.y, a.y_stride, a.partial,
-                              a.split_counters, a.status);
+    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, num_kb, tok, npad, stages, n_acc, la, (float*)a.y, a.y_stride, vec_ok,
+                              a.status);
   return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16>, w, x, u, a.T, a.N, num_kb, tok, npad, stages, n_acc, la, (__nv_bfloat16*)a.y, a.y_stride,
-                            a.partial, a.split_counters, a.status);
+                            vec_ok, a.status);
 }
 
 cudaError_t launch_project_large(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,
