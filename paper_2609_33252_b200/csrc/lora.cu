@@ -11,7 +11,7 @@ struct cep_lora_plan {
   cep_lora_config cfg;
   int device, n_sms;
   const void* weight; int64_t weight_stride;
-  GemmTensorMap tm_w, tm_up;
+  GemmTensorMap tm_w, tm_up, tm_down;
   LoraBank bank;
   uint8_t* ws;
   int32_t* status; int32_t* tile_counter;
@@ -39,13 +39,6 @@ int check_config(const cep_lora_config* c) {
   return CEP_OK;
 }
 
-// K parts of the down projection: enough blocks to fill the device with few tokens, one part with many (every part is a
-// [T, rank] array that the projection's tiles read again)
-int shrink_parts(int T, int K) {
-  const int tiles = (T + kShrinkRows - 1) / kShrinkRows, steps = (K + 63) / 64;
-  return std::max(1, std::min(std::min(8, 296 / tiles), steps / 2));
-}
-
 struct Carve { size_t status, tile_counter, ids, n_jobs, jobs, s, total; };
 Carve carve(const cep_lora_config& c) {
   Carve w{};
@@ -58,9 +51,7 @@ Carve carve(const cep_lora_config& c) {
     take(w.ids, T * 4);
     take(w.n_jobs, (T / 64 + 1) * 4);
     take(w.jobs, up_to(T, kLargeTok) * 4);
-    // parts * T rows for every T <= max_tokens: at most 8 T, and at most 296 tiles' rows or T
-    const size_t rows = std::min<size_t>(8 * T, std::max<size_t>(296 * kShrinkRows, T));
-    take(w.s, rows * rank_pad_of(c) * 4);
+    take(w.s, T * rank_pad_of(c) * 4);
   }
   w.total = o;
   return w;
@@ -159,7 +150,10 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
   e = lora_shrink_setup();
   if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaFuncSetAttribute", e);
   int m = make_tile_map(&p->tm_w, weight, cfg->in_features, cfg->out_features, weight_stride * 2, 0, 0, 64, 128, 128);
-  p->tm_up = p->tm_w;                                     // (not read without adapters)
+  p->tm_up = p->tm_down = p->tm_w;                        // (not read without adapters)
+  if (!m && cfg->max_adapters)
+    m = make_tile_map(&p->tm_down, p->bank.down, cfg->in_features, (long long)cfg->max_adapters * p->bank.rank_pad, cfg->in_features * 2ll, 0, 0, 64,
+                      kLoraChunk, 128);
   if (!m && cfg->max_adapters)
     m = make_tile_map(&p->tm_up, p->bank.up, kLoraChunk, cfg->out_features, kLoraChunk * 2, (long long)cfg->max_adapters * (p->bank.rank_pad / kLoraChunk),
                       (long long)cfg->out_features * kLoraChunk * 2, kLoraChunk, 128, 32);
@@ -223,11 +217,10 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
   a.y = y; a.y_stride = y_stride; a.tile_counter = p->tile_counter; a.status = p->status;
   cudaError_t e = cudaSuccess;
   if (adapter_ids) {
-    const int parts = shrink_parts(n_tokens, c.in_features);
-    e = launch_lora_shrink(static_cast<const uint16_t*>(x), x_stride, n_tokens, c.in_features, adapter_ids, p->bank, parts, token_tile, p->ids, p->n_jobs,
-                           p->jobs, p->s, p->tile_counter, p->status, st);
+    e = launch_lora_shrink(tm_x, p->tm_down, box, n_tokens, c.in_features, adapter_ids, p->bank, token_tile, p->ids, p->n_jobs, p->jobs, p->s,
+                           p->tile_counter, p->status, st);
     a.bank = &p->bank;
-    a.step = LoraStep{p->ids, p->n_jobs, p->jobs, p->s, parts};
+    a.step = LoraStep{p->ids, p->n_jobs, p->jobs, p->s};
   }
   if (e == cudaSuccess) e = small ? launch_project_small(a, p->tm_w, tm_x, p->tm_up, st) : launch_project_large(a, p->tm_w, tm_x, p->tm_up, p->n_sms, st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: a launch failed: %s", cudaGetErrorString(e));

@@ -9,7 +9,6 @@ namespace cep {
 constexpr int kLoraChunk = 16;               // ranks per K step of the up projection (one bf16 MMA)
 constexpr int kLoraMaxRank = 256;
 constexpr int kLoraMaxAdapters = 4096;
-constexpr int kShrinkRows = 64;              // tokens per block of the down projection
 constexpr int kSms = 148;                    // K is split while the tiles are fewer than this
 constexpr int kSmallTok = 128;               // tokens per tile of the small kernel (fp32 outputs: 64)
 constexpr int kLargeTok = 256;               // tokens per tile of the large kernel
@@ -18,7 +17,7 @@ constexpr int kLargeTok = 256;               // tokens per tile of the large ker
 struct LoraBank {
   const int32_t* rank;                       // [slots], 0: nothing loaded
   const float* scale;                        // [slots]
-  const uint16_t* down;                      // bf16 [slots][rank_pad][K]; rows at or beyond the rank are not read
+  const uint16_t* down;                      // bf16 [slots][rank_pad][K]; rows at or beyond the rank count for nothing
   const uint16_t* up;                        // bf16 [slots][rank_pad/16][N][16]; ranks beyond the adapter's are zero
   int slots, rank_pad;
 };
@@ -28,17 +27,17 @@ struct LoraStep {
   const int32_t* ids;                        // [T] usable adapter slot of each token, -1: none
   const int32_t* n_jobs;                     // [token tiles] distinct adapters of a tile
   const int32_t* jobs;                       // [token tiles][tile tokens] their slots, in order of first appearance
-  const float* s;                            // [parts][T][rank_pad] scale * x A^T, one partial sum per K part
-  int parts;
+  const float* s;                            // [T][rank_pad] scale * A_a x
 };
 
 cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const uint16_t* up, int64_t up_stride, int rank, float scale, int slot,
                              int K, int N, const LoraBank& bank, cudaStream_t s);
 cudaError_t lora_shrink_setup();             // once per plan, with its device current
-// token_tile: tokens per tile of the projection kernel that follows (its job lists are made here).
-cudaError_t launch_lora_shrink(const uint16_t* x, int64_t x_stride, int T, int K, const int32_t* ids, const LoraBank& bank, int parts,
-                               int token_tile, int32_t* out_ids, int32_t* n_jobs, int32_t* jobs, float* s_out, int32_t* tile_counter,
-                               int32_t* status, cudaStream_t s);
+// tm_x: 64 columns x `box` rows; tm_down: the bank's down rows, 64 columns x 16 rows.  token_tile: tokens per tile of the
+// projection kernel that follows (its job lists are made here).
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, const int32_t* ids,
+                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_jobs, int32_t* jobs, float* s_out,
+                               int32_t* tile_counter, int32_t* status, cudaStream_t s);
 
 struct ProjectArgs {
   int T, K, N;

@@ -20,7 +20,7 @@
 #include <cuda_bf16.h>
 
 #include "lora.h"
-#include "tcgen05_ptx.cuh"
+#include "lora_ptx.cuh"
 
 namespace cep {
 namespace {
@@ -32,18 +32,6 @@ constexpr int kKBytes = 128;                          // bytes of K per stage: o
 constexpr int kUpBytes = 128 * 32;                    // 128 columns x one chunk of 16 ranks, 32-byte rows
 
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-                 "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-               : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 // K-major operand with rows of 32 bytes (16 ranks), 32-byte swizzle, 8-row groups 256 bytes apart
 __device__ __forceinline__ uint64_t make_smem_desc_32b(uint32_t saddr) {
   uint64_t d = 0;
@@ -59,19 +47,15 @@ __device__ __forceinline__ uint64_t make_smem_desc_32b(uint32_t saddr) {
 // One step covers two chunks of 16 ranks.  Its operand row is 128 bytes: [value c0 | remainder c0 | value c1 | remainder c1].
 struct SRow {
   uint32_t w[32];
-  // Sums the K parts of chunks c0 and c0+1 (of nc) in order and splits the result.
-  __device__ __forceinline__ void fetch(const float* __restrict__ s, size_t part_stride, int parts, int c0, int nc) {
+  // Splits chunks c0 and c0+1 (of nc) of a token's row of s.
+  __device__ __forceinline__ void fetch(const float* __restrict__ s, int c0, int nc) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       if (c0 + c >= nc) break;
       const float4* p = reinterpret_cast<const float4*>(s + (c0 + c) * kLoraChunk);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        float4 v = __ldcg(p + q);
-        for (int k = 1; k < parts; ++k) {
-          const float4 u = __ldcg(reinterpret_cast<const float4*>(s + k * part_stride + (c0 + c) * kLoraChunk) + q);
-          v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-        }
+        const float4 v = __ldcg(p + q);
         const uint32_t h0 = pack_bf16(v.x, v.y), h1 = pack_bf16(v.z, v.w);
         w[c * 16 + 2 * q] = h0; w[c * 16 + 2 * q + 1] = h1;
         w[c * 16 + 8 + 2 * q] = pack_bf16(v.x - __uint_as_float(h0 << 16), v.y - __uint_as_float(h0 & 0xffff0000u));
@@ -95,7 +79,7 @@ template <> __device__ __forceinline__ void put_out<float>(float* p, float v) { 
 template <> __device__ __forceinline__ void put_out<__nv_bfloat16>(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 struct LoraArgs {                                      // bank == nullptr on the host: has == 0
-  int has, parts, rank_pad;
+  int has, rank_pad;
   const int32_t* rank; const int32_t* ids; const int32_t* n_jobs; const int32_t* jobs;
   const float* s;
 };
@@ -110,6 +94,7 @@ constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
 #define CEP_LORA_SMALL_RING (200 * 1024)
 #endif
 constexpr int kSmallRing = CEP_LORA_SMALL_RING;       // ring + s tiles
+constexpr int kSharedRing = 136 * 1024;               // the same beside a block of the down projection
 struct __align__(8) SmallBarriers {
   uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], sfull[kSBufs], sempty[kSBufs], acc_full;
   uint32_t tmem_base;
@@ -244,10 +229,9 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       const int t = t0 + tid;
       const int my = tid < npad && t < T ? la.ids[t] : -1;
       const float* srow = la.s + (size_t)(my >= 0 ? t : 0) * la.rank_pad;
-      const size_t part_stride = (size_t)T * la.rank_pad;
       const int my_nc = my >= 0 ? (la.rank[my] + kLoraChunk - 1) / kLoraChunk : 0;
       SRow row0, row1;                                 // the first 64 ranks of this thread's token, fetched ahead
-      if (my >= 0) { row0.fetch(srow, part_stride, la.parts, 0, my_nc); row1.fetch(srow, part_stride, la.parts, 2, my_nc); }
+      if (my >= 0) { row0.fetch(srow, 0, my_nc); row1.fetch(srow, 2, my_nc); }
       const int m = la.n_jobs[blockIdx.z];
       int sb = 0; uint32_t sphase = 0;
       for (int j = split; ok && j < m; j += splits) {
@@ -263,7 +247,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             else if (c == 2) row1.put(tile, tid, mine);
             else {
               SRow r;
-              if (mine) r.fetch(srow, part_stride, la.parts, c, nc);
+              if (mine) r.fetch(srow, c, nc);
               r.put(tile, tid, mine);
             }
           }
@@ -572,14 +556,13 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       const int t = m * kLargeTok + (int)rank * 128 + r;
       const int my = t < T ? la.ids[t] : -1;
       const float* srow = la.s + (size_t)(my >= 0 ? t : 0) * la.rank_pad;
-      const size_t part_stride = (size_t)T * la.rank_pad;
       const int jobs = la.n_jobs[m];
       for (int j = 0; ok && j < jobs; ++j) {
         const int a = la.jobs[(size_t)m * kLargeTok + j];
         const int nc = (la.rank[a] + kLoraChunk - 1) / kLoraChunk;
         for (int c = 0; c < nc; c += 2) {
           SRow row;
-          if (my == a) row.fetch(srow, part_stride, la.parts, c, nc);
+          if (my == a) row.fetch(srow, c, nc);
           ok = mbar_wait(smem_u32(&bars->sempty[sb]), sphase ^ 1u, abort_flag, status);
           if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
           row.put(s_tiles + sb * kHalf, r, my == a);
@@ -679,7 +662,7 @@ cudaError_t device_slot(int* dev) {
 LoraArgs lora_args(const ProjectArgs& a) {
   LoraArgs la{};
   if (!a.bank) return la;
-  la.has = 1; la.parts = a.step.parts; la.rank_pad = a.bank->rank_pad; la.rank = a.bank->rank;
+  la.has = 1; la.rank_pad = a.bank->rank_pad; la.rank = a.bank->rank;
   la.ids = a.step.ids; la.n_jobs = a.step.n_jobs; la.jobs = a.step.jobs; la.s = a.step.s;
   return la;
 }
@@ -756,7 +739,9 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   if (n_acc > 512 / npad) n_acc = 512 / npad;
   if (n_acc < 1) n_acc = 1;
   const int stage = kWStage + npad * kKBytes;
-  int stages = (kSmallRing - kSBufs * npad * kKBytes) / stage;
+  // With adapters and few tokens the ring leaves room for a block of the down projection, so that both run at once.
+  const int ring = a.bank && a.T <= 64 ? kSharedRing : kSmallRing;
+  int stages = (ring - kSBufs * npad * kKBytes) / stage;
   if (stages > kSmallMaxStages) stages = kSmallMaxStages;
   const size_t smem = 1024 + (size_t)stages * stage + kSBufs * npad * kKBytes + 512;
   const size_t elt = a.out_f32 ? 4 : 2;

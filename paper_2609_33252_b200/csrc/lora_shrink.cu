@@ -1,35 +1,39 @@
 // Down projection of the low-rank adapters: s[t] = scale_a * A_a x[t] for every token t with adapter a, and the lists of
 // adapters per token tile that the projection kernel walks.  Also packs an adapter into the bank.
 //
-// One block takes 64 tokens and one part of K, and one adapter present among them after the other: the tokens' rows of x
-// (only those with this adapter) times the adapter's rows, 16x8x16 matrix instructions with fp32 accumulators, four
-// asynchronous copy stages.  The work is 2 T r K operations against 2 T K bytes of x, at most r operations per byte: memory
-// (long batches) or latency (a few tokens) bounds it, not the matrix pipe.  With few tokens K is split over several
-// blocks: each part's partial sum is stored and the reader adds the parts in order, so the result does not depend on timing.
+// The work is 2 T r K operations against 2 T K bytes of x: at most r operations per byte, so memory (long batches) or
+// latency (a few tokens) bounds it.  A block takes 128 consecutive tokens as the M side of a matrix product whose N side is
+// the rows of every adapter among them, 16 ranks at a time: x is read once however many adapters the tokens have (up to
+// kChunks * 16 ranks; more take further passes), and of the product each token keeps the columns of its own adapter.
+// Operands come by TMA, accumulators are fp32 in tensor memory.  While there are few token tiles, K is split over the CTAs
+// of a cluster, which add their partial sums in order through shared memory, so results do not depend on timing.
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "lora.h"
+#include "lora_ptx.cuh"
 
 namespace cep {
 namespace {
 
-constexpr int kStages = 3;
-constexpr int kTileBytes = 64 * 128;                 // 64 rows x 64 bf16
-constexpr int kShrinkSmem = kStages * 2 * kTileBytes;
+using namespace ptx;
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool in) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// 16-byte chunk c of row r in a tile of 128-byte rows, chunks exchanged so that eight rows of a column hit all banks
-__device__ __forceinline__ uint32_t tile_at(uint32_t base, int r, int c) { return base + r * 128 + ((c ^ (r & 7)) << 4); }
+constexpr int kThreads = 192;                        // warp 0 loads, 1 MMA, 2-5 read the accumulator
+constexpr int kRows = 128;                           // tokens per block
+constexpr int kXStage = kRows * 128;                 // 64 bf16 of K
+constexpr int kChunkStage = kLoraChunk * 128;
+constexpr int kMaxStages = 8;
+constexpr int kChainSteps = 12;                      // K steps per accumulation chain (the tensor core's additions truncate)
+constexpr int kMaxParts = 8;
+struct __align__(8) ShrinkBarriers {
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+struct ShrinkLists {                                 // scratch of the list building
+  int id[kLargeTok], job[kLargeTok], n_chunks, warp_count[8];
+  int chunk[kRows * (kLoraMaxRank / kLoraChunk)];    // adapter * 16 + chunk of its ranks
+};
 
 // The slot a token's adapter id names, -1 for none; an id that names nothing loaded is reported and treated as none.
 __device__ __forceinline__ int usable_id(const int32_t* __restrict__ ids, int t, const LoraBank& b, int32_t* status, bool report) {
@@ -39,137 +43,217 @@ __device__ __forceinline__ int usable_id(const int32_t* __restrict__ ids, int t,
   return -1;
 }
 
-// Distinct non-negative values of v[0..n), n <= 256, in order of first appearance; returns their number.  All 128 threads.
-__device__ int distinct_in_order(const int* v, int n, int* out, int* warp_count) {
+// Distinct non-negative values of v[0..n), n <= 256, in order of first appearance -> out; returns their number.  All threads.
+// table: one int per slot.
+__device__ int distinct_in_order(const int* v, int n, int* table, int* out, int* warp_count) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < n; i += kThreads) if (v[i] >= 0) table[v[i]] = n;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kThreads) if (v[i] >= 0) atomicMin(&table[v[i]], i);
+  __syncthreads();
   int total = 0;
-  for (int base = 0; base < n; base += 128) {
+  for (int base = 0; base < n; base += kThreads) {
     const int i = base + threadIdx.x;
-    bool first = i < n && v[i] >= 0;
-    for (int j = 0; first && j < i; ++j) first = v[j] != v[i];
+    const bool first = i < n && v[i] >= 0 && table[v[i]] == i;
     const unsigned m = __ballot_sync(0xffffffffu, first);
     if (lane == 0) warp_count[warp] = __popc(m);
     __syncthreads();
     int before = total;
-    for (int w = 0; w < 4; ++w) { if (w < warp) before += warp_count[w]; total += warp_count[w]; }
+    for (int w = 0; w < kThreads / 32; ++w) { if (w < warp) before += warp_count[w]; total += warp_count[w]; }
     if (first) out[before + __popc(m & ((1u << lane) - 1))] = v[i];
     __syncthreads();
   }
   return total;
 }
 
-// Blocks (token tile, K part, job stripe): job j of the tile belongs to stripe j mod gridDim.z.
-__global__ void __launch_bounds__(128, 3)
-lora_shrink_kernel(const uint16_t* __restrict__ x, int64_t x_stride, int T, int K, const int32_t* __restrict__ ids, const LoraBank bank,
-                   int token_tile, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_jobs, int32_t* __restrict__ jobs,
+// Grid (token tiles, pass stripes, K parts); the parts are a cluster.  box: rows of x one TMA load brings.
+__global__ void __launch_bounds__(kThreads)
+lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K,
+                   const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int chunks, int stages, int n_acc,
+                   int tmem_cols, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_jobs, int32_t* __restrict__ jobs,
                    float* __restrict__ s_out, int32_t* __restrict__ tile_counter, int32_t* __restrict__ status) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int id_s[kLargeTok], job_s[kLargeTok], warp_count[4];
-  const int t0 = blockIdx.x * kShrinkRows;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ ShrinkBarriers bars;
+  __shared__ ShrinkLists L;
+  const int stage_bytes = kXStage + chunks * kChunkStage;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool reporter = blockIdx.y == 0 && blockIdx.z == 0;
-  if (reporter && blockIdx.x == 0 && threadIdx.x == 0) *tile_counter = 0;
-  if (reporter && t0 % token_tile == 0) {
-    const int n = min(token_tile, T - t0), tile = t0 / token_tile;
-    for (int i = threadIdx.x; i < n; i += 128) id_s[i] = usable_id(ids, t0 + i, bank, status, false);
-    __syncthreads();
-    const int m = distinct_in_order(id_s, n, job_s, warp_count);
-    for (int i = threadIdx.x; i < m; i += 128) jobs[(size_t)tile * token_tile + i] = job_s[i];
-    if (threadIdx.x == 0) n_jobs[tile] = m;
-    __syncthreads();
+  volatile int* abort_flag = &bars.abort_flag;
+  const int t0 = blockIdx.x * kRows, rows = min(kRows, T - t0);
+  const int part = blockIdx.z, parts = gridDim.z;
+  const bool reporter = blockIdx.y == 0 && part == 0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars.full[s]), 1); mbar_init(smem_u32(&bars.empty[s]), 1); }
+    mbar_init(smem_u32(&bars.acc_full), 1);
+    bars.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (reporter && blockIdx.x == 0) *tile_counter = 0;
   }
-  const int rows = min(kShrinkRows, T - t0);
-  for (int i = threadIdx.x; i < kShrinkRows; i += 128) {
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(&bars.tmem_base)), "r"(tmem_cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+
+  // The projection kernel may be scheduled from here on.  Not earlier: its blocks allocate tensor memory too and wait for this
+  // grid, so every block of this grid has to hold its own first.
+  __syncthreads();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---------------------------------------------------------------- lists (the ring is not in use yet and holds the table)
+  int* table = reinterpret_cast<int*>(smem);
+  if (reporter) {
+    // the projection kernel's tiles that start among these tokens: two of 64, one of 128, every other time one of 256
+    for (int a = t0; a < t0 + rows && a % token_tile == 0; a += token_tile) {
+      const int n = min(token_tile, T - a);
+      for (int i = threadIdx.x; i < n; i += kThreads) L.id[i] = usable_id(ids, a + i, bank, status, false);
+      __syncthreads();
+      const int m = distinct_in_order(L.id, n, table, L.job, L.warp_count);
+      for (int i = threadIdx.x; i < m; i += kThreads) jobs[(size_t)a + i] = L.job[i];
+      if (threadIdx.x == 0) n_jobs[a / token_tile] = m;
+      __syncthreads();
+    }
+  }
+  for (int i = threadIdx.x; i < kRows; i += kThreads) {
     const int id = i < rows ? usable_id(ids, t0 + i, bank, status, reporter) : -1;
-    id_s[i] = id;
+    L.id[i] = id;
     if (reporter && i < rows) out_ids[t0 + i] = id;
   }
   __syncthreads();
-  const int m = distinct_in_order(id_s, rows, job_s, warp_count);
+  const int m = distinct_in_order(L.id, rows, table, L.job, L.warp_count);
+  if (warp == 0) {
+    int base = 0;
+    for (int j0 = 0; j0 < m; j0 += 32) {
+      const int a = j0 + lane < m ? L.job[j0 + lane] : -1;
+      const int nc = a >= 0 ? (bank.rank[a] + kLoraChunk - 1) / kLoraChunk : 0;
+      int incl = nc;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+      for (int c = 0; c < nc; ++c) L.chunk[base + incl - nc + c] = a * (kLoraMaxRank / kLoraChunk) + c;
+      base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) L.n_chunks = base;
+  }
+  fence_proxy_async_smem();                          // the table's words become TMA destinations
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars.tmem_base;
+  const int total = L.n_chunks, steps = (K + 63) >> 6;
+  const int k0 = (int)((long long)steps * part / parts), k1 = (int)((long long)steps * (part + 1) / parts);
+  const int cols = chunks * kLoraChunk;              // columns of an accumulator
+  int stage = 0; uint32_t phase = 0, acc_phase = 0;  // the loading and the issuing thread each keep their own
 
-  const int steps = (K + 63) >> 6;
-  const int k0 = (int)((long long)steps * blockIdx.y / gridDim.y), k1 = (int)((long long)steps * (blockIdx.y + 1) / gridDim.y);
-  const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
-  float* s_part = s_out + (size_t)blockIdx.y * T * bank.rank_pad;
-  for (int j = blockIdx.z; j < m; j += gridDim.z) {
-    const int a = job_s[j], rank = bank.rank[a];
-    const float scale = bank.scale[a];
-    const uint16_t* down = bank.down + (size_t)a * bank.rank_pad * K;
-    const bool live = __any_sync(0xffffffffu, id_s[warp * 16 + (lane & 15)] == a);    // this warp's 16 tokens
-    for (int r0 = 0; r0 < rank; r0 += 64) {
-      const int cols = min(64, (rank - r0 + kLoraChunk - 1) / kLoraChunk * kLoraChunk);
-      auto load = [&](int step, int buf) {
-        const uint32_t xs = base + buf * 2 * kTileBytes, as = xs + kTileBytes;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int i = q * 128 + threadIdx.x, r = i >> 3, c = i & 7, k = step * 64 + c * 8;
-          // rows that are not read keep whatever is there: they meet only outputs that are not written
-          if (id_s[r] == a) cp16(tile_at(xs, r, c), x + (size_t)(t0 + r) * x_stride + (k < K ? k : 0), k < K);
-          if (r0 + r < rank) cp16(tile_at(as, r, c), down + (size_t)(r0 + r) * K + (k < K ? k : 0), k < K);
+  for (int c0 = blockIdx.y * chunks; c0 < total; c0 += gridDim.y * chunks) {
+    const int n = min(chunks, total - c0);
+    if (warp == 0 && lane == 0) {
+      const int boxes = (rows + box - 1) / box;
+      for (int k = k0; k < k1; ++k) {
+        if (!mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag, status)) break;
+        const uint32_t full = smem_u32(&bars.full[stage]);
+        uint8_t* st = smem + stage * stage_bytes;
+        mbar_expect_tx(full, boxes * box * 128 + n * kChunkStage);
+        for (int b = 0; b < boxes; ++b) tma_load_2d(smem_u32(st + b * box * 128), &tm_x, k * 64, t0 + b * box, full);
+        for (int i = 0; i < n; ++i) {
+          const int v = L.chunk[c0 + i], a = v / (kLoraMaxRank / kLoraChunk), c = v % (kLoraMaxRank / kLoraChunk);
+          tma_load_2d(smem_u32(st + kXStage + i * kChunkStage), &tm_down, k * 64, a * bank.rank_pad + c * kLoraChunk, full);
         }
-      };
-      float acc[8][4], sum[8][4];
-#pragma unroll
-      for (int n = 0; n < 8; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][i] = sum[n][i] = 0.f;
-#pragma unroll
-      for (int p = 0; p < kStages - 1; ++p) {
-        if (k0 + p < k1) load(k0 + p, p);
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
-      for (int step = k0, buf = 0; step < k1; ++step) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-        __syncthreads();
-        const int next = step + kStages - 1;
-        if (next < k1) load(next, buf == 0 ? kStages - 1 : buf - 1);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        if (live) {
-          const uint32_t xs = base + buf * 2 * kTileBytes, as = xs + kTileBytes;
+    } else if (warp == 1 && lane == 0) {
+      const uint32_t idesc = make_idesc_bf16(kRows, n * kLoraChunk);
+      int slab = 0, slab_end = k0 + (k1 - k0) / n_acc;
+      uint32_t more = 0;
+      bool ok = true;
+      for (int k = k0; k < k1; ++k) {
+        if (!mbar_wait(smem_u32(&bars.full[stage]), phase, abort_flag, status)) { ok = false; break; }
+        tc_fence_after();
+        if (k == slab_end) { ++slab; slab_end = k0 + (int)((long long)(k1 - k0) * (slab + 1) / n_acc); more = 0; }
+        const uint64_t xdesc = make_smem_desc(smem_u32(smem + stage * stage_bytes));
+        const uint64_t adesc = make_smem_desc(smem_u32(smem + stage * stage_bytes + kXStage));
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            uint32_t af[4];
-            ldmatrix4(af, tile_at(xs, warp * 16 + (lane & 15), kk * 2 + (lane >> 4)));
+        for (int k4 = 0; k4 < 4; ++k4)
+          tc_mma_f16(tmem + (uint32_t)(slab * cols), xdesc + (uint64_t)(k4 * 2), adesc + (uint64_t)(k4 * 2), idesc, k4 != 0 ? 1u : more);
+        more = 1;
+        tc_commit(smem_u32(&bars.empty[stage]));
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
+      if (ok) tc_commit(smem_u32(&bars.acc_full));
+    } else if (warp >= 2) {
+      bool got = mbar_wait_relaxed(smem_u32(&bars.acc_full), acc_phase, abort_flag, status);
+      got = __all_sync(0xffffffffu, got);
+      const int row = (warp & 3) * 32 + lane, my = L.id[row];
+      const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+      if (got) {
+        tc_fence_after();
+        for (int i = 0; i < n; ++i) {
+          __syncwarp();                              // the loads are warp-collective
+          uint32_t d[16];
+          tc_ld16(taddr + i * kLoraChunk, d);
+          tc_wait_ld();
+          for (int s = 1; s < n_acc; ++s) {
+            uint32_t e[16];
+            tc_ld16(taddr + s * cols + i * kLoraChunk, e);
+            tc_wait_ld();
 #pragma unroll
-            for (int n = 0; n < 8; n += 2) {
-              if (n * 8 < cols) {                       // cols is a multiple of 16: both column groups are there
-                uint32_t bf[4];
-                ldmatrix4(bf, tile_at(as, n * 8 + (lane & 7) + ((lane >> 4) << 3), kk * 2 + ((lane >> 3) & 1)));
-                mma16816(acc[n], af, bf[0], bf[1]);
-                mma16816(acc[n + 1], af, bf[2], bf[3]);
-              }
-            }
+            for (int j = 0; j < 16; ++j) d[j] = __float_as_uint(__uint_as_float(d[j]) + __uint_as_float(e[j]));
           }
-        }
-        if (++buf == kStages) buf = 0;
-        if (((step - k0) & 15) == 15 || step + 1 == k1) {         // the matrix unit's additions truncate: chains of 1024 products
+          const int v = L.chunk[c0 + i], a = v / (kLoraMaxRank / kLoraChunk), c = v % (kLoraMaxRank / kLoraChunk);
+          if (my == a) {
+            const int left = bank.rank[a] - c * kLoraChunk;         // ranks between the adapter's and the chunk's end are zero
+            const float scale = bank.scale[a];
+            float4* dst = reinterpret_cast<float4*>(parts == 1 ? s_out + (size_t)(t0 + row) * bank.rank_pad + c * kLoraChunk
+                                                               : reinterpret_cast<float*>(smem) + row * cols + i * kLoraChunk);
 #pragma unroll
-          for (int n = 0; n < 8; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { sum[n][i] += acc[n][i]; acc[n][i] = 0.f; }
-        }
-      }
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
-      __syncthreads();                                  // the next round overwrites the stages
-      if (live) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = warp * 16 + (lane >> 2) + h * 8;
-          if (id_s[r] != a) continue;
-          float* dst = s_part + (size_t)(t0 + r) * bank.rank_pad + r0;
-#pragma unroll
-          for (int n = 0; n < 8; ++n) {
-            const int c = n * 8 + (lane & 3) * 2;
-            if (c < cols) {
-              // ranks between the adapter's and the next multiple of 16 are exact zeros
-              float2 v = make_float2(r0 + c < rank ? scale * sum[n][2 * h] : 0.f, r0 + c + 1 < rank ? scale * sum[n][2 * h + 1] : 0.f);
-              *reinterpret_cast<float2*>(dst + c) = v;
+            for (int q = 0; q < 4; ++q) {
+              float4 f;
+              f.x = 4 * q + 0 < left ? scale * __uint_as_float(d[4 * q + 0]) : 0.f;
+              f.y = 4 * q + 1 < left ? scale * __uint_as_float(d[4 * q + 1]) : 0.f;
+              f.z = 4 * q + 2 < left ? scale * __uint_as_float(d[4 * q + 2]) : 0.f;
+              f.w = 4 * q + 3 < left ? scale * __uint_as_float(d[4 * q + 3]) : 0.f;
+              dst[q] = f;
             }
           }
         }
       }
     }
+    acc_phase ^= 1u;
+    if (parts > 1) {
+      // the ring holds the partial sums: every load of this pass has been consumed
+      cluster_sync_all();
+      const int r0 = rows * part / parts, r1 = rows * (part + 1) / parts;
+      const uint32_t base = smem_u32(smem);
+      for (int x = r0 * n * 4 + threadIdx.x; x < r1 * n * 4; x += kThreads) {
+        const int row = x / (n * 4), i = x / 4 % n, q = x % 4;
+        const int v = L.chunk[c0 + i], a = v / (kLoraMaxRank / kLoraChunk), c = v % (kLoraMaxRank / kLoraChunk);
+        if (L.id[row] != a) continue;
+        float4 f[kMaxParts];
+#pragma unroll
+        for (int p = 0; p < kMaxParts; ++p)
+          if (p < parts) f[p] = ld_cluster_f4(mapa(base + (uint32_t)((row * cols + i * kLoraChunk + q * 4) * 4), (uint32_t)p));
+        float4 o = f[0];
+#pragma unroll
+        for (int p = 1; p < kMaxParts; ++p)
+          if (p < parts) { o.x += f[p].x; o.y += f[p].y; o.z += f[p].z; o.w += f[p].w; }
+        *reinterpret_cast<float4*>(s_out + (size_t)(t0 + row) * bank.rank_pad + c * kLoraChunk + q * 4) = o;
+      }
+      fence_proxy_async_smem();                      // the next pass's loads write where the partial sums were
+      tc_fence_before();
+      cluster_sync_all();
+      tc_fence_after();
+    } else {
+      tc_fence_before();
+      __syncthreads();                               // the accumulator is read before the next pass writes it
+      tc_fence_after();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols) : "memory");
   }
 }
 
@@ -191,6 +275,8 @@ lora_pack_kernel(const uint16_t* __restrict__ down, int64_t down_stride, const u
   if (first == 0) { bank_rank[slot] = rank; bank_scale[slot] = scale; }
 }
 
+constexpr int kShortSmem = 76 * 1024, kLongSmem = 200 * 1024;
+
 }  // namespace
 
 cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const uint16_t* up, int64_t up_stride, int rank, float scale, int slot,
@@ -201,19 +287,45 @@ cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const ui
 }
 
 cudaError_t lora_shrink_setup() {
-  return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShrinkSmem);
+  return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLongSmem);
 }
 
-cudaError_t launch_lora_shrink(const uint16_t* x, int64_t x_stride, int T, int K, const int32_t* ids, const LoraBank& bank, int parts,
-                               int token_tile, int32_t* out_ids, int32_t* n_jobs, int32_t* jobs, float* s_out, int32_t* tile_counter,
-                               int32_t* status, cudaStream_t s) {
-  const int tiles = (T + kShrinkRows - 1) / kShrinkRows;
-  int stripes = 592 / (tiles * parts);                   // enough blocks to fill the device when a tile has many adapters
-  stripes = stripes < 1 ? 1 : stripes > 32 ? 32 : stripes;
-  if (stripes > bank.slots) stripes = bank.slots;
-  lora_shrink_kernel<<<dim3(tiles, parts, stripes), 128, kShrinkSmem, s>>>(x, x_stride, T, K, ids, bank, token_tile, out_ids, n_jobs, jobs,
-                                                                           s_out, tile_counter, status);
-  return cudaGetLastError();
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, const int32_t* ids,
+                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_jobs, int32_t* jobs, float* s_out,
+                               int32_t* tile_counter, int32_t* status, cudaStream_t s) {
+  // Short batches (those of the small projection kernel) leave shared memory for that kernel's blocks on the same SM and
+  // spread the adapters over many blocks; long ones take more ranks per pass and keep more of x in flight.
+  const bool is_short = token_tile != kLargeTok;
+  const int chunks = is_short ? 4 : 8, smem = is_short ? kShortSmem : kLongSmem;
+  const int stage = kXStage + chunks * kChunkStage;
+  int stages = (smem - 1024) / stage;
+  if (stages > kMaxStages) stages = kMaxStages;
+  const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
+  int parts = is_short ? kMaxParts : kSms / tiles;
+  if (parts > kMaxParts) parts = kMaxParts;
+  if (parts > steps) parts = steps;
+  if (parts < 1) parts = 1;
+  // passes a tile can need, and how many blocks share them
+  const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
+  const int passes = (adapters * (bank.rank_pad / kLoraChunk) + chunks - 1) / chunks;
+  int stripes = (is_short ? 2 : 1) * kSms / (tiles * parts);
+  if (stripes > passes) stripes = passes;
+  if (stripes < 1) stripes = 1;
+  const int part_steps = steps / parts;
+  int n_acc = (part_steps + kChainSteps - 1) / kChainSteps;
+  const int most = (is_short ? 128 : 512) / (chunks * kLoraChunk);
+  if (n_acc > most) n_acc = most;
+  if (n_acc < 1) n_acc = 1;
+  int tmem_cols = 32;
+  while (tmem_cols < n_acc * chunks * kLoraChunk) tmem_cols *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = (unsigned)parts;
+  cfg.gridDim = dim3(tiles, stripes, parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, lora_shrink_kernel, reinterpret_cast<const CUtensorMap&>(tm_x), reinterpret_cast<const CUtensorMap&>(tm_down), T, K,
+                            ids, bank, token_tile, box, chunks, stages, n_acc, tmem_cols, out_ids, n_jobs, jobs, s_out, tile_counter, status);
 }
 
 }  // namespace cep
