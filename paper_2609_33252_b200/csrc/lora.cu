@@ -15,7 +15,7 @@ struct cep_lora_plan {
   LoraBank bank;
   uint8_t* ws;
   int32_t* status; int32_t* tile_counter;
-  int32_t* ids; int32_t* n_jobs; int32_t* jobs;
+  int32_t* ids; int32_t* n_chunks; int32_t* chunks;
   float* s;
   // The plan's last enqueued work.  Work on another stream waits for it: the workspace and the bank are shared.
   cudaEvent_t last; cudaStream_t last_stream; bool have_last;
@@ -39,7 +39,7 @@ int check_config(const cep_lora_config* c) {
   return CEP_OK;
 }
 
-struct Carve { size_t status, tile_counter, ids, n_jobs, jobs, s, total; };
+struct Carve { size_t status, tile_counter, ids, n_chunks, chunks, s, total; };
 Carve carve(const cep_lora_config& c) {
   Carve w{};
   size_t o = 0;
@@ -49,8 +49,8 @@ Carve carve(const cep_lora_config& c) {
   take(w.tile_counter, 4);
   if (c.max_adapters) {
     take(w.ids, T * 4);
-    take(w.n_jobs, (T / 64 + 1) * 4);
-    take(w.jobs, up_to(T, kLargeTok) * 4);
+    take(w.n_chunks, (T / 64 + 1) * 4);
+    take(w.chunks, up_to(T, kLargeTok) * kLoraMaxChunks * 4);
     take(w.s, T * rank_pad_of(c) * 4);
   }
   w.total = o;
@@ -131,7 +131,7 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
   p->ws = static_cast<uint8_t*>(workspace);
   auto ints = [&](size_t off) { return reinterpret_cast<int32_t*>(p->ws + off); };
   p->status = ints(w.status); p->tile_counter = ints(w.tile_counter);
-  p->ids = ints(w.ids); p->n_jobs = ints(w.n_jobs); p->jobs = ints(w.jobs);
+  p->ids = ints(w.ids); p->n_chunks = ints(w.n_chunks); p->chunks = ints(w.chunks);
   p->s = reinterpret_cast<float*>(p->ws + w.s);
   uint8_t* bk = static_cast<uint8_t*>(bank);
   p->bank = LoraBank{reinterpret_cast<int32_t*>(bk + b.rank), reinterpret_cast<float*>(bk + b.scale), reinterpret_cast<uint16_t*>(bk + b.down),
@@ -217,10 +217,10 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
   a.y = y; a.y_stride = y_stride; a.tile_counter = p->tile_counter; a.status = p->status;
   cudaError_t e = cudaSuccess;
   if (adapter_ids) {
-    e = launch_lora_shrink(tm_x, p->tm_down, box, n_tokens, c.in_features, adapter_ids, p->bank, token_tile, p->ids, p->n_jobs, p->jobs, p->s,
+    e = launch_lora_shrink(tm_x, p->tm_down, box, n_tokens, c.in_features, adapter_ids, p->bank, token_tile, p->ids, p->n_chunks, p->chunks, p->s,
                            p->tile_counter, p->status, st);
     a.bank = &p->bank;
-    a.step = LoraStep{p->ids, p->n_jobs, p->jobs, p->s};
+    a.step = LoraStep{p->ids, p->n_chunks, p->chunks, p->s};
   }
   if (e == cudaSuccess) e = small ? launch_project_small(a, p->tm_w, tm_x, p->tm_up, st) : launch_project_large(a, p->tm_w, tm_x, p->tm_up, p->n_sms, st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: a launch failed: %s", cudaGetErrorString(e));

@@ -8,6 +8,7 @@ namespace cep {
 
 constexpr int kLoraChunk = 16;               // ranks per K step of the up projection (one bf16 MMA)
 constexpr int kLoraMaxRank = 256;
+constexpr int kLoraMaxChunks = kLoraMaxRank / kLoraChunk;
 constexpr int kLoraMaxAdapters = 4096;
 constexpr int kSms = 148;                    // K is split while the tiles are fewer than this
 constexpr int kSmallTok = 128;               // tokens per tile of the small kernel (fp32 outputs: 64)
@@ -25,18 +26,19 @@ struct LoraBank {
 // What the down projection leaves for the projection kernel.
 struct LoraStep {
   const int32_t* ids;                        // [T] usable adapter slot of each token, -1: none
-  const int32_t* n_jobs;                     // [token tiles] distinct adapters of a tile
-  const int32_t* jobs;                       // [token tiles][tile tokens] their slots, in order of first appearance
+  const int32_t* n_chunks;                   // [token tiles] chunks of 16 ranks of all distinct adapters of a tile
+  const int32_t* chunks;                     // [token tiles][tile tokens * 16] slot * 16 + chunk, adapters in order of appearance
   const float* s;                            // [T][rank_pad] scale * A_a x
 };
 
 cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const uint16_t* up, int64_t up_stride, int rank, float scale, int slot,
                              int K, int N, const LoraBank& bank, cudaStream_t s);
+bool lora_beside(int T);                     // the down projection runs beside the projection kernel on the same SMs
 cudaError_t lora_shrink_setup();             // once per plan, with its device current
 // tm_x: 64 columns x `box` rows; tm_down: the bank's down rows, 64 columns x 16 rows.  token_tile: tokens per tile of the
 // projection kernel that follows (its job lists are made here).
 cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, const int32_t* ids,
-                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_jobs, int32_t* jobs, float* s_out,
+                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* tile_counter, int32_t* status, cudaStream_t s);
 
 struct ProjectArgs {

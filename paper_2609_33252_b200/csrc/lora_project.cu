@@ -43,33 +43,32 @@ __device__ __forceinline__ uint64_t make_smem_desc_32b(uint32_t saddr) {
   return d;
 }
 
-// ------------------------------------------------------------------ rows of s as MMA operands
-// One step covers two chunks of 16 ranks.  Its operand row is 128 bytes: [value c0 | remainder c0 | value c1 | remainder c1].
-struct SRow {
-  uint32_t w[32];
-  // Splits chunks c0 and c0+1 (of nc) of a token's row of s.
-  __device__ __forceinline__ void fetch(const float* __restrict__ s, int c0, int nc) {
+// ------------------------------------------------------------------ the up projection's steps
+// A step covers kStep chunks of 16 ranks and takes a stage of the ring: the adapter's columns of B (by TMA) where the K steps
+// have W, and the tokens' rows of s (by the s-row warps) where they have x.  The loading thread tells those warps that the
+// stage is free (ready); they tell the MMA thread that the rows are written (sfull).
+constexpr int kStep = 2;
+
+// A chunk (16 ranks) of a token is 64 bytes of operand row, [value | remainder]; a 128-byte row holds two chunks.
+struct SChunk {
+  uint32_t w[16];
+  __device__ __forceinline__ void fetch(const float* __restrict__ s) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      if (c0 + c >= nc) break;
-      const float4* p = reinterpret_cast<const float4*>(s + (c0 + c) * kLoraChunk);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float4 v = __ldcg(p + q);
-        const uint32_t h0 = pack_bf16(v.x, v.y), h1 = pack_bf16(v.z, v.w);
-        w[c * 16 + 2 * q] = h0; w[c * 16 + 2 * q + 1] = h1;
-        w[c * 16 + 8 + 2 * q] = pack_bf16(v.x - __uint_as_float(h0 << 16), v.y - __uint_as_float(h0 & 0xffff0000u));
-        w[c * 16 + 8 + 2 * q + 1] = pack_bf16(v.z - __uint_as_float(h1 << 16), v.w - __uint_as_float(h1 & 0xffff0000u));
-      }
+    for (int q = 0; q < 4; ++q) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(s) + q);
+      const uint32_t h0 = pack_bf16(v.x, v.y), h1 = pack_bf16(v.z, v.w);
+      w[2 * q] = h0; w[2 * q + 1] = h1;
+      w[8 + 2 * q] = pack_bf16(v.x - __uint_as_float(h0 << 16), v.y - __uint_as_float(h0 & 0xffff0000u));
+      w[8 + 2 * q + 1] = pack_bf16(v.z - __uint_as_float(h1 << 16), v.w - __uint_as_float(h1 & 0xffff0000u));
     }
   }
-  // Writes row r of a 128-byte-swizzled tile (zeros when the token has another adapter).
-  __device__ __forceinline__ void put(uint8_t* tile, int r, bool mine) const {
+  // Writes half h of row r of a 128-byte-swizzled tile (zeros when the token has another adapter).
+  __device__ __forceinline__ void put(uint8_t* tile, int r, int h, bool mine) const {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < 4; ++j) {
       uint4 v = make_uint4(0, 0, 0, 0);
       if (mine) v = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-      *reinterpret_cast<uint4*>(tile + r * 128 + ((j ^ (r & 7)) << 4)) = v;
+      *reinterpret_cast<uint4*>(tile + r * 128 + (((h * 4 + j) ^ (r & 7)) << 4)) = v;
     }
   }
 };
@@ -78,9 +77,12 @@ template <typename OT> __device__ __forceinline__ void put_out(OT* p, float v);
 template <> __device__ __forceinline__ void put_out<float>(float* p, float v) { *p = v; }
 template <> __device__ __forceinline__ void put_out<__nv_bfloat16>(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
+// Index of a chunk's [N][16] block in the up bank.
+__device__ __forceinline__ int up_block(int v, int rank_pad) { return v / kLoraMaxChunks * (rank_pad / kLoraChunk) + v % kLoraMaxChunks; }
+
 struct LoraArgs {                                      // bank == nullptr on the host: has == 0
   int has, rank_pad;
-  const int32_t* rank; const int32_t* ids; const int32_t* n_jobs; const int32_t* jobs;
+  const int32_t* ids; const int32_t* n_chunks; const int32_t* chunks;
   const float* s;
 };
 
@@ -88,7 +90,7 @@ struct LoraArgs {                                      // bank == nullptr on the
 constexpr int kSmallThreads = 192;
 constexpr int kSmallMaxStages = 12;
 constexpr int kMaxSplits = 8;                          // CTAs of a portable cluster
-constexpr int kSBufs = 2;
+
 constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
 #ifndef CEP_LORA_SMALL_RING
 #define CEP_LORA_SMALL_RING (200 * 1024)
@@ -96,7 +98,7 @@ constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
 constexpr int kSmallRing = CEP_LORA_SMALL_RING;       // ring + s tiles
 constexpr int kSharedRing = 136 * 1024;               // the same beside a block of the down projection
 struct __align__(8) SmallBarriers {
-  uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], sfull[kSBufs], sempty[kSBufs], acc_full;
+  uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], ready[kSmallMaxStages], sfull[kSmallMaxStages], acc_full;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -112,8 +114,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const int x_stage = npad * kKBytes, stage_bytes = kWStage + x_stage;
-  uint8_t* s_tiles = smem + stages * stage_bytes;
-  SmallBarriers* bars = reinterpret_cast<SmallBarriers*>(s_tiles + kSBufs * x_stage);
+  SmallBarriers* bars = reinterpret_cast<SmallBarriers*>(smem + stages * stage_bytes);
   volatile int* abort_flag = &bars->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n0 = blockIdx.x * 128, t0 = blockIdx.z * tok;
@@ -122,8 +123,10 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   const int kb0 = (int)((long long)num_kb * split / splits), kb1 = (int)((long long)num_kb * (split + 1) / splits);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
-    for (int s = 0; s < kSBufs; ++s) { mbar_init(smem_u32(&bars->sfull[s]), 4); mbar_init(smem_u32(&bars->sempty[s]), 1); }
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1);
+      mbar_init(smem_u32(&bars->ready[s]), 1); mbar_init(smem_u32(&bars->sfull[s]), 4);
+    }
     mbar_init(smem_u32(&bars->acc_full), 1);
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -154,20 +157,17 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       }
       if (la.has && ok) {
         pdl_wait();
-        const int m = la.n_jobs[blockIdx.z];
-        for (int j = split; ok && j < m; j += splits) {
-          const int a = la.jobs[(size_t)blockIdx.z * tok + j];
-          const int nc = (la.rank[a] + kLoraChunk - 1) / kLoraChunk;
-          for (int c = 0; c < nc; c += 2) {
-            if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
-            const uint32_t full = smem_u32(&bars->full[stage]);
-            uint8_t* st = smem + stage * stage_bytes;
-            const int two = c + 1 < nc;
-            mbar_expect_tx(full, two ? 2 * kUpBytes : kUpBytes);
-            tma_load_3d(smem_u32(st), &tm_up, 0, n0, a * (la.rank_pad / kLoraChunk) + c, full);
-            if (two) tma_load_3d(smem_u32(st + kUpBytes), &tm_up, 0, n0, a * (la.rank_pad / kLoraChunk) + c + 1, full);
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
-          }
+        const int total = la.n_chunks[blockIdx.z];
+        const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
+        for (int c0 = split * kStep; c0 < total; c0 += splits * kStep) {
+          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) break;
+          const uint32_t full = smem_u32(&bars->full[stage]);
+          uint8_t* st = smem + stage * stage_bytes;
+          const int n = min(kStep, total - c0);
+          mbar_expect_tx(full, n * kUpBytes);
+          mbar_arrive(smem_u32(&bars->ready[stage]));
+          for (int i = 0; i < n; ++i) tma_load_3d(smem_u32(st + i * kUpBytes), &tm_up, 0, n0, up_block(list[c0 + i], la.rank_pad), full);
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
       }
     }
@@ -194,28 +194,24 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       }
       if (la.has && ok) {
         pdl_wait();
-        const int m = la.n_jobs[blockIdx.z];
+        const int total = la.n_chunks[blockIdx.z];
         const uint32_t last_acc = tmem + (uint32_t)(slab * npad);
-        int sb = 0; uint32_t sphase = 0;
-        for (int j = split; ok && j < m; j += splits) {
-          const int nc = (la.rank[la.jobs[(size_t)blockIdx.z * tok + j]] + kLoraChunk - 1) / kLoraChunk;
-          for (int c = 0; c < nc; c += 2) {
-            if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status) ||
-                !mbar_wait(smem_u32(&bars->sfull[sb]), sphase, abort_flag, status)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t up = smem_u32(smem + stage * stage_bytes);
-            const uint64_t sdesc = make_smem_desc(smem_u32(s_tiles + sb * x_stage));
-            const int n = c + 1 < nc ? 2 : 1;
-            for (int q = 0; q < n; ++q) {
-              const uint64_t udesc = make_smem_desc_32b(up + q * kUpBytes);
-              tc_mma_f16(last_acc, udesc, sdesc + (uint64_t)(q * 4), idesc, 1u);
-              tc_mma_f16(last_acc, udesc, sdesc + (uint64_t)(q * 4 + 2), idesc, 1u);
-            }
-            tc_commit(smem_u32(&bars->empty[stage]));
-            tc_commit(smem_u32(&bars->sempty[sb]));
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
-            if (++sb == kSBufs) { sb = 0; sphase ^= 1u; }
+        uint32_t sphase = 0;                             // one parity bit per stage
+        for (int c0 = split * kStep; c0 < total; c0 += splits * kStep) {
+          if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status) ||
+              !mbar_wait(smem_u32(&bars->sfull[stage]), (sphase >> stage) & 1u, abort_flag, status)) { ok = false; break; }
+          sphase ^= 1u << stage;
+          tc_fence_after();
+          const uint32_t up = smem_u32(smem + stage * stage_bytes);
+          const int n = min(kStep, total - c0);
+          for (int i = 0; i < n; ++i) {
+            const uint64_t udesc = make_smem_desc_32b(up + i * kUpBytes);
+            const uint64_t sdesc = make_smem_desc(up + kWStage) + (uint64_t)(i * 4);
+            tc_mma_f16(last_acc, udesc, sdesc, idesc, 1u);
+            tc_mma_f16(last_acc, udesc, sdesc + 2, idesc, 1u);
           }
+          tc_commit(smem_u32(&bars->empty[stage]));
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
       }
       if (ok) tc_commit(smem_u32(&bars->acc_full));
@@ -229,33 +225,44 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       const int t = t0 + tid;
       const int my = tid < npad && t < T ? la.ids[t] : -1;
       const float* srow = la.s + (size_t)(my >= 0 ? t : 0) * la.rank_pad;
-      const int my_nc = my >= 0 ? (la.rank[my] + kLoraChunk - 1) / kLoraChunk : 0;
-      SRow row0, row1;                                 // the first 64 ranks of this thread's token, fetched ahead
-      if (my >= 0) { row0.fetch(srow, 0, my_nc); row1.fetch(srow, 2, my_nc); }
-      const int m = la.n_jobs[blockIdx.z];
-      int sb = 0; uint32_t sphase = 0;
-      for (int j = split; ok && j < m; j += splits) {
-        const int a = la.jobs[(size_t)blockIdx.z * tok + j];
-        const int nc = (la.rank[a] + kLoraChunk - 1) / kLoraChunk;
-        for (int c = 0; c < nc; c += 2) {
-          ok = mbar_wait(smem_u32(&bars->sempty[sb]), sphase ^ 1u, abort_flag, status);
-          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-          uint8_t* tile = s_tiles + sb * x_stage;
-          if (tid < npad) {
-            const bool mine = my == a;
-            if (c == 0) row0.put(tile, tid, mine);
-            else if (c == 2) row1.put(tile, tid, mine);
-            else {
-              SRow r;
-              if (mine) r.fetch(srow, c, nc);
-              r.put(tile, tid, mine);
+      constexpr int kAhead = 4;
+      SChunk row[kAhead];                              // the first 64 ranks of this thread's token, fetched ahead
+#pragma unroll
+      for (int c = 0; c < kAhead; ++c)
+        if (my >= 0 && c * kLoraChunk < la.rank_pad) row[c].fetch(srow + c * kLoraChunk);
+      const int total = la.n_chunks[blockIdx.z];
+      const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
+      int stage = (kb1 - kb0) % stages;                // where the K steps end
+      uint32_t phase = 0;                              // one parity bit per stage
+      for (int c0 = split * kStep; c0 < total; c0 += splits * kStep) {
+        int v[kStep];
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) v[i] = c0 + i < total ? list[c0 + i] : -1;
+        ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        phase ^= 1u << stage;
+        uint8_t* rows = smem + stage * stage_bytes + kWStage;
+        if (tid < npad) {
+#pragma unroll
+          for (int i = 0; i < kStep; ++i) {
+            if (v[i] < 0) break;
+            const int c = v[i] % kLoraMaxChunks;
+            const bool mine = my == v[i] / kLoraMaxChunks;
+            if (c >= kAhead) {
+              SChunk r;
+              if (mine) r.fetch(srow + c * kLoraChunk);
+              r.put(rows, tid, i, mine);
+            } else {
+#pragma unroll
+              for (int k = 0; k < kAhead; ++k)
+                if (c == k) row[k].put(rows, tid, i, mine);
             }
           }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&bars->sfull[sb]));
-          if (++sb == kSBufs) { sb = 0; sphase ^= 1u; }
         }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->sfull[stage]));
+        if (++stage == stages) stage = 0;
       }
     }
     const bool got = ok && mbar_wait_relaxed(smem_u32(&bars->acc_full), 0u, abort_flag, status);
@@ -332,21 +339,24 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
 }
 
 // ------------------------------------------------------------------ large kernel
-constexpr int kLargeStages = 6;
+#ifndef CEP_LORA_LARGE_STAGES
+#define CEP_LORA_LARGE_STAGES 6
+#endif
+constexpr int kLargeStages = CEP_LORA_LARGE_STAGES;
 constexpr int kHalf = 128 * kKBytes;                   // one CTA's 128 rows of either operand: 16 KiB
 constexpr int kRing = 4;                               // tile ids in flight
 constexpr int kPoison = -2;
 constexpr int kLargeThreads = 352;                     // warp 0 loads, 1 MMA, 2-5 epilogue, 6 tile ids, 7-10 rows of s
 constexpr int kReaders = 19;                           // leader: loads, MMA, 4 epilogue, 4 s-row warps; peer: loads, 4, 4
 struct __align__(8) LargeBarriers {
-  uint64_t full[kLargeStages], empty[kLargeStages], acc_full[2], acc_empty[2], sfull[kSBufs], sempty[kSBufs];
+  uint64_t full[kLargeStages], empty[kLargeStages], ready[kLargeStages], sfull[kLargeStages], acc_full[2], acc_empty[2];
   uint64_t ring_full[kRing], ring_empty[kRing];
   int32_t ring_tile[kRing];
   uint32_t tmem_base;
   int abort_flag;
 };
 static_assert(sizeof(LargeBarriers) <= 512, "barrier block");
-constexpr int kLargeSmem = (kLargeStages * 2 + kSBufs) * kHalf + 512 + 1024;
+constexpr int kLargeSmem = kLargeStages * 2 * kHalf + 512 + 1024;
 static_assert(kLargeSmem <= 227 * 1024, "shared memory");
 
 // Reader side of the ring of tile ids (written by the leader's warp 6, into both CTAs); -1 ends the kernel.
@@ -386,17 +396,18 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* smem_x = smem;
   uint8_t* smem_w = smem + kLargeStages * kHalf;
-  uint8_t* s_tiles = smem_w + kLargeStages * kHalf;
-  LargeBarriers* bars = reinterpret_cast<LargeBarriers*>(s_tiles + kSBufs * kHalf);
+  LargeBarriers* bars = reinterpret_cast<LargeBarriers*>(smem_w + kLargeStages * kHalf);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const bool is_peer = rank != 0;
   volatile int* abort_flag = &bars->abort_flag;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kLargeStages; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
+    for (int s = 0; s < kLargeStages; ++s) {
+      mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1);
+      mbar_init(smem_u32(&bars->ready[s]), 1); mbar_init(smem_u32(&bars->sfull[s]), 8);
+    }
     for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->acc_full[s]), 1); mbar_init(smem_u32(&bars->acc_empty[s]), 8); }
-    for (int s = 0; s < kSBufs; ++s) { mbar_init(smem_u32(&bars->sfull[s]), 8); mbar_init(smem_u32(&bars->sempty[s]), 1); }
     for (int s = 0; s < kRing; ++s) {
       mbar_init(smem_u32(&bars->ring_full[s]), 1); mbar_init(smem_u32(&bars->ring_empty[s]), kReaders);
       bars->ring_tile[s] = kPoison;
@@ -439,21 +450,17 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           tma_load_2d_pair(smem_u32(smem_w + stage * kHalf), &tm_w, kb * (kKBytes / 2), n0, full);
           if (++stage == kLargeStages) { stage = 0; phase ^= 1u; }
         }
-        if (!la.has) continue;
-        const int jobs = la.n_jobs[m];
-        for (int j = 0; ok && j < jobs; ++j) {
-          const int a = la.jobs[(size_t)m * kLargeTok + j];
-          const int nc = (la.rank[a] + kLoraChunk - 1) / kLoraChunk;
-          for (int c = 0; c < nc; c += 2) {
-            if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
-            const uint32_t full = mapa(smem_u32(&bars->full[stage]), 0);
-            const int two = c + 1 < nc;
-            if (rank == 0) mbar_expect_tx(smem_u32(&bars->full[stage]), (two ? 4 : 2) * kUpBytes);
-            const int z = a * (la.rank_pad / kLoraChunk) + c;
-            tma_load_3d_pair(smem_u32(smem_w + stage * kHalf), &tm_up, 0, n0, z, full);
-            if (two) tma_load_3d_pair(smem_u32(smem_w + stage * kHalf + kUpBytes), &tm_up, 0, n0, z + 1, full);
-            if (++stage == kLargeStages) { stage = 0; phase ^= 1u; }
-          }
+        const int total = la.has ? la.n_chunks[m] : 0;
+        const int32_t* list = la.chunks + (size_t)m * kLargeTok * kLoraMaxChunks;
+        for (int c0 = 0; ok && c0 < total; c0 += kStep) {
+          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
+          const uint32_t full = mapa(smem_u32(&bars->full[stage]), 0);
+          const int n = min(kStep, total - c0);
+          if (rank == 0) mbar_expect_tx(smem_u32(&bars->full[stage]), 2 * n * kUpBytes);
+          mbar_arrive(smem_u32(&bars->ready[stage]));
+          for (int i = 0; i < n; ++i)
+            tma_load_3d_pair(smem_u32(smem_w + stage * kHalf + i * kUpBytes), &tm_up, 0, n0, up_block(list[c0 + i], la.rank_pad), full);
+          if (++stage == kLargeStages) { stage = 0; phase ^= 1u; }
         }
       }
     }
@@ -463,7 +470,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       constexpr uint32_t idesc = make_idesc_bf16(256, 256);
       int stage = 0; uint32_t phase = 0;
       int acc = 0; uint32_t acc_phase = 0;
-      int sb = 0; uint32_t sphase = 0;
+      uint32_t sphase = 0;                               // one parity bit per stage
       bool ok = true;
       RingReader rd;
       while (ok) {
@@ -497,25 +504,21 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         if (ok && la.has) {
           int m, nb;
           large_tile(tile, m_tiles, n_blocks, n_group, &m, &nb);
-          const int jobs = la.n_jobs[m];
-          for (int j = 0; ok && j < jobs; ++j) {
-            const int nc = (la.rank[la.jobs[(size_t)m * kLargeTok + j]] + kLoraChunk - 1) / kLoraChunk;
-            for (int c = 0; c < nc; c += 2) {
-              if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status) ||
-                  !mbar_wait_acq_cluster(smem_u32(&bars->sfull[sb]), sphase, abort_flag, status)) { ok = false; break; }
-              tc_fence_after();
-              const uint64_t sdesc = make_smem_desc(smem_u32(s_tiles + sb * kHalf));
-              const int n = c + 1 < nc ? 2 : 1;
-              for (int q = 0; q < n; ++q) {
-                const uint64_t udesc = make_smem_desc_32b(smem_u32(smem_w + stage * kHalf) + q * kUpBytes);
-                tc_mma_f16_pair(d, sdesc + (uint64_t)(q * 4), udesc, idesc, 1u);
-                tc_mma_f16_pair(d, sdesc + (uint64_t)(q * 4 + 2), udesc, idesc, 1u);
-              }
-              tc_commit_pair_both(smem_u32(&bars->empty[stage]), 3);
-              tc_commit_pair_both(smem_u32(&bars->sempty[sb]), 3);
-              if (++stage == kLargeStages) { stage = 0; phase ^= 1u; }
-              if (++sb == kSBufs) { sb = 0; sphase ^= 1u; }
+          const int total = la.n_chunks[m];
+          for (int c0 = 0; c0 < total; c0 += kStep) {
+            if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status) ||
+                !mbar_wait_acq_cluster(smem_u32(&bars->sfull[stage]), (sphase >> stage) & 1u, abort_flag, status)) { ok = false; break; }
+            sphase ^= 1u << stage;
+            tc_fence_after();
+            const uint64_t sdesc = make_smem_desc(smem_u32(smem_x + stage * kHalf));
+            const int n = min(kStep, total - c0);
+            for (int i = 0; i < n; ++i) {
+              const uint64_t udesc = make_smem_desc_32b(smem_u32(smem_w + stage * kHalf) + i * kUpBytes);
+              tc_mma_f16_pair(d, sdesc + (uint64_t)(i * 4), udesc, idesc, 1u);
+              tc_mma_f16_pair(d, sdesc + (uint64_t)(i * 4 + 2), udesc, idesc, 1u);
             }
+            tc_commit_pair_both(smem_u32(&bars->empty[stage]), 3);
+            if (++stage == kLargeStages) { stage = 0; phase ^= 1u; }
           }
         }
         if (!ok) break;
@@ -542,7 +545,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   } else if (warp >= 7) {
     // ---------------------------------------------------------------- rows of s (both CTAs, one token per thread)
     const int r = threadIdx.x - 7 * 32;
-    int sb = 0; uint32_t sphase = 0;
+    int stage = 0; uint32_t phase = 0;                   // phase: one parity bit per stage
     bool ok = true;
     RingReader rd;
     while (ok) {
@@ -556,21 +559,28 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       const int t = m * kLargeTok + (int)rank * 128 + r;
       const int my = t < T ? la.ids[t] : -1;
       const float* srow = la.s + (size_t)(my >= 0 ? t : 0) * la.rank_pad;
-      const int jobs = la.n_jobs[m];
-      for (int j = 0; ok && j < jobs; ++j) {
-        const int a = la.jobs[(size_t)m * kLargeTok + j];
-        const int nc = (la.rank[a] + kLoraChunk - 1) / kLoraChunk;
-        for (int c = 0; c < nc; c += 2) {
-          SRow row;
-          if (my == a) row.fetch(srow, c, nc);
-          ok = mbar_wait(smem_u32(&bars->sempty[sb]), sphase ^ 1u, abort_flag, status);
-          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-          row.put(s_tiles + sb * kHalf, r, my == a);
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_release_cluster(mapa(smem_u32(&bars->sfull[sb]), 0));
-          if (++sb == kSBufs) { sb = 0; sphase ^= 1u; }
+      const int total = la.n_chunks[m];
+      const int32_t* list = la.chunks + (size_t)m * kLargeTok * kLoraMaxChunks;
+      stage = (stage + num_kb) % kLargeStages;           // past the tile's K steps
+      for (int c0 = 0; c0 < total; c0 += kStep) {
+        SChunk row[kStep];
+        bool mine[kStep];
+        const int n = min(kStep, total - c0);
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) {
+          const int v = i < n ? list[c0 + i] : -1;
+          mine[i] = v >= 0 && my == v / kLoraMaxChunks;
+          if (mine[i]) row[i].fetch(srow + v % kLoraMaxChunks * kLoraChunk);
         }
+        ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        phase ^= 1u << stage;
+#pragma unroll
+        for (int i = 0; i < kStep; ++i) if (i < n) row[i].put(smem_x + stage * kHalf, r, i, mine[i]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_release_cluster(mapa(smem_u32(&bars->sfull[stage]), 0));
+        if (++stage == kLargeStages) stage = 0;
       }
     }
   } else {
@@ -662,8 +672,8 @@ cudaError_t device_slot(int* dev) {
 LoraArgs lora_args(const ProjectArgs& a) {
   LoraArgs la{};
   if (!a.bank) return la;
-  la.has = 1; la.rank_pad = a.bank->rank_pad; la.rank = a.bank->rank;
-  la.ids = a.step.ids; la.n_jobs = a.step.n_jobs; la.jobs = a.step.jobs; la.s = a.step.s;
+  la.has = 1; la.rank_pad = a.bank->rank_pad;
+  la.ids = a.step.ids; la.n_chunks = a.step.n_chunks; la.chunks = a.step.chunks; la.s = a.step.s;
   return la;
 }
 
@@ -740,10 +750,10 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   if (n_acc < 1) n_acc = 1;
   const int stage = kWStage + npad * kKBytes;
   // With adapters and few tokens the ring leaves room for a block of the down projection, so that both run at once.
-  const int ring = a.bank && a.T <= 64 ? kSharedRing : kSmallRing;
-  int stages = (ring - kSBufs * npad * kKBytes) / stage;
+  const int ring = a.bank && lora_beside(a.T) ? kSharedRing : kSmallRing;
+  int stages = ring / stage;
   if (stages > kSmallMaxStages) stages = kSmallMaxStages;
-  const size_t smem = 1024 + (size_t)stages * stage + kSBufs * npad * kKBytes + 512;
+  const size_t smem = 1024 + (size_t)stages * stage + 512;
   const size_t elt = a.out_f32 ? 4 : 2;
   const int vec_ok = reinterpret_cast<uintptr_t>(a.y) % (4 * elt) == 0 && a.y_stride % 4 == 0;
   attr[0].val.clusterDim.y = (unsigned)splits;

@@ -32,7 +32,7 @@ struct __align__(8) ShrinkBarriers {
 };
 struct ShrinkLists {                                 // scratch of the list building
   int id[kLargeTok], job[kLargeTok], n_chunks, warp_count[8];
-  int chunk[kRows * (kLoraMaxRank / kLoraChunk)];    // adapter * 16 + chunk of its ranks
+  int chunk[kRows * kLoraMaxChunks];    // adapter * 16 + chunk of its ranks
 };
 
 // The slot a token's adapter id names, -1 for none; an id that names nothing loaded is reported and treated as none.
@@ -66,17 +66,33 @@ __device__ int distinct_in_order(const int* v, int n, int* table, int* out, int*
   return total;
 }
 
+// The adapters job[0..m) as chunks of 16 ranks, in order -> out; returns their number (warp 0 only, all lanes).
+__device__ int expand_chunks(const int* job, int m, const LoraBank& bank, int* out) {
+  const int lane = threadIdx.x & 31;
+  int base = 0;
+  for (int j0 = 0; j0 < m; j0 += 32) {
+    const int a = j0 + lane < m ? job[j0 + lane] : -1;
+    const int nc = a >= 0 ? (bank.rank[a] + kLoraChunk - 1) / kLoraChunk : 0;
+    int incl = nc;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+    for (int c = 0; c < nc; ++c) out[base + incl - nc + c] = a * kLoraMaxChunks + c;
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return base;
+}
+
 // Grid (token tiles, pass stripes, K parts); the parts are a cluster.  box: rows of x one TMA load brings.
 __global__ void __launch_bounds__(kThreads)
 lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K,
-                   const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int chunks, int stages, int n_acc,
-                   int tmem_cols, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_jobs, int32_t* __restrict__ jobs,
+                   const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int x_stage, int chunks, int stages, int n_acc,
+                   int tmem_cols, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_chunks, int32_t* __restrict__ chunk_lists,
                    float* __restrict__ s_out, int32_t* __restrict__ tile_counter, int32_t* __restrict__ status) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ ShrinkBarriers bars;
   __shared__ ShrinkLists L;
-  const int stage_bytes = kXStage + chunks * kChunkStage;
+  const int stage_bytes = x_stage + chunks * kChunkStage;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &bars.abort_flag;
   const int t0 = blockIdx.x * kRows, rows = min(kRows, T - t0);
@@ -103,15 +119,17 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
 
   // ---------------------------------------------------------------- lists (the ring is not in use yet and holds the table)
   int* table = reinterpret_cast<int*>(smem);
-  if (reporter) {
-    // the projection kernel's tiles that start among these tokens: two of 64, one of 128, every other time one of 256
+  if (reporter && token_tile != kRows) {
+    // the projection kernel's tiles that start among these tokens: two of 64, every other time one of 256
     for (int a = t0; a < t0 + rows && a % token_tile == 0; a += token_tile) {
       const int n = min(token_tile, T - a);
       for (int i = threadIdx.x; i < n; i += kThreads) L.id[i] = usable_id(ids, a + i, bank, status, false);
       __syncthreads();
       const int m = distinct_in_order(L.id, n, table, L.job, L.warp_count);
-      for (int i = threadIdx.x; i < m; i += kThreads) jobs[(size_t)a + i] = L.job[i];
-      if (threadIdx.x == 0) n_jobs[a / token_tile] = m;
+      if (warp == 0) {
+        const int nc = expand_chunks(L.job, m, bank, chunk_lists + (size_t)a * kLoraMaxChunks);
+        if (lane == 0) n_chunks[a / token_tile] = nc;
+      }
       __syncthreads();
     }
   }
@@ -123,17 +141,8 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   __syncthreads();
   const int m = distinct_in_order(L.id, rows, table, L.job, L.warp_count);
   if (warp == 0) {
-    int base = 0;
-    for (int j0 = 0; j0 < m; j0 += 32) {
-      const int a = j0 + lane < m ? L.job[j0 + lane] : -1;
-      const int nc = a >= 0 ? (bank.rank[a] + kLoraChunk - 1) / kLoraChunk : 0;
-      int incl = nc;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
-      for (int c = 0; c < nc; ++c) L.chunk[base + incl - nc + c] = a * (kLoraMaxRank / kLoraChunk) + c;
-      base += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    if (lane == 0) L.n_chunks = base;
+    const int nc = expand_chunks(L.job, m, bank, L.chunk);
+    if (lane == 0) L.n_chunks = nc;
   }
   fence_proxy_async_smem();                          // the table's words become TMA destinations
   tc_fence_before();
@@ -141,6 +150,10 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   tc_fence_after();
   const uint32_t tmem = bars.tmem_base;
   const int total = L.n_chunks, steps = (K + 63) >> 6;
+  if (reporter && token_tile == kRows) {
+    for (int i = threadIdx.x; i < total; i += kThreads) chunk_lists[(size_t)t0 * kLoraMaxChunks + i] = L.chunk[i];
+    if (threadIdx.x == 0) n_chunks[blockIdx.x] = total;
+  }
   const int k0 = (int)((long long)steps * part / parts), k1 = (int)((long long)steps * (part + 1) / parts);
   const int cols = chunks * kLoraChunk;              // columns of an accumulator
   int stage = 0; uint32_t phase = 0, acc_phase = 0;  // the loading and the issuing thread each keep their own
@@ -156,8 +169,8 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
         mbar_expect_tx(full, boxes * box * 128 + n * kChunkStage);
         for (int b = 0; b < boxes; ++b) tma_load_2d(smem_u32(st + b * box * 128), &tm_x, k * 64, t0 + b * box, full);
         for (int i = 0; i < n; ++i) {
-          const int v = L.chunk[c0 + i], a = v / (kLoraMaxRank / kLoraChunk), c = v % (kLoraMaxRank / kLoraChunk);
-          tma_load_2d(smem_u32(st + kXStage + i * kChunkStage), &tm_down, k * 64, a * bank.rank_pad + c * kLoraChunk, full);
+          const int v = L.chunk[c0 + i], a = v / kLoraMaxChunks, c = v % kLoraMaxChunks;
+          tma_load_2d(smem_u32(st + x_stage + i * kChunkStage), &tm_down, k * 64, a * bank.rank_pad + c * kLoraChunk, full);
         }
         if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
@@ -171,7 +184,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
         tc_fence_after();
         if (k == slab_end) { ++slab; slab_end = k0 + (int)((long long)(k1 - k0) * (slab + 1) / n_acc); more = 0; }
         const uint64_t xdesc = make_smem_desc(smem_u32(smem + stage * stage_bytes));
-        const uint64_t adesc = make_smem_desc(smem_u32(smem + stage * stage_bytes + kXStage));
+        const uint64_t adesc = make_smem_desc(smem_u32(smem + stage * stage_bytes + x_stage));
 #pragma unroll
         for (int k4 = 0; k4 < 4; ++k4)
           tc_mma_f16(tmem + (uint32_t)(slab * cols), xdesc + (uint64_t)(k4 * 2), adesc + (uint64_t)(k4 * 2), idesc, k4 != 0 ? 1u : more);
@@ -199,7 +212,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
 #pragma unroll
             for (int j = 0; j < 16; ++j) d[j] = __float_as_uint(__uint_as_float(d[j]) + __uint_as_float(e[j]));
           }
-          const int v = L.chunk[c0 + i], a = v / (kLoraMaxRank / kLoraChunk), c = v % (kLoraMaxRank / kLoraChunk);
+          const int v = L.chunk[c0 + i], a = v / kLoraMaxChunks, c = v % kLoraMaxChunks;
           if (my == a) {
             const int left = bank.rank[a] - c * kLoraChunk;         // ranks between the adapter's and the chunk's end are zero
             const float scale = bank.scale[a];
@@ -226,7 +239,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
       const uint32_t base = smem_u32(smem);
       for (int x = r0 * n * 4 + threadIdx.x; x < r1 * n * 4; x += kThreads) {
         const int row = x / (n * 4), i = x / 4 % n, q = x % 4;
-        const int v = L.chunk[c0 + i], a = v / (kLoraMaxRank / kLoraChunk), c = v % (kLoraMaxRank / kLoraChunk);
+        const int v = L.chunk[c0 + i], a = v / kLoraMaxChunks, c = v % kLoraMaxChunks;
         if (L.id[row] != a) continue;
         float4 f[kMaxParts];
 #pragma unroll
@@ -275,7 +288,7 @@ lora_pack_kernel(const uint16_t* __restrict__ down, int64_t down_stride, const u
   if (first == 0) { bank_rank[slot] = rank; bank_scale[slot] = scale; }
 }
 
-constexpr int kShortSmem = 76 * 1024, kLongSmem = 200 * 1024;
+constexpr int kShortSmem = 76 * 1024, kLongSmem = 97 * 1024;
 
 }  // namespace
 
@@ -286,34 +299,38 @@ cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const ui
   return cudaGetLastError();
 }
 
+bool lora_beside(int T) { return T <= 64; }
+
 cudaError_t lora_shrink_setup() {
   return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLongSmem);
 }
 
 cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, const int32_t* ids,
-                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_jobs, int32_t* jobs, float* s_out,
+                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* tile_counter, int32_t* status, cudaStream_t s) {
-  // Short batches (those of the small projection kernel) leave shared memory for that kernel's blocks on the same SM and
-  // spread the adapters over many blocks; long ones take more ranks per pass and keep more of x in flight.
-  const bool is_short = token_tile != kLargeTok;
-  const int chunks = is_short ? 4 : 8, smem = is_short ? kShortSmem : kLongSmem;
-  const int stage = kXStage + chunks * kChunkStage;
-  int stages = (smem - 1024) / stage;
+  // Up to 64 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
+  const bool beside = lora_beside(T);
+  const int chunks = 8, smem = beside ? kShortSmem : kLongSmem;
+  // With fewer than 128 tokens the M side's missing rows are whatever follows in shared memory (their products are not read):
+  // a stage may be smaller than the operand, the ring as a whole may not.
+  const int x_stage = T < kRows ? (T + box - 1) / box * box * 128 : kXStage;
+  const int stage = x_stage + chunks * kChunkStage;
+  int stages = 1 + (smem - 1024 - (stage > kXStage ? stage : kXStage)) / stage;
   if (stages > kMaxStages) stages = kMaxStages;
   const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
-  int parts = is_short ? kMaxParts : kSms / tiles;
+  int parts = kSms / tiles;
   if (parts > kMaxParts) parts = kMaxParts;
   if (parts > steps) parts = steps;
   if (parts < 1) parts = 1;
   // passes a tile can need, and how many blocks share them
   const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
   const int passes = (adapters * (bank.rank_pad / kLoraChunk) + chunks - 1) / chunks;
-  int stripes = (is_short ? 2 : 1) * kSms / (tiles * parts);
+  int stripes = 2 * kSms / (tiles * parts);
   if (stripes > passes) stripes = passes;
   if (stripes < 1) stripes = 1;
   const int part_steps = steps / parts;
   int n_acc = (part_steps + kChainSteps - 1) / kChainSteps;
-  const int most = (is_short ? 128 : 512) / (chunks * kLoraChunk);
+  const int most = (beside ? 128 : 256) / (chunks * kLoraChunk);        // two blocks share an SM's tensor memory
   if (n_acc > most) n_acc = most;
   if (n_acc < 1) n_acc = 1;
   int tmem_cols = 32;
@@ -325,7 +342,7 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   cfg.gridDim = dim3(tiles, stripes, parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
   cfg.attrs = attr; cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, lora_shrink_kernel, reinterpret_cast<const CUtensorMap&>(tm_x), reinterpret_cast<const CUtensorMap&>(tm_down), T, K,
-                            ids, bank, token_tile, box, chunks, stages, n_acc, tmem_cols, out_ids, n_jobs, jobs, s_out, tile_counter, status);
+                            ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, tile_counter, status);
 }
 
 }  // namespace cep
