@@ -122,6 +122,14 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   constexpr int kCols = sizeof(OT) == 4 ? 512 : kSmallTok;           // tensor-memory columns
   const int kb0 = (int)((long long)num_kb * split / splits), kb1 = (int)((long long)num_kb * (split + 1) / splits);
 
+  // The K steps of x and W do not depend on the down projection: they start before it has finished.
+  auto load_k_step = [&](int kb, int stage) {
+    const uint32_t full = smem_u32(&bars->full[stage]);
+    uint8_t* st = smem + stage * stage_bytes;
+    mbar_expect_tx(full, stage_bytes);
+    tma_load_2d(smem_u32(st), &tm_w, kb * (kKBytes / 2), n0, full);
+    tma_load_2d(smem_u32(st + kWStage), &tm_x, kb * (kKBytes / 2), t0, full);
+  };
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
       mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1);
@@ -130,6 +138,8 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     mbar_init(smem_u32(&bars->acc_full), 1);
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    // the ring is empty: its first loads go out before the rest of the block is set up
+    for (int s = 0; s < stages && kb0 + s < kb1; ++s) load_k_step(kb0 + s, s);
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -141,18 +151,14 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
 
-  // The K steps of x and W do not depend on the down projection: they start before it has finished.
   if (warp == 0) {
     if (lane == 0) {
-      int stage = 0; uint32_t phase = 0;
+      const int ahead = min(stages, kb1 - kb0);        // loaded above
+      int stage = ahead % stages; uint32_t phase = ahead == stages;
       bool ok = true;
-      for (int kb = kb0; kb < kb1; ++kb) {
+      for (int kb = kb0 + ahead; kb < kb1; ++kb) {
         if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
-        const uint32_t full = smem_u32(&bars->full[stage]);
-        uint8_t* st = smem + stage * stage_bytes;
-        mbar_expect_tx(full, stage_bytes);
-        tma_load_2d(smem_u32(st), &tm_w, kb * (kKBytes / 2), n0, full);
-        tma_load_2d(smem_u32(st + kWStage), &tm_x, kb * (kKBytes / 2), t0, full);
+        load_k_step(kb, stage);
         if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
       if (la.has && ok) {

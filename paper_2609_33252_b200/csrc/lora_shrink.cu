@@ -99,6 +99,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   const int part = blockIdx.z, parts = gridDim.z;
   const bool reporter = blockIdx.y == 0 && part == 0;
 
+  if (threadIdx.x == 32) { prefetch_map(&tm_x); prefetch_map(&tm_down); }
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars.full[s]), 1); mbar_init(smem_u32(&bars.empty[s]), 1); }
     mbar_init(smem_u32(&bars.acc_full), 1);
@@ -302,7 +303,11 @@ cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const ui
 bool lora_beside(int T) { return T <= 64; }
 
 cudaError_t lora_shrink_setup() {
-  return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLongSmem);
+  cudaError_t e = cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLongSmem);
+  if (e != cudaSuccess) return e;
+  // all of the SM's memory as shared memory: with a smaller split the projection kernel's blocks would have to wait for the
+  // SM to run empty before the split can change
+  return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
 cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, const int32_t* ids,
@@ -318,14 +323,14 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   int stages = 1 + (smem - 1024 - (stage > kXStage ? stage : kXStage)) / stage;
   if (stages > kMaxStages) stages = kMaxStages;
   const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
-  int parts = kSms / tiles;
+  int parts = 2 * kSms / tiles;
   if (parts > kMaxParts) parts = kMaxParts;
   if (parts > steps) parts = steps;
   if (parts < 1) parts = 1;
   // passes a tile can need, and how many blocks share them
   const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
   const int passes = (adapters * (bank.rank_pad / kLoraChunk) + chunks - 1) / chunks;
-  int stripes = 2 * kSms / (tiles * parts);
+  int stripes = 4 * kSms / (tiles * parts);
   if (stripes > passes) stripes = passes;
   if (stripes < 1) stripes = 1;
   const int part_steps = steps / parts;
