@@ -333,7 +333,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         if (left > 3) put_out(row + 3, o.w);
       }
     }
-    cluster_sync_all();                                // no CTA leaves while another reads its sums
+    cluster_sync_reads();                              // no CTA leaves while another reads its sums
   }
   tc_fence_before();
   __syncthreads();

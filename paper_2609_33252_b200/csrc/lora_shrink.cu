@@ -84,7 +84,7 @@ __device__ int expand_chunks(const int* job, int m, const LoraBank& bank, int* o
 
 // Grid (token tiles, pass stripes, K parts); the parts are a cluster.  box: rows of x one TMA load brings.
 __global__ void __launch_bounds__(kThreads)
-lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K,
+lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K, int N,
                    const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int x_stage, int chunks, int stages, int n_acc,
                    int tmem_cols, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_chunks, int32_t* __restrict__ chunk_lists,
                    float* __restrict__ s_out, int32_t* __restrict__ tile_counter, int32_t* __restrict__ status) {
@@ -161,6 +161,15 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
 
   for (int c0 = blockIdx.y * chunks; c0 < total; c0 += gridDim.y * chunks) {
     const int n = min(chunks, total - c0);
+    if (N > 0 && warp == 5 && lane < n) {
+      // a short batch meets each adapter's columns of B for the first time in the projection's last steps: have them in the
+      // L2 by then (each part asks for its share)
+      const size_t block = (size_t)N * kLoraChunk * 2;
+      const size_t b0 = block * part / parts / 16 * 16, b1 = part + 1 == parts ? block : block * (part + 1) / parts / 16 * 16;
+      const int v = L.chunk[c0 + lane];
+      const uint8_t* up = reinterpret_cast<const uint8_t*>(bank.up) + (size_t)(v / kLoraMaxChunks * (bank.rank_pad / kLoraChunk) + v % kLoraMaxChunks) * block;
+      if (b1 > b0) prefetch_l2(up + b0, (uint32_t)(b1 - b0));
+    }
     if (warp == 0 && lane == 0) {
       const int boxes = (rows + box - 1) / box;
       for (int k = k0; k < k1; ++k) {
@@ -310,12 +319,12 @@ cudaError_t lora_shrink_setup() {
   return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
-cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, const int32_t* ids,
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* tile_counter, int32_t* status, cudaStream_t s) {
   // Up to 64 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
   const bool beside = lora_beside(T);
-  const int chunks = 8, smem = beside ? kShortSmem : kLongSmem;
+  const int chunks = beside ? 4 : 8, smem = beside ? kShortSmem : kLongSmem;
   // With fewer than 128 tokens the M side's missing rows are whatever follows in shared memory (their products are not read):
   // a stage may be smaller than the operand, the ring as a whole may not.
   const int x_stage = T < kRows ? (T + box - 1) / box * box * 128 : kXStage;
@@ -347,7 +356,7 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   cfg.gridDim = dim3(tiles, stripes, parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
   cfg.attrs = attr; cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, lora_shrink_kernel, reinterpret_cast<const CUtensorMap&>(tm_x), reinterpret_cast<const CUtensorMap&>(tm_down), T, K,
-                            ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, tile_counter, status);
+                            token_tile == kLargeTok ? 0 : N, ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, tile_counter, status);
 }
 
 }  // namespace cep
