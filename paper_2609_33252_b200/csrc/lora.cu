@@ -148,7 +148,9 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
   e = cudaEventCreateWithFlags(&p->last, cudaEventDisableTiming);
   if (e != cudaSuccess) { p->last = nullptr; return give_up(CEP_ERR_CUDA, "cudaEventCreateWithFlags", e); }
   e = lora_shrink_setup();
-  if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaFuncSetAttribute", e);
+  if (e == cudaSuccess) e = project_small_setup(p->device);
+  if (e == cudaSuccess) e = project_large_setup(p->device, p->n_sms);
+  if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "setting up the kernels", e);
   int m = make_tile_map(&p->tm_w, weight, cfg->in_features, cfg->out_features, weight_stride * 2, 0, 0, 64, 128, 128);
   p->tm_up = p->tm_down = p->tm_w;                        // (not read without adapters)
   if (!m && cfg->max_adapters)
@@ -202,7 +204,10 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
     return record_error(CEP_ERR_ARG, "lora: y is misaligned or its rows lie less than out_features apart");
   if (adapter_ids && !c.max_adapters) return record_error(CEP_ERR_ARG, "lora: adapter ids given to a plan without adapters");
   if (!on(adapter_ids, 4)) return record_error(CEP_ERR_ARG, "lora: adapter_ids is misaligned");
-  const bool small = project_is_small(n_tokens, c.out_features);
+  // Up to 128 tokens the small kernel's tile is no wider than the batch; beyond, the kernel whose busiest SM has less to do.
+  const bool small = n_tokens <= kSmallTok || (n_tokens <= 4 * kSmallTok &&
+                     project_small_cost(p->device, n_tokens, c.out_features, c.in_features, c.out_elem == CEP_ELEM_FP32) <=
+                     project_large_cost(p->device, n_tokens, c.out_features, c.in_features));
   const int f32 = c.out_elem == CEP_ELEM_FP32;
   const int token_tile = small ? project_small_tile(f32) : kLargeTok, box = small ? project_small_tokens(n_tokens, f32) : 128;
   GemmTensorMap tm_x;
@@ -222,7 +227,8 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
     a.bank = &p->bank;
     a.step = LoraStep{p->ids, p->n_chunks, p->chunks, p->s};
   }
-  if (e == cudaSuccess) e = small ? launch_project_small(a, p->tm_w, tm_x, p->tm_up, st) : launch_project_large(a, p->tm_w, tm_x, p->tm_up, p->n_sms, st);
+  if (e == cudaSuccess) e = small ? launch_project_small(a, p->tm_w, tm_x, p->tm_up, p->device, st)
+                                  : launch_project_large(a, p->tm_w, tm_x, p->tm_up, p->device, st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: a launch failed: %s", cudaGetErrorString(e));
   return leave(p, st, capturing);
 }

@@ -1,5 +1,6 @@
 // Internal interface of the projection with per-request low-rank adapters (lora.cu: plan and C ABI; lora_shrink.cu: the
-// down projection x A^T; lora_project.cu: the shared projection with the up projection inside its accumulator).
+// down projection A x; lora_project_small.cu, lora_project_large.cu: the shared projection with the up projection inside its
+// accumulator).
 #pragma once
 #include "cep_common.h"
 #include "gemm_tcgen05.h"
@@ -53,11 +54,16 @@ struct ProjectArgs {
 // Tensor maps are encoded per call for x and once for the weight and the up bank.
 int make_tile_map(GemmTensorMap* out, const void* base, long long cols, long long rows, long long row_stride, long long depth,
                   long long depth_stride, int box_cols, int box_rows, int swizzle_bytes);
+// Once per plan, with the device current: launch attributes and how many clusters fit.
+cudaError_t project_small_setup(int dev);
+cudaError_t project_large_setup(int dev, int n_sms);
+// Work of the busiest SM, in K steps of a tile (both kernels' steps take about the same time).
+long long project_small_cost(int dev, int T, int N, int K, int out_f32);
+long long project_large_cost(int dev, int T, int N, int K);
 cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,
-                                 cudaStream_t s);
+                                 int dev, cudaStream_t s);
 cudaError_t launch_project_large(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,
-                                 int n_sms, cudaStream_t s);
-bool project_is_small(int T, int N);
+                                 int dev, cudaStream_t s);
 int project_small_tile(int out_f32);                // tokens per tile of the small kernel
 int project_small_tokens(int T, int out_f32);       // token columns of its MMA: T rounded up to 16, at most the tile's
 

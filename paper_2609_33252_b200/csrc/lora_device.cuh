@@ -1,0 +1,80 @@
+// What the two projection kernels share: operand descriptors, rows of s as operands, the lists of the down projection.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "lora.h"
+#include "lora_ptx.cuh"
+
+namespace cep {
+
+using ptx::pack_bf16;
+
+constexpr int kKBytes = 128;                          // bytes of K per stage: one 128-byte swizzle span, 64 bf16
+constexpr int kUpBytes = 128 * 32;                    // 128 columns x one chunk of 16 ranks, 32-byte rows
+constexpr int kSlabSteps = 12;                        // K steps (of 64) per accumulation chain of an fp32 output
+// The up projection's steps.  A step covers kStep chunks of 16 ranks and takes a stage of the ring: the adapter's columns of
+// B (by TMA) where the K steps have W, and the tokens' rows of s (by the s-row warps) where they have x.  The loading thread
+// tells those warps that the stage is free (ready); they tell the MMA thread that the rows are written (sfull).  The fence
+// between their stores and the MMA costs as much as the stores, so kBatch steps share one.
+constexpr int kStep = 2;
+constexpr int kBatch = 2;
+
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// K-major operand with rows of 32 bytes (16 ranks), 32-byte swizzle, 8-row groups 256 bytes apart
+__device__ __forceinline__ uint64_t make_smem_desc_32b(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)1 << 16;
+  d |= (uint64_t)(256 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)6 << 61;
+  return d;
+}
+
+// A chunk (16 ranks) of a token is 64 bytes of operand row, [value | remainder]; a 128-byte row holds two chunks.
+struct SChunk {
+  uint32_t w[16];
+  __device__ __forceinline__ void fetch(const float* __restrict__ s) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(s) + q);
+      const uint32_t h0 = pack_bf16(v.x, v.y), h1 = pack_bf16(v.z, v.w);
+      w[2 * q] = h0; w[2 * q + 1] = h1;
+      w[8 + 2 * q] = pack_bf16(v.x - __uint_as_float(h0 << 16), v.y - __uint_as_float(h0 & 0xffff0000u));
+      w[8 + 2 * q + 1] = pack_bf16(v.z - __uint_as_float(h1 << 16), v.w - __uint_as_float(h1 & 0xffff0000u));
+    }
+  }
+  // Writes half h of row r of a 128-byte-swizzled tile (zeros when the token has another adapter).
+  __device__ __forceinline__ void put(uint8_t* tile, int r, int h, bool mine) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (mine) v = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+      *reinterpret_cast<uint4*>(tile + r * 128 + (((h * 4 + j) ^ (r & 7)) << 4)) = v;
+    }
+  }
+};
+
+template <typename OT> __device__ __forceinline__ void put_out(OT* p, float v);
+template <> __device__ __forceinline__ void put_out<float>(float* p, float v) { *p = v; }
+template <> __device__ __forceinline__ void put_out<__nv_bfloat16>(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// The lists and s as the kernels read them; has == 0: no adapters in this call.  The lists are read past the L1: they are
+// rewritten by every call.
+struct LoraArgs {
+  int has, rank_pad;
+  const int32_t* ids; const int32_t* n_chunks; const int32_t* chunks;
+  const float* s;
+};
+// Index of a chunk's [N][16] block in the up bank.
+__device__ __forceinline__ int up_block(int v, int rank_pad) { return v / kLoraMaxChunks * (rank_pad / kLoraChunk) + v % kLoraMaxChunks; }
+
+inline LoraArgs lora_args(const ProjectArgs& a) {
+  LoraArgs la{};
+  if (!a.bank) return la;
+  la.has = 1; la.rank_pad = a.bank->rank_pad;
+  la.ids = a.step.ids; la.n_chunks = a.step.n_chunks; la.chunks = a.step.chunks; la.s = a.step.s;
+  return la;
+}
+
+}  // namespace cep

@@ -1,0 +1,386 @@
+// The shared projection with the adapters' up projection inside its accumulator, for short batches (for long ones:
+// lora_project_large.cu):
+//
+//   y[t,n] = sum_k x[t,k] W[n,k] + sum_r s[t,r] B_a[n,r],   a = adapter of token t, s = scale_a * A_a x (lora_shrink.cu)
+//
+// The adapters are further K steps of the same matrix product: for every 32 ranks of the adapters present among the tokens
+// one more step multiplies the tokens' rows of s (rows of other adapters: zeros) with the adapter's columns of B.  So the up
+// projection adds neither a pass over y nor a rounding of it.  s is fp32; the tensor core takes it as the sum of two bf16
+// terms (value and remainder, 2^-17 relative), two MMAs against the same columns of B.
+//
+// A short batch is bound by reading W once.  W is the M side of the MMA (128 columns of y), up to 128 tokens the N side, so a
+// token costs a column of the accumulator and not a row of 128; K is split over the CTAs of a cluster so that W streams
+// through as many SMs as there are, and the CTAs exchange their partial sums through shared memory, each adding a share of
+// the tokens in split order (the result does not depend on timing).  Warp-specialised, TMA-fed, fp32 accumulators in tensor
+// memory, every wait bounded (status word).
+//
+// The tensor core's fp32 additions truncate: one chain over K = 7168 ends 8e-6 low on average (measured), which a bf16
+// output does not see and an fp32 output does.  fp32 outputs are summed from several accumulators of about 768 products.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "lora_device.cuh"
+
+namespace cep {
+namespace {
+
+using namespace ptx;
+
+constexpr int kSmallThreads = 192;
+constexpr int kSmallMaxStages = 12;
+constexpr int kMaxSplits = 8;                          // CTAs of a portable cluster
+constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
+constexpr int kSmallRing = 200 * 1024;
+constexpr int kSharedRing = 136 * 1024;               // the same beside a block of the down projection
+struct __align__(8) SmallBarriers {
+  uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], ready[kSmallMaxStages], sfull[kSmallMaxStages], acc_full;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(SmallBarriers) <= 512, "barrier block");
+
+// Grid (column tiles, K splits, token tiles of `tok`).  npad: token columns of the MMA, a multiple of 16.  n_acc: accumulators
+// (npad columns each) that share the CTA's K steps.
+template <typename OT>
+__global__ void __launch_bounds__(kSmallThreads, 1)
+project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
+                     const __grid_constant__ CUtensorMap tm_up, int T, int N, int num_kb, int tok, int npad, int stages, int n_acc, const LoraArgs la,
+                     OT* __restrict__ y, int64_t y_stride, int vec_ok, int32_t* __restrict__ status) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const int x_stage = npad * kKBytes, stage_bytes = kWStage + x_stage;
+  SmallBarriers* bars = reinterpret_cast<SmallBarriers*>(smem + stages * stage_bytes);
+  volatile int* abort_flag = &bars->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n0 = blockIdx.x * 128, t0 = blockIdx.z * tok;
+  const int split = blockIdx.y, splits = gridDim.y;
+  constexpr int kCols = sizeof(OT) == 4 ? 512 : kSmallTok;           // tensor-memory columns
+  const int kb0 = (int)((long long)num_kb * split / splits), kb1 = (int)((long long)num_kb * (split + 1) / splits);
+
+  // The K steps of x and W do not depend on the down projection: they start before it has finished.
+  auto load_k_step = [&](int kb, int stage) {
+    const uint32_t full = smem_u32(&bars->full[stage]);
+    uint8_t* st = smem + stage * stage_bytes;
+    mbar_expect_tx(full, stage_bytes);
+    tma_load_2d(smem_u32(st), &tm_w, kb * (kKBytes / 2), n0, full);
+    tma_load_2d(smem_u32(st + kWStage), &tm_x, kb * (kKBytes / 2), t0, full);
+  };
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1);
+      mbar_init(smem_u32(&bars->ready[s]), 1); mbar_init(smem_u32(&bars->sfull[s]), 4);
+    }
+    mbar_init(smem_u32(&bars->acc_full), 1);
+    bars->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    // the ring is empty: its first loads go out before the rest of the block is set up
+    for (int s = 0; s < stages && kb0 + s < kb1; ++s) load_k_step(kb0 + s, s);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(&bars->tmem_base)), "n"(kCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const int ahead = min(stages, kb1 - kb0);        // loaded above
+      int stage = ahead % stages; uint32_t phase = ahead == stages;
+      bool ok = true;
+      for (int kb = kb0 + ahead; kb < kb1; ++kb) {
+        if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
+        load_k_step(kb, stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
+      if (la.has && ok) {
+        pdl_wait();
+        const int total = __ldcg(la.n_chunks + blockIdx.z);
+        const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
+        for (int c0 = split * kStep; c0 < total; c0 += splits * kStep) {
+          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) break;
+          const uint32_t full = smem_u32(&bars->full[stage]);
+          uint8_t* st = smem + stage * stage_bytes;
+          const int n = min(kStep, total - c0);
+          mbar_expect_tx(full, n * kUpBytes);
+          mbar_arrive(smem_u32(&bars->ready[stage]));
+          for (int i = 0; i < n; ++i) tma_load_3d(smem_u32(st + i * kUpBytes), &tm_up, 0, n0, up_block(__ldcg(list + c0 + i), la.rank_pad), full);
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = make_idesc_bf16(128, npad);
+      int stage = 0; uint32_t phase = 0;
+      bool ok = true;
+      int slab = 0, slab_end = kb0 + (kb1 - kb0) / n_acc;           // chain `slab` ends before K step slab_end
+      uint32_t first = 1;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status)) { ok = false; break; }
+        tc_fence_after();
+        if (kb == slab_end) { ++slab; slab_end = kb0 + (int)((long long)(kb1 - kb0) * (slab + 1) / n_acc); first = 1; }
+        const uint32_t d = tmem + (uint32_t)(slab * npad);
+        const uint64_t wdesc = make_smem_desc(smem_u32(smem + stage * stage_bytes));
+        const uint64_t xdesc = make_smem_desc(smem_u32(smem + stage * stage_bytes + kWStage));
+#pragma unroll
+        for (int k4 = 0; k4 < 4; ++k4)
+          tc_mma_f16(d, wdesc + (uint64_t)(k4 * 2), xdesc + (uint64_t)(k4 * 2), idesc, k4 != 0 ? 1u : first ^ 1u);
+        first = 0;
+        tc_commit(smem_u32(&bars->empty[stage]));
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+      }
+      if (la.has && ok) {
+        pdl_wait();
+        const int total = __ldcg(la.n_chunks + blockIdx.z);
+        const uint32_t last_acc = tmem + (uint32_t)(slab * npad);
+        uint32_t sphase = 0;                             // one parity bit per stage
+        for (int c0 = split * kStep; c0 < total; c0 += splits * kStep) {
+          if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status) ||
+              !mbar_wait(smem_u32(&bars->sfull[stage]), (sphase >> stage) & 1u, abort_flag, status)) { ok = false; break; }
+          sphase ^= 1u << stage;
+          tc_fence_after();
+          const uint32_t up = smem_u32(smem + stage * stage_bytes);
+          const int n = min(kStep, total - c0);
+          for (int i = 0; i < n; ++i) {
+            const uint64_t udesc = make_smem_desc_32b(up + i * kUpBytes);
+            const uint64_t sdesc = make_smem_desc(up + kWStage) + (uint64_t)(i * 4);
+            tc_mma_f16(last_acc, udesc, sdesc, idesc, 1u);
+            tc_mma_f16(last_acc, udesc, sdesc + 2, idesc, 1u);
+          }
+          tc_commit(smem_u32(&bars->empty[stage]));
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      if (ok) tc_commit(smem_u32(&bars->acc_full));
+    }
+  } else {
+    // ---------------------------------------------------------------- warps 2..5: rows of s, then the epilogue
+    const int lane_grp = warp & 3, tid = threadIdx.x - 64;
+    bool ok = true;
+    if (la.has) {
+      pdl_wait();
+      const int t = t0 + tid;
+      const bool real = tid < npad && t < T;
+      const float* srow = la.s + (size_t)(real ? t : 0) * la.rank_pad;
+      constexpr int kAhead = 4;
+      SChunk row[kAhead];                              // the first 64 ranks of this thread's token, fetched ahead
+#pragma unroll
+      for (int c = 0; c < kAhead; ++c)
+        if (real && c * kLoraChunk < la.rank_pad) row[c].fetch(srow + c * kLoraChunk);
+      const int my = real ? __ldcg(la.ids + t) : -1;
+      const int total = __ldcg(la.n_chunks + blockIdx.z);
+      const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
+      int stage = (kb1 - kb0) % stages;                // where the K steps end
+      uint32_t phase = 0;                              // one parity bit per stage
+      for (int c0 = split * kStep; ok && c0 < total;) {
+        const int first = stage;
+        int n = 0;
+        for (; ok && n < kBatch && c0 < total; ++n, c0 += splits * kStep) {
+          int v[kStep];
+#pragma unroll
+          for (int i = 0; i < kStep; ++i) v[i] = c0 + i < total ? __ldcg(list + c0 + i) : -1;
+          ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          phase ^= 1u << stage;
+          uint8_t* rows = smem + stage * stage_bytes + kWStage;
+          if (tid < npad) {
+#pragma unroll
+            for (int i = 0; i < kStep; ++i) {
+              if (v[i] < 0) break;
+              const int c = v[i] % kLoraMaxChunks;
+              const bool mine = my == v[i] / kLoraMaxChunks;
+              if (c >= kAhead) {
+                SChunk r;
+                if (mine) r.fetch(srow + c * kLoraChunk);
+                r.put(rows, tid, i, mine);
+              } else {
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k)
+                  if (c == k) row[k].put(rows, tid, i, mine);
+              }
+            }
+          }
+          if (++stage == stages) stage = 0;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0)
+          for (int i = 0, s = first; i < n; ++i) { mbar_arrive(smem_u32(&bars->sfull[s])); if (++s == stages) s = 0; }
+      }
+    }
+    const bool got = ok && mbar_wait_relaxed(smem_u32(&bars->acc_full), 0u, abort_flag, status);
+    const bool all = __all_sync(0xffffffffu, got);
+    const int cols = min(tok, T - t0);                 // token columns that exist
+    const uint32_t taddr = tmem + ((uint32_t)(lane_grp * 32) << 16);
+    float* mine = reinterpret_cast<float*>(smem);      // [token][128] sums, in the ring: every load has been consumed
+    if (all) {
+      tc_fence_after();
+      for (int c = 0; c < cols; c += 16) {
+        __syncwarp();                                  // the load is warp-collective
+        uint32_t d[16];
+        tc_ld16(taddr + c, d);
+        tc_wait_ld();
+        for (int s = 1; s < n_acc; ++s) {
+          uint32_t e[16];
+          tc_ld16(taddr + s * npad + c, e);
+          tc_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) d[i] = __float_as_uint(__uint_as_float(d[i]) + __uint_as_float(e[i]));
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (c + i < cols) mine[(c + i) * 128 + lane_grp * 32 + lane] = __uint_as_float(d[i]);
+      }
+    }
+  }
+  {
+    // (a CTA that gave up still takes both barriers; its sums are then meaningless and the status word says so)
+    if (splits > 1) cluster_sync_all(); else __syncthreads();
+    const int cols = min(tok, T - t0);
+    const int c0 = cols * split / splits, c1 = cols * (split + 1) / splits;
+    const uint32_t base = smem_u32(smem);
+    // four columns of y per lane, a token per warp
+    for (int c = c0 + warp; c < c1; c += kSmallThreads / 32) {
+      float4 v[kMaxSplits];
+#pragma unroll
+      for (int s = 0; s < kMaxSplits; ++s)
+        if (s < splits) v[s] = ld_cluster_f4(mapa(base + (uint32_t)((c * 128 + lane * 4) * 4), (uint32_t)s));
+      float4 o = v[0];
+#pragma unroll
+      for (int s = 1; s < kMaxSplits; ++s)
+        if (s < splits) { o.x += v[s].x; o.y += v[s].y; o.z += v[s].z; o.w += v[s].w; }
+      OT* row = y + (size_t)(t0 + c) * y_stride + n0 + lane * 4;
+      const int left = N - n0 - lane * 4;
+      if (left >= 4 && vec_ok) {
+        if (sizeof(OT) == 2) *reinterpret_cast<uint2*>(row) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+        else *reinterpret_cast<float4*>(row) = o;
+      } else {
+        if (left > 0) put_out(row, o.x);
+        if (left > 1) put_out(row + 1, o.y);
+        if (left > 2) put_out(row + 2, o.z);
+        if (left > 3) put_out(row + 3, o.w);
+      }
+    }
+    if (splits > 1) cluster_sync_reads();              // no CTA leaves while another reads its sums
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCols) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------ host side
+constexpr int kMaxDevices = 64;
+int g_clusters[kMaxDevices][kMaxSplits + 1];           // co-resident clusters by size; [0]: set up
+
+struct Plan { int npad, tok, n_tiles, t_tiles, num_kb, splits; long long cost; };
+
+// The cluster size with the least work for the busiest SM, in K steps: a cluster needs that many free SMs in one GPC, so
+// fewer SMs are usable for some sizes.
+Plan plan(const int* clusters, int T, int N, int K, int out_f32) {
+  constexpr long long kExchange = 6;                   // what the exchange of partial sums costs (2 us)
+  Plan p{};
+  p.npad = project_small_tokens(T, out_f32); p.tok = project_small_tile(out_f32);
+  p.n_tiles = (N + 127) / 128; p.t_tiles = (T + p.tok - 1) / p.tok; p.num_kb = (K + 63) / 64;
+  const long long tiles = (long long)p.n_tiles * p.t_tiles;
+  p.splits = 1; p.cost = 1ll << 60;
+  for (int c = 1; c <= kMaxSplits && c <= p.num_kb; ++c) {
+    if (clusters[c] < 1) continue;
+    const long long cost = (tiles + clusters[c] - 1) / clusters[c] * ((p.num_kb + c - 1) / c) + (c > 1 ? kExchange : 0);
+    if (cost < p.cost) { p.cost = cost; p.splits = c; }
+  }
+  return p;
+}
+
+}  // namespace
+
+int project_small_tile(int out_f32) { return out_f32 ? 64 : kSmallTok; }       // (8 accumulators of 64 columns fill the tensor memory)
+int project_small_tokens(int T, int out_f32) { return T >= project_small_tile(out_f32) ? project_small_tile(out_f32) : (T + 15) / 16 * 16; }
+
+cudaError_t project_small_setup(int dev) {
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  int* clusters = g_clusters[dev];
+  if (clusters[0]) return cudaSuccess;
+  cudaError_t e = cudaFuncSetAttribute(project_small_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(project_small_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.z = 1;
+  cfg.blockDim = dim3(kSmallThreads, 1, 1); cfg.dynamicSmemBytes = kSmallRing + 2048; cfg.attrs = attr; cfg.numAttrs = 1;
+  for (int c = 1; c <= kMaxSplits; ++c) {
+    attr[0].val.clusterDim.y = (unsigned)c;
+    cfg.gridDim = dim3(kSms, c, 1);
+    e = cudaOccupancyMaxActiveClusters(&clusters[c], project_small_kernel<__nv_bfloat16>, &cfg);
+    if (e != cudaSuccess) return e;
+  }
+  clusters[0] = 1;
+  return cudaSuccess;
+}
+
+long long project_small_cost(int dev, int T, int N, int K, int out_f32) { return plan(g_clusters[dev], T, N, K, out_f32).cost; }
+
+int make_tile_map(GemmTensorMap* out, const void* base, long long cols, long long rows, long long row_stride, long long depth,
+                  long long depth_stride, int box_cols, int box_rows, int swizzle_bytes) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static Encode enc = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return ok ? reinterpret_cast<Encode>(p) : nullptr;
+  }();
+  if (!enc) return -1;
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
+  cuuint64_t strides[2] = {(cuuint64_t)row_stride, (cuuint64_t)depth_stride};
+  cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, es[3] = {1, 1, 1};
+  const CUresult r = enc(reinterpret_cast<CUtensorMap*>(out), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, depth > 0 ? 3 : 2, const_cast<void*>(base), dims,
+                         strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle_bytes == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? 0 : -2;
+}
+
+cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,
+                                 int dev, cudaStream_t s) {
+  const Plan p = plan(g_clusters[dev], a.T, a.N, a.K, a.out_f32);
+  const int steps = p.num_kb / p.splits;               // K steps a CTA has at least
+  int n_acc = a.out_f32 ? (steps + kSlabSteps - 1) / kSlabSteps : 1;
+  if (n_acc > 512 / p.npad) n_acc = 512 / p.npad;
+  if (n_acc < 1) n_acc = 1;
+  const int stage = kWStage + p.npad * kKBytes;
+  // With adapters and few tokens the ring leaves room for a block of the down projection, so that both run at once.
+  const int ring = a.bank && lora_beside(a.T) ? kSharedRing : kSmallRing;
+  int stages = ring / stage;
+  if (stages > kSmallMaxStages) stages = kSmallMaxStages;
+  const size_t elt = a.out_f32 ? 4 : 2;
+  const int vec_ok = reinterpret_cast<uintptr_t>(a.y) % (4 * elt) == 0 && a.y_stride % 4 == 0;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = (unsigned)p.splits; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(p.n_tiles, p.splits, p.t_tiles); cfg.blockDim = dim3(kSmallThreads, 1, 1);
+  cfg.dynamicSmemBytes = 1024 + (size_t)stages * stage + 512; cfg.stream = s; cfg.attrs = attr;
+  cfg.numAttrs = a.bank ? 2 : 1;                       // only ever overlaps this call's own down projection
+  const CUtensorMap& w = reinterpret_cast<const CUtensorMap&>(tm_w);
+  const CUtensorMap& x = reinterpret_cast<const CUtensorMap&>(tm_x);
+  const CUtensorMap& u = reinterpret_cast<const CUtensorMap&>(tm_up);
+  const LoraArgs la = lora_args(a);
+  if (a.out_f32)
+    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, la, (float*)a.y, a.y_stride,
+                              vec_ok, a.status);
+  return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, la,
+                            (__nv_bfloat16*)a.y, a.y_stride, vec_ok, a.status);
+}
+
+}  // namespace cep
