@@ -23,13 +23,14 @@ constexpr int kStages = 6;
 constexpr int kHalf = 128 * kKBytes;                   // one CTA's 128 rows of either operand: 16 KiB
 constexpr int kRing = 4;                               // tile ids in flight
 constexpr int kPoison = -2;
+constexpr int kAsk = 10;                               // K steps before a tile's end at which the next id is fetched
 constexpr int kThreads = 352;                          // warp 0 loads, 1 MMA, 2-5 epilogue, 6 tile ids, 7-10 rows of s
 constexpr int kReaders = 19;                           // leader: loads, MMA, 4 epilogue, 4 s-row warps; peer: loads, 4, 4
 constexpr int kMaxSplits = 4;                          // CTA pairs of a portable cluster
 constexpr int kPitch = 260;                            // floats per row of exchanged sums: rows four banks apart
 struct __align__(8) Barriers {
   uint64_t full[kStages], empty[kStages], ready[kStages], sfull[kStages], acc_full[2], acc_empty[2];
-  uint64_t ring_full[kRing], ring_empty[kRing];
+  uint64_t ring_full[kRing], ring_empty[kRing], want;
   int32_t ring_tile[kRing];
   uint32_t tmem_base;
   int abort_flag;
@@ -122,6 +123,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       mbar_init(smem_u32(&bars->ring_full[s]), 1); mbar_init(smem_u32(&bars->ring_empty[s]), kReaders);
       bars->ring_tile[s] = kPoison;
     }
+    mbar_init(smem_u32(&bars->want), 1);
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -137,10 +139,14 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
-  // What precedes this launch is the down projection, whose results are read here; or (after_peer) the launch with the full
-  // rounds of tiles, which touches nothing of this one's and began after the down projection had ended.
-  if (!after_peer) pdl_wait();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // What precedes this launch is the down projection.  The K steps do not need it and start at once; who reads its lists and s
+  // waits for it (the tile counter was zeroed before any of its blocks let this launch start).  Or (after_peer) it is the launch
+  // with the full rounds of tiles, which touches nothing of this one's and let it start only after the down projection's end.
+  const bool wait = la.has && !after_peer;
+  if (!kSplit && (wait ? warp >= 7 : true)) {
+    if (wait) pdl_wait();
+    if (threadIdx.x == 7 * 32) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  }
 
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA loads (both CTAs)
@@ -155,6 +161,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         int m, nb;
         tile_at(sh, tile, &m, &nb);
         const int t0 = m * kLargeTok + half * 128, n0 = nb * 256 + half * 128;
+        const int ask = max(kb0, kb1 - kAsk);
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
           const uint32_t full = mapa(smem_u32(&bars->full[stage]), lead);
@@ -162,7 +169,9 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           tma_load_2d_pair(smem_u32(smem_x + stage * kHalf), &tm_x, kb * (kKBytes / 2), t0, full);
           tma_load_2d_pair(smem_u32(smem_w + stage * kHalf), &tm_w, kb * (kKBytes / 2), n0, full);
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          if (!kSplit && !is_peer && kb == ask) mbar_arrive(smem_u32(&bars->want));
         }
+        if (wait) pdl_wait();
         const int total = la.has ? __ldcg(la.n_chunks + m) : 0;
         const int32_t* list = la.chunks + (size_t)m * kLargeTok * kLoraMaxChunks;
         for (int c0 = c_first; ok && c0 < total; c0 += c_stride) {
@@ -215,6 +224,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
         if (ok && la.has) {
+          if (wait) pdl_wait();
           int m, nb;
           tile_at(sh, tile, &m, &nb);
           const int total = __ldcg(la.n_chunks + m);
@@ -243,7 +253,10 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     // ---------------------------------------------------------------- tile ids (leader only)
     if (!kSplit && lane == 0 && !is_peer) {
       int slot = 0; uint32_t phase = 0;
-      for (;;) {
+      // The next id is fetched shortly before the loading thread needs it, not as soon as there is room for it: pairs start at
+      // different times, and the first ones would take the tiles of those that start later.
+      for (uint32_t n = 0;; ++n) {
+        if (n > 0 && !mbar_wait_relaxed(smem_u32(&bars->want), (n - 1) & 1u, abort_flag, status)) break;
         if (!mbar_wait_relaxed(smem_u32(&bars->ring_empty[slot]), phase ^ 1u, abort_flag, status)) break;
         int t = atomicAdd(tile_counter, 1);
         t = t < sh.n_tiles ? sh.tile0 + t : -1;
@@ -279,6 +292,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       for (int kb = kb0; ok && kb < kb1; kb += sh.slab_steps) {          // one accumulation chain after the other
         if (s_warp && la.has && kb + sh.slab_steps >= kb1) {
           // the adapters' steps end the last chain
+          if (wait) pdl_wait();
           const int ts = m * kLargeTok + half * 128 + r;
           const int my = ts < sh.T ? __ldcg(la.ids + ts) : -1;
           const float* srow = la.s + (size_t)(my >= 0 ? ts : 0) * la.rank_pad;

@@ -82,7 +82,8 @@ __device__ int expand_chunks(const int* job, int m, const LoraBank& bank, int* o
   return base;
 }
 
-// Grid (token tiles, pass stripes, K parts); the parts are a cluster.  box: rows of x one TMA load brings.
+// Grid (token tiles, pass stripes, K parts); the parts are a cluster.  box: rows of x one TMA load brings.  With token_tile
+// other than 128 the first stripe only builds the projection kernel's lists, beside the others' work.
 __global__ void __launch_bounds__(kThreads)
 lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K, int N,
                    const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int x_stage, int chunks, int stages, int n_acc,
@@ -98,6 +99,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   const int t0 = blockIdx.x * kRows, rows = min(kRows, T - t0);
   const int part = blockIdx.z, parts = gridDim.z;
   const bool reporter = blockIdx.y == 0 && part == 0;
+  const int list_stripes = token_tile != kRows;
 
   if (threadIdx.x == 32) { prefetch_map(&tm_x); prefetch_map(&tm_down); }
   if (threadIdx.x == 0) {
@@ -105,7 +107,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
     mbar_init(smem_u32(&bars.acc_full), 1);
     bars.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (reporter && blockIdx.x == 0) *tile_counter = 0;
+    if (reporter && blockIdx.x == 0) { atomicExch(tile_counter, 0); __threadfence(); }        // in place before the projection starts
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -159,7 +161,8 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   const int cols = chunks * kLoraChunk;              // columns of an accumulator
   int stage = 0; uint32_t phase = 0, acc_phase = 0;  // the loading and the issuing thread each keep their own
 
-  for (int c0 = blockIdx.y * chunks; c0 < total; c0 += gridDim.y * chunks) {
+  for (int c0 = ((int)blockIdx.y - list_stripes) * chunks; c0 < total; c0 += ((int)gridDim.y - list_stripes) * chunks) {
+    if (c0 < 0) break;                               // (the stripe that builds lists)
     const int n = min(chunks, total - c0);
     if (N > 0 && warp == 5 && lane < n) {
       // a short batch meets each adapter's columns of B for the first time in the projection's last steps: have them in the
@@ -247,23 +250,26 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
       cluster_sync_all();
       const int r0 = rows * part / parts, r1 = rows * (part + 1) / parts;
       const uint32_t base = smem_u32(smem);
-      for (int x = r0 * n * 4 + threadIdx.x; x < r1 * n * 4; x += kThreads) {
-        const int row = x / (n * 4), i = x / 4 % n, q = x % 4;
-        const int v = L.chunk[c0 + i], a = v / kLoraMaxChunks, c = v % kLoraMaxChunks;
-        if (L.id[row] != a) continue;
-        float4 f[kMaxParts];
+      // a row per half warp and four ranks per lane: up to four chunks of the row's adapter at a time
+      for (int row = r0 + 2 * warp + (lane >> 4); row < r1; row += 2 * kThreads / 32) {
+        const int my = L.id[row];
+        for (int i = (lane & 15) >> 2; i < n; i += 4) {
+          const int v = L.chunk[c0 + i];
+          if (v / kLoraMaxChunks != my) continue;
+          float4 f[kMaxParts];
 #pragma unroll
-        for (int p = 0; p < kMaxParts; ++p)
-          if (p < parts) f[p] = ld_cluster_f4(mapa(base + (uint32_t)((row * cols + i * kLoraChunk + q * 4) * 4), (uint32_t)p));
-        float4 o = f[0];
+          for (int p = 0; p < kMaxParts; ++p)
+            if (p < parts) f[p] = ld_cluster_f4(mapa(base + (uint32_t)((row * cols + i * kLoraChunk + (lane & 3) * 4) * 4), (uint32_t)p));
+          float4 o = f[0];
 #pragma unroll
-        for (int p = 1; p < kMaxParts; ++p)
-          if (p < parts) { o.x += f[p].x; o.y += f[p].y; o.z += f[p].z; o.w += f[p].w; }
-        *reinterpret_cast<float4*>(s_out + (size_t)(t0 + row) * bank.rank_pad + c * kLoraChunk + q * 4) = o;
+          for (int p = 1; p < kMaxParts; ++p)
+            if (p < parts) { o.x += f[p].x; o.y += f[p].y; o.z += f[p].z; o.w += f[p].w; }
+          *reinterpret_cast<float4*>(s_out + (size_t)(t0 + row) * bank.rank_pad + v % kLoraMaxChunks * kLoraChunk + (lane & 3) * 4) = o;
+        }
       }
       fence_proxy_async_smem();                      // the next pass's loads write where the partial sums were
       tc_fence_before();
-      cluster_sync_all();
+      cluster_sync_reads();
       tc_fence_after();
     } else {
       tc_fence_before();
@@ -353,7 +359,7 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = (unsigned)parts;
-  cfg.gridDim = dim3(tiles, stripes, parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+  cfg.gridDim = dim3(tiles, stripes + (token_tile != kRows), parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
   cfg.attrs = attr; cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, lora_shrink_kernel, reinterpret_cast<const CUtensorMap&>(tm_x), reinterpret_cast<const CUtensorMap&>(tm_down), T, K,
                             token_tile == kLargeTok ? 0 : N, ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, tile_counter, status);
