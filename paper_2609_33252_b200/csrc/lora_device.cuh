@@ -31,6 +31,14 @@ __device__ __forceinline__ uint64_t make_smem_desc_32b(uint32_t saddr) {
   return d;
 }
 
+// The lists and s as the kernels read them; has == 0: no adapters in this call.  The lists are read past the L1: they are
+// rewritten by every call.
+struct LoraArgs {
+  int has, rank_pad;
+  const int32_t* ids; const int32_t* n_chunks; const int32_t* chunks;
+  const float* s;
+};
+
 // A chunk (16 ranks) of a token is 64 bytes of operand row, [value | remainder]; a 128-byte row holds two chunks.
 struct SChunk {
   uint32_t w[16];
@@ -55,17 +63,47 @@ struct SChunk {
   }
 };
 
+// The first kAhead chunks of a token's own adapter, fetched before its steps come up.
+template <int kAhead>
+struct SRow {
+  const float* s;
+  int my;                                              // the token's adapter, -1: none
+  SChunk chunk[kAhead];
+  // t: the token, or negative where there is none
+  __device__ __forceinline__ void fetch(const LoraArgs& la, int t) {
+    s = la.s + (size_t)(t >= 0 ? t : 0) * la.rank_pad;
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c)
+      if (t >= 0 && c * kLoraChunk < la.rank_pad) chunk[c].fetch(s + c * kLoraChunk);      // (of use only if my >= 0)
+    my = t >= 0 ? __ldcg(la.ids + t) : -1;
+  }
+  // Writes entry v of the list into half h of row r.
+  __device__ __forceinline__ void put(uint8_t* tile, int r, int h, int v) const {
+    const int c = v % kLoraMaxChunks;
+    const bool mine = my == v / kLoraMaxChunks;
+    if (c >= kAhead) {
+      SChunk far;
+      if (mine) far.fetch(s + c * kLoraChunk);
+      far.put(tile, r, h, mine);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (c == k) chunk[k].put(tile, r, h, mine);
+    }
+  }
+};
+
 template <typename OT> __device__ __forceinline__ void put_out(OT* p, float v);
 template <> __device__ __forceinline__ void put_out<float>(float* p, float v) { *p = v; }
 template <> __device__ __forceinline__ void put_out<__nv_bfloat16>(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// The lists and s as the kernels read them; has == 0: no adapters in this call.  The lists are read past the L1: they are
-// rewritten by every call.
-struct LoraArgs {
-  int has, rank_pad;
-  const int32_t* ids; const int32_t* n_chunks; const int32_t* chunks;
-  const float* s;
-};
+// The list entries of a step (kStep of them, the second -1 past the end).
+__device__ __forceinline__ int2 list_pair(const int32_t* list, int c, int total) {
+  if (c >= total) return make_int2(-1, -1);
+  return make_int2(__ldcg(list + c), c + 1 < total ? __ldcg(list + c + 1) : -1);
+}
+constexpr int kLookAhead = 8;                          // steps whose entries the loading thread reads at once
+
 // Index of a chunk's [N][16] block in the up bank.
 __device__ __forceinline__ int up_block(int v, int rank_pad) { return v / kLoraMaxChunks * (rank_pad / kLoraChunk) + v % kLoraMaxChunks; }
 

@@ -174,15 +174,22 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         if (wait) pdl_wait();
         const int total = la.has ? __ldcg(la.n_chunks + m) : 0;
         const int32_t* list = la.chunks + (size_t)m * kLargeTok * kLoraMaxChunks;
-        for (int c0 = c_first; ok && c0 < total; c0 += c_stride) {
-          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
-          const uint32_t full = mapa(smem_u32(&bars->full[stage]), lead);
-          const int n = min(kStep, total - c0);
-          if (!is_peer) mbar_expect_tx(smem_u32(&bars->full[stage]), 2 * n * kUpBytes);
-          mbar_arrive(smem_u32(&bars->ready[stage]));
-          for (int i = 0; i < n; ++i)
-            tma_load_3d_pair(smem_u32(smem_w + stage * kHalf + i * kUpBytes), &tm_up, 0, n0, up_block(__ldcg(list + c0 + i), la.rank_pad), full);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        for (int c0 = c_first; ok && c0 < total; c0 += kLookAhead * c_stride) {
+          int2 e[kLookAhead];
+#pragma unroll
+          for (int j = 0; j < kLookAhead; ++j) e[j] = list_pair(list, c0 + j * c_stride, total);
+#pragma unroll
+          for (int j = 0; j < kLookAhead; ++j) {
+            if (e[j].x < 0) break;
+            if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
+            const uint32_t full = mapa(smem_u32(&bars->full[stage]), lead);
+            if (!is_peer) mbar_expect_tx(smem_u32(&bars->full[stage]), (e[j].y < 0 ? 2 : 4) * kUpBytes);
+            mbar_arrive(smem_u32(&bars->ready[stage]));
+            uint8_t* st = smem_w + stage * kHalf;
+            tma_load_3d_pair(smem_u32(st), &tm_up, 0, n0, up_block(e[j].x, la.rank_pad), full);
+            if (e[j].y >= 0) tma_load_3d_pair(smem_u32(st + kUpBytes), &tm_up, 0, n0, up_block(e[j].y, la.rank_pad), full);
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+          }
         }
       }
     }
@@ -294,39 +301,26 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           // the adapters' steps end the last chain
           if (wait) pdl_wait();
           const int ts = m * kLargeTok + half * 128 + r;
-          const int my = ts < sh.T ? __ldcg(la.ids + ts) : -1;
-          const float* srow = la.s + (size_t)(my >= 0 ? ts : 0) * la.rank_pad;
+          SRow<kF32 ? 1 : 4> row;                        // (fp32: the sums need the registers)
+          row.fetch(la, ts < sh.T ? ts : -1);
           const int total = __ldcg(la.n_chunks + m);
           const int32_t* list = la.chunks + (size_t)m * kLargeTok * kLoraMaxChunks;
           stage = (stage + kb1 - kb0) % kStages;         // past the tile's K steps
+          int2 e = make_int2(-1, -1);                    // lane i: the i-th of the next 32 steps
+          int step = 0;
           for (int c0 = c_first; ok && c0 < total;) {
-            constexpr int kBatch = kF32 ? 1 : cep::kBatch;             // (the sums need the registers)
-            SChunk row[kBatch][kStep];
-            bool mine[kBatch][kStep];
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b)
-#pragma unroll
-              for (int i = 0; i < kStep; ++i) {
-                const int c = c0 + b * c_stride + i;
-                const int v = c < total ? __ldcg(list + c) : -1;
-                mine[b][i] = v >= 0 && my == v / kLoraMaxChunks;
-                if (mine[b][i]) row[b][i].fetch(srow + v % kLoraMaxChunks * kLoraChunk);
-              }
             const int first = stage;
             int n = 0;
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-              if (!ok || c0 >= total) break;
+            for (; n < kBatch && c0 < total; ++n, c0 += c_stride, ++step) {
+              if ((step & 31) == 0) e = list_pair(list, c0 + lane * c_stride, total);
+              const int v0 = __shfl_sync(0xffffffffu, e.x, step & 31), v1 = __shfl_sync(0xffffffffu, e.y, step & 31);
               ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
               phase ^= 1u << stage;
-#pragma unroll
-              for (int i = 0; i < kStep; ++i)
-                if (c0 + i < total) row[b][i].put(smem_x + stage * kHalf, r, i, mine[b][i]);
+              row.put(smem_x + stage * kHalf, r, 0, v0);
+              if (v1 >= 0) row.put(smem_x + stage * kHalf, r, 1, v1);
               if (++stage == kStages) stage = 0;
-              ++n;
-              c0 += c_stride;
             }
             fence_proxy_async_smem();
             __syncwarp();

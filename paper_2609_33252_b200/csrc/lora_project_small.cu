@@ -100,15 +100,23 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         pdl_wait();
         const int total = __ldcg(la.n_chunks + blockIdx.z);
         const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
-        for (int c0 = split * kStep; c0 < total; c0 += splits * kStep) {
-          if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) break;
-          const uint32_t full = smem_u32(&bars->full[stage]);
-          uint8_t* st = smem + stage * stage_bytes;
-          const int n = min(kStep, total - c0);
-          mbar_expect_tx(full, n * kUpBytes);
-          mbar_arrive(smem_u32(&bars->ready[stage]));
-          for (int i = 0; i < n; ++i) tma_load_3d(smem_u32(st + i * kUpBytes), &tm_up, 0, n0, up_block(__ldcg(list + c0 + i), la.rank_pad), full);
-          if (++stage == stages) { stage = 0; phase ^= 1u; }
+        for (int c0 = split * kStep; ok && c0 < total;) {
+          int2 e[kLookAhead];
+#pragma unroll
+          for (int j = 0; j < kLookAhead; ++j) e[j] = list_pair(list, c0 + j * splits * kStep, total);
+#pragma unroll
+          for (int j = 0; j < kLookAhead; ++j) {
+            if (e[j].x < 0) break;
+            if (!mbar_wait(smem_u32(&bars->empty[stage]), phase ^ 1u, abort_flag, status)) { ok = false; break; }
+            const uint32_t full = smem_u32(&bars->full[stage]);
+            uint8_t* st = smem + stage * stage_bytes;
+            mbar_expect_tx(full, (e[j].y < 0 ? 1 : 2) * kUpBytes);
+            mbar_arrive(smem_u32(&bars->ready[stage]));
+            tma_load_3d(smem_u32(st), &tm_up, 0, n0, up_block(e[j].x, la.rank_pad), full);
+            if (e[j].y >= 0) tma_load_3d(smem_u32(st + kUpBytes), &tm_up, 0, n0, up_block(e[j].y, la.rank_pad), full);
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
+          }
+          c0 += kLookAhead * splits * kStep;
         }
       }
     }
@@ -163,47 +171,28 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     bool ok = true;
     if (la.has) {
       pdl_wait();
-      const int t = t0 + tid;
-      const bool real = tid < npad && t < T;
-      const float* srow = la.s + (size_t)(real ? t : 0) * la.rank_pad;
-      constexpr int kAhead = 4;
-      SChunk row[kAhead];                              // the first 64 ranks of this thread's token, fetched ahead
-#pragma unroll
-      for (int c = 0; c < kAhead; ++c)
-        if (real && c * kLoraChunk < la.rank_pad) row[c].fetch(srow + c * kLoraChunk);
-      const int my = real ? __ldcg(la.ids + t) : -1;
+      SRow<4> row;
+      row.fetch(la, tid < npad && t0 + tid < T ? t0 + tid : -1);
       const int total = __ldcg(la.n_chunks + blockIdx.z);
       const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
       int stage = (kb1 - kb0) % stages;                // where the K steps end
       uint32_t phase = 0;                              // one parity bit per stage
+      int2 e = make_int2(-1, -1);                      // lane i: the i-th of the next 32 steps
+      int step = 0;
       for (int c0 = split * kStep; ok && c0 < total;) {
         const int first = stage;
         int n = 0;
-        for (; ok && n < kBatch && c0 < total; ++n, c0 += splits * kStep) {
-          int v[kStep];
-#pragma unroll
-          for (int i = 0; i < kStep; ++i) v[i] = c0 + i < total ? __ldcg(list + c0 + i) : -1;
+        for (; n < kBatch && c0 < total; ++n, c0 += splits * kStep, ++step) {
+          if ((step & 31) == 0) e = list_pair(list, c0 + lane * splits * kStep, total);
+          const int v0 = __shfl_sync(0xffffffffu, e.x, step & 31), v1 = __shfl_sync(0xffffffffu, e.y, step & 31);
           ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           phase ^= 1u << stage;
           uint8_t* rows = smem + stage * stage_bytes + kWStage;
           if (tid < npad) {
-#pragma unroll
-            for (int i = 0; i < kStep; ++i) {
-              if (v[i] < 0) break;
-              const int c = v[i] % kLoraMaxChunks;
-              const bool mine = my == v[i] / kLoraMaxChunks;
-              if (c >= kAhead) {
-                SChunk r;
-                if (mine) r.fetch(srow + c * kLoraChunk);
-                r.put(rows, tid, i, mine);
-              } else {
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k)
-                  if (c == k) row[k].put(rows, tid, i, mine);
-              }
-            }
+            row.put(rows, tid, 0, v0);
+            if (v1 >= 0) row.put(rows, tid, 1, v1);
           }
           if (++stage == stages) stage = 0;
         }
