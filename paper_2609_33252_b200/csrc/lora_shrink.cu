@@ -315,7 +315,7 @@ cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const ui
   return cudaGetLastError();
 }
 
-bool lora_beside(int T) { return T <= 64; }
+bool lora_beside(int T) { return T <= 128; }
 
 cudaError_t lora_shrink_setup() {
   cudaError_t e = cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLongSmem);
@@ -328,7 +328,7 @@ cudaError_t lora_shrink_setup() {
 cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* tile_counter, int32_t* status, cudaStream_t s) {
-  // Up to 64 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
+  // Up to 128 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
   const bool beside = lora_beside(T);
   const int chunks = beside ? 4 : 8, smem = beside ? kShortSmem : kLongSmem;
   // With fewer than 128 tokens the M side's missing rows are whatever follows in shared memory (their products are not read):
