@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -167,6 +168,22 @@ def _stream_handle(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _current_stream() -> int:
+    """Handle of the current stream of the current device, without a Python stream object around it."""
+    return _torch()._C._cuda_getCurrentRawStream(_torch()._C._cuda_getDevice())
+
+
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 # ---------------------------------------------------------------- same-named wrappers
 def moe_plan_workspace_bytes(cfg: CepConfig) -> int:
     n = ctypes.c_size_t(0)
@@ -208,13 +225,27 @@ def moe_route(logits, top_k: int, topk_ids, topk_weights, stream=None):
                            topk_weights.data_ptr(), _stream_handle(stream)))
 
 
-def _rows(t, name, n_tokens, hidden, dtypes):
-    """Row stride of a [T,H] CUDA tensor whose rows are contiguous; raises for anything the call cannot take."""
-    if t.dtype not in dtypes:
+_NORM_DESC = struct.Struct("6i4qf4x")                  # NormDesc, packed in one call
+_ELEM = {}                                             # torch dtype -> CEP_ELEM_*, filled with the first call
+
+
+def _norm_rows(t, name, T, H, dtype=None):
+    """(element type, row stride) of a [T,H] CUDA tensor with contiguous rows; raises for what the call cannot take."""
+    elem = _ELEM.get(t.dtype)
+    if elem is None or (dtype is not None and t.dtype is not dtype):
         raise CepError(-1, "%s has dtype %s" % (name, t.dtype))
-    if t.dim() != 2 or t.shape[0] != n_tokens or t.shape[1] != hidden or (hidden > 1 and t.stride(1) != 1) or not t.is_cuda:
-        raise CepError(-1, "%s must be a [%d, %d] CUDA tensor with contiguous rows" % (name, n_tokens, hidden))
-    return t.stride(0) if n_tokens > 1 else hidden
+    if t.shape != (T, H) or not t.is_cuda:
+        raise CepError(-1, "%s must be a [%d, %d] CUDA tensor" % (name, T, H))
+    stride, inner = t.stride()
+    if inner != 1 and H > 1:
+        raise CepError(-1, "the rows of %s must be contiguous" % name)
+    return elem, stride if T > 1 else H                # (the stride of a single row means nothing)
+
+
+def _norm_dense(t, name, shape, dtypes):
+    if t.dtype not in dtypes or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise CepError(-1, "%s must be a contiguous CUDA tensor of %s %s" % (name, list(shape), dtypes[0]))
+    return t.data_ptr()
 
 
 def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None, y=None, codes=None, scales=None,
@@ -224,29 +255,40 @@ def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None
     x [T,H] bf16 or fp32; residual / residual_out [T,H] bf16 or fp32 (one type); weight [H] bf16 or fp32; y bf16 [T,H];
     codes float8_e4m3fn [T,H] and scales fp32 [T,ceil(H/128)] (CEP_FP8_E4M3_BLOCK128) or uint8 [T,ceil(H/32)]
     (CEP_MXFP4_E4M3).  Rows of x, residual, residual_out and y may be strided."""
-    import torch
-    f32, plain = torch.float32, (torch.bfloat16, torch.float32)
+    torch = _torch()
+    bf16 = torch.bfloat16
+    if not _ELEM:
+        _ELEM.update({bf16: CEP_ELEM_BF16, torch.float32: CEP_ELEM_FP32})
+    if x.dim() != 2:
+        raise CepError(-1, "x must be a [T, H] tensor")
     T, H = x.shape
-    xs = _rows(x, "x", T, H, plain)
+    xe, xs = _norm_rows(x, "x", T, H)
+    re = we = 0
     rs = os_ = ys = H
+    rp = op = yp = wp = cp = sp = None
     if residual is not None:
-        rs = _rows(residual, "residual", T, H, plain)
+        re, rs = _norm_rows(residual, "residual", T, H)
+        rp = residual.data_ptr()
     if residual_out is not None:
-        os_ = _rows(residual_out, "residual_out", T, H, plain if residual is None else (residual.dtype,))
+        os_ = _norm_rows(residual_out, "residual_out", T, H, None if residual is None else residual.dtype)[1]
+        op = residual_out.data_ptr()
     if y is not None:
-        ys = _rows(y, "y", T, H, (torch.bfloat16,))
-    if weight is not None and (weight.dtype not in plain or weight.shape != (H,) or not weight.is_contiguous() or not weight.is_cuda):
-        raise CepError(-1, "weight must be a contiguous CUDA tensor of [%d] bf16 or fp32" % H)
-    if codes is not None and (codes.dtype not in (torch.float8_e4m3fn, torch.uint8) or codes.shape != (T, H) or not codes.is_contiguous()):
-        raise CepError(-1, "codes must be a contiguous [%d, %d] float8_e4m3fn tensor" % (T, H))
+        ys = _norm_rows(y, "y", T, H, bf16)[1]
+        yp = y.data_ptr()
+    if weight is not None:
+        wp = _norm_dense(weight, "weight", (H,), (bf16, torch.float32))
+        we = _ELEM[weight.dtype]
+    if codes is not None:
+        cp = _norm_dense(codes, "codes", (T, H), (torch.float8_e4m3fn, torch.uint8))
     if scales is not None:
-        block, want = (32, torch.uint8) if dtype == CEP_MXFP4_E4M3 else (128, f32)
-        if scales.dtype != want or scales.shape != (T, (H + block - 1) // block) or not scales.is_contiguous():
-            raise CepError(-1, "scales must be a contiguous [%d, %d] %s tensor" % (T, (H + block - 1) // block, want))
-    desc = NormDesc(T, H, dtype, x.dtype == f32, residual is not None and residual.dtype == f32,
-                    weight is not None and weight.dtype == f32, xs, rs, os_, ys, eps)
-    _check(lib().moe_norm(ctypes.byref(desc), x.data_ptr(), _dptr(residual), _dptr(weight), _dptr(residual_out), _dptr(y),
-                          _dptr(codes), _dptr(scales), _stream_handle(stream)))
+        if dtype == CEP_MXFP4_E4M3:
+            sp = _norm_dense(scales, "scales", (T, (H + 31) // 32), (torch.uint8,))
+        else:
+            sp = _norm_dense(scales, "scales", (T, (H + 127) // 128), (torch.float32,))
+    rc = (_lib or lib()).moe_norm(_NORM_DESC.pack(T, H, dtype, xe, re, we, xs, rs, os_, ys, eps), x.data_ptr(), rp, wp, op, yp, cp, sp,
+                                  _current_stream() if stream is None else _stream_handle(stream))
+    if rc:
+        _check(rc)
 
 
 def lora_plan_workspace_bytes(cfg: LoraConfig) -> int:
@@ -276,8 +318,11 @@ def lora_load_adapter(plan, slot: int, rank: int, scale: float, down, up, stream
 
 def lora_project(plan, x, adapter_ids, y, stream=None):
     T = x.shape[0]                                        # (the stride of a single row means nothing)
-    _check(lib().lora_project(plan, x.data_ptr(), x.stride(0) if T > 1 else x.shape[1], T, _dptr(adapter_ids), y.data_ptr(),
-                              y.stride(0) if T > 1 else y.shape[1], _stream_handle(stream)))
+    rc = (_lib or lib()).lora_project(plan, x.data_ptr(), x.stride(0) if T > 1 else x.shape[1], T,
+                                      None if adapter_ids is None else adapter_ids.data_ptr(), y.data_ptr(),
+                                      y.stride(0) if T > 1 else y.shape[1], _current_stream() if stream is None else _stream_handle(stream))
+    if rc:
+        _check(rc)
 
 
 def lora_status(plan) -> int:
@@ -500,7 +545,8 @@ class LoRAProjection:
             raise CepError(-1, "weight must be a bf16 CUDA tensor [out, in] with contiguous rows")
         self.weight = weight
         self.out_dtype = torch.float32 if out_elem == CEP_ELEM_FP32 else torch.bfloat16
-        self.cfg = LoraConfig(weight.shape[1], weight.shape[0], max_tokens, max_adapters, max_rank, out_elem)
+        self.out_features, self.in_features = weight.shape
+        self.cfg = LoraConfig(self.in_features, self.out_features, max_tokens, max_adapters, max_rank, out_elem)
         self.workspace = torch.empty(lora_plan_workspace_bytes(self.cfg), dtype=torch.uint8, device=weight.device)
         nb = lora_bank_bytes(self.cfg)
         self.bank = torch.empty(nb, dtype=torch.uint8, device=weight.device) if nb else None
@@ -521,18 +567,17 @@ class LoRAProjection:
 
     def run(self, x, adapter_ids=None, out=None, stream=None):
         """x bf16 [T,in], adapter_ids int32 [T] (-1: none) or None; returns out [T,out] (allocated if not given)."""
-        import torch
-        c = self.cfg
-        T = x.shape[0]
-        if x.dtype != torch.bfloat16 or not x.is_cuda or x.dim() != 2 or x.shape[1] != c.in_features or x.stride(1) != 1:
-            raise CepError(-1, "x must be a bf16 CUDA tensor [T, %d] with contiguous rows" % c.in_features)
-        if adapter_ids is not None and (adapter_ids.dtype != torch.int32 or adapter_ids.shape != (T,) or
+        torch = _torch()
+        if x.dim() != 2 or x.dtype is not torch.bfloat16 or not x.is_cuda or x.shape[1] != self.in_features or x.stride(1) != 1:
+            raise CepError(-1, "x must be a bf16 CUDA tensor [T, %d] with contiguous rows" % self.in_features)
+        T, N = x.shape[0], self.out_features
+        if adapter_ids is not None and (adapter_ids.dtype is not torch.int32 or adapter_ids.shape != (T,) or
                                         not adapter_ids.is_contiguous() or not adapter_ids.is_cuda):
             raise CepError(-1, "adapter_ids must be a contiguous int32 CUDA tensor [%d]" % T)
         if out is None:
-            out = torch.empty((T, c.out_features), dtype=self.out_dtype, device=x.device)
-        elif out.dtype != self.out_dtype or out.shape != (T, c.out_features) or not out.is_cuda or (c.out_features > 1 and out.stride(1) != 1):
-            raise CepError(-1, "out must be a %s CUDA tensor [%d, %d] with contiguous rows" % (self.out_dtype, T, c.out_features))
+            out = torch.empty((T, N), dtype=self.out_dtype, device=x.device)
+        elif out.dtype is not self.out_dtype or out.shape != (T, N) or not out.is_cuda or (N > 1 and out.stride(1) != 1):
+            raise CepError(-1, "out must be a %s CUDA tensor [%d, %d] with contiguous rows" % (self.out_dtype, T, N))
         lora_project(self.plan, x, adapter_ids, out, stream)
         return out
 
