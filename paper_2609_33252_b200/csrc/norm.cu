@@ -26,29 +26,38 @@ __device__ __forceinline__ uint32_t pack2_e4m3(float lo, float hi) {
   return r;
 }
 
-// Eight consecutive elements as they are loaded: one 16-byte register quad of bf16, two of fp32.
+// Two fp32 values in one 64-bit register pair: one instruction adds, multiplies or accumulates both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ float lo(f32x2 v) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); return a; }
+__device__ __forceinline__ float hi(f32x2 v) { float a, b; asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); return b; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ float max_abs3(float a, float b, float c) { float r; asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+
+// Eight consecutive elements as they are loaded: one 16-byte register quad of bf16, two of fp32; and as four pairs.
 template <typename T> struct Vec8;
 template <> struct Vec8<__nv_bfloat16> {
   uint4 a;
   __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
+  __device__ __forceinline__ void get(f32x2 (&f)[4]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    for (int i = 0; i < 4; ++i) f[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
   }
-  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&f)[8]) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(f[0], f[1]), pack2_bf16(f[2], f[3]), pack2_bf16(f[4], f[5]), pack2_bf16(f[6], f[7]));
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, const f32x2 (&f)[4]) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2_bf16(lo(f[0]), hi(f[0])), pack2_bf16(lo(f[1]), hi(f[1])), pack2_bf16(lo(f[2]), hi(f[2])),
+                                              pack2_bf16(lo(f[3]), hi(f[3])));
   }
 };
 template <> struct Vec8<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-  }
-  static __device__ __forceinline__ void store(float* p, const float (&f)[8]) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  __device__ __forceinline__ void get(f32x2 (&f)[4]) const { f[0] = pair(a.x, a.y); f[1] = pair(a.z, a.w); f[2] = pair(b.x, b.y); f[3] = pair(b.z, b.w); }
+  static __device__ __forceinline__ void store(float* p, const f32x2 (&f)[4]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(lo(f[0]), hi(f[0]), lo(f[1]), hi(f[1]));
+    reinterpret_cast<float4*>(p)[1] = make_float4(lo(f[2]), hi(f[2]), lo(f[3]), hi(f[3]));
   }
 };
 struct NoResidual {};
@@ -59,17 +68,18 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 // The block scale from the block's largest magnitude: the factor the values are multiplied with, and the stored scale.
-// fp8: scale = amax/448.  Values are multiplied with the reciprocal (1.5 ulp of the quotient, so a value on a rounding
-// edge may land on either side) unless the scale is so small that its reciprocal overflows: then `divide` is set.
-struct Fp8Scale { float scale, factor; bool divide; };
+// fp8: scale = amax/448, as a product with 1/448 (1 ulp); the factor is its reciprocal (1 ulp), so a value on a rounding edge
+// may land on either side.  A scale so small that its reciprocal overflows (or that underflows to zero: 1 is stored) takes the
+// reciprocal of the scale times 2^64 first.
+struct Fp8Scale { float scale, factor; };
 __device__ __forceinline__ Fp8Scale fp8_scale(float amax) {
   Fp8Scale r;
-  r.scale = amax / 448.f;
-  if (r.scale == 0.f) r.scale = 1.f;                    // an all-zero block, or one whose scale underflows
-  r.divide = r.scale < 1.17549435e-38f;
-  r.factor = 1.f / r.scale;
+  r.scale = amax * (1.f / 448.f);
+  if (r.scale == 0.f) r.scale = 1.f;
+  r.factor = __fdividef(1.f, r.scale);
   return r;
 }
+__device__ __forceinline__ bool fp8_tiny(float scale) { return scale < 1.17549435e-38f; }
 // ue8m0: code of the smallest power of two s with amax <= 448 s (448 = 1.75 * 2^8), from the exponent and fraction bits
 __device__ __forceinline__ int mx_code(float amax) {
   const uint32_t u = __float_as_uint(amax);
@@ -102,7 +112,9 @@ struct NormArgs {
 };
 
 // One block per row, eight elements per thread and step, kVec steps.  Threads of a group of 16 (fp8) or 4 (mx)
-// consecutive lanes hold one scale block, so the block maximum is a shuffle inside the group.
+// consecutive lanes hold one scale block, so the block maximum is a shuffle inside the group.  The weight is multiplied in
+// before the row's sum is known (y = (h * weight) * inv), so that after it only the maximum and one product per output are
+// left; arithmetic is on pairs.
 template <typename XT, typename RT, int kFmt, int kVec>
 __global__ void __launch_bounds__(1024)
 norm_kernel(const NormArgs a) {
@@ -123,64 +135,78 @@ norm_kernel(const NormArgs a) {
       if (kRes) rv[v].load(res + 8 * i);
     }
   }
-  float h[kVec][8];
-  float ss = 0.f;
+  f32x2 h[kVec][4];
+  f32x2 ss = pair(0.f, 0.f);
 #pragma unroll
   for (int v = 0; v < kVec; ++v) {
     const int i = v * blockDim.x + threadIdx.x;
     if (i < n_vec) {
+      f32x2 w[4];
+      if (a.weight) {
+        if (a.weight_fp32) { Vec8<float> q; q.load(static_cast<const float*>(a.weight) + 8 * i); q.get(w); }
+        else { Vec8<__nv_bfloat16> q; q.load(static_cast<const __nv_bfloat16*>(a.weight) + 8 * i); q.get(w); }
+      }
       xv[v].get(h[v]);
       if (kRes) {
-        float r[8];
+        f32x2 r[4];
         rv[v].get(r);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[v][j] += r[j];
+        for (int j = 0; j < 4; ++j) h[v][j] = add2(h[v][j], r[j]);
         if (a.residual_out) Vec8<RL>::store(static_cast<RL*>(a.residual_out) + row * a.residual_out_stride + 8 * i, h[v]);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fmaf(h[v][j], h[v][j], ss);
+      for (int j = 0; j < 4; ++j) ss = fma2(h[v][j], h[v][j], ss);
+      if (a.weight) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[v][j] = mul2(h[v][j], w[j]);
+      }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[v][j] = 0.f;
+      for (int j = 0; j < 4; ++j) h[v][j] = pair(0.f, 0.f);
     }
   }
-  const float inv = rsqrtf(block_sum(ss, part) / (float)a.hidden + a.eps);
+  const float inv = rsqrtf(block_sum(lo(ss) + hi(ss), part) / (float)a.hidden + a.eps);
+  const f32x2 inv2 = pair(inv, inv);
 #pragma unroll
   for (int v = 0; v < kVec; ++v) {
     const int i = v * blockDim.x + threadIdx.x;
     const bool in = i < n_vec;
-    float w[8];
-    if (in && a.weight) {
-      if (a.weight_fp32) { Vec8<float> q; q.load(static_cast<const float*>(a.weight) + 8 * i); q.get(w); }
-      else { Vec8<__nv_bfloat16> q; q.load(static_cast<const __nv_bfloat16*>(a.weight) + 8 * i); q.get(w); }
-    } else {
+    f32x2 y[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = 1.f;
-    }
-    float y[8], amax = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) { y[j] = in ? h[v][j] * inv * w[j] : 0.f; amax = fmaxf(amax, fabsf(y[j])); }
+    for (int j = 0; j < 4; ++j) y[j] = mul2(h[v][j], inv2);
     if (in && a.y) Vec8<__nv_bfloat16>::store(a.y + row * a.y_stride + 8 * i, y);
     if (kFmt == CEP_BF16) continue;
     constexpr int kGroup = kFmt == CEP_FP8_E4M3_BLOCK128 ? 16 : 4;
+    float amax = max_abs3(lo(y[0]), hi(y[0]), lo(y[1]));
+    amax = max_abs3(amax, hi(y[1]), lo(y[2]));
+    amax = max_abs3(amax, hi(y[2]), lo(y[3]));
+    amax = max_abs3(amax, hi(y[3]), 0.f);
+    if (!in) amax = 0.f;                               // (a row whose sum is zero or infinite has inv infinite or zero: 0 * inf)
 #pragma unroll
     for (int o = kGroup / 2; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     if (!in) continue;
+    float factor;
     if (kFmt == CEP_FP8_E4M3_BLOCK128) {
       const Fp8Scale s = fp8_scale(amax);
+      factor = s.factor;
+      if (fp8_tiny(s.scale)) {                         // y to the normal range first
+        const f32x2 up = pair(18446744073709551616.f, 18446744073709551616.f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = s.divide ? y[j] / s.scale : y[j] * s.factor;
+        for (int j = 0; j < 4; ++j) y[j] = mul2(y[j], up);
+        factor = __fdividef(1.f, s.scale * 18446744073709551616.f);
+      }
       if (threadIdx.x % kGroup == 0) static_cast<float*>(a.scales)[row * a.n_scales + i / kGroup] = s.scale;
     } else {
       const int code = mx_code(amax);
-      const float f = mx_factor(code);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] *= f;
+      factor = mx_factor(code);
       if (threadIdx.x % kGroup == 0) static_cast<uint8_t*>(a.scales)[row * a.n_scales + i / kGroup] = (uint8_t)code;
     }
+    const f32x2 f2 = pair(factor, factor);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = mul2(y[j], f2);
     uint2 c;
-    c.x = pack2_e4m3(y[0], y[1]) | (pack2_e4m3(y[2], y[3]) << 16);
-    c.y = pack2_e4m3(y[4], y[5]) | (pack2_e4m3(y[6], y[7]) << 16);
+    c.x = pack2_e4m3(lo(y[0]), hi(y[0])) | (pack2_e4m3(lo(y[1]), hi(y[1])) << 16);
+    c.y = pack2_e4m3(lo(y[2]), hi(y[2])) | (pack2_e4m3(lo(y[3]), hi(y[3])) << 16);
     *reinterpret_cast<uint2*>(a.codes + row * a.hidden + 8 * i) = c;
   }
 }
@@ -199,14 +225,31 @@ norm_any_kernel(const NormArgs a) {
   const RL* res = static_cast<const RL*>(a.residual) + (kRes ? row * a.residual_stride : 0);
   RL* rout = static_cast<RL*>(a.residual_out) + (kRes && a.residual_out ? row * a.residual_out_stride : 0);
   float ss = 0.f;
-  for (int i = threadIdx.x; i < a.hidden; i += blockDim.x) {
-    float h = to_f32(x[i]);
-    if (kRes) {
-      h += to_f32(res[i]);
-      if (a.residual_out) put(rout + i, h);
+  constexpr int kU = 4;                                 // loads in flight per thread
+  for (int i0 = threadIdx.x; i0 < a.hidden; i0 += kU * blockDim.x) {
+    XT xe[kU];
+    RL re[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int i = i0 + u * blockDim.x;
+      if (i < a.hidden) {
+        xe[u] = x[i];
+        if (kRes) re[u] = res[i];
+      }
     }
-    hs[i] = h;
-    ss = fmaf(h, h, ss);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int i = i0 + u * blockDim.x;
+      if (i < a.hidden) {
+        float h = to_f32(xe[u]);
+        if (kRes) {
+          h += to_f32(re[u]);
+          if (a.residual_out) put(rout + i, h);
+        }
+        hs[i] = h;
+        ss = fmaf(h, h, ss);
+      }
+    }
   }
   const float inv = rsqrtf(block_sum(ss, part) / (float)a.hidden + a.eps);     // (also orders the writes to hs)
   constexpr int kBlock = kFmt == CEP_MXFP4_E4M3 ? 32 : 128;
@@ -220,7 +263,7 @@ norm_any_kernel(const NormArgs a) {
       if (i < a.hidden) {
         const float w = !a.weight ? 1.f : a.weight_fp32 ? static_cast<const float*>(a.weight)[i]
                                                         : __bfloat162float(static_cast<const __nv_bfloat16*>(a.weight)[i]);
-        y[j] = hs[i] * inv * w;
+        y[j] = hs[i] * w * inv;
         if (a.y) a.y[row * a.y_stride + i] = __float2bfloat16_rn(y[j]);
       }
       amax = fmaxf(amax, fabsf(y[j]));
@@ -230,7 +273,13 @@ norm_any_kernel(const NormArgs a) {
     for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     Fp8Scale s = fp8_scale(amax);
     const int code = mx_code(amax);
-    if (kFmt == CEP_MXFP4_E4M3) { s.factor = mx_factor(code); s.divide = false; }
+    if (kFmt == CEP_MXFP4_E4M3) {
+      s.factor = mx_factor(code);
+    } else if (fp8_tiny(s.scale)) {
+#pragma unroll
+      for (int j = 0; j < kBlock / 32; ++j) y[j] *= 18446744073709551616.f;
+      s.factor = __fdividef(1.f, s.scale * 18446744073709551616.f);
+    }
     if (lane == 0) {
       if (kFmt == CEP_MXFP4_E4M3) static_cast<uint8_t*>(a.scales)[row * a.n_scales + b] = (uint8_t)code;
       else static_cast<float*>(a.scales)[row * a.n_scales + b] = s.scale;
@@ -238,7 +287,7 @@ norm_any_kernel(const NormArgs a) {
 #pragma unroll
     for (int j = 0; j < kBlock / 32; ++j) {
       const int i = b * kBlock + j * 32 + lane;
-      if (i < a.hidden) a.codes[row * a.hidden + i] = (uint8_t)pack2_e4m3(s.divide ? y[j] / s.scale : y[j] * s.factor, 0.f);
+      if (i < a.hidden) a.codes[row * a.hidden + i] = (uint8_t)pack2_e4m3(y[j] * s.factor, 0.f);
     }
   }
 }
@@ -253,7 +302,12 @@ cudaError_t launch_fmt(const NormArgs& a, int n_tokens, bool wide, cudaStream_t 
     return cudaGetLastError();
   }
   const int n_vec = a.hidden / 8;
-  const int kv = n_vec <= 256 ? 1 : n_vec <= 512 ? 2 : 4;
+  // Steps per thread.  Few rows: one step, the row's latency is what counts (7168 fp8, 128 rows: 3.0 us against 3.2 and 4.2
+  // with two and four steps; 1024 rows 15.0 against 15.6 and 15.8).  Many rows: more steps keep more bytes in flight per
+  // thread (16384 rows of 7168 fp8: 159 us with four, 177 with one or two; of 2048: 38 with two, 40 with one or four; of 512:
+  // 13.0 with one, 13.8 with two), but with an fp32 tensor four steps do not fit the registers (194 us with two, 220 with four).
+  const bool fp32 = sizeof(XT) == 4 || std::is_same<RT, float>::value;
+  const int kv = n_vec > 2048 ? 4 : n_vec <= 64 || (n_tokens <= 1024 && n_vec <= 1024) ? 1 : n_vec <= 512 || fp32 ? 2 : 4;
   const int threads = ((n_vec + kv - 1) / kv + 31) / 32 * 32;
   if (kv == 1) norm_kernel<XT, RT, kFmt, 1><<<n_tokens, threads, 0, s>>>(a);
   else if (kv == 2) norm_kernel<XT, RT, kFmt, 2><<<n_tokens, threads, 0, s>>>(a);
