@@ -90,12 +90,15 @@ __device__ __forceinline__ void put4(OT* p, float4 v, int left, bool vec_ok) {
   if (left > 3) put_out(p + 3, v.w);
 }
 
-template <typename OT, bool kSplit>
+// kLora: the call may have adapters.  (Without, an fp32 output's running sums fit the registers.)
+template <typename OT, bool kSplit, bool kLora>
 __global__ void __launch_bounds__(kThreads, 1)
 project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
-                     const __grid_constant__ CUtensorMap tm_up, const Shape sh, int splits, int after_peer, const LoraArgs la, OT* __restrict__ y,
+                     const __grid_constant__ CUtensorMap tm_up, const Shape sh, int splits, int after_peer, const LoraArgs la_, OT* __restrict__ y,
                      int64_t y_stride, int vec_ok, int32_t* __restrict__ tile_counter, int32_t* __restrict__ status) {
   constexpr bool kF32 = sizeof(OT) == 4;
+  LoraArgs la = la_;
+  if (!kLora) la.has = 0;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* smem_x = smem;
@@ -296,6 +299,9 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       const int left = sh.N - nb * 256;                  // columns of this block that exist
       constexpr int kSum = kF32 ? 128 : 1;
       float sum[kSum];
+#pragma unroll
+      for (int c = 0; c < kSum; ++c) sum[c] = 0.f;
+#pragma unroll 1
       for (int kb = kb0; ok && kb < kb1; kb += sh.slab_steps) {          // one accumulation chain after the other
         if (s_warp && la.has && kb + sh.slab_steps >= kb1) {
           // the adapters' steps end the last chain
@@ -344,7 +350,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             tc_ld16(taddr + (s_warp ? 128 : 0) + c, d);
             tc_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[c + i] = kb == kb0 ? __uint_as_float(d[i]) : sum[c + i] + __uint_as_float(d[i]);
+            for (int i = 0; i < 16; ++i) sum[c + i] += __uint_as_float(d[i]);
           }
         } else {
           OT* row = y + (size_t)t * y_stride + nb * 256;
@@ -461,6 +467,9 @@ cudaError_t launch(const ProjectArgs& a, const Plan& p, const CUtensorMap& w, co
   const size_t elt = sizeof(OT);
   const int vec_ok = reinterpret_cast<uintptr_t>(a.y) % 16 == 0 && (size_t)a.y_stride * elt % 16 == 0;
   const LoraArgs la = lora_args(a);
+  // (an fp32 output without adapters has kernels of its own, see there)
+  const auto rounds = a.bank || elt == 2 ? project_large_kernel<OT, false, true> : project_large_kernel<OT, false, sizeof(OT) == 2>;
+  const auto shared = a.bank || elt == 2 ? project_large_kernel<OT, true, true> : project_large_kernel<OT, true, sizeof(OT) == 2>;
   Shape sh{a.T, a.N, p.num_kb, sizeof(OT) == 4 ? kSlabSteps : p.num_kb, p.m_tiles, p.n_blocks, n_group_for(p.n_blocks, 256, a.K, 2), 0, p.full};
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[2];
@@ -477,7 +486,7 @@ cudaError_t launch(const ProjectArgs& a, const Plan& p, const CUtensorMap& w, co
     }
     const int resident = g_clusters[dev][1];
     cfg.gridDim = dim3(2 * (unsigned)(p.full < resident ? p.full : resident), 1, 1);
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, project_large_kernel<OT, false>, w, x, u, sh, 1, 0, la, static_cast<OT*>(a.y), a.y_stride, vec_ok,
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, rounds, w, x, u, sh, 1, 0, la, static_cast<OT*>(a.y), a.y_stride, vec_ok,
                                              a.tile_counter, a.status);
     if (e != cudaSuccess) return e;
     cfg.numAttrs = 2;                                  // the rest starts on SMs as they run out of tiles
@@ -486,7 +495,7 @@ cudaError_t launch(const ProjectArgs& a, const Plan& p, const CUtensorMap& w, co
     sh.tile0 = p.full; sh.n_tiles = p.rest;
     attr[0].val.clusterDim.x = (unsigned)(2 * p.splits);
     cfg.gridDim = dim3((unsigned)(p.rest * 2 * p.splits), 1, 1);
-    return cudaLaunchKernelEx(&cfg, project_large_kernel<OT, true>, w, x, u, sh, p.splits, p.full > 0 ? 1 : 0, la, static_cast<OT*>(a.y), a.y_stride,
+    return cudaLaunchKernelEx(&cfg, shared, w, x, u, sh, p.splits, p.full > 0 ? 1 : 0, la, static_cast<OT*>(a.y), a.y_stride,
                               vec_ok, a.tile_counter, a.status);
   }
   return cudaSuccess;
@@ -498,8 +507,9 @@ cudaError_t project_large_setup(int dev, int n_sms) {
   if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
   int* clusters = g_clusters[dev];
   if (clusters[0]) return cudaSuccess;
-  const void* kernels[4] = {(const void*)project_large_kernel<__nv_bfloat16, false>, (const void*)project_large_kernel<__nv_bfloat16, true>,
-                            (const void*)project_large_kernel<float, false>, (const void*)project_large_kernel<float, true>};
+  const void* kernels[6] = {(const void*)project_large_kernel<__nv_bfloat16, false, true>, (const void*)project_large_kernel<__nv_bfloat16, true, true>,
+                            (const void*)project_large_kernel<float, false, true>, (const void*)project_large_kernel<float, true, true>,
+                            (const void*)project_large_kernel<float, false, false>, (const void*)project_large_kernel<float, true, false>};
   for (const void* k : kernels) {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
@@ -512,7 +522,7 @@ cudaError_t project_large_setup(int dev, int n_sms) {
   for (int c = 1; c <= kMaxSplits; ++c) {
     attr[0].val.clusterDim.x = (unsigned)(2 * c);
     cfg.gridDim = dim3((unsigned)(n_sms / (2 * c) * 2 * c), 1, 1);
-    const cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters[c], project_large_kernel<__nv_bfloat16, true>, &cfg);
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(&clusters[c], project_large_kernel<__nv_bfloat16, true, true>, &cfg);
     if (e != cudaSuccess) return e;
   }
   if (clusters[1] < 1) return cudaErrorNotSupported;
