@@ -32,6 +32,7 @@ struct __align__(8) ShrinkBarriers {
 };
 struct ShrinkLists {                                 // scratch of the list building
   int id[kLargeTok], job[kLargeTok], n_chunks, warp_count[8];
+  int first[kRows], count[kRows];                    // a token's own chunks among the pass's (they are consecutive)
   int chunk[kRows * kLoraMaxChunks];    // adapter * 16 + chunk of its ranks
 };
 
@@ -84,7 +85,7 @@ __device__ int expand_chunks(const int* job, int m, const LoraBank& bank, int* o
 
 // Grid (token tiles, pass stripes, K parts); the parts are a cluster.  box: rows of x one TMA load brings.  With token_tile
 // other than 128 the first stripe only builds the projection kernel's lists, beside the others' work.
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)              // (few registers: blocks of the projection kernel share the SM)
 lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K, int N,
                    const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int x_stage, int chunks, int stages, int n_acc,
                    int tmem_cols, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_chunks, int32_t* __restrict__ chunk_lists,
@@ -159,6 +160,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   }
   const int k0 = (int)((long long)steps * part / parts), k1 = (int)((long long)steps * (part + 1) / parts);
   const int cols = chunks * kLoraChunk;              // columns of an accumulator
+  const int pitch = cols + 4;                        // floats per row of exchanged sums
   int stage = 0; uint32_t phase = 0, acc_phase = 0;  // the loading and the issuing thread each keep their own
 
   for (int c0 = ((int)blockIdx.y - list_stripes) * chunks; c0 < total; c0 += ((int)gridDim.y - list_stripes) * chunks) {
@@ -211,10 +213,15 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
       got = __all_sync(0xffffffffu, got);
       const int row = (warp & 3) * 32 + lane, my = L.id[row];
       const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+      int first = 0, count = 0;
       if (got) {
         tc_fence_after();
+        const float scale = my >= 0 ? bank.scale[my] : 0.f;
+        const int rank = my >= 0 ? bank.rank[my] : 0;
         for (int i = 0; i < n; ++i) {
-          __syncwarp();                              // the loads are warp-collective
+          const int v = L.chunk[c0 + i];
+          const bool mine = my == v / kLoraMaxChunks;
+          if (!__any_sync(0xffffffffu, mine)) continue;                    // (the loads are warp-collective)
           uint32_t d[16];
           tc_ld16(taddr + i * kLoraChunk, d);
           tc_wait_ld();
@@ -225,14 +232,14 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
 #pragma unroll
             for (int j = 0; j < 16; ++j) d[j] = __float_as_uint(__uint_as_float(d[j]) + __uint_as_float(e[j]));
           }
-          const int v = L.chunk[c0 + i], a = v / kLoraMaxChunks, c = v % kLoraMaxChunks;
-          if (my == a) {
-            const int left = bank.rank[a] - c * kLoraChunk;         // ranks between the adapter's and the chunk's end are zero
-            const float scale = bank.scale[a];
+          if (mine) {
+            if (count++ == 0) first = i;
+            const int c = v % kLoraMaxChunks, left = rank - c * kLoraChunk;
             float4* dst = reinterpret_cast<float4*>(parts == 1 ? s_out + (size_t)(t0 + row) * bank.rank_pad + c * kLoraChunk
-                                                               : reinterpret_cast<float*>(smem) + row * cols + i * kLoraChunk);
+                                                               : reinterpret_cast<float*>(smem) + row * pitch + i * kLoraChunk);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
+              // ranks between the adapter's and the chunk's end are zero
               float4 f;
               f.x = 4 * q + 0 < left ? scale * __uint_as_float(d[4 * q + 0]) : 0.f;
               f.y = 4 * q + 1 < left ? scale * __uint_as_float(d[4 * q + 1]) : 0.f;
@@ -241,8 +248,11 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
               dst[q] = f;
             }
           }
+          __syncwarp();
         }
       }
+      L.first[row] = first;
+      L.count[row] = count;
     }
     acc_phase ^= 1u;
     if (parts > 1) {
@@ -250,21 +260,19 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
       cluster_sync_all();
       const int r0 = rows * part / parts, r1 = rows * (part + 1) / parts;
       const uint32_t base = smem_u32(smem);
-      // a row per half warp and four ranks per lane: up to four chunks of the row's adapter at a time
+      // a row per half warp and four ranks per lane: up to four of the row's chunks at a time
       for (int row = r0 + 2 * warp + (lane >> 4); row < r1; row += 2 * kThreads / 32) {
-        const int my = L.id[row];
-        for (int i = (lane & 15) >> 2; i < n; i += 4) {
-          const int v = L.chunk[c0 + i];
-          if (v / kLoraMaxChunks != my) continue;
+        const int end = L.first[row] + L.count[row];
+        for (int i = L.first[row] + ((lane & 15) >> 2); i < end; i += 4) {
           float4 f[kMaxParts];
 #pragma unroll
           for (int p = 0; p < kMaxParts; ++p)
-            if (p < parts) f[p] = ld_cluster_f4(mapa(base + (uint32_t)((row * cols + i * kLoraChunk + (lane & 3) * 4) * 4), (uint32_t)p));
+            if (p < parts) f[p] = ld_cluster_f4(mapa(base + (uint32_t)((row * pitch + i * kLoraChunk + (lane & 3) * 4) * 4), (uint32_t)p));
           float4 o = f[0];
 #pragma unroll
           for (int p = 1; p < kMaxParts; ++p)
             if (p < parts) { o.x += f[p].x; o.y += f[p].y; o.z += f[p].z; o.w += f[p].w; }
-          *reinterpret_cast<float4*>(s_out + (size_t)(t0 + row) * bank.rank_pad + v % kLoraMaxChunks * kLoraChunk + (lane & 3) * 4) = o;
+          *reinterpret_cast<float4*>(s_out + (size_t)(t0 + row) * bank.rank_pad + L.chunk[c0 + i] % kLoraMaxChunks * kLoraChunk + (lane & 3) * 4) = o;
         }
       }
       fence_proxy_async_smem();                      // the next pass's loads write where the partial sums were
