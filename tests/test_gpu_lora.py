@@ -261,6 +261,27 @@ def test_fp32_outputs_keep_fp32_accuracy(T, N):
     assert ((got - y).norm() / y.norm()).item() <= 1.3e-6
 
 
+@pytest.mark.parametrize("T,K,N,ranks,out", [(1, 64, 7, (8,), "bf16"), (77, 328, 520, (16, 33), "bf16"), (128, 512, 256, (4,) * 40, "fp32"),
+                                             (513, 264, 300, (64, 8), "bf16"), (1030, 128, 100, (256, 1), "fp32")])
+def test_nothing_is_written_past_the_buffers(T, K, N, ranks, out):
+    # workspace, bank and output inside larger buffers filled with a pattern
+    cfg = cep.LoraConfig(K, N, T, len(ranks), max(ranks), cep.CEP_ELEM_FP32 if out == "fp32" else cep.CEP_ELEM_BF16)
+    big = {n: torch.full((size + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+           for n, size in (("ws", cep.lora_plan_workspace_bytes(cfg)), ("bank", cep.lora_bank_bytes(cfg)))}
+    w, x = rand((N, K), 1, K ** -0.5), rand((T, K), 2)
+    plan = cep.lora_plan(cfg, w, big["bank"][:-8192], big["ws"][:-8192])
+    for s, r in enumerate(ranks):
+        cep.lora_load_adapter(plan, s, r, 1.0, rand((r, K), 10 + s, K ** -0.5), rand((N, r), 50 + s))
+    dtype = torch.float32 if out == "fp32" else torch.bfloat16
+    y = torch.full((T + 64, N), -77.0, dtype=dtype, device="cuda")
+    for ids in (ids_of(T, len(ranks), 3), None):
+        cep.lora_project(plan, x, ids, y[:T])
+        assert cep.lora_status(plan) == 0
+        assert (y[T:] == -77.0).all() and torch.isfinite(y[:T]).all()
+        assert all((b[-8192:] == 0xA5).all() for b in big.values())
+    cep.lora_plan_destroy(plan)
+
+
 def test_python_refusals():
     c = Case(64, 64, ranks=(8,), max_tokens=16)
     x = rand((4, 64), 1)
