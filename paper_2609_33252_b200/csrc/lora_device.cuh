@@ -97,11 +97,12 @@ template <typename OT> __device__ __forceinline__ void put_out(OT* p, float v);
 template <> __device__ __forceinline__ void put_out<float>(float* p, float v) { *p = v; }
 template <> __device__ __forceinline__ void put_out<__nv_bfloat16>(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// The list entries of a step (kStep of them, the second -1 past the end).
-__device__ __forceinline__ int2 list_pair(const int32_t* list, int c, int total) {
-  if (c >= total) return make_int2(-1, -1);
-  return make_int2(__ldcg(list + c), c + 1 < total ? __ldcg(list + c + 1) : -1);
+// The list entries of a step (kStep of them, -1 past the end).  They are read whether there are that many or not, so that
+// the reads do not wait for the list's length; `cap` entries exist.
+__device__ __forceinline__ int2 list_pair(const int32_t* list, int c, int cap) {
+  return c + 1 < cap ? __ldcg(reinterpret_cast<const int2*>(list + c)) : make_int2(-1, -1);
 }
+__device__ __forceinline__ int2 up_to(int2 e, int c, int total) { return make_int2(c < total ? e.x : -1, c + 1 < total ? e.y : -1); }
 constexpr int kLookAhead = 8;                          // steps whose entries the loading thread reads at once
 
 // Index of a chunk's [N][16] block in the up bank.

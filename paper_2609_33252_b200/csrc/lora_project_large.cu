@@ -182,7 +182,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         for (int c0 = c_first; ok && c0 < total; c0 += kLookAhead * c_stride) {
           int2 e[kLookAhead];
 #pragma unroll
-          for (int j = 0; j < kLookAhead; ++j) e[j] = list_pair(list, c0 + j * c_stride, total);
+          for (int j = 0; j < kLookAhead; ++j) e[j] = up_to(list_pair(list, c0 + j * c_stride, kLargeTok * kLoraMaxChunks), c0 + j * c_stride, total);
 #pragma unroll
           for (int j = 0; j < kLookAhead; ++j) {
             if (e[j].x < 0) break;
@@ -320,7 +320,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             const int first = stage;
             int n = 0;
             for (; n < kBatch && c0 < total; ++n, c0 += c_stride, ++step) {
-              if ((step & 31) == 0) e = list_pair(list, c0 + lane * c_stride, total);
+              if ((step & 31) == 0) e = up_to(list_pair(list, c0 + lane * c_stride, kLargeTok * kLoraMaxChunks), c0 + lane * c_stride, total);
               const int v0 = __shfl_sync(0xffffffffu, e.x, step & 31), v1 = __shfl_sync(0xffffffffu, e.y, step & 31);
               ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
               ok = __all_sync(0xffffffffu, ok);

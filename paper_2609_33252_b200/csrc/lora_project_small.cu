@@ -98,12 +98,16 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       }
       if (la.has && ok) {
         pdl_wait();
-        const int total = __ldcg(la.n_chunks + blockIdx.z);
         const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
+        const int cap = tok * kLoraMaxChunks;
+        int total = cap;                               // (until it is read)
         for (int c0 = split * kStep; ok && c0 < total;) {
           int2 e[kLookAhead];
 #pragma unroll
-          for (int j = 0; j < kLookAhead; ++j) e[j] = list_pair(list, c0 + j * splits * kStep, total);
+          for (int j = 0; j < kLookAhead; ++j) e[j] = list_pair(list, c0 + j * splits * kStep, cap);
+          total = __ldcg(la.n_chunks + blockIdx.z);
+#pragma unroll
+          for (int j = 0; j < kLookAhead; ++j) e[j] = up_to(e[j], c0 + j * splits * kStep, total);
 #pragma unroll
           for (int j = 0; j < kLookAhead; ++j) {
             if (e[j].x < 0) break;
@@ -171,19 +175,20 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     bool ok = true;
     if (la.has) {
       pdl_wait();
+      const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
+      const int cap = tok * kLoraMaxChunks;
+      int2 e = list_pair(list, (split + lane * splits) * kStep, cap);      // lane i: the i-th of the next 32 steps
+      const int total = __ldcg(la.n_chunks + blockIdx.z);
       SRow<4> row;
       row.fetch(la, tid < npad && t0 + tid < T ? t0 + tid : -1);
-      const int total = __ldcg(la.n_chunks + blockIdx.z);
-      const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
       int stage = (kb1 - kb0) % stages;                // where the K steps end
       uint32_t phase = 0;                              // one parity bit per stage
-      int2 e = make_int2(-1, -1);                      // lane i: the i-th of the next 32 steps
       int step = 0;
       for (int c0 = split * kStep; ok && c0 < total;) {
         const int first = stage;
         int n = 0;
         for (; n < kBatch && c0 < total; ++n, c0 += splits * kStep, ++step) {
-          if ((step & 31) == 0) e = list_pair(list, c0 + lane * splits * kStep, total);
+          if ((step & 31) == 0) e = up_to(step == 0 ? e : list_pair(list, c0 + lane * splits * kStep, cap), c0 + lane * splits * kStep, total);
           const int v0 = __shfl_sync(0xffffffffu, e.x, step & 31), v1 = __shfl_sync(0xffffffffu, e.y, step & 31);
           ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
           ok = __all_sync(0xffffffffu, ok);
