@@ -46,7 +46,7 @@ Carve carve(const cep_lora_config& c) {
   auto take = [&](size_t& f, size_t bytes) { f = o; o = up_to(o + bytes, 256); };
   const size_t T = c.max_tokens;
   take(w.status, kStWords * 4);
-  take(w.tile_counter, 4);
+  take(w.tile_counter, 8);
   if (c.max_adapters) {
     take(w.ids, T * 4);
     take(w.n_chunks, (T / 64 + 1) * 4);
@@ -161,7 +161,7 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
                       (long long)cfg->out_features * kLoraChunk * 2, kLoraChunk, 128, 32);
   if (m) { lora_plan_destroy(p); return record_error(CEP_ERR_CUDA, "lora: cuTensorMapEncodeTiled failed (%d)", m); }
   // the status word and the counters start at zero, every slot of the bank empty
-  e = cudaMemsetAsync(p->ws, 0, w.tile_counter + 4, st);
+  e = cudaMemsetAsync(p->ws, 0, w.tile_counter + 8, st);
   if (e == cudaSuccess && b.total) e = cudaMemsetAsync(bk, 0, b.down, st);
   if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaMemsetAsync", e);
   rc = leave(p, st, false);
@@ -223,7 +223,7 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
   cudaError_t e = cudaSuccess;
   if (adapter_ids) {
     e = launch_lora_shrink(tm_x, p->tm_down, box, n_tokens, c.in_features, c.out_features, adapter_ids, p->bank, token_tile, p->ids, p->n_chunks, p->chunks, p->s,
-                           p->tile_counter, p->status, st);
+                           p->status, st);
     a.bank = &p->bank;
     a.step = LoraStep{p->ids, p->n_chunks, p->chunks, p->s};
   }

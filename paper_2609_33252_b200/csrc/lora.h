@@ -40,7 +40,7 @@ cudaError_t lora_shrink_setup();             // once per plan, with its device c
 // projection kernel that follows (its job lists are made here).
 cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
-                               int32_t* tile_counter, int32_t* status, cudaStream_t s);
+                               int32_t* status, cudaStream_t s);
 
 struct ProjectArgs {
   int T, K, N;
@@ -48,7 +48,7 @@ struct ProjectArgs {
   void* y; int64_t y_stride;
   const LoraBank* bank;                      // nullptr: no adapters in this call
   LoraStep step;
-  int32_t* tile_counter;
+  int32_t* tile_counter;                     // [2], zero between calls: tiles handed out, CTA pairs done
   int32_t* status;
 };
 // Tensor maps are encoded per call for x and once for the weight and the up bank.

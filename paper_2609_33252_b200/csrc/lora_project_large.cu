@@ -145,7 +145,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
   // What precedes this launch is the down projection.  The K steps do not need it and start at once; who reads its lists and s
-  // waits for it (the tile counter was zeroed before any of its blocks let this launch start).  Or (after_peer) it is the launch
+  // waits for it.  Or (after_peer) it is the launch
   // with the full rounds of tiles, which touches nothing of this one's and let it start only after the down projection's end.
   const bool wait = la.has && !after_peer;
   if (!kSplit && (wait ? warp >= 7 : true)) {
@@ -404,6 +404,10 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();                 // no CTA leaves while another may still signal it; kSplit: the partial sums are there
+  if (!kSplit && !is_peer && threadIdx.x == 0) {
+    // the last pair puts the counters back (every pair has fetched its last id)
+    if (atomicInc(reinterpret_cast<unsigned*>(tile_counter) + 1, gridDim.x / 2 - 1) == gridDim.x / 2 - 1) atomicExch(tile_counter, 0);
+  }
   if (kSplit) {
     // this pair adds its share of the tile's rows over the cluster's pairs, in order (after a wait that ran out the sums mean
     // nothing and the status word says so)
@@ -483,10 +487,6 @@ cudaError_t launch(const ProjectArgs& a, const Plan& p, const CUtensorMap& w, co
   cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = kSmem; cfg.stream = s; cfg.attrs = attr;
   cfg.numAttrs = a.bank ? 2 : 1;                       // only ever overlaps this call's own down projection
   if (p.full) {
-    if (!a.bank) {                                     // (the down projection zeroes the counter)
-      const cudaError_t e = cudaMemsetAsync(a.tile_counter, 0, sizeof(int32_t), s);
-      if (e != cudaSuccess) return e;
-    }
     const int resident = g_clusters[dev][1];
     cfg.gridDim = dim3(2 * (unsigned)(p.full < resident ? p.full : resident), 1, 1);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, rounds, w, x, u, sh, 1, 0, la, static_cast<OT*>(a.y), a.y_stride, vec_ok,

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kThreads, 3)              // (few registers: b
 lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K, int N,
                    const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int x_stage, int chunks, int stages, int n_acc,
                    int tmem_cols, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_chunks, int32_t* __restrict__ chunk_lists,
-                   float* __restrict__ s_out, int32_t* __restrict__ tile_counter, int32_t* __restrict__ status) {
+                   float* __restrict__ s_out, int32_t* __restrict__ status) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ ShrinkBarriers bars;
@@ -108,7 +108,6 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
     mbar_init(smem_u32(&bars.acc_full), 1);
     bars.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (reporter && blockIdx.x == 0) { atomicExch(tile_counter, 0); __threadfence(); }        // in place before the projection starts
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -335,7 +334,7 @@ cudaError_t lora_shrink_setup() {
 
 cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
-                               int32_t* tile_counter, int32_t* status, cudaStream_t s) {
+                               int32_t* status, cudaStream_t s) {
   // Up to 128 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
   const bool beside = lora_beside(T);
   const int chunks = beside ? 4 : 8, smem = beside ? kShortSmem : kLongSmem;
@@ -348,7 +347,11 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
   int parts = 2 * kSms / tiles;
   if (parts > kMaxParts) parts = kMaxParts;
-  if (parts > steps) parts = steps;
+  // Long batches: at least 8 steps a part, fewer blocks leave SMs to the projection's first tiles (6821 tokens of 896 -> 640:
+  // 28 us with, 33 without; 4096 of 2048 -> 7168: 102 and 105).  Short ones: the down projection's latency is what counts
+  // (519 of 2048 -> 2048: 24 and 22; 64: 17 and 14).
+  const int least = tiles >= 16 ? 8 : 1;
+  if (parts > steps / least) parts = steps / least;
   if (parts < 1) parts = 1;
   // passes a tile can need, and how many blocks share them
   const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
@@ -370,7 +373,7 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   cfg.gridDim = dim3(tiles, stripes + (token_tile != kRows), parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
   cfg.attrs = attr; cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, lora_shrink_kernel, reinterpret_cast<const CUtensorMap&>(tm_x), reinterpret_cast<const CUtensorMap&>(tm_down), T, K,
-                            token_tile == kLargeTok ? 0 : N, ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, tile_counter, status);
+                            token_tile == kLargeTok ? 0 : N, ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, status);
 }
 
 }  // namespace cep
