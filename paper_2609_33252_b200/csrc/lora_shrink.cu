@@ -165,6 +165,13 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   for (int c0 = ((int)blockIdx.y - list_stripes) * chunks; c0 < total; c0 += ((int)gridDim.y - list_stripes) * chunks) {
     if (c0 < 0) break;                               // (the stripe that builds lists)
     const int n = min(chunks, total - c0);
+    if (N > 0 && warp >= 2 && (int)threadIdx.x - 64 < n * kLoraChunk) {
+      // a short batch meets its adapters' rows of A for the first time here, while the projection kernel beside this one keeps
+      // the memory busy: ask for all of them now, not a stage at a time
+      const int r = threadIdx.x - 64, v = L.chunk[c0 + r / kLoraChunk], a = v / kLoraMaxChunks, row = v % kLoraMaxChunks * kLoraChunk + r % kLoraChunk;
+      if (row < bank.rank[a])
+        prefetch_l2(bank.down + ((size_t)a * bank.rank_pad + row) * K + k0 * 64, (uint32_t)(min(K, k1 * 64) - k0 * 64) * 2);
+    }
     if (N > 0 && warp == 5 && lane < n) {
       // a short batch meets each adapter's columns of B for the first time in the projection's last steps: have them in the
       // L2 by then (each part asks for its share)
