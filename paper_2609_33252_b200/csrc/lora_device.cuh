@@ -15,9 +15,8 @@ constexpr int kSlabSteps = 12;                        // K steps (of 64) per acc
 // The up projection's steps.  A step covers kStep chunks of 16 ranks and takes a stage of the ring: the adapter's columns of
 // B (by TMA) where the K steps have W, and the tokens' rows of s (by the s-row warps) where they have x.  The loading thread
 // tells those warps that the stage is free (ready); they tell the MMA thread that the rows are written (sfull).  The fence
-// between their stores and the MMA costs as much as the stores, so kBatch steps share one.
+// between their stores and the MMA costs as much as the stores, so a few steps share one (kBatch in either kernel).
 constexpr int kStep = 2;
-constexpr int kBatch = 2;
 
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // K-major operand with rows of 32 bytes (16 ranks), 32-byte swizzle, 8-row groups 256 bytes apart

@@ -28,6 +28,7 @@ constexpr int kPoison = -2;
 constexpr int kAsk = 10;                               // K steps before a tile's end at which the next id is fetched
 constexpr int kThreads = 352;                          // warp 0 loads, 1 MMA, 2-5 epilogue, 6 tile ids, 7-10 rows of s
 constexpr int kReaders = 19;                           // leader: loads, MMA, 4 epilogue, 4 s-row warps; peer: loads, 4, 4
+constexpr int kBatch = 4;                              // (1000 tokens, 24 adapters in every tile: 157 us with four, 164 with two)
 constexpr int kMaxSplits = 4;                          // CTA pairs of a portable cluster
 constexpr int kPitch = 260;                            // floats per row of exchanged sums: rows four banks apart
 struct __align__(8) Barriers {
