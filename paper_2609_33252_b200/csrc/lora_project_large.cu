@@ -454,7 +454,7 @@ Plan plan(const int* clusters, int T, int N, int K) {
   constexpr long long kTile = 4;                       // a tile's start and end, in K steps
   constexpr long long kExchange = 12;                  // exchanging partial sums (3.5 us)
   constexpr long long kAlone = 3;                      // one tile per pair, stored through shared memory: whole rows of 256 columns
-  constexpr long long kSecond = 6;
+  constexpr long long kSecond = 10;
   Plan p{};
   p.m_tiles = (T + kLargeTok - 1) / kLargeTok; p.n_blocks = (N + 255) / 256; p.num_kb = (K + 63) / 64;
   const long long total = (long long)p.m_tiles * p.n_blocks, round = clusters[1];
@@ -464,7 +464,7 @@ Plan plan(const int* clusters, int T, int N, int K) {
   for (int s = 1; s <= kMaxSplits && s <= p.num_kb && rest > 0; ++s) {
     if (clusters[s] < 1) continue;
     const long long cost = rounds * (p.num_kb + kTile) + (rounds > 0 ? kSecond : 0) +
-                           (rest + clusters[s] - 1) / clusters[s] * ((p.num_kb + s - 1) / s + (s > 1 ? kExchange : kAlone));
+                           (rest + clusters[s] - 1) / clusters[s] * ((p.num_kb + s - 1) / s + (s > 1 ? kExchange + kTile : kAlone));
     if (cost < p.cost) { p.cost = cost; p.full = (int)(rounds * round); p.rest = (int)rest; p.splits = s; }
   }
   return p;
