@@ -206,7 +206,7 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
   if (!on(adapter_ids, 4)) return record_error(CEP_ERR_ARG, "lora: adapter_ids is misaligned");
   // Up to 128 tokens the small kernel's tile is no wider than the batch; beyond, the kernel whose busiest SM has less to do.
   const bool small = n_tokens <= kSmallTok || (n_tokens <= 4 * kSmallTok &&
-                     project_small_cost(p->device, n_tokens, c.out_features, c.in_features, c.out_elem == CEP_ELEM_FP32) <=
+                     project_small_cost(p->device, n_tokens, c.out_features, c.in_features, c.out_elem == CEP_ELEM_FP32) + 3 <=
                      project_large_cost(p->device, n_tokens, c.out_features, c.in_features));
   const int f32 = c.out_elem == CEP_ELEM_FP32;
   const int token_tile = small ? project_small_tile(f32) : kLargeTok, box = small ? project_small_tokens(n_tokens, f32) : 128;

@@ -298,14 +298,17 @@ struct Plan { int npad, tok, n_tiles, t_tiles, num_kb, splits; long long cost; }
 // fewer SMs are usable for some sizes.
 Plan plan(const int* clusters, int T, int N, int K, int out_f32) {
   constexpr long long kExchange = 6;                   // what the exchange of partial sums costs (2 us)
+  constexpr long long kStart = 5;                      // a round's start and end
   Plan p{};
   p.npad = project_small_tokens(T, out_f32); p.tok = project_small_tile(out_f32);
   p.n_tiles = (N + 127) / 128; p.t_tiles = (T + p.tok - 1) / p.tok; p.num_kb = (K + 63) / 64;
   const long long tiles = (long long)p.n_tiles * p.t_tiles;
   p.splits = 1; p.cost = 1ll << 60;
   for (int c = 1; c <= kMaxSplits && c <= p.num_kb; ++c) {
-    if (clusters[c] < 1) continue;
-    const long long cost = (tiles + clusters[c] - 1) / clusters[c] * ((p.num_kb + c - 1) / c) + (c > 1 ? kExchange : 0);
+    if (clusters[c] < 2) continue;
+    // (of clusters of odd size a few fewer run at once than the occupancy query says: 48 of three took two rounds)
+    const long long at_once = c > 1 && c % 2 ? clusters[c] * 15 / 16 : clusters[c];
+    const long long cost = (tiles + at_once - 1) / at_once * ((p.num_kb + c - 1) / c + kStart) + (c > 1 ? kExchange : 0) - kStart;
     if (cost < p.cost) { p.cost = cost; p.splits = c; }
   }
   return p;
