@@ -293,7 +293,8 @@ CEP_API int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t we
 /*
  * Puts an adapter into a slot (replacing what was there; rank 0 empties it): down = A [device] bf16 [rank, K], up = B
  * [device] bf16 [N, rank], rows down_stride / up_stride elements apart.  Copied on `stream`; both may be freed once that
- * stream has completed.  Errors: CEP_ERR_CAPACITY for a slot or rank beyond the plan's.
+ * stream has completed.  A B that holds a NaN or an infinity leaves the slot empty, which lora_status reports: its columns
+ * would meet other tokens' zeros in the accumulator.  Errors: CEP_ERR_CAPACITY for a slot or rank beyond the plan's.
  */
 CEP_API int lora_load_adapter(cep_lora_plan* plan, int32_t slot, int32_t rank, float scale, const void* down,
                               int64_t down_stride, const void* up, int64_t up_stride, void* stream);
@@ -308,7 +309,8 @@ CEP_API int lora_project(cep_lora_plan* plan, const void* x, int64_t x_stride, i
                          void* y, int64_t y_stride, void* stream);
 
 /* Waits for the plan's work and returns what its kernels reported since the last call of this function: CEP_OK,
- * CEP_ERR_BAD_ROUTING (an id without a loaded adapter) or CEP_ERR_DEVICE_TIMEOUT.  Off the hot path. */
+ * CEP_ERR_DEVICE_TIMEOUT, CEP_ERR_ARG (an adapter that could not be loaded) or CEP_ERR_BAD_ROUTING (an id without a loaded
+ * adapter).  Off the hot path. */
 CEP_API int lora_status(cep_lora_plan* plan);
 CEP_API int lora_plan_destroy(cep_lora_plan* plan);
 

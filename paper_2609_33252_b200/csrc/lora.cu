@@ -46,7 +46,7 @@ Carve carve(const cep_lora_config& c) {
   auto take = [&](size_t& f, size_t bytes) { f = o; o = up_to(o + bytes, 256); };
   const size_t T = c.max_tokens;
   take(w.status, kStWords * 4);
-  take(w.tile_counter, 8);
+  take(w.tile_counter, 12);                               // and the mark of a load under way
   if (c.max_adapters) {
     take(w.ids, T * 4);
     take(w.n_chunks, (T / 64 + 1) * 4);
@@ -161,7 +161,7 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
                       (long long)cfg->out_features * kLoraChunk * 2, kLoraChunk, 128, 32);
   if (m) { lora_plan_destroy(p); return record_error(CEP_ERR_CUDA, "lora: cuTensorMapEncodeTiled failed (%d)", m); }
   // the status word and the counters start at zero, every slot of the bank empty
-  e = cudaMemsetAsync(p->ws, 0, w.tile_counter + 8, st);
+  e = cudaMemsetAsync(p->ws, 0, w.tile_counter + 12, st);
   if (e == cudaSuccess && b.total) e = cudaMemsetAsync(bk, 0, b.down, st);
   if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaMemsetAsync", e);
   rc = leave(p, st, false);
@@ -185,7 +185,7 @@ int lora_load_adapter(cep_lora_plan* p, int32_t slot, int32_t rank, float scale,
   int rc = enter(p, st, &capturing);
   if (rc) return rc;
   const cudaError_t e = launch_lora_pack(static_cast<const uint16_t*>(down), down_stride, static_cast<const uint16_t*>(up), up_stride, rank, scale, slot,
-                                         p->cfg.in_features, p->cfg.out_features, p->bank, st);
+                                         p->cfg.in_features, p->cfg.out_features, p->bank, p->tile_counter + 2, p->status, st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: the pack launch failed: %s", cudaGetErrorString(e));
   return leave(p, st, capturing);
 }
@@ -238,9 +238,10 @@ int lora_status(cep_lora_plan* p) {
   int32_t st[kStWords] = {};
   cudaError_t e = p->have_last ? cudaEventSynchronize(p->last) : cudaSuccess;
   if (e == cudaSuccess) e = cudaMemcpy(st, p->status, sizeof st, cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess && (st[kStTimeout] || st[kStBadRouting])) e = cudaMemset(p->status, 0, sizeof st);
+  if (e == cudaSuccess && (st[kStTimeout] || st[kStBadRouting] || st[kStBoundsViolation])) e = cudaMemset(p->status, 0, sizeof st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: reading the status failed: %s", cudaGetErrorString(e));
   if (st[kStTimeout]) return record_error(CEP_ERR_DEVICE_TIMEOUT, "lora: a bounded wait inside a kernel expired");
+  if (st[kStBoundsViolation]) return record_error(CEP_ERR_ARG, "lora: an adapter's B held a value that is not finite; its slot was left empty");
   if (st[kStBadRouting]) return record_error(CEP_ERR_BAD_ROUTING, "lora: an adapter id named no loaded adapter");
   return CEP_OK;
 }

@@ -33,11 +33,11 @@ struct LoraStep {
 };
 
 cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const uint16_t* up, int64_t up_stride, int rank, float scale, int slot,
-                             int K, int N, const LoraBank& bank, cudaStream_t s);
+                             int K, int N, const LoraBank& bank, int32_t* bad, int32_t* status, cudaStream_t s);
 bool lora_beside(int T);                     // the down projection runs beside the projection kernel on the same SMs
 cudaError_t lora_shrink_setup();             // once per plan, with its device current
 // tm_x: 64 columns x `box` rows; tm_down: the bank's down rows, 64 columns x 16 rows.  token_tile: tokens per tile of the
-// projection kernel that follows (its job lists are made here).
+// projection kernel that follows (its lists are made here).
 cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* status, cudaStream_t s);

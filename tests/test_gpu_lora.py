@@ -171,6 +171,57 @@ def test_a_token_without_an_adapter_is_not_touched_by_its_neighbours(T):
     assert (torch.abs(got.double() - y)[keep] <= tol[keep]).all()
 
 
+@pytest.mark.parametrize("T", [33, 150, 600])
+@pytest.mark.parametrize("value", [float("inf"), float("nan"), -float("inf")])
+def test_an_adapter_that_is_not_finite_reaches_nobody_else(T, value):
+    # one value of one adapter's B; tokens of both adapters share every tile
+    c = Case(256, 320, ranks=(16, 20), max_tokens=T)
+    bad = c.b[1].clone()
+    bad[100, 3] = value
+    c.layer.load_adapter(1, c.a[1], bad, 1.0)
+    assert c.layer.status() == -1
+    x, ids = rand((T, 256), 3), ids_of(T, 2, 5)
+    c.ranks[1] = 0                                           # the slot is empty: its tokens get the shared projection alone
+    c.check(x, ids, status=-6)
+    c.layer.load_adapter(1, c.a[1], c.b[1], c.scale[1])      # and takes an adapter again
+    c.ranks[1] = 20
+    c.check(x, ids)
+
+
+def test_infinite_products_stay_with_their_token():
+    # values of x and A whose product overflows fp32: the token's own row, and no other
+    c = Case(256, 256, ranks=(16,), max_tokens=200)
+    a = c.a[0].clone()
+    a[0] = 3e38
+    c.layer.load_adapter(0, a, c.b[0], 1.0)
+    x, ids = rand((200, 256), 3), torch.full((200,), -1, dtype=torch.int32, device="cuda")
+    x[7] = 1e30
+    ids[7] = 0
+    got = c.layer.run(x, ids)
+    assert not torch.isfinite(got[7]).any()
+    keep = torch.arange(200, device="cuda") != 7
+    y, tol = c.reference(x, None)
+    assert (torch.abs(got.double() - y)[keep] <= tol[keep]).all()
+
+
+def test_the_most_slots():
+    c = cep.LoRAProjection(rand((48, 64), 1), 300, 4096, 16)
+    slots = [0, 5, 4095]
+    ad = {s: (rand((3 + s % 7, 64), 10 + s, 0.1), rand((48, 3 + s % 7), 20 + s)) for s in slots}
+    for s, (a, b) in ad.items():
+        c.load_adapter(s, a, b, 2.0)
+    x = rand((300, 64), 2)
+    ids = torch.tensor(slots + [-1], dtype=torch.int32, device="cuda")[torch.arange(300, device="cuda") % 4].contiguous()
+    for T in (1, 3, 130, 300):
+        y = x[:T].double() @ c.weight.double().t()
+        for s, (a, b) in ad.items():
+            m = (ids[:T] == s).double()[:, None]
+            y += m * 2.0 * (x[:T].double() @ a.double().t()) @ b.double().t()
+        got = c.run(x[:T], ids[:T])
+        assert c.status() == 0
+        assert (torch.abs(got.double() - y) <= 2 ** -8 * y.abs() + 1e-3).all()
+
+
 @pytest.mark.parametrize("T", [20, 400])
 def test_ids_that_name_nothing_are_reported_and_skipped(T):
     c = Case(256, 192, ranks=(16, 0, 16), max_tokens=T)
