@@ -168,6 +168,17 @@ def _stream_handle(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_object(stream):
+    import torch
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+
+
+def _allocating_on(stream):
+    """Context in which torch allocates for use on `stream` (memory from another stream's pool may still be in use there)."""
+    import torch
+    return torch.cuda.stream(None if stream is None else _stream_object(stream))
+
+
 def _current_stream() -> int:
     """Handle of the current stream of the current device, without a Python stream object around it."""
     return _torch()._C._cuda_getCurrentRawStream(_torch()._C._cuda_getDevice())
@@ -229,22 +240,22 @@ _NORM_DESC = struct.Struct("6i4qf4x")                  # NormDesc, packed in one
 _ELEM = {}                                             # torch dtype -> CEP_ELEM_*, filled with the first call
 
 
-def _norm_rows(t, name, T, H, dtype=None):
-    """(element type, row stride) of a [T,H] CUDA tensor with contiguous rows; raises for what the call cannot take."""
+def _norm_rows(t, name, T, H, dev, dtype=None):
+    """(element type, row stride) of a [T,H] tensor on device `dev` with contiguous rows; raises for what the call cannot take."""
     elem = _ELEM.get(t.dtype)
     if elem is None or (dtype is not None and t.dtype is not dtype):
         raise CepError(-1, "%s has dtype %s" % (name, t.dtype))
-    if t.shape != (T, H) or not t.is_cuda:
-        raise CepError(-1, "%s must be a [%d, %d] CUDA tensor" % (name, T, H))
+    if t.shape != (T, H) or t.get_device() != dev:
+        raise CepError(-1, "%s must be a [%d, %d] CUDA tensor on the current device" % (name, T, H))
     stride, inner = t.stride()
     if inner != 1 and H > 1:
         raise CepError(-1, "the rows of %s must be contiguous" % name)
     return elem, stride if T > 1 else H                # (the stride of a single row means nothing)
 
 
-def _norm_dense(t, name, shape, dtypes):
-    if t.dtype not in dtypes or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise CepError(-1, "%s must be a contiguous CUDA tensor of %s %s" % (name, list(shape), dtypes[0]))
+def _norm_dense(t, name, shape, dtypes, dev):
+    if t.dtype not in dtypes or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise CepError(-1, "%s must be a contiguous CUDA tensor of %s %s on the current device" % (name, list(shape), dtypes[0]))
     return t.data_ptr()
 
 
@@ -262,29 +273,32 @@ def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None
     if x.dim() != 2:
         raise CepError(-1, "x must be a [T, H] tensor")
     T, H = x.shape
-    xe, xs = _norm_rows(x, "x", T, H)
+    if not x.is_cuda:                                  # (before the device is asked: there may be none)
+        raise CepError(-1, "x must be a CUDA tensor")
+    dev = torch._C._cuda_getDevice()
+    xe, xs = _norm_rows(x, "x", T, H, dev)
     re = we = 0
     rs = os_ = ys = H
     rp = op = yp = wp = cp = sp = None
     if residual is not None:
-        re, rs = _norm_rows(residual, "residual", T, H)
+        re, rs = _norm_rows(residual, "residual", T, H, dev)
         rp = residual.data_ptr()
     if residual_out is not None:
-        os_ = _norm_rows(residual_out, "residual_out", T, H, None if residual is None else residual.dtype)[1]
+        os_ = _norm_rows(residual_out, "residual_out", T, H, dev, None if residual is None else residual.dtype)[1]
         op = residual_out.data_ptr()
     if y is not None:
-        ys = _norm_rows(y, "y", T, H, bf16)[1]
+        ys = _norm_rows(y, "y", T, H, dev, bf16)[1]
         yp = y.data_ptr()
     if weight is not None:
-        wp = _norm_dense(weight, "weight", (H,), (bf16, torch.float32))
+        wp = _norm_dense(weight, "weight", (H,), (bf16, torch.float32), dev)
         we = _ELEM[weight.dtype]
     if codes is not None:
-        cp = _norm_dense(codes, "codes", (T, H), (torch.float8_e4m3fn, torch.uint8))
+        cp = _norm_dense(codes, "codes", (T, H), (torch.float8_e4m3fn, torch.uint8), dev)
     if scales is not None:
         if dtype == CEP_MXFP4_E4M3:
-            sp = _norm_dense(scales, "scales", (T, (H + 31) // 32), (torch.uint8,))
+            sp = _norm_dense(scales, "scales", (T, (H + 31) // 32), (torch.uint8,), dev)
         else:
-            sp = _norm_dense(scales, "scales", (T, (H + 127) // 128), (torch.float32,))
+            sp = _norm_dense(scales, "scales", (T, (H + 127) // 128), (torch.float32,), dev)
     rc = (_lib or lib()).moe_norm(_NORM_DESC.pack(T, H, dtype, xe, re, we, xs, rs, os_, ys, eps), x.data_ptr(), rp, wp, op, yp, cp, sp,
                                   _current_stream() if stream is None else _stream_handle(stream))
     if rc:
@@ -547,9 +561,11 @@ class LoRAProjection:
         self.out_dtype = torch.float32 if out_elem == CEP_ELEM_FP32 else torch.bfloat16
         self.out_features, self.in_features = weight.shape
         self.cfg = LoraConfig(self.in_features, self.out_features, max_tokens, max_adapters, max_rank, out_elem)
-        self.workspace = torch.empty(lora_plan_workspace_bytes(self.cfg), dtype=torch.uint8, device=weight.device)
+        self.device_index = weight.get_device()
         nb = lora_bank_bytes(self.cfg)
-        self.bank = torch.empty(nb, dtype=torch.uint8, device=weight.device) if nb else None
+        with _allocating_on(stream):                     # (lora_plan clears both on `stream`)
+            self.workspace = torch.empty(lora_plan_workspace_bytes(self.cfg), dtype=torch.uint8, device=weight.device)
+            self.bank = torch.empty(nb, dtype=torch.uint8, device=weight.device) if nb else None
         self.plan = lora_plan(self.cfg, weight, self.bank, self.workspace, stream)
 
     def load_adapter(self, slot, down, up, scale=1.0, stream=None):
@@ -557,9 +573,12 @@ class LoRAProjection:
         import torch
         rank = down.shape[0]
         for t, name, shape in ((down, "down", (rank, self.cfg.in_features)), (up, "up", (self.cfg.out_features, rank))):
-            if t.dtype != torch.bfloat16 or not t.is_cuda or tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1):
-                raise CepError(-1, "%s must be a bf16 CUDA tensor [%d, %d] with contiguous rows" % ((name,) + shape))
+            if t.dtype != torch.bfloat16 or t.get_device() != self.device_index or tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1):
+                raise CepError(-1, "%s must be a bf16 tensor [%d, %d] on the weight's device with contiguous rows" % ((name,) + shape))
         lora_load_adapter(self.plan, slot, rank, scale, down, up, stream)
+        if stream is not None:                           # the caller may drop both at once
+            down.record_stream(_stream_object(stream))
+            up.record_stream(_stream_object(stream))
 
     def drop_adapter(self, slot, stream=None):
         """Empties a slot: its id then names no adapter."""
@@ -568,16 +587,21 @@ class LoRAProjection:
     def run(self, x, adapter_ids=None, out=None, stream=None):
         """x bf16 [T,in], adapter_ids int32 [T] (-1: none) or None; returns out [T,out] (allocated if not given)."""
         torch = _torch()
-        if x.dim() != 2 or x.dtype is not torch.bfloat16 or not x.is_cuda or x.shape[1] != self.in_features or x.stride(1) != 1:
-            raise CepError(-1, "x must be a bf16 CUDA tensor [T, %d] with contiguous rows" % self.in_features)
+        dev = self.device_index
+        if x.dim() != 2 or x.dtype is not torch.bfloat16 or x.get_device() != dev or x.shape[1] != self.in_features or x.stride(1) != 1:
+            raise CepError(-1, "x must be a bf16 tensor [T, %d] on the weight's device with contiguous rows" % self.in_features)
         T, N = x.shape[0], self.out_features
         if adapter_ids is not None and (adapter_ids.dtype is not torch.int32 or adapter_ids.shape != (T,) or
-                                        not adapter_ids.is_contiguous() or not adapter_ids.is_cuda):
-            raise CepError(-1, "adapter_ids must be a contiguous int32 CUDA tensor [%d]" % T)
+                                        not adapter_ids.is_contiguous() or adapter_ids.get_device() != dev):
+            raise CepError(-1, "adapter_ids must be a contiguous int32 tensor [%d] on the weight's device" % T)
         if out is None:
-            out = torch.empty((T, N), dtype=self.out_dtype, device=x.device)
-        elif out.dtype is not self.out_dtype or out.shape != (T, N) or not out.is_cuda or (N > 1 and out.stride(1) != 1):
-            raise CepError(-1, "out must be a %s CUDA tensor [%d, %d] with contiguous rows" % (self.out_dtype, T, N))
+            if stream is None:
+                out = torch.empty((T, N), dtype=self.out_dtype, device=x.device)
+            else:
+                with _allocating_on(stream):
+                    out = torch.empty((T, N), dtype=self.out_dtype, device=x.device)
+        elif out.dtype is not self.out_dtype or out.shape != (T, N) or out.get_device() != dev or (N > 1 and out.stride(1) != 1):
+            raise CepError(-1, "out must be a %s tensor [%d, %d] on the weight's device with contiguous rows" % (self.out_dtype, T, N))
         lora_project(self.plan, x, adapter_ids, out, stream)
         return out
 

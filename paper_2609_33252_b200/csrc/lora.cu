@@ -73,8 +73,12 @@ BankLayout bank_layout(const cep_lora_config& c) {
 
 // Orders `s` after the plan's last work if that went to another stream.  Inside a stream capture the caller orders.
 int enter(cep_lora_plan* p, cudaStream_t s, bool* capturing) {
+  int dev = -1;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: cudaGetDevice failed: %s", cudaGetErrorString(e));
+  if (dev != p->device) return record_error(CEP_ERR_ARG, "lora: the plan was made on device %d, device %d is current", p->device, dev);
   cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
-  cudaError_t e = cudaStreamIsCapturing(s, &st);
+  e = cudaStreamIsCapturing(s, &st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: cudaStreamIsCapturing failed: %s", cudaGetErrorString(e));
   *capturing = st != cudaStreamCaptureStatusNone;
   if (!*capturing && p->have_last && p->last_stream != s) {

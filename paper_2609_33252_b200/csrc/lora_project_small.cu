@@ -80,7 +80,7 @@ __device__ __forceinline__ void add_splits(uint32_t base, int splits, int first,
 template <typename OT>
 __global__ void __launch_bounds__(kSmallThreads, 1)
 project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
-                     const __grid_constant__ CUtensorMap tm_up, int T, int N, int num_kb, int tok, int npad, int stages, int n_acc, const LoraArgs la,
+                     const __grid_constant__ CUtensorMap tm_up, int T, int N, int num_kb, int tok, int npad, int stages, int n_acc, int tmem_cols, const LoraArgs la,
                      OT* __restrict__ y, int64_t y_stride, int vec_ok, int32_t* __restrict__ status) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -90,7 +90,6 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n0 = blockIdx.x * 128, t0 = blockIdx.z * tok;
   const int split = blockIdx.y, splits = gridDim.y;
-  constexpr int kCols = sizeof(OT) == 4 ? 512 : kSmallTok;           // tensor-memory columns
   const int kb0 = (int)((long long)num_kb * split / splits), kb1 = (int)((long long)num_kb * (split + 1) / splits);
 
   // The K steps of x and W do not depend on the down projection: they start before it has finished.
@@ -114,7 +113,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32(&bars->tmem_base)), "n"(kCols) : "memory");
+                 ::"r"(smem_u32(&bars->tmem_base)), "r"(tmem_cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -284,7 +283,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols) : "memory");
   }
 }
 
@@ -371,8 +370,12 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   if (n_acc > 512 / p.npad) n_acc = 512 / p.npad;
   if (n_acc < 1) n_acc = 1;
   const int stage = kWStage + p.npad * kKBytes;
-  // With adapters and few tokens the ring leaves room for a block of the down projection, so that both run at once.
-  const int ring = a.bank && lora_beside(a.T) ? kSharedRing : kSmallRing;
+  int tmem_cols = 32;
+  while (tmem_cols < n_acc * p.npad) tmem_cols *= 2;
+  // With adapters and few tokens the ring leaves room for a block of the down projection (128 columns of tensor memory), so
+  // that both run at once; an allocation that it might have to wait for takes the whole of the SM's shared memory instead.  So
+  // no block ever waits for tensor memory with another plan's block on its SM: two clusters could wait for each other.
+  const int ring = a.bank && lora_beside(a.T) && tmem_cols <= 256 ? kSharedRing : kSmallRing;
   int stages = ring / stage;
   if (stages > kSmallMaxStages) stages = kSmallMaxStages;
   const size_t elt = a.out_f32 ? 4 : 2;
@@ -391,9 +394,9 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   const CUtensorMap& u = reinterpret_cast<const CUtensorMap&>(tm_up);
   const LoraArgs la = lora_args(a);
   if (a.out_f32)
-    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, la, (float*)a.y, a.y_stride,
+    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, tmem_cols, la, (float*)a.y, a.y_stride,
                               vec_ok, a.status);
-  return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, la,
+  return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, tmem_cols, la,
                             (__nv_bfloat16*)a.y, a.y_stride, vec_ok, a.status);
 }
 

@@ -354,3 +354,31 @@ def test_python_refusals():
 def test_no_tokens():
     c = Case(64, 64, ranks=(8,), max_tokens=16)
     assert c.layer.run(rand((0, 64), 1), torch.empty(0, dtype=torch.int32, device="cuda")).shape == (0, 64)
+
+
+@pytest.mark.parametrize("T", [64, 300])
+def test_outputs_and_adapters_of_another_stream(T):
+    # the stream that computes is not the one the tensors' memory comes from, and that one is busy and reuses what it frees
+    c = Case(512, 2048, ranks=(16, 32), max_tokens=T)
+    x, ids = rand((T, 512), 1), ids_of(T, 2, 1)
+    want = c.check(x, ids)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for handle in (side, side.cuda_stream):
+        layer = cep.LoRAProjection(c.w, T, 2, 32, stream=handle)
+        for s in range(2):
+            layer.load_adapter(s, c.a[s].clone(), c.b[s].clone(), c.scale[s], stream=handle)     # dropped at once
+            for r in (16, 32):
+                torch.full((r, 512), 9.0, dtype=torch.bfloat16, device="cuda"), torch.full((2048, r), 9.0, dtype=torch.bfloat16, device="cuda")
+        side.wait_stream(torch.cuda.current_stream())
+        outs = []
+        for _ in range(8):
+            junk = torch.empty((T, 2048), dtype=torch.bfloat16, device="cuda")
+            for _ in range(20):
+                junk.fill_(3.0)
+            del junk
+            outs.append(layer.run(x, ids, stream=handle))
+        torch.cuda.synchronize()
+        assert layer.status() == 0
+        for o in outs:
+            assert torch.equal(o, want)
