@@ -238,19 +238,20 @@ def moe_route(logits, top_k: int, topk_ids, topk_weights, stream=None):
 
 _NORM_DESC = struct.Struct("6i4qf4x")                  # NormDesc, packed in one call
 _ELEM = {}                                             # torch dtype -> CEP_ELEM_*, filled with the first call
+_NORM_DTYPES = []                                      # of weight, codes, ue8m0 scales, fp32 scales
 
 
-def _norm_rows(t, name, T, H, dev, dtype=None):
+def _norm_rows(t, name, shape, dev):
     """(element type, row stride) of a [T,H] tensor on device `dev` with contiguous rows; raises for what the call cannot take."""
     elem = _ELEM.get(t.dtype)
-    if elem is None or (dtype is not None and t.dtype is not dtype):
+    if elem is None:
         raise CepError(-1, "%s has dtype %s" % (name, t.dtype))
-    if t.shape != (T, H) or t.get_device() != dev:
-        raise CepError(-1, "%s must be a [%d, %d] CUDA tensor on the current device" % (name, T, H))
+    if t.shape != shape or t.get_device() != dev:
+        raise CepError(-1, "%s must be a %s CUDA tensor on the current device" % (name, list(shape)))
     stride, inner = t.stride()
-    if inner != 1 and H > 1:
+    if inner != 1 and shape[1] > 1:
         raise CepError(-1, "the rows of %s must be contiguous" % name)
-    return elem, stride if T > 1 else H                # (the stride of a single row means nothing)
+    return elem, stride
 
 
 def _norm_dense(t, name, shape, dtypes, dev):
@@ -266,41 +267,45 @@ def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None
     x [T,H] bf16 or fp32; residual / residual_out [T,H] bf16 or fp32 (one type); weight [H] bf16 or fp32; y bf16 [T,H];
     codes float8_e4m3fn [T,H] and scales fp32 [T,ceil(H/128)] (CEP_FP8_E4M3_BLOCK128) or uint8 [T,ceil(H/32)]
     (CEP_MXFP4_E4M3).  Rows of x, residual, residual_out and y may be strided."""
-    torch = _torch()
-    bf16 = torch.bfloat16
+    torch = _torch_module or _torch()
     if not _ELEM:
-        _ELEM.update({bf16: CEP_ELEM_BF16, torch.float32: CEP_ELEM_FP32})
-    if x.dim() != 2:
-        raise CepError(-1, "x must be a [T, H] tensor")
-    T, H = x.shape
-    if not x.is_cuda:                                  # (before the device is asked: there may be none)
-        raise CepError(-1, "x must be a CUDA tensor")
+        _ELEM.update({torch.bfloat16: CEP_ELEM_BF16, torch.float32: CEP_ELEM_FP32})
+        _NORM_DTYPES.extend(((torch.bfloat16, torch.float32), (torch.float8_e4m3fn, torch.uint8), (torch.uint8,), (torch.float32,)))
+    shape = x.shape
+    if len(shape) != 2 or not x.is_cuda:
+        raise CepError(-1, "x must be a [T, H] CUDA tensor")
+    T, H = shape
     dev = torch._C._cuda_getDevice()
-    xe, xs = _norm_rows(x, "x", T, H, dev)
-    re = we = 0
-    rs = os_ = ys = H
+    xe, xs = _norm_rows(x, "x", shape, dev)
+    re = we = rs = os_ = ys = 0
     rp = op = yp = wp = cp = sp = None
     if residual is not None:
-        re, rs = _norm_rows(residual, "residual", T, H, dev)
+        re, rs = _norm_rows(residual, "residual", shape, dev)
         rp = residual.data_ptr()
     if residual_out is not None:
-        os_ = _norm_rows(residual_out, "residual_out", T, H, dev, None if residual is None else residual.dtype)[1]
+        oe, os_ = _norm_rows(residual_out, "residual_out", shape, dev)
+        if rp is not None and oe != re:
+            raise CepError(-1, "residual_out has dtype %s" % residual_out.dtype)
         op = residual_out.data_ptr()
     if y is not None:
-        ys = _norm_rows(y, "y", T, H, dev, bf16)[1]
+        ye, ys = _norm_rows(y, "y", shape, dev)
+        if ye != CEP_ELEM_BF16:
+            raise CepError(-1, "y has dtype %s" % y.dtype)
         yp = y.data_ptr()
+    if T <= 1:                                         # the stride of a single row means nothing
+        xs = rs = os_ = ys = H
     if weight is not None:
-        wp = _norm_dense(weight, "weight", (H,), (bf16, torch.float32), dev)
+        wp = _norm_dense(weight, "weight", (H,), _NORM_DTYPES[0], dev)
         we = _ELEM[weight.dtype]
     if codes is not None:
-        cp = _norm_dense(codes, "codes", (T, H), (torch.float8_e4m3fn, torch.uint8), dev)
+        cp = _norm_dense(codes, "codes", shape, _NORM_DTYPES[1], dev)
     if scales is not None:
         if dtype == CEP_MXFP4_E4M3:
-            sp = _norm_dense(scales, "scales", (T, (H + 31) // 32), (torch.uint8,), dev)
+            sp = _norm_dense(scales, "scales", (T, (H + 31) // 32), _NORM_DTYPES[2], dev)
         else:
-            sp = _norm_dense(scales, "scales", (T, (H + 127) // 128), (torch.float32,), dev)
+            sp = _norm_dense(scales, "scales", (T, (H + 127) // 128), _NORM_DTYPES[3], dev)
     rc = (_lib or lib()).moe_norm(_NORM_DESC.pack(T, H, dtype, xe, re, we, xs, rs, os_, ys, eps), x.data_ptr(), rp, wp, op, yp, cp, sp,
-                                  _current_stream() if stream is None else _stream_handle(stream))
+                                  torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream_handle(stream))
     if rc:
         _check(rc)
 
