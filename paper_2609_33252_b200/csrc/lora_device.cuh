@@ -18,7 +18,9 @@ constexpr int kSlabSteps = 12;                        // K steps (of 64) per acc
 // between their stores and the MMA costs as much as the stores, so a few steps share one (kBatch in either kernel).
 constexpr int kStep = 2;
 
+// Waits for the end of the launch before this one / lets the next one be scheduled (it waits for this one's end in turn).
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 // K-major operand with rows of 32 bytes (16 ranks), 32-byte swizzle, 8-row groups 256 bytes apart
 __device__ __forceinline__ uint64_t make_smem_desc_32b(uint32_t saddr) {
   uint64_t d = 0;

@@ -134,6 +134,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (threadIdx.x == 64) { prefetch_map(&tm_x); prefetch_map(&tm_w); }
+  if (!la.has && !after_peer) pdl_wait();                // (what wrote x)
   __syncthreads();
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -145,13 +146,13 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
-  // What precedes this launch is the down projection.  The K steps do not need it and start at once; who reads its lists and s
-  // waits for it.  Or (after_peer) it is the launch
-  // with the full rounds of tiles, which touches nothing of this one's and let it start only after the down projection's end.
+  // What precedes this launch may be the down projection.  The K steps do not need it and start at once (it began after what
+  // wrote x had ended); who reads its lists and s waits for it.  Or (after_peer) the launch with the full rounds of tiles, which
+  // touches nothing of this one's and let it start only after the down projection's end.
   const bool wait = la.has && !after_peer;
-  if (!kSplit && (wait ? warp >= 7 : true)) {
+  if (wait ? warp >= 7 : true) {
     if (wait) pdl_wait();
-    if (threadIdx.x == 7 * 32) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 7 * 32) pdl_release();
   }
 
   if (warp == 0) {
@@ -486,16 +487,15 @@ cudaError_t launch(const ProjectArgs& a, const Plan& p, const CUtensorMap& w, co
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = kSmem; cfg.stream = s; cfg.attrs = attr;
-  cfg.numAttrs = a.bank ? 2 : 1;                       // only ever overlaps this call's own down projection
+  cfg.numAttrs = 2;
   if (p.full) {
     const int resident = g_clusters[dev][1];
     cfg.gridDim = dim3(2 * (unsigned)(p.full < resident ? p.full : resident), 1, 1);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, rounds, w, x, u, sh, 1, 0, la, static_cast<OT*>(a.y), a.y_stride, vec_ok,
                                              a.tile_counter, a.status);
     if (e != cudaSuccess) return e;
-    cfg.numAttrs = 2;                                  // the rest starts on SMs as they run out of tiles
   }
-  if (p.rest) {
+  if (p.rest) {                                        // after full rounds: starts on SMs as they run out of tiles
     sh.tile0 = p.full; sh.n_tiles = p.rest;
     attr[0].val.clusterDim.x = (unsigned)(2 * p.splits);
     cfg.gridDim = dim3((unsigned)(p.rest * 2 * p.splits), 1, 1);

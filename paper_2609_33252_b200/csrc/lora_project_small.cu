@@ -92,7 +92,9 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   const int split = blockIdx.y, splits = gridDim.y;
   const int kb0 = (int)((long long)num_kb * split / splits), kb1 = (int)((long long)num_kb * (split + 1) / splits);
 
-  // The K steps of x and W do not depend on the down projection: they start before it has finished.
+  // The K steps of x and W do not depend on the down projection: they start before it has finished.  Without one the launch
+  // before this is whatever wrote x.
+  if (!la.has) pdl_wait();
   auto load_k_step = [&](int kb, int stage) {
     const uint32_t full = smem_u32(&bars->full[stage]);
     uint8_t* st = smem + stage * stage_bytes;
@@ -208,8 +210,9 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     // ---------------------------------------------------------------- warps 2..5: rows of s, then the epilogue
     const int lane_grp = warp & 3, tid = threadIdx.x - 64;
     bool ok = true;
+    if (la.has) pdl_wait();
+    if (tid == 0) pdl_release();
     if (la.has) {
-      pdl_wait();
       const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
       const int cap = tok * kLoraMaxChunks;
       int2 e = list_pair(list, (split + lane * splits) * kStep, cap);      // lane i: the i-th of the next 32 steps
@@ -388,7 +391,7 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.gridDim = dim3(p.n_tiles, p.splits, p.t_tiles); cfg.blockDim = dim3(kSmallThreads, 1, 1);
   cfg.dynamicSmemBytes = 1024 + (size_t)stages * stage + 512; cfg.stream = s; cfg.attrs = attr;
-  cfg.numAttrs = a.bank ? 2 : 1;                       // only ever overlaps this call's own down projection
+  cfg.numAttrs = 2;
   const CUtensorMap& w = reinterpret_cast<const CUtensorMap&>(tm_w);
   const CUtensorMap& x = reinterpret_cast<const CUtensorMap&>(tm_x);
   const CUtensorMap& u = reinterpret_cast<const CUtensorMap&>(tm_up);

@@ -121,10 +121,11 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
 
-  // The projection kernel may be scheduled from here on.  Not earlier: its blocks allocate tensor memory too and wait for this
-  // grid, so every block of this grid has to hold its own first.
+  // What precedes this launch has ended.  The projection kernel may be scheduled from here on; its first loads rely on that end.
+  // Not earlier for another reason too: its blocks allocate tensor memory and wait for this grid, so every block of this grid
+  // has to hold its own first.
   __syncthreads();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  pdl_enter();
 
   // ---------------------------------------------------------------- lists (the ring is not in use yet and holds the table)
   int* table = reinterpret_cast<int*>(smem);
@@ -392,11 +393,13 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   int tmem_cols = 32;
   while (tmem_cols < n_acc * chunks * kLoraChunk) tmem_cols *= 2;
   cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = (unsigned)parts;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.gridDim = dim3(tiles, stripes + (token_tile != kRows), parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
-  cfg.attrs = attr; cfg.numAttrs = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, lora_shrink_kernel, reinterpret_cast<const CUtensorMap&>(tm_x), reinterpret_cast<const CUtensorMap&>(tm_down), T, K,
                             token_tile == kLargeTok ? 0 : N, ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, status);
 }

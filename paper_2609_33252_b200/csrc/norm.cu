@@ -119,6 +119,7 @@ template <typename XT, typename RT, int kFmt, int kVec>
 __global__ void __launch_bounds__(1024)
 norm_kernel(const NormArgs a) {
   __shared__ float part[kMaxWarps];
+  pdl_enter();
   const size_t row = blockIdx.x;
   const int n_vec = a.hidden >> 3;
   constexpr bool kRes = !std::is_same<RT, NoResidual>::value;
@@ -218,6 +219,7 @@ __global__ void __launch_bounds__(256)
 norm_any_kernel(const NormArgs a) {
   extern __shared__ float hs[];
   __shared__ float part[kMaxWarps];
+  pdl_enter();
   const size_t row = blockIdx.x;
   constexpr bool kRes = !std::is_same<RT, NoResidual>::value;
   using RL = typename std::conditional<kRes, RT, float>::type;
@@ -298,8 +300,7 @@ cudaError_t launch_fmt(const NormArgs& a, int n_tokens, bool wide, cudaStream_t 
     const size_t smem = (size_t)a.hidden * 4;
     cudaError_t e = cudaFuncSetAttribute(norm_any_kernel<XT, RT, kFmt>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormMaxHidden * 4);
     if (e != cudaSuccess) return e;
-    norm_any_kernel<XT, RT, kFmt><<<n_tokens, 256, smem, s>>>(a);
-    return cudaGetLastError();
+    return launch_pdl(norm_any_kernel<XT, RT, kFmt>, dim3(n_tokens), dim3(256), smem, s, 1, a);
   }
   const int n_vec = a.hidden / 8;
   // Steps per thread.  Few rows: one step, the row's latency is what counts (7168 fp8, 128 rows: 3.0 us against 3.2 and 4.2
@@ -309,10 +310,8 @@ cudaError_t launch_fmt(const NormArgs& a, int n_tokens, bool wide, cudaStream_t 
   const bool fp32 = sizeof(XT) == 4 || std::is_same<RT, float>::value;
   const int kv = n_vec > 2048 ? 4 : n_vec <= 64 || (n_tokens <= 1024 && n_vec <= 1024) ? 1 : n_vec <= 512 || fp32 ? 2 : 4;
   const int threads = ((n_vec + kv - 1) / kv + 31) / 32 * 32;
-  if (kv == 1) norm_kernel<XT, RT, kFmt, 1><<<n_tokens, threads, 0, s>>>(a);
-  else if (kv == 2) norm_kernel<XT, RT, kFmt, 2><<<n_tokens, threads, 0, s>>>(a);
-  else norm_kernel<XT, RT, kFmt, 4><<<n_tokens, threads, 0, s>>>(a);
-  return cudaGetLastError();
+  return launch_pdl(kv == 1 ? norm_kernel<XT, RT, kFmt, 1> : kv == 2 ? norm_kernel<XT, RT, kFmt, 2> : norm_kernel<XT, RT, kFmt, 4>, dim3(n_tokens),
+                    dim3(threads), 0, s, 1, a);
 }
 
 template <typename XT, typename RT>
