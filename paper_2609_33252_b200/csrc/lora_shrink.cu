@@ -93,14 +93,13 @@ __device__ int expand_chunks(const int* job, int m, const LoraBank& bank, int* o
 // other than 128 the first stripe only builds the projection kernel's lists, beside the others' work.
 __global__ void __launch_bounds__(kThreads, 3)              // (few registers: blocks of the projection kernel share the SM)
 lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_down, int T, int K, int N,
-                   const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int x_stage, int chunks, int stages, int n_acc,
+                   const int32_t* __restrict__ ids, const LoraBank bank, int token_tile, int box, int x_stage, int ring, int chunks, int n_acc,
                    int tmem_cols, int32_t* __restrict__ out_ids, int32_t* __restrict__ n_chunks, int32_t* __restrict__ chunk_lists,
                    float* __restrict__ s_out, int32_t* __restrict__ status) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ ShrinkBarriers bars;
   __shared__ ShrinkLists L;
-  const int stage_bytes = x_stage + chunks * kChunkStage;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = &bars.abort_flag;
   const int t0 = blockIdx.x * kRows, rows = min(kRows, T - t0);
@@ -110,7 +109,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
 
   if (threadIdx.x == 32) { prefetch_map(&tm_x); prefetch_map(&tm_down); }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bars.full[s]), 1); mbar_init(smem_u32(&bars.empty[s]), 1); }
+    for (int s = 0; s < kMaxStages; ++s) { mbar_init(smem_u32(&bars.full[s]), 1); mbar_init(smem_u32(&bars.empty[s]), 1); }
     mbar_init(smem_u32(&bars.acc_full), 1);
     bars.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -167,11 +166,16 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
   const int k0 = (int)((long long)steps * part / parts), k1 = (int)((long long)steps * (part + 1) / parts);
   const int cols = chunks * kLoraChunk;              // columns of an accumulator
   const int pitch = cols + 4;                        // floats per row of exchanged sums
-  int stage = 0; uint32_t phase = 0, acc_phase = 0;  // the loading and the issuing thread each keep their own
+  uint32_t phase = 0, acc_phase = 0;                 // phase: a parity bit per stage, of `empty` (loading warp) or `full` (issuing thread)
 
   for (int c0 = ((int)blockIdx.y - list_stripes) * chunks; c0 < total; c0 += ((int)gridDim.y - list_stripes) * chunks) {
     if (c0 < 0) break;                               // (the stripe that builds lists)
     const int n = min(chunks, total - c0);
+    // as many stages as the pass's chunks leave room for.  With fewer than 128 tokens the M side's missing rows are whatever
+    // follows in shared memory (their products are not read): a stage may be smaller than the operand, the ring as a whole not.
+    const int stage_bytes = x_stage + n * kChunkStage;
+    const int stages = min(kMaxStages, 1 + (ring - max(stage_bytes, kXStage)) / stage_bytes);
+    int stage = 0;
     if (N > 0 && warp >= 2 && (int)threadIdx.x - 64 < n * kLoraChunk) {
       // a short batch meets its adapters' rows of A for the first time here, while the projection kernel beside this one keeps
       // the memory busy: ask for all of them now, not a stage at a time
@@ -188,19 +192,23 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
       const uint8_t* up = reinterpret_cast<const uint8_t*>(bank.up) + (size_t)(v / kLoraMaxChunks * (bank.rank_pad / kLoraChunk) + v % kLoraMaxChunks) * block;
       if (b1 > b0) prefetch_l2(up + b0, (uint32_t)(b1 - b0));
     }
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+      // lane i brings chunk i's rows of A; lane 0 the tokens' rows of x too
       const int boxes = (rows + box - 1) / box;
+      const int v = lane < n ? L.chunk[c0 + lane] : 0, down_row = v / kLoraMaxChunks * bank.rank_pad + v % kLoraMaxChunks * kLoraChunk;
       for (int k = k0; k < k1; ++k) {
-        if (!mbar_wait(smem_u32(&bars.empty[stage]), phase ^ 1u, abort_flag, status)) break;
+        const bool ok = mbar_wait(smem_u32(&bars.empty[stage]), ~(phase >> stage) & 1u, abort_flag, status);
+        if (!__all_sync(0xffffffffu, ok)) break;
         const uint32_t full = smem_u32(&bars.full[stage]);
         uint8_t* st = smem + stage * stage_bytes;
-        mbar_expect_tx(full, boxes * box * 128 + n * kChunkStage);
-        for (int b = 0; b < boxes; ++b) tma_load_2d(smem_u32(st + b * box * 128), &tm_x, k * 64, t0 + b * box, full);
-        for (int i = 0; i < n; ++i) {
-          const int v = L.chunk[c0 + i], a = v / kLoraMaxChunks, c = v % kLoraMaxChunks;
-          tma_load_2d(smem_u32(st + x_stage + i * kChunkStage), &tm_down, k * 64, a * bank.rank_pad + c * kLoraChunk, full);
+        if (lane == 0) {
+          mbar_expect_tx(full, boxes * box * 128 + n * kChunkStage);
+          for (int b = 0; b < boxes; ++b) tma_load_2d(smem_u32(st + b * box * 128), &tm_x, k * 64, t0 + b * box, full);
         }
-        if (++stage == stages) { stage = 0; phase ^= 1u; }
+        __syncwarp();
+        if (lane < n) tma_load_2d(smem_u32(st + x_stage + lane * kChunkStage), &tm_down, k * 64, down_row, full);
+        phase ^= 1u << stage;
+        if (++stage == stages) stage = 0;
       }
     } else if (warp == 1 && lane == 0) {
       const uint32_t idesc = make_idesc_bf16(kRows, n * kLoraChunk);
@@ -208,7 +216,7 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
       uint32_t more = 0;
       bool ok = true;
       for (int k = k0; k < k1; ++k) {
-        if (!mbar_wait(smem_u32(&bars.full[stage]), phase, abort_flag, status)) { ok = false; break; }
+        if (!mbar_wait(smem_u32(&bars.full[stage]), (phase >> stage) & 1u, abort_flag, status)) { ok = false; break; }
         tc_fence_after();
         if (k == slab_end) { ++slab; slab_end = k0 + (int)((long long)(k1 - k0) * (slab + 1) / n_acc); more = 0; }
         const uint64_t xdesc = make_smem_desc(smem_u32(smem + stage * stage_bytes));
@@ -218,7 +226,8 @@ lora_shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_consta
           tc_mma_f16(tmem + (uint32_t)(slab * cols), xdesc + (uint64_t)(k4 * 2), adesc + (uint64_t)(k4 * 2), idesc, k4 != 0 ? 1u : more);
         more = 1;
         tc_commit(smem_u32(&bars.empty[stage]));
-        if (++stage == stages) { stage = 0; phase ^= 1u; }
+        phase ^= 1u << stage;
+        if (++stage == stages) stage = 0;
       }
       if (ok) tc_commit(smem_u32(&bars.acc_full));
     } else if (warp >= 2) {
@@ -364,12 +373,7 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   // Up to 128 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
   const bool beside = lora_beside(T);
   const int chunks = beside ? 4 : 8, smem = beside ? kShortSmem : kLongSmem;
-  // With fewer than 128 tokens the M side's missing rows are whatever follows in shared memory (their products are not read):
-  // a stage may be smaller than the operand, the ring as a whole may not.
   const int x_stage = T < kRows ? (T + box - 1) / box * box * 128 : kXStage;
-  const int stage = x_stage + chunks * kChunkStage;
-  int stages = 1 + (smem - 1024 - (stage > kXStage ? stage : kXStage)) / stage;
-  if (stages > kMaxStages) stages = kMaxStages;
   const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
   int parts = 2 * kSms / tiles;
   if (parts > kMaxParts) parts = kMaxParts;
@@ -401,7 +405,7 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   cfg.gridDim = dim3(tiles, stripes + (token_tile != kRows), parts); cfg.blockDim = dim3(kThreads, 1, 1); cfg.dynamicSmemBytes = smem; cfg.stream = s;
   cfg.attrs = attr; cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, lora_shrink_kernel, reinterpret_cast<const CUtensorMap&>(tm_x), reinterpret_cast<const CUtensorMap&>(tm_down), T, K,
-                            token_tile == kLargeTok ? 0 : N, ids, bank, token_tile, box, x_stage, chunks, stages, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, status);
+                            token_tile == kLargeTok ? 0 : N, ids, bank, token_tile, box, x_stage, smem - 1024, chunks, n_acc, tmem_cols, out_ids, n_chunks, chunk_lists, s_out, status);
 }
 
 }  // namespace cep
