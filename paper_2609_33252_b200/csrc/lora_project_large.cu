@@ -534,6 +534,11 @@ cudaError_t project_large_setup(int dev, int n_sms) {
   return cudaSuccess;
 }
 
+int project_large_free_sms(int dev, int T, int N, int K) {
+  const Plan p = plan(g_clusters[dev], T, N, K);
+  return p.full > 0 || p.rest * 2 * p.splits >= kSms ? 0 : kSms - p.rest * 2 * p.splits;
+}
+
 long long project_large_cost(int dev, int T, int N, int K) { return plan(g_clusters[dev], T, N, K).cost; }
 
 cudaError_t launch_project_large(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,

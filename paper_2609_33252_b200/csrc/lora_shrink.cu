@@ -367,7 +367,7 @@ cudaError_t lora_shrink_setup() {
   return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
-cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int T, int K, int N, const int32_t* ids,
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int free_sms, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* status, cudaStream_t s) {
   // Up to 128 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
@@ -375,17 +375,27 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   const int chunks = beside ? 4 : 8, smem = beside ? kShortSmem : kLongSmem;
   const int x_stage = T < kRows ? (T + box - 1) / box * box * 128 : kXStage;
   const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
+  // passes a tile can need
+  const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
+  const int passes = (adapters * (bank.rank_pad / kLoraChunk) + chunks - 1) / chunks;
+  // Blocks that find an SM of their own beside the projection's (free_sms) run while it multiplies: then as many parts as keep
+  // them few (700 tokens of 7168 -> 2048 with eight adapters: 31 us with six parts, 42 with eight; 1500: 49 with four, 62 with
+  // eight).  Otherwise the projection waits for most of them and their latency counts (1000 tokens: 44 with eight, 50 with
+  // four), unless the bank holds so many adapters that the blocks may not run at once (30 of rank 64 in every tile: 82 with
+  // eight, 66 with four).
   int parts = 2 * kSms / tiles;
   if (parts > kMaxParts) parts = kMaxParts;
+  if (tiles > 1 && 4 * tiles <= free_sms) {
+    if (parts > 32 / tiles) parts = 32 / tiles > 4 ? 32 / tiles : 4;
+  } else if (tiles > 1 && parts > 4 && (long long)passes * tiles * parts > 4 * kSms) {
+    parts = 4;
+  }
   // Long batches: at least 8 steps a part, fewer blocks leave SMs to the projection's first tiles (6821 tokens of 896 -> 640:
-  // 28 us with, 33 without; 4096 of 2048 -> 7168: 102 and 105).  Short ones: the down projection's latency is what counts
-  // (519 of 2048 -> 2048: 24 and 22; 64: 17 and 14).
+  // 28 us with, 33 without; 4096 of 2048 -> 7168: 102 and 105).
   const int least = tiles >= 16 ? 8 : 1;
   if (parts > steps / least) parts = steps / least;
   if (parts < 1) parts = 1;
-  // passes a tile can need, and how many blocks share them
-  const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
-  const int passes = (adapters * (bank.rank_pad / kLoraChunk) + chunks - 1) / chunks;
+  // how many blocks share the passes
   int stripes = 4 * kSms / (tiles * parts);
   if (stripes > passes) stripes = passes;
   if (stripes < 1) stripes = 1;
