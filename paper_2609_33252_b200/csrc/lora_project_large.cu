@@ -100,6 +100,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
                      const __grid_constant__ CUtensorMap tm_up, const Shape sh, int splits, int after_peer, const LoraArgs la_, OT* __restrict__ y,
                      int64_t y_stride, int vec_ok, int32_t* __restrict__ tile_counter, int32_t* __restrict__ status) {
   constexpr bool kF32 = sizeof(OT) == 4;
+  constexpr bool kBothHalves = kF32 || kSplit;           // the s-row warps read half of the accumulator
   LoraArgs la = la_;
   if (!kLora) la.has = 0;
   extern __shared__ uint8_t smem_raw[];
@@ -124,7 +125,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1);
       mbar_init(smem_u32(&bars->ready[s]), 1); mbar_init(smem_u32(&bars->sfull[s]), 8);
     }
-    for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->acc_full[s]), 1); mbar_init(smem_u32(&bars->acc_empty[s]), kF32 ? 16 : 8); }
+    for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->acc_full[s]), 1); mbar_init(smem_u32(&bars->acc_empty[s]), kBothHalves ? 16 : 8); }
     for (int s = 0; s < kRing; ++s) {
       mbar_init(smem_u32(&bars->ring_full[s]), 1); mbar_init(smem_u32(&bars->ring_empty[s]), kReaders);
       bars->ring_tile[s] = kPoison;
@@ -283,8 +284,8 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       }
     }
   } else {
-    // ---------------------------------------------------------------- rows of s (warps 7..10) and epilogue (warps 2..5;
-    // fp32 outputs: 2..5 columns 0-127, 7..10 columns 128-255), both CTAs, one token per thread
+    // ---------------------------------------------------------------- rows of s (warps 7..10) and epilogue (warps 2..5; fp32
+    // outputs and kSplit: 2..5 columns 0-127, 7..10 columns 128-255), both CTAs, one token per thread
     const bool s_warp = warp >= 7;
     const int lane_grp = warp & 3;                       // the tensor-memory lanes a warp may read
     const int r = threadIdx.x - 7 * 32;                  // an s-row warp's row
@@ -341,7 +342,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
               }
           }
         }
-        if (s_warp && !kF32) continue;
+        if (s_warp && !kBothHalves) continue;
         ok = ok && mbar_wait_relaxed(smem_u32(&bars->acc_full[acc]), acc_phase, abort_flag, status);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
@@ -359,8 +360,9 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         } else {
           OT* row = y + (size_t)t * y_stride + nb * 256;
           float* sums = reinterpret_cast<float*>(smem) + (lane_grp * 32 + lane) * kPitch;   // (kSplit: the ring, all consumed)
+          const int c_end = min(left, kBothHalves && !s_warp ? 128 : 256);
 #pragma unroll 1
-          for (int c = 0; c < 256 && c < left; c += 32) {
+          for (int c = kBothHalves && s_warp ? 128 : 0; c < c_end; c += 32) {
             __syncwarp();                                // the load is warp-collective
             uint32_t d[32];
             tc_ld32(taddr + c, d);
@@ -418,19 +420,30 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     const int t0 = m * kLargeTok + half * 128, rows = min(128, sh.T - t0);
     const int r1 = 128 * (part + 1) / splits;
     const uint32_t base = smem_u32(smem);
-    for (int r = 128 * part / splits + warp; r < r1 && r < rows; r += kThreads / 32) {
+    const int end = min(r1, rows);
+    constexpr int kWarps = kThreads / 32, kTogether = 2;  // rows read at once: a remote read takes 0.3 us whatever it brings
+    for (int r = 128 * part / splits + warp; r < end; r += kTogether * kWarps) {
+      float4 v[kTogether][2][kMaxSplits];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = h * 128 + lane * 4;
-        float4 v[kMaxSplits];
+      for (int u = 0; u < kTogether; ++u)
 #pragma unroll
-        for (int p = 0; p < kMaxSplits; ++p)
-          if (p < splits) v[p] = ld_cluster_f4(mapa(base + (uint32_t)((r * kPitch + c) * 4), (uint32_t)(2 * p + half)));
-        float4 o = v[0];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int p = 1; p < kMaxSplits; ++p)
-          if (p < splits) { o.x += v[p].x; o.y += v[p].y; o.z += v[p].z; o.w += v[p].w; }
-        put4(y + (size_t)(t0 + r) * y_stride + nb * 256 + c, o, sh.N - nb * 256 - c, vec_ok);
+          for (int p = 0; p < kMaxSplits; ++p)
+            if (p < splits)
+              v[u][h][p] = ld_cluster_f4(mapa(base + (uint32_t)((min(r + u * kWarps, end - 1) * kPitch + h * 128 + lane * 4) * 4), (uint32_t)(2 * p + half)));
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) {
+        if (r + u * kWarps >= end) break;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = h * 128 + lane * 4;
+          float4 o = v[u][h][0];
+#pragma unroll
+          for (int p = 1; p < kMaxSplits; ++p)
+            if (p < splits) { o.x += v[u][h][p].x; o.y += v[u][h][p].y; o.z += v[u][h][p].z; o.w += v[u][h][p].w; }
+          put4(y + (size_t)(t0 + r + u * kWarps) * y_stride + nb * 256 + c, o, sh.N - nb * 256 - c, vec_ok);
+        }
       }
     }
     cluster_sync_reads();             // no CTA leaves while another reads its sums
