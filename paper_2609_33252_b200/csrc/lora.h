@@ -32,13 +32,15 @@ struct LoraStep {
   const float* s;                            // [T][rank_pad] scale * A_a x
 };
 
+// SMs without a block of the projection kernel, and how many of them clusters of four or more can still use.
+struct FreeSms { int sms, in_clusters; };
 cudaError_t launch_lora_pack(const uint16_t* down, int64_t down_stride, const uint16_t* up, int64_t up_stride, int rank, float scale, int slot,
                              int K, int N, const LoraBank& bank, int32_t* bad, int32_t* status, cudaStream_t s);
 bool lora_beside(int T);                     // the down projection runs beside the projection kernel on the same SMs
 cudaError_t lora_shrink_setup();             // once per plan, with its device current
 // tm_x: 64 columns x `box` rows; tm_down: the bank's down rows, 64 columns x 16 rows.  token_tile: tokens per tile of the
-// projection kernel that follows (its lists are made here); free_sms: SMs that it leaves free.
-cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int free_sms, int T, int K, int N, const int32_t* ids,
+// projection kernel that follows (its lists are made here); free: what that kernel leaves.
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, const FreeSms& free, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* status, cudaStream_t s);
 
@@ -60,7 +62,7 @@ cudaError_t project_large_setup(int dev, int n_sms);
 // Work of the busiest SM, in K steps of a tile (both kernels' steps take about the same time).
 long long project_small_cost(int dev, int T, int N, int K, int out_f32);
 long long project_large_cost(int dev, int T, int N, int K);
-int project_large_free_sms(int dev, int T, int N, int K);      // SMs without a block of the large kernel
+FreeSms project_large_free(int dev, int T, int N, int K);
 cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,
                                  int dev, cudaStream_t s);
 cudaError_t launch_project_large(const ProjectArgs& a, const GemmTensorMap& tm_w, const GemmTensorMap& tm_x, const GemmTensorMap& tm_up,

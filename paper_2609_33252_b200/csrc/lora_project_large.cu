@@ -547,9 +547,14 @@ cudaError_t project_large_setup(int dev, int n_sms) {
   return cudaSuccess;
 }
 
-int project_large_free_sms(int dev, int T, int N, int K) {
+FreeSms project_large_free(int dev, int T, int N, int K) {
   const Plan p = plan(g_clusters[dev], T, N, K);
-  return p.full > 0 || p.rest * 2 * p.splits >= kSms ? 0 : kSms - p.rest * 2 * p.splits;
+  const int blocks = 2 * p.splits * p.rest;
+  if (p.full > 0 || blocks >= kSms) return FreeSms{0, 0};
+  // clusters of four and more leave fewer whole groups of SMs than pairs do (measured: 16 blocks of 4 find room beside 28
+  // clusters of four, not beside 30; 12 of four beside 48 pairs)
+  const int lost = p.splits > 1 ? 16 : 2;
+  return FreeSms{kSms - blocks, kSms - blocks > lost ? kSms - blocks - lost : 0};
 }
 
 long long project_large_cost(int dev, int T, int N, int K) { return plan(g_clusters[dev], T, N, K).cost; }

@@ -367,7 +367,7 @@ cudaError_t lora_shrink_setup() {
   return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
-cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, int free_sms, int T, int K, int N, const int32_t* ids,
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, const FreeSms& free, int T, int K, int N, const int32_t* ids,
                                const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* status, cudaStream_t s) {
   // Up to 128 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
@@ -378,15 +378,16 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   // passes a tile can need
   const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
   const int passes = (adapters * (bank.rank_pad / kLoraChunk) + chunks - 1) / chunks;
-  // Blocks that find an SM of their own beside the projection's (free_sms) run while it multiplies: then as many parts as keep
-  // them few (700 tokens of 7168 -> 2048 with eight adapters: 31 us with six parts, 42 with eight; 1500: 49 with four, 62 with
-  // eight).  Otherwise the projection waits for most of them and their latency counts (1000 tokens: 44 with eight, 50 with
-  // four), unless the bank holds so many adapters that the blocks may not run at once (30 of rank 64 in every tile: 82 with
-  // eight, 66 with four).
+  // Blocks that find SMs of their own beside the projection's run while it multiplies (free): then as many parts as still find
+  // them, a cluster of `parts` SMs in one GPC per tile (700 tokens of 7168 -> 2048 with eight adapters: 31 us with six parts, 42
+  // with eight; 1500: 49 with four, 62 with eight; 512 of 7168 -> 3584: 35 with four, 39 with six, 42 with eight).  Otherwise
+  // the projection waits for most of them and their latency counts (1000 tokens: 44 with eight, 50 with four), unless the bank
+  // holds so many adapters that the blocks may not run at once (30 of rank 64 in every tile: 82 with eight, 66 with four; beside the projection, 700 tokens: 68 with six, 61 with five, 62 with four).
   int parts = 2 * kSms / tiles;
   if (parts > kMaxParts) parts = kMaxParts;
-  if (tiles > 1 && 4 * tiles <= free_sms) {
-    if (parts > 32 / tiles) parts = 32 / tiles > 4 ? 32 / tiles : 4;
+  if (tiles > 1 && 4 * tiles <= free.in_clusters) {
+    if (parts > 6 && (2 * tiles * parts > free.sms || tiles * parts > free.in_clusters)) parts = 6;
+    if (parts > 4 && (10 * tiles * parts > 7 * free.sms || tiles * parts > free.in_clusters || (long long)passes * tiles * parts > 3 * kSms)) parts = 4;
   } else if (tiles > 1 && parts > 4 && (long long)passes * tiles * parts > 4 * kSms) {
     parts = 4;
   }
