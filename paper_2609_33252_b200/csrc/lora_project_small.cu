@@ -28,7 +28,7 @@ using namespace ptx;
 
 constexpr int kSmallThreads = 192;
 constexpr int kSmallMaxStages = 12;
-constexpr int kBatch = 2;                              // (64 tokens, 24 adapters: 37.0 us with two, 37.6 with four)
+constexpr int kBatch = 2;                              // (64 tokens, 24 adapters: 36.3 us with two, 37.2 with four)
 constexpr int kMaxSplits = 8;                          // CTAs of a portable cluster
 constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
 constexpr int kSmallRing = 200 * 1024;

@@ -9,7 +9,7 @@
 // of a cluster, which add their partial sums in order through shared memory, so results do not depend on timing.
 //
 // A short batch's latency is 7 to 8 us (lists 2, loads and products 3 to 5, exchange 2): up to 128 tokens its blocks run beside
-// the projection's on the same SMs and the weight streams meanwhile.  16384 tokens of 7168 with 30 adapters: 62 us, against 36
+// the projection's on the same SMs and the weight streams meanwhile.  16384 tokens of 7168 with 30 adapters: 55 us, against 36
 // for reading x once (tiles with many adapters take several passes); matrix instructions of one warp (16x8x16, fragments by
 // copies through shared memory) took 120.  Fragments straight from global memory, no copy stages: 28 against 30 us with eight
 // rank-16 adapters and 64 tokens, 51 against 37 with ranks up to 64; not kept.
@@ -382,7 +382,8 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   // them, a cluster of `parts` SMs in one GPC per tile (700 tokens of 7168 -> 2048 with eight adapters: 31 us with six parts, 42
   // with eight; 1500: 49 with four, 62 with eight; 512 of 7168 -> 3584: 35 with four, 39 with six, 42 with eight).  Otherwise
   // the projection waits for most of them and their latency counts (1000 tokens: 44 with eight, 50 with four), unless the bank
-  // holds so many adapters that the blocks may not run at once (30 of rank 64 in every tile: 82 with eight, 66 with four; beside the projection, 700 tokens: 68 with six, 61 with five, 62 with four).
+  // holds so many adapters that the blocks may not run at once (30 of rank 64 in every tile: 82 with eight, 66 with four;
+  // beside the projection, 700 tokens: 68 with six, 62 with four).
   int parts = 2 * kSms / tiles;
   if (parts > kMaxParts) parts = kMaxParts;
   if (tiles > 1 && 4 * tiles <= free.in_clusters) {
