@@ -422,6 +422,8 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     const uint32_t base = smem_u32(smem);
     const int end = min(r1, rows);
     constexpr int kWarps = kThreads / 32, kTogether = 2;  // rows read at once: a remote read takes 0.3 us whatever it brings
+    const int left = sh.N - nb * 256;                     // columns that exist.  Only what is used is read: the barrier below
+                                                          // does not wait for a read whose value nothing needs
     for (int r = 128 * part / splits + warp; r < end; r += kTogether * kWarps) {
       float4 v[kTogether][2][kMaxSplits];
 #pragma unroll
@@ -430,19 +432,20 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int p = 0; p < kMaxSplits; ++p)
-            if (p < splits)
-              v[u][h][p] = ld_cluster_f4(mapa(base + (uint32_t)((min(r + u * kWarps, end - 1) * kPitch + h * 128 + lane * 4) * 4), (uint32_t)(2 * p + half)));
+            if (p < splits && r + u * kWarps < end && h * 128 + lane * 4 < left)
+              v[u][h][p] = ld_cluster_f4(mapa(base + (uint32_t)(((r + u * kWarps) * kPitch + h * 128 + lane * 4) * 4), (uint32_t)(2 * p + half)));
 #pragma unroll
       for (int u = 0; u < kTogether; ++u) {
         if (r + u * kWarps >= end) break;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int c = h * 128 + lane * 4;
+          if (c >= left) break;
           float4 o = v[u][h][0];
 #pragma unroll
           for (int p = 1; p < kMaxSplits; ++p)
             if (p < splits) { o.x += v[u][h][p].x; o.y += v[u][h][p].y; o.z += v[u][h][p].z; o.w += v[u][h][p].w; }
-          put4(y + (size_t)(t0 + r + u * kWarps) * y_stride + nb * 256 + c, o, sh.N - nb * 256 - c, vec_ok);
+          put4(y + (size_t)(t0 + r + u * kWarps) * y_stride + nb * 256 + c, o, left - c, vec_ok);
         }
       }
     }

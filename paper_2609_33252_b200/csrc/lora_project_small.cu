@@ -41,7 +41,8 @@ struct __align__(8) SmallBarriers {
 static_assert(sizeof(SmallBarriers) <= 512, "barrier block");
 
 // A warp's share of the tokens first, first + kWarps, ...: adds the cluster's sums in split order and stores, four columns of y
-// per lane.  kTogether tokens are read at once, as a remote read takes 0.3 us whatever it brings.
+// per lane.  kTogether tokens are read at once, as a remote read takes 0.3 us whatever it brings.  Only what is used is read:
+// the barrier behind this does not wait for a read whose value nothing needs, and the CTA read from could be gone by then.
 template <int kSplits, int kTogether, typename OT>
 __device__ __forceinline__ void add_splits(uint32_t base, int splits, int first, int end, int t0, int n0, int N, OT* __restrict__ y,
                                            int64_t y_stride, int vec_ok) {
@@ -53,10 +54,10 @@ __device__ __forceinline__ void add_splits(uint32_t base, int splits, int first,
     for (int u = 0; u < kTogether; ++u)
 #pragma unroll
       for (int s = 0; s < kSplits; ++s)
-        if (s < splits) v[u][s] = ld_cluster_f4(mapa(base + (uint32_t)((min(c + u * kWarps, end - 1) * 128 + lane * 4) * 4), (uint32_t)s));
+        if (s < splits && c + u * kWarps < end && left > 0) v[u][s] = ld_cluster_f4(mapa(base + (uint32_t)(((c + u * kWarps) * 128 + lane * 4) * 4), (uint32_t)s));
 #pragma unroll
     for (int u = 0; u < kTogether; ++u) {
-      if (c + u * kWarps >= end) break;
+      if (c + u * kWarps >= end || left <= 0) break;
       float4 o = v[u][0];
 #pragma unroll
       for (int s = 1; s < kSplits; ++s)

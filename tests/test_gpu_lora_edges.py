@@ -1,0 +1,25 @@
+"""The projection with adapters where shares, chains, devices and streams end: complements test_gpu_lora.py, same cases and
+tolerances (Case.check)."""
+import pytest
+import torch
+
+import paper_2609_33252_b200 as cep
+
+from test_gpu_lora import Case, ids_of, rand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,K,N", [(13, 1024, 7168), (14, 1024, 7168), (27, 1024, 7100), (61, 1024, 7168), (63, 1024, 7042), (125, 1024, 7168),
+                                   (300, 2048, 2148), (519, 2048, 2148), (385, 2048, 2304), (700, 2048, 1794), (257, 2048, 4164)])
+def test_ragged_shares_of_the_exchange(T, K, N, out):
+    # K split over two or more CTAs (or pairs) whose shares of the rows do not fill a round of a warp's reads, and column
+    # blocks that end inside a half: only rows and columns that exist are read from the other CTAs
+    c = Case(K, N, ranks=(16,), max_tokens=T, out=out)
+    x = rand((T, K), 5)
+    want = c.check(x, None)
+    c.check(x, ids_of(T, 1, 6))
+    for _ in range(20):
+        assert torch.equal(c.layer.run(x), want)
+    assert c.layer.status() == 0
