@@ -562,11 +562,16 @@ class LoRAProjection:
         import torch
         if not weight.is_cuda or weight.dtype != torch.bfloat16 or weight.dim() != 2 or weight.stride(1) != 1:
             raise CepError(-1, "weight must be a bf16 CUDA tensor [out, in] with contiguous rows")
+        dev = torch.cuda.current_device()                # the plan is made for this one
+        if weight.get_device() != dev:
+            raise CepError(-1, "the weight is on device %d, device %d is current" % (weight.get_device(), dev))
+        if getattr(stream, "device", None) is not None and stream.device.index != dev:
+            raise CepError(-1, "the stream is of device %s, device %d is current" % (stream.device.index, dev))
         self.weight = weight
         self.out_dtype = torch.float32 if out_elem == CEP_ELEM_FP32 else torch.bfloat16
         self.out_features, self.in_features = weight.shape
         self.cfg = LoraConfig(self.in_features, self.out_features, max_tokens, max_adapters, max_rank, out_elem)
-        self.device_index = weight.get_device()
+        self.device_index = dev
         nb = lora_bank_bytes(self.cfg)
         with _allocating_on(stream):                     # (lora_plan clears both on `stream`)
             self.workspace = torch.empty(lora_plan_workspace_bytes(self.cfg), dtype=torch.uint8, device=weight.device)

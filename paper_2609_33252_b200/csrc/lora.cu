@@ -147,6 +147,18 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
   };
   cudaError_t e = cudaGetDevice(&p->device);
   if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaGetDevice", e);
+  // kernels of one device never get another one's memory
+  const void* given[3] = {weight, workspace, b.total ? bank : workspace};
+  for (const void* m : given) {
+    cudaPointerAttributes at{};
+    e = cudaPointerGetAttributes(&at, m);
+    if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaPointerGetAttributes", e);
+    if (at.type == cudaMemoryTypeDevice && at.device != p->device) {
+      const int current = p->device;
+      lora_plan_destroy(p);
+      return record_error(CEP_ERR_ARG, "lora: the weight, the bank or the workspace is on device %d, device %d is current", at.device, current);
+    }
+  }
   e = cudaDeviceGetAttribute(&p->n_sms, cudaDevAttrMultiProcessorCount, p->device);
   if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaDeviceGetAttribute", e);
   e = cudaEventCreateWithFlags(&p->last, cudaEventDisableTiming);
