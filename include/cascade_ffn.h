@@ -285,8 +285,8 @@ CEP_API int lora_bank_bytes(const cep_lora_config* cfg, size_t* bytes);
  * `weight` [device] bf16 [N, K], rows weight_stride elements apart (a multiple of 8), 16-byte aligned; `bank` and
  * `workspace` [device], 256-byte aligned.  All three stay owned by the caller and must outlive the plan.  Must be called
  * with the target device current (memory of another device is refused); clears the counters and the bank's slots on
- * `stream`.  A plan is not thread-safe.  Its calls may go to different streams: each waits for the plan's previous work
- * (inside a stream capture the caller orders).
+ * `stream`, which may not be under capture (CEP_ERR_STATE).  A plan is not thread-safe.  Its calls may go to different
+ * streams: each waits for the plan's previous work (inside a stream capture the caller orders).
  */
 CEP_API int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_stride, void* bank, size_t bank_bytes,
                       void* workspace, size_t workspace_bytes, void* stream, cep_lora_plan** out);

@@ -147,6 +147,14 @@ int lora_plan(const cep_lora_config* cfg, const void* weight, int64_t weight_str
   };
   cudaError_t e = cudaGetDevice(&p->device);
   if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaGetDevice", e);
+  // A capture would only record the clearing of the counters and slots: the plan's first calls would read them as they are.
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  e = cudaStreamIsCapturing(st, &capture);
+  if (e != cudaSuccess) return give_up(CEP_ERR_CUDA, "cudaStreamIsCapturing", e);
+  if (capture != cudaStreamCaptureStatusNone) {
+    lora_plan_destroy(p);
+    return record_error(CEP_ERR_STATE, "lora: a plan cannot be made on a stream that is being captured");
+  }
   // kernels of one device never get another one's memory
   const void* given[3] = {weight, workspace, b.total ? bank : workspace};
   for (const void* m : given) {

@@ -23,3 +23,20 @@ def test_ragged_shares_of_the_exchange(T, K, N, out):
     for _ in range(20):
         assert torch.equal(c.layer.run(x), want)
     assert c.layer.status() == 0
+
+
+def test_a_plan_is_not_made_inside_a_capture():
+    # the clearing of its slots and counters would only be recorded
+    w, x = rand((64, 64), 1), rand((4, 64), 2)
+    g, y = torch.cuda.CUDAGraph(), torch.zeros(8, device="cuda")
+    with torch.cuda.graph(g):
+        with pytest.raises(cep.CepError, match="captured"):
+            cep.LoRAProjection(w, 16, 2, 8)
+        y += 1                                               # the capture goes on
+    g.replay()
+    torch.cuda.synchronize()
+    assert (y == 1).all()
+    layer = cep.LoRAProjection(w, 16, 2, 8)
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    layer.run(x, ids)
+    assert layer.status() == -6                              # every slot is empty
