@@ -311,7 +311,8 @@ CEP_API int lora_project(cep_lora_plan* plan, const void* x, int64_t x_stride, i
 
 /* Waits for the plan's work and returns what its kernels reported since the last call of this function: CEP_OK,
  * CEP_ERR_DEVICE_TIMEOUT, CEP_ERR_ARG (an adapter that could not be loaded) or CEP_ERR_BAD_ROUTING (an id without a loaded
- * adapter).  Off the hot path. */
+ * adapter).  Calls that were captured and replayed are not waited for: the caller synchronises with a replay first.  Off the
+ * hot path. */
 CEP_API int lora_status(cep_lora_plan* plan);
 CEP_API int lora_plan_destroy(cep_lora_plan* plan);
 

@@ -263,7 +263,11 @@ int lora_status(cep_lora_plan* p) {
   int32_t st[kStWords] = {};
   cudaError_t e = p->have_last ? cudaEventSynchronize(p->last) : cudaSuccess;
   if (e == cudaSuccess) e = cudaMemcpy(st, p->status, sizeof st, cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess && (st[kStTimeout] || st[kStBadRouting] || st[kStBoundsViolation])) e = cudaMemset(p->status, 0, sizeof st);
+  if (e == cudaSuccess && (st[kStTimeout] || st[kStBadRouting] || st[kStBoundsViolation])) {
+    e = cudaMemset(p->status, 0, sizeof st);
+    // the next call's stream may not wait for the default one: what its kernels report must not be cleared with this
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
+  }
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: reading the status failed: %s", cudaGetErrorString(e));
   if (st[kStTimeout]) return record_error(CEP_ERR_DEVICE_TIMEOUT, "lora: a bounded wait inside a kernel expired");
   if (st[kStBoundsViolation]) return record_error(CEP_ERR_ARG, "lora: an adapter's B held a value that is not finite; its slot was left empty");

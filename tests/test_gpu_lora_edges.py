@@ -40,3 +40,20 @@ def test_a_plan_is_not_made_inside_a_capture():
     ids = torch.zeros(4, dtype=torch.int32, device="cuda")
     layer.run(x, ids)
     assert layer.status() == -6                              # every slot is empty
+
+
+def test_a_report_is_not_cleared_with_the_one_before():
+    # reports in turn, each call enqueued as soon as the status of the one before has been read and cleared, on a stream that
+    # does not wait for the default one
+    c = Case(64, 64, ranks=(8,), max_tokens=4)
+    x, out = rand((4, 64), 1), torch.empty(4, 64, dtype=torch.bfloat16, device="cuda")
+    good = torch.zeros(4, dtype=torch.int32, device="cuda")
+    bad = good + 1
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(300):
+        c.layer.run(x, bad, out, stream=side)
+        assert c.layer.status() == -6, i
+        if i % 3 == 0:
+            c.layer.run(x, good, out, stream=side)
+            assert c.layer.status() == 0, i
