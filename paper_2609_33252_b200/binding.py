@@ -173,6 +173,14 @@ def _stream_object(stream):
     return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
 
 
+def _record(stream, *tensors):
+    """Tells torch's allocator that `stream` uses the tensors (those that are given): the caller may drop them at once."""
+    s = _stream_object(stream)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(s)
+
+
 def _allocating_on(stream):
     """Context in which torch allocates for use on `stream` (memory from another stream's pool may still be in use there)."""
     import torch
@@ -266,7 +274,7 @@ def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None
 
     x [T,H] bf16 or fp32; residual / residual_out [T,H] bf16 or fp32 (one type); weight [H] bf16 or fp32; y bf16 [T,H];
     codes float8_e4m3fn [T,H] and scales fp32 [T,ceil(H/128)] (CEP_FP8_E4M3_BLOCK128) or uint8 [T,ceil(H/32)]
-    (CEP_MXFP4_E4M3).  Rows of x, residual, residual_out and y may be strided."""
+    (CEP_MXFP4_E4M3).  Rows of x, residual, residual_out and y may be strided.  Tensors are recorded on a `stream` that is given."""
     torch = _torch_module or _torch()
     if not _ELEM:
         _ELEM.update({torch.bfloat16: CEP_ELEM_BF16, torch.float32: CEP_ELEM_FP32})
@@ -308,6 +316,8 @@ def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None
                                   torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream_handle(stream))
     if rc:
         _check(rc)
+    if stream is not None:
+        _record(stream, x, weight, residual, residual_out, y, codes, scales)
 
 
 def lora_plan_workspace_bytes(cfg: LoraConfig) -> int:
@@ -586,16 +596,16 @@ class LoRAProjection:
             if t.dtype != torch.bfloat16 or t.get_device() != self.device_index or tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1):
                 raise CepError(-1, "%s must be a bf16 tensor [%d, %d] on the weight's device with contiguous rows" % ((name,) + shape))
         lora_load_adapter(self.plan, slot, rank, scale, down, up, stream)
-        if stream is not None:                           # the caller may drop both at once
-            down.record_stream(_stream_object(stream))
-            up.record_stream(_stream_object(stream))
+        if stream is not None:
+            _record(stream, down, up)
 
     def drop_adapter(self, slot, stream=None):
         """Empties a slot: its id then names no adapter."""
         lora_load_adapter(self.plan, slot, 0, 0.0, None, None, stream)
 
     def run(self, x, adapter_ids=None, out=None, stream=None):
-        """x bf16 [T,in], adapter_ids int32 [T] (-1: none) or None; returns out [T,out] (allocated if not given)."""
+        """x bf16 [T,in], adapter_ids int32 [T] (-1: none) or None; returns out [T,out] (allocated if not given).  Tensors are
+        recorded on a `stream` that is given."""
         torch = _torch()
         dev = self.device_index
         if x.dim() != 2 or x.dtype is not torch.bfloat16 or x.get_device() != dev or x.shape[1] != self.in_features or x.stride(1) != 1:
@@ -613,6 +623,8 @@ class LoRAProjection:
         elif out.dtype is not self.out_dtype or out.shape != (T, N) or out.get_device() != dev or (N > 1 and out.stride(1) != 1):
             raise CepError(-1, "out must be a %s tensor [%d, %d] on the weight's device with contiguous rows" % (self.out_dtype, T, N))
         lora_project(self.plan, x, adapter_ids, out, stream)
+        if stream is not None:
+            _record(stream, x, adapter_ids, out)
         return out
 
     def status(self) -> int:

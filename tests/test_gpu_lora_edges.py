@@ -57,3 +57,31 @@ def test_a_report_is_not_cleared_with_the_one_before():
         if i % 3 == 0:
             c.layer.run(x, good, out, stream=side)
             assert c.layer.status() == 0, i
+
+
+@pytest.mark.parametrize("T", [64, 300])
+def test_inputs_dropped_while_another_stream_uses_them(T):
+    c = Case(512, 2048, ranks=(16, 32), max_tokens=T)
+    x, ids = rand((T, 512), 1), ids_of(T, 2, 1)
+    want = c.check(x, ids)
+    h, w = rand((T, 2048), 4), rand((2048,), 3)
+    normed = torch.empty_like(h)
+    cep.moe_norm(h, w, y=normed)
+    side = torch.cuda.Stream()
+    busy = torch.empty(1 << 26, device="cuda")
+    for stream in (side, side.cuda_stream):
+        for _ in range(4):
+            y = torch.empty_like(h)
+            x1, ids1, h1, w1 = x.clone(), ids.clone(), h.clone(), w.clone()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                busy.fill_(1.0)                              # the calls begin after the memory could have been given away
+            got = c.layer.run(x1, ids1, stream=stream)
+            cep.moe_norm(h1, w1, y=y, stream=stream)
+            del x1, ids1, h1, w1
+            for like in (x, ids, h, w):
+                for _ in range(3):
+                    torch.empty_like(like).fill_(1)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and torch.equal(y, normed)
+    assert c.layer.status() == 0

@@ -10,10 +10,14 @@ from paper_2609_33252_b200 import binding
 
 
 def on_device(t, index):
-    """A CPU tensor as a CUDA tensor of device `index` looks to the binding."""
+    """A CPU tensor as a CUDA tensor of device `index` looks to the binding; `recorded`: the streams it was recorded on."""
     class Fake:
         is_cuda = True
         get_device = staticmethod(lambda: index)
+        recorded = ()
+
+        def record_stream(self, stream):
+            self.recorded += (stream,)
 
         def __getattr__(self, name):
             return getattr(t, name)
@@ -25,8 +29,7 @@ def plans(monkeypatch):
     """No GPU, device 0 current; returns the list of (what, arguments) that reach the library."""
     made = []
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    monkeypatch.setattr(binding, "lora_plan", lambda *a: made.append(("plan", a)) or 1)
-    monkeypatch.setattr(binding, "lora_plan_destroy", lambda plan: None)
+    monkeypatch.setattr(binding, "lora_plan", lambda *a: made.append(("plan", a)))                # (no handle: nothing to destroy)
     return made
 
 
@@ -44,3 +47,33 @@ def test_a_stream_of_another_device_is_refused(plans):
     with pytest.raises(cep.CepError, match="device"):
         cep.LoRAProjection(on_device(torch.zeros(16, 64, dtype=torch.bfloat16), 0), 4, stream=stream)
     assert not plans
+
+
+def test_run_records_its_tensors_on_the_stream_it_is_given(plans, monkeypatch):
+    # the caller may drop them at once: their memory is not to be given away before the stream has used it
+    monkeypatch.setattr(binding, "lora_project", lambda *a: plans.append(("project", a)))
+    layer = cep.LoRAProjection(on_device(torch.zeros(16, 64, dtype=torch.bfloat16), 0), 4, 1, 8)
+    x, ids = on_device(torch.zeros(4, 64, dtype=torch.bfloat16), 0), on_device(torch.zeros(4, dtype=torch.int32), 0)
+    out = on_device(torch.zeros(4, 16, dtype=torch.bfloat16), 0)
+    layer.run(x, ids, out)
+    assert x.recorded == ids.recorded == out.recorded == ()                  # the current stream's order is torch's
+    stream = types.SimpleNamespace(cuda_stream=5)
+    layer.run(x, ids, out, stream=stream)
+    assert x.recorded == ids.recorded == out.recorded == (stream,)
+    layer.run(x, None, out, stream=stream)
+
+
+def test_norm_records_its_tensors_on_the_stream_it_is_given(monkeypatch):
+    monkeypatch.setattr(binding, "_lib", types.SimpleNamespace(moe_norm=lambda *a: 0))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0)
+    t = dict(x=torch.zeros(3, 256, dtype=torch.bfloat16), weight=torch.zeros(256), residual=torch.zeros(3, 256),
+             residual_out=torch.zeros(3, 256), y=torch.zeros(3, 256, dtype=torch.bfloat16),
+             codes=torch.zeros(3, 256, dtype=torch.float8_e4m3fn), scales=torch.zeros(3, 2))
+    t = {k: on_device(v, 0) for k, v in t.items()}
+    cep.moe_norm(**t, dtype=cep.CEP_FP8_E4M3_BLOCK128)
+    assert all(v.recorded == () for v in t.values())
+    stream = types.SimpleNamespace(cuda_stream=5)
+    cep.moe_norm(**t, dtype=cep.CEP_FP8_E4M3_BLOCK128, stream=stream)
+    assert all(v.recorded == (stream,) for v in t.values())
+    cep.moe_norm(t["x"], y=t["y"], stream=stream)
