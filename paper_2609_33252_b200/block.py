@@ -19,7 +19,8 @@ class MoEBlock:
     """Owns the plans and the buffers between the steps.  All weights are the caller's tensors.
 
     w_out bf16 [H, A] (attention width A), norm_weight bf16 or fp32 [H], w_router bf16 [E_global, H]; ``load_experts``
-    takes what ``MoELayer.load_weights`` takes.
+    takes what ``MoELayer.load_weights`` takes.  ``run`` may be called on different streams: each call waits for the one
+    before, as the buffers between the steps are shared (who runs ``steps`` orders them).
     """
 
     def __init__(self, w_out, norm_weight, w_router, inter, n_experts_local, top_k, max_tokens, max_chunks=1, dtype=cep.CEP_BF16,
@@ -37,6 +38,7 @@ class MoEBlock:
         self.logits = empty(max_tokens, E, dtype=torch.float32)
         self.ids = empty(max_tokens, top_k, dtype=torch.int32)
         self.weights = empty(max_tokens, top_k, dtype=torch.float32)
+        self.done, self.last_stream = torch.cuda.Event(), None       # the end of the last call, where it ran
         self.codes = self.scales = None
         if dtype != cep.CEP_BF16:
             self.codes = empty(max_tokens, H, dtype=torch.float8_e4m3fn)
@@ -68,8 +70,13 @@ class MoEBlock:
         Returns the experts' output bf16 [T,H], to be added to the residual by the next layer's norm."""
         if out is None:
             out = torch.empty(attention.shape[0], self.H, dtype=torch.bfloat16, device=attention.device)
+        stream = torch.cuda.current_stream(attention.device)
+        if self.last_stream is not None and self.last_stream != stream:
+            stream.wait_event(self.done)
         for _, call in self.steps(attention, residual, adapter_ids, out, n_chunks):
             call()
+        self.done.record(stream)
+        self.last_stream = stream
         return out
 
     def close(self):
