@@ -70,6 +70,8 @@ class MoEBlock:
         Returns the experts' output bf16 [T,H], to be added to the residual by the next layer's norm."""
         if out is None:
             out = torch.empty(attention.shape[0], self.H, dtype=torch.bfloat16, device=attention.device)
+        if attention.shape[0] == 0:                          # (empty tensors have no address, which the layer's calls refuse)
+            return out
         stream = torch.cuda.current_stream(attention.device)
         if self.last_stream is not None and self.last_stream != stream:
             stream.wait_event(self.done)

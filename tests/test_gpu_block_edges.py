@@ -28,3 +28,26 @@ def test_calls_on_different_streams(dtype):
     for n, (out, r1) in enumerate(got):
         assert torch.equal(r1, want[n % 2][1]) and torch.equal(out, want[n % 2][0]), n
     block.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "mxfp4"])
+def test_no_tokens(dtype):
+    # a rank without tokens in this step
+    cfg, host, w, block, ad, attention, residual, ids = make(dtype, 40)
+    want = block.run(attention, residual.clone(), ids)
+    out = block.run(attention[:0], residual[:0], ids[:0])
+    assert out.shape == (0, cfg.H) and out.dtype == torch.bfloat16
+    assert block.run(attention[:0], residual[:0], n_chunks=3).shape == (0, cfg.H)
+    assert torch.equal(block.run(attention, residual, ids), want)
+    torch.cuda.synchronize()
+    assert cep.ffn_status(block.layer.plan) == 0
+    block.close()
+
+
+def test_fewer_tokens_than_chunks():
+    cfg, host, w, block, ad, attention, residual, ids = make("bf16", 2)
+    want = block.run(attention, residual.clone(), ids)
+    assert torch.equal(block.run(attention, residual, ids, n_chunks=3), want)
+    torch.cuda.synchronize()
+    assert cep.ffn_status(block.layer.plan) == 0
+    block.close()
