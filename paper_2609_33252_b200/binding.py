@@ -276,9 +276,11 @@ def moe_norm(x, weight=None, eps: float = 1e-6, residual=None, residual_out=None
     codes float8_e4m3fn [T,H] and scales fp32 [T,ceil(H/128)] (CEP_FP8_E4M3_BLOCK128) or uint8 [T,ceil(H/32)]
     (CEP_MXFP4_E4M3).  Rows of x, residual, residual_out and y may be strided.  Tensors are recorded on a `stream` that is given."""
     torch = _torch_module or _torch()
-    if not _ELEM:
-        _ELEM.update({torch.bfloat16: CEP_ELEM_BF16, torch.float32: CEP_ELEM_FP32})
-        _NORM_DTYPES.extend(((torch.bfloat16, torch.float32), (torch.float8_e4m3fn, torch.uint8), (torch.uint8,), (torch.float32,)))
+    if not _ELEM:                                      # (another thread's first call may come at any point: the marker last)
+        dtypes = ((torch.bfloat16, torch.float32), (torch.float8_e4m3fn, torch.uint8), (torch.uint8,), (torch.float32,))
+        elem = {torch.bfloat16: CEP_ELEM_BF16, torch.float32: CEP_ELEM_FP32}
+        _NORM_DTYPES[:] = dtypes
+        _ELEM.update(elem)
     shape = x.shape
     if len(shape) != 2 or not x.is_cuda:
         raise CepError(-1, "x must be a [T, H] CUDA tensor")

@@ -77,3 +77,30 @@ def test_norm_records_its_tensors_on_the_stream_it_is_given(monkeypatch):
     cep.moe_norm(**t, dtype=cep.CEP_FP8_E4M3_BLOCK128, stream=stream)
     assert all(v.recorded == (stream,) for v in t.values())
     cep.moe_norm(t["x"], y=t["y"], stream=stream)
+
+
+@pytest.mark.parametrize("at", range(9))
+def test_the_first_norm_of_one_thread_does_not_disturb_anothers(monkeypatch, at):
+    # another thread's first call in the middle of this one's: here where the first call looks up its `at`-th type
+    monkeypatch.setattr(binding, "_lib", types.SimpleNamespace(moe_norm=lambda *a: 0))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0)
+    fresh = dict(vars(binding))
+    for name in ("_ELEM", "_NORM_DTYPES", "_norm_types"):
+        if name in fresh:
+            monkeypatch.setattr(binding, name, type(fresh[name])() if fresh[name] is not None else None)
+    x, weight = on_device(torch.zeros(3, 256, dtype=torch.bfloat16), 0), on_device(torch.zeros(256), 0)
+    y = on_device(torch.zeros(3, 256, dtype=torch.bfloat16), 0)
+    calls = []
+
+    class Torch:
+        def __getattr__(self, name):
+            if name != "_C":
+                calls.append(name)
+                if len(calls) == at + 1:
+                    cep.moe_norm(x, weight, y=y)
+            return getattr(torch, name)
+
+    monkeypatch.setattr(binding, "_torch_module", Torch())
+    cep.moe_norm(x, weight, y=y)
+    assert len(calls) >= 5
