@@ -343,8 +343,8 @@ def lora_plan(cfg: LoraConfig, weight, bank, workspace, stream=None) -> int:
 
 
 def lora_load_adapter(plan, slot: int, rank: int, scale: float, down, up, stream=None):
-    _check(lib().lora_load_adapter(plan, slot, rank, scale, _dptr(down), 0 if down is None else down.stride(0), _dptr(up),
-                                   0 if up is None else up.stride(0), _stream_handle(stream)))
+    stride = lambda t: 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]     # (that of a single row means nothing)
+    _check(lib().lora_load_adapter(plan, slot, rank, scale, _dptr(down), stride(down), _dptr(up), stride(up), _stream_handle(stream)))
 
 
 def lora_project(plan, x, adapter_ids, y, stream=None):

@@ -104,3 +104,18 @@ def test_the_first_norm_of_one_thread_does_not_disturb_anothers(monkeypatch, at)
     monkeypatch.setattr(binding, "_torch_module", Torch())
     cep.moe_norm(x, weight, y=y)
     assert len(calls) >= 5
+
+
+def test_an_adapter_of_one_row_may_have_any_row_stride(plans, monkeypatch):
+    # the stride of a dimension of one element means nothing; torch calls these tensors contiguous
+    given = []
+    monkeypatch.setattr(binding, "lib", lambda: types.SimpleNamespace(lora_load_adapter=lambda *a: given.append(a) or 0))
+    down = torch.zeros(64, 1, dtype=torch.bfloat16).t()
+    up = torch.zeros(16, 1, dtype=torch.bfloat16)
+    assert down.is_contiguous() and down.stride(0) == 1
+    binding.lora_load_adapter(7, 0, 1, 1.0, down, up, stream=5)
+    assert given[0][5] >= 64 and given[0][7] >= 1
+    up = torch.zeros(8, 1, dtype=torch.bfloat16).t()           # one output column
+    assert up.stride(0) == 1
+    binding.lora_load_adapter(7, 0, 8, 1.0, torch.zeros(8, 64, dtype=torch.bfloat16), up, stream=5)
+    assert given[1][5] == 64 and given[1][7] >= 8
