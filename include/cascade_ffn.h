@@ -263,8 +263,8 @@ CEP_API int moe_norm(const cep_norm_desc* desc, const void* x, const void* resid
 /*
  * A projection shared by all requests of a batch with one low-rank adapter per request beside it:
  *   y[t] = W x[t] + scale_a * B_a (A_a x[t]),   a = adapter_ids[t];   -1: no adapter, y[t] = W x[t]
- * bf16 operands, fp32 accumulation; A_a x[t] is carried in fp32 and enters the accumulator of W x[t] as two bf16 terms
- * (2^-17 relative), so y is rounded once.  Without adapters and with CEP_ELEM_FP32 it is the router's logits (moe_route).
+ * bf16 operands, fp32 accumulation; A_a x[t] is carried in fp32 and enters the accumulator of W x[t] as bf16 terms, two
+ * for a bf16 y (2^-17 relative), three for an fp32 one (2^-25), so y is rounded once.  Without adapters and with CEP_ELEM_FP32 it is the router's logits (moe_route).
  */
 typedef struct cep_lora_plan cep_lora_plan;
 

@@ -100,6 +100,8 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
                      const __grid_constant__ CUtensorMap tm_up, const Shape sh, int splits, int after_peer, const LoraArgs la_, OT* __restrict__ y,
                      int64_t y_stride, int vec_ok, int32_t* __restrict__ tile_counter, int32_t* __restrict__ status) {
   constexpr bool kF32 = sizeof(OT) == 4;
+  // (without adapters neither is of use, but with those of fp32 the compiler spills registers: 2048 tokens of 7168 -> 256 21.0 -> 22.8 us)
+  constexpr int kStep = kLora ? UpStep<OT>::kChunks : 2, kTerms = kLora ? UpStep<OT>::kTerms : 2;
   constexpr bool kBothHalves = kF32 || kSplit;           // the s-row warps read half of the accumulator
   LoraArgs la = la_;
   if (!kLora) la.has = 0;
@@ -185,7 +187,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         for (int c0 = c_first; ok && c0 < total; c0 += kLookAhead * c_stride) {
           int2 e[kLookAhead];
 #pragma unroll
-          for (int j = 0; j < kLookAhead; ++j) e[j] = up_to(list_pair(list, c0 + j * c_stride, kLargeTok * kLoraMaxChunks), c0 + j * c_stride, total);
+          for (int j = 0; j < kLookAhead; ++j) e[j] = up_to(list_step<kStep>(list, c0 + j * c_stride, kLargeTok * kLoraMaxChunks), c0 + j * c_stride, total);
 #pragma unroll
           for (int j = 0; j < kLookAhead; ++j) {
             if (e[j].x < 0) break;
@@ -252,8 +254,9 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             const int n = min(kStep, total - c0);
             for (int i = 0; i < n; ++i) {
               const uint64_t udesc = make_smem_desc_32b(smem_u32(smem_w + stage * kHalf) + i * kUpBytes);
-              tc_mma_f16_pair(d, sdesc + (uint64_t)(i * 4), udesc, idesc, 1u);
-              tc_mma_f16_pair(d, sdesc + (uint64_t)(i * 4 + 2), udesc, idesc, 1u);
+              tc_mma_f16_pair(d, sdesc + (uint64_t)(i * 2 * kTerms), udesc, idesc, 1u);
+              tc_mma_f16_pair(d, sdesc + (uint64_t)(i * 2 * kTerms + 2), udesc, idesc, 1u);
+              if (kTerms == 3) tc_mma_f16_pair(d, sdesc + (uint64_t)(i * 2 * kTerms + 4), udesc, idesc, 1u);
             }
             tc_commit_pair_both(smem_u32(&bars->empty[stage]), both);
             if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -312,7 +315,8 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           // the adapters' steps end the last chain
           if (wait) pdl_wait();
           const int ts = m * kLargeTok + half * 128 + r;
-          SRow<kF32 ? 1 : 4> row;                        // (fp32: the sums need the registers)
+          SRow<kF32 ? 0 : 4, kTerms> row;                // (fp32: the sums need the registers; 519 tokens with nine
+                                                         // adapters 26.9 us, with one chunk ahead 29.0)
           row.fetch(la, ts < sh.T ? ts : -1);
           const int total = __ldcg(la.n_chunks + m);
           const int32_t* list = la.chunks + (size_t)m * kLargeTok * kLoraMaxChunks;
@@ -323,7 +327,7 @@ project_large_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
             const int first = stage;
             int n = 0;
             for (; n < kBatch && c0 < total; ++n, c0 += c_stride, ++step) {
-              if ((step & 31) == 0) e = up_to(list_pair(list, c0 + lane * c_stride, kLargeTok * kLoraMaxChunks), c0 + lane * c_stride, total);
+              if ((step & 31) == 0) e = up_to(list_step<kStep>(list, c0 + lane * c_stride, kLargeTok * kLoraMaxChunks), c0 + lane * c_stride, total);
               const int v0 = __shfl_sync(0xffffffffu, e.x, step & 31), v1 = __shfl_sync(0xffffffffu, e.y, step & 31);
               ok = mbar_wait(smem_u32(&bars->ready[stage]), (phase >> stage) & 1u, abort_flag, status);
               ok = __all_sync(0xffffffffu, ok);

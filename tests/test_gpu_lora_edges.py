@@ -85,3 +85,25 @@ def test_inputs_dropped_while_another_stream_uses_them(T):
             torch.cuda.synchronize()
             assert torch.equal(got, want) and torch.equal(y, normed)
     assert c.layer.status() == 0
+
+
+# An fp32 output is as exact as a 32-bit evaluation.  By norm: the matrix unit's additions truncate, so a chain of n of them
+# drifts by n/2 units of 2^-23 of its end at the worst, and below a third of that as a drift that grows with the sum
+# (test_fp32_outputs_keep_fp32_accuracy).  Chains hold at most 1024 products (64 additions): 1.3e-6 for W x and for s = A x.
+# The up projection adds 3R/16 products to one chain (R = 64: 12 additions, 2.4e-7); s as three bf16 terms and the scale's
+# product are below 2^-23.
+EXACT, EXACT_ADAPTERS = 1.3e-6, 1.3e-6 + 2.4e-7 + 1.2e-7
+
+
+@pytest.mark.parametrize("T,K,N", [(1, 7168, 128), (40, 7168, 128), (64, 7168, 1024), (100, 7168, 128), (300, 7168, 128), (700, 7168, 512),
+                                   (2048, 7168, 128)])
+def test_fp32_outputs_keep_fp32_accuracy_with_adapters(T, K, N):
+    # without the shared projection's part, so that nothing hides the adapters'
+    c = Case(K, N, ranks=(64, 64), max_tokens=T, out="fp32", weight=torch.zeros(N, K, dtype=torch.bfloat16, device="cuda"))
+    x, ids = rand((T, K), 2), (torch.arange(T, device="cuda") % 2).to(torch.int32)
+    got, y = c.check(x, ids).double(), c.reference(x, ids)[0]
+    assert ((got - y).norm() / y.norm()).item() <= EXACT_ADAPTERS
+    # and with it
+    c = Case(K, N, ranks=(64, 64), max_tokens=T, out="fp32")
+    got, y = c.check(x, ids).double(), c.reference(x, ids)[0]
+    assert ((got - y).norm() / y.norm()).item() <= EXACT + EXACT_ADAPTERS
