@@ -247,7 +247,7 @@ int lora_project(cep_lora_plan* p, const void* x, int64_t x_stride, int32_t n_to
   cudaError_t e = cudaSuccess;
   if (adapter_ids) {
     const FreeSms free = small ? FreeSms{0, 0} : project_large_free(p->device, n_tokens, c.out_features, c.in_features);
-    e = launch_lora_shrink(tm_x, p->tm_down, box, free, n_tokens, c.in_features, c.out_features, adapter_ids, p->bank, token_tile, p->ids, p->n_chunks, p->chunks, p->s,
+    e = launch_lora_shrink(tm_x, p->tm_down, box, free, n_tokens, c.in_features, c.out_features, f32, adapter_ids, p->bank, token_tile, p->ids, p->n_chunks, p->chunks, p->s,
                            p->status, st);
     a.bank = &p->bank;
     a.step = LoraStep{p->ids, p->n_chunks, p->chunks, p->s};

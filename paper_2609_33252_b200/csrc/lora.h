@@ -40,8 +40,8 @@ bool lora_beside(int T);                     // the down projection runs beside 
 cudaError_t lora_shrink_setup();             // once per plan, with its device current
 // tm_x: 64 columns x `box` rows; tm_down: the bank's down rows, 64 columns x 16 rows.  token_tile: tokens per tile of the
 // projection kernel that follows (its lists are made here); free: what that kernel leaves.
-cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, const FreeSms& free, int T, int K, int N, const int32_t* ids,
-                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, const FreeSms& free, int T, int K, int N, int out_f32,
+                               const int32_t* ids, const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* status, cudaStream_t s);
 
 struct ProjectArgs {

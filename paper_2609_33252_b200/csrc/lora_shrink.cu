@@ -29,7 +29,9 @@ constexpr int kRows = 128;                           // tokens per block
 constexpr int kXStage = kRows * 128;                 // 64 bf16 of K
 constexpr int kChunkStage = kLoraChunk * 128;
 constexpr int kMaxStages = 8;
-constexpr int kChainSteps = 12;                      // K steps per accumulation chain (the tensor core's additions truncate)
+// K steps per accumulation chain (the tensor core's additions truncate): kChainSteps while the accumulators last, at most
+// kLongestChain (1024 products) for an fp32 output.  A bf16 output does not see longer ones (7168 products end 8e-6 low).
+constexpr int kChainSteps = 12, kLongestChain = 16;
 constexpr int kMaxParts = 8;
 struct __align__(8) ShrinkBarriers {
   uint64_t full[kMaxStages], empty[kMaxStages], acc_full;
@@ -367,17 +369,20 @@ cudaError_t lora_shrink_setup() {
   return cudaFuncSetAttribute(lora_shrink_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
-cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, const FreeSms& free, int T, int K, int N, const int32_t* ids,
-                               const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
+cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& tm_down, int box, const FreeSms& free, int T, int K, int N, int out_f32,
+                               const int32_t* ids, const LoraBank& bank, int token_tile, int32_t* out_ids, int32_t* n_chunks, int32_t* chunk_lists, float* s_out,
                                int32_t* status, cudaStream_t s) {
   // Up to 128 tokens the blocks leave shared memory for the projection kernel's on the same SM (lora_beside).
   const bool beside = lora_beside(T);
-  const int chunks = beside ? 4 : 8, smem = beside ? kShortSmem : kLongSmem;
+  int chunks = beside ? 4 : 8;
+  const int smem = beside ? kShortSmem : kLongSmem;
+  const int acc_chunks = beside ? 8 : 16;              // of 16 columns in all accumulators: two blocks share an SM's tensor memory
   const int x_stage = T < kRows ? (T + box - 1) / box * box * 128 : kXStage;
   const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
   // passes a tile can need
   const int n = T < kRows ? T : kRows, adapters = bank.slots < n ? bank.slots : n;
-  const int passes = (adapters * (bank.rank_pad / kLoraChunk) + chunks - 1) / chunks;
+  const int most_chunks = adapters * (bank.rank_pad / kLoraChunk);
+  int passes = (most_chunks + chunks - 1) / chunks;
   // Blocks that find SMs of their own beside the projection's run while it multiplies (free): then as many parts as still find
   // them, a cluster of `parts` SMs in one GPC per tile (700 tokens of 7168 -> 2048 with eight adapters: 31 us with six parts, 42
   // with eight; 1500: 49 with four, 62 with eight; 512 of 7168 -> 3584: 35 with four, 39 with six, 42 with eight).  Otherwise
@@ -397,13 +402,22 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   const int least = tiles >= 16 ? 8 : 1;
   if (parts > steps / least) parts = steps / least;
   if (parts < 1) parts = 1;
+  if (out_f32) {
+    // chains short enough for the output: fewer chunks a pass leave room for more accumulators (up to K = 65536 beside the
+    // projection and 131072 in long batches, from where on chains grow)
+    const int longest = kLongestChain * acc_chunks;
+    if (parts < (steps + longest - 1) / longest) parts = (steps + longest - 1) / longest < kMaxParts ? (steps + longest - 1) / longest : kMaxParts;
+    const int chains = ((steps + parts - 1) / parts + kLongestChain - 1) / kLongestChain;
+    if (chunks > acc_chunks / chains) chunks = acc_chunks / chains > 1 ? acc_chunks / chains : 1;
+    passes = (most_chunks + chunks - 1) / chunks;
+  }
   // how many blocks share the passes
   int stripes = 4 * kSms / (tiles * parts);
   if (stripes > passes) stripes = passes;
   if (stripes < 1) stripes = 1;
   const int part_steps = steps / parts;
   int n_acc = (part_steps + kChainSteps - 1) / kChainSteps;
-  const int most = (beside ? 128 : 256) / (chunks * kLoraChunk);        // two blocks share an SM's tensor memory
+  const int most = acc_chunks / chunks;
   if (n_acc > most) n_acc = most;
   if (n_acc < 1) n_acc = 1;
   int tmem_cols = 32;

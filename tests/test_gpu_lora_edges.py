@@ -107,3 +107,12 @@ def test_fp32_outputs_keep_fp32_accuracy_with_adapters(T, K, N):
     c = Case(K, N, ranks=(64, 64), max_tokens=T, out="fp32")
     got, y = c.check(x, ids).double(), c.reference(x, ids)[0]
     assert ((got - y).norm() / y.norm()).item() <= EXACT + EXACT_ADAPTERS
+
+
+@pytest.mark.parametrize("T,K,N", [(16384, 7168, 128), (3000, 16384, 256), (20000, 7168, 64), (33, 32768, 128), (600, 49152, 128)])
+def test_fp32_accuracy_of_long_sums_in_the_down_projection(T, K, N):
+    # few K parts a tile, or a K that is long even in eight: more accumulation chains, not longer ones
+    c = Case(K, N, ranks=(64, 40), max_tokens=T, out="fp32", weight=torch.zeros(N, K, dtype=torch.bfloat16, device="cuda"))
+    x, ids = rand((T, K), 2), (torch.arange(T, device="cuda") % 2).to(torch.int32)
+    got, y = c.check(x, ids).double(), c.reference(x, ids)[0]
+    assert ((got - y).norm() / y.norm()).item() <= EXACT_ADAPTERS
