@@ -17,7 +17,8 @@
 // memory, every wait bounded (status word).
 //
 // The tensor core's fp32 additions truncate: one chain over K = 7168 ends 8e-6 low on average (measured), which a bf16
-// output does not see and an fp32 output does.  fp32 outputs are summed from several accumulators of about 768 products.
+// output does not see and an fp32 output does.  fp32 outputs are summed from several accumulators of about 768 products,
+// at most 1024; where K needs more chains than there are accumulators, the epilogue's warps empty them on the way.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -30,13 +31,16 @@ using namespace ptx;
 
 constexpr int kSmallThreads = 192;
 constexpr int kSmallMaxStages = 12;
+constexpr int kTmemCols = 512;                         // tensor memory of an SM
 constexpr int kBatch = 2;                              // (64 tokens, 24 adapters: 36.3 us with two, 37.2 with four)
 constexpr int kMaxSplits = 8;                          // CTAs of a portable cluster
+constexpr int kMostF32 = 64;                           // token columns of a tile with fp32 outputs
+constexpr int kLongestChain = 16;                      // K steps of a chain of an fp32 output
 constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
 constexpr int kSmallRing = 200 * 1024;
 constexpr int kSharedRing = 136 * 1024;               // the same beside a block of the down projection
 struct __align__(8) SmallBarriers {
-  uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], ready[kSmallMaxStages], sfull[kSmallMaxStages], acc_full;
+  uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], ready[kSmallMaxStages], sfull[kSmallMaxStages], acc_full, acc_empty;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -78,14 +82,15 @@ __device__ __forceinline__ void add_splits(uint32_t base, int splits, int first,
   }
 }
 
-// Grid (column tiles, K splits, token tiles of `tok`).  npad: token columns of the MMA, a multiple of 16.  n_acc: accumulators
-// (npad columns each) that share the CTA's K steps.
+// Grid (column tiles, K splits, token tiles of `tok`).  npad: token columns of the MMA, a multiple of 16.  chains: accumulation
+// chains that share the CTA's K steps, in turn in n_acc accumulators of npad columns.
 template <typename OT>
 __global__ void __launch_bounds__(kSmallThreads, 1)
 project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
-                     const __grid_constant__ CUtensorMap tm_up, int T, int N, int num_kb, int tok, int npad, int stages, int n_acc, int tmem_cols, const LoraArgs la,
+                     const __grid_constant__ CUtensorMap tm_up, int T, int N, int num_kb, int tok, int npad, int stages, int n_acc, int chains, int tmem_cols, const LoraArgs la,
                      OT* __restrict__ y, int64_t y_stride, int vec_ok, int32_t* __restrict__ status) {
   constexpr int kStep = UpStep<OT>::kChunks, kTerms = UpStep<OT>::kTerms;
+  constexpr bool kF32 = sizeof(OT) == 4;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const int x_stage = npad * kKBytes, stage_bytes = kWStage + x_stage;
@@ -111,7 +116,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1);
       mbar_init(smem_u32(&bars->ready[s]), 1); mbar_init(smem_u32(&bars->sfull[s]), 4);
     }
-    mbar_init(smem_u32(&bars->acc_full), 1);
+    mbar_init(smem_u32(&bars->acc_full), 1); mbar_init(smem_u32(&bars->acc_empty), 4);
     bars->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     // the ring is empty: its first loads go out before the rest of the block is set up
@@ -170,13 +175,22 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       const uint32_t idesc = make_idesc_bf16(128, npad);
       int stage = 0; uint32_t phase = 0;
       bool ok = true;
-      int slab = 0, slab_end = kb0 + (kb1 - kb0) / n_acc;           // chain `slab` ends before K step slab_end
-      uint32_t first = 1;
+      int chain = 0, acc = 0, chain_end = kb0 + (kb1 - kb0) / chains;      // the chain ends before K step chain_end
+      uint32_t first = 1, emptied = 0;
       for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status)) { ok = false; break; }
         tc_fence_after();
-        if (kb == slab_end) { ++slab; slab_end = kb0 + (int)((long long)(kb1 - kb0) * (slab + 1) / n_acc); first = 1; }
-        const uint32_t d = tmem + (uint32_t)(slab * npad);
+        if (kb == chain_end) {
+          ++chain; chain_end = kb0 + (int)((long long)(kb1 - kb0) * (chain + 1) / chains); first = 1;
+          if (++acc == n_acc) {                          // all in use
+            acc = 0;
+            tc_commit(smem_u32(&bars->acc_full));
+            if (!mbar_wait(smem_u32(&bars->acc_empty), emptied, abort_flag, status)) { ok = false; break; }
+            emptied ^= 1u;
+            tc_fence_after();
+          }
+        }
+        const uint32_t d = tmem + (uint32_t)(acc * npad);
         const uint64_t wdesc = make_smem_desc(smem_u32(smem + stage * stage_bytes));
         const uint64_t xdesc = make_smem_desc(smem_u32(smem + stage * stage_bytes + kWStage));
 #pragma unroll
@@ -189,7 +203,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       if (la.has && ok) {
         pdl_wait();
         const int total = __ldcg(la.n_chunks + blockIdx.z);
-        const uint32_t last_acc = tmem + (uint32_t)(slab * npad);
+        const uint32_t last_acc = tmem + (uint32_t)(acc * npad);
         uint32_t sphase = 0;                             // one parity bit per stage
         for (int c0 = split * kStep; c0 < total; c0 += splits * kStep) {
           if (!mbar_wait(smem_u32(&bars->full[stage]), phase, abort_flag, status) ||
@@ -213,10 +227,45 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
   } else {
     // ---------------------------------------------------------------- warps 2..5: rows of s, then the epilogue
     const int lane_grp = warp & 3, tid = threadIdx.x - 64;
+    const int cols = min(tok, T - t0);                 // token columns that exist
+    const uint32_t taddr = tmem + ((uint32_t)(lane_grp * 32) << 16);
     bool ok = true;
-    if (la.has) pdl_wait();
-    if (tid == 0) pdl_release();
+    float sum[kF32 ? kMostF32 : 1];                    // fp32: the sum of the chains, a column per token
+    auto add_accumulators = [&](int n) {
+#pragma unroll
+      for (int c = 0; c < (kF32 ? kMostF32 : 0); c += 16) {
+        if (c >= cols) break;
+        for (int a = 0; a < n; ++a) {
+          __syncwarp();                                // the load is warp-collective
+          uint32_t d[16];
+          tc_ld16(taddr + a * npad + c, d);
+          tc_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[kF32 ? c + i : 0] += __uint_as_float(d[i]);
+        }
+      }
+    };
+    uint32_t full = 0;
+    int left = chains;                                 // not yet added
+    if (!la.has && tid == 0) pdl_release();
+    if constexpr (kF32) {
+#pragma unroll
+      for (int c = 0; c < kMostF32; ++c) sum[c] = 0.f;
+      for (; left > n_acc; left -= n_acc) {
+        ok = ok && mbar_wait_relaxed(smem_u32(&bars->acc_full), full, abort_flag, status);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        full ^= 1u;
+        tc_fence_after();
+        add_accumulators(n_acc);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->acc_empty));
+      }
+    }
     if (la.has) {
+      pdl_wait();
+      if (tid == 0) pdl_release();
       const int32_t* list = la.chunks + (size_t)t0 * kLoraMaxChunks;
       const int cap = tok * kLoraMaxChunks;
       int2 e = list_step<kStep>(list, (split + lane * splits) * kStep, cap);      // lane i: the i-th of the next 32 steps
@@ -249,28 +298,26 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
           for (int i = 0, s = first; i < n; ++i) { mbar_arrive(smem_u32(&bars->sfull[s])); if (++s == stages) s = 0; }
       }
     }
-    const bool got = ok && mbar_wait_relaxed(smem_u32(&bars->acc_full), 0u, abort_flag, status);
+    const bool got = ok && mbar_wait_relaxed(smem_u32(&bars->acc_full), full, abort_flag, status);
     const bool all = __all_sync(0xffffffffu, got);
-    const int cols = min(tok, T - t0);                 // token columns that exist
-    const uint32_t taddr = tmem + ((uint32_t)(lane_grp * 32) << 16);
-    float* mine = reinterpret_cast<float*>(smem);      // [token][128] sums, in the ring: every load has been consumed
+    float* mine = reinterpret_cast<float*>(smem) + lane_grp * 32 + lane;       // [token][128] sums, in the ring: every load has been consumed
     if (all) {
       tc_fence_after();
-      for (int c = 0; c < cols; c += 16) {
-        __syncwarp();                                  // the load is warp-collective
-        uint32_t d[16];
-        tc_ld16(taddr + c, d);
-        tc_wait_ld();
-        for (int s = 1; s < n_acc; ++s) {
-          uint32_t e[16];
-          tc_ld16(taddr + s * npad + c, e);
+      if constexpr (kF32) {
+        add_accumulators(left);
+#pragma unroll
+        for (int c = 0; c < kMostF32; ++c)
+          if (c < cols) mine[c * 128] = sum[c];
+      } else {
+        for (int c = 0; c < cols; c += 16) {
+          __syncwarp();                                // the load is warp-collective
+          uint32_t d[16];
+          tc_ld16(taddr + c, d);
           tc_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) d[i] = __float_as_uint(__uint_as_float(d[i]) + __uint_as_float(e[i]));
+          for (int i = 0; i < 16; ++i)
+            if (c + i < cols) mine[(c + i) * 128] = __uint_as_float(d[i]);
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (c + i < cols) mine[(c + i) * 128 + lane_grp * 32 + lane] = __uint_as_float(d[i]);
       }
     }
   }
@@ -322,7 +369,7 @@ Plan plan(const int* clusters, int T, int N, int K, int out_f32) {
 
 }  // namespace
 
-int project_small_tile(int out_f32) { return out_f32 ? 64 : kSmallTok; }       // (8 accumulators of 64 columns fill the tensor memory)
+int project_small_tile(int out_f32) { return out_f32 ? kMostF32 : kSmallTok; }       // (8 accumulators of 64 columns fill the tensor memory)
 int project_small_tokens(int T, int out_f32) { return T >= project_small_tile(out_f32) ? project_small_tile(out_f32) : (T + 15) / 16 * 16; }
 
 cudaError_t project_small_setup(int dev) {
@@ -373,9 +420,11 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
                                  int dev, cudaStream_t s) {
   const Plan p = plan(g_clusters[dev], a.T, a.N, a.K, a.out_f32);
   const int steps = p.num_kb / p.splits;               // K steps a CTA has at least
-  int n_acc = a.out_f32 ? (steps + kSlabSteps - 1) / kSlabSteps : 1;
-  if (n_acc > 512 / p.npad) n_acc = 512 / p.npad;
-  if (n_acc < 1) n_acc = 1;
+  // Chains of kSlabSteps K steps, or of up to kLongestChain where the accumulators then suffice.
+  int chains = a.out_f32 ? (steps + kSlabSteps - 1) / kSlabSteps : 1;
+  int n_acc = kTmemCols / p.npad;
+  if (chains <= n_acc) n_acc = chains;
+  else if ((p.num_kb + p.splits - 1) / p.splits <= n_acc * kLongestChain) chains = n_acc;
   const int stage = kWStage + p.npad * kKBytes;
   int tmem_cols = 32;
   while (tmem_cols < n_acc * p.npad) tmem_cols *= 2;
@@ -401,9 +450,9 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   const CUtensorMap& u = reinterpret_cast<const CUtensorMap&>(tm_up);
   const LoraArgs la = lora_args(a);
   if (a.out_f32)
-    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, tmem_cols, la, (float*)a.y, a.y_stride,
+    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, chains, tmem_cols, la, (float*)a.y, a.y_stride,
                               vec_ok, a.status);
-  return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, tmem_cols, la,
+  return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, chains, tmem_cols, la,
                             (__nv_bfloat16*)a.y, a.y_stride, vec_ok, a.status);
 }
 

@@ -116,3 +116,23 @@ def test_fp32_accuracy_of_long_sums_in_the_down_projection(T, K, N):
     x, ids = rand((T, K), 2), (torch.arange(T, device="cuda") % 2).to(torch.int32)
     got, y = c.check(x, ids).double(), c.reference(x, ids)[0]
     assert ((got - y).norm() / y.norm()).item() <= EXACT_ADAPTERS
+
+
+@pytest.mark.parametrize("T,K,N", [(64, 7168, 18944), (64, 16384, 18944), (40, 12288, 18944), (128, 16384, 9472), (64, 32768, 9472), (17, 57344, 9472), (64, 81920, 256)])
+def test_fp32_accuracy_of_long_sums_over_wide_outputs(T, K, N):
+    # as many column blocks as SMs, so that K is not split, or a K that is long even when it is: more accumulation chains than
+    # accumulators
+    c = Case(K, N, max_tokens=T, out="fp32")
+    x = rand((T, K), 2)
+    got, y = c.check(x, None).double(), c.reference(x, None)[0]
+    assert ((got - y).norm() / y.norm()).item() <= EXACT
+
+
+def test_fp32_long_sums_with_adapters_over_wide_outputs():
+    c = Case(16384, 9472, ranks=(64, 20), max_tokens=64, out="fp32")
+    for T in (3, 64):
+        x, ids = rand((T, 16384), 2), ids_of(T, 2, 3)
+        got, y = c.check(x, ids).double(), c.reference(x, ids)[0]
+        assert ((got - y).norm() / y.norm()).item() <= EXACT + EXACT_ADAPTERS
+        for _ in range(5):
+            assert torch.equal(c.layer.run(x, ids).double(), got)
