@@ -23,6 +23,16 @@ __host__ __device__ inline bool dtype_is_bytes(int dtype) { return dtype != CEP_
 
 constexpr int kNormMaxHidden = 32768;           // moe_norm keeps a row in registers or shared memory
 
+// What may share an SM.  A block that finds too little tensor memory free waits inside its allocation, and clusters of two
+// kernels (two plans on two streams) could each hold what the other waits for.  So no block of this library ever waits there:
+// at most two blocks that use tensor memory fit an SM, those that can have a neighbour take at most half of the columns, and
+// those that take more leave no shared memory for one.  Checked where the sizes are set.
+constexpr int kSmShared = 228 * 1024, kBlockShared = 1024;       // of an SM; taken by each block beside its own
+constexpr int kSmTmemColumns = 512;
+constexpr int kLeastTmemBlock = 76 * 1024;                       // shared memory of the smallest of these blocks
+constexpr bool alone_on_its_sm(int smem) { return smem + kLeastTmemBlock + 2 * kBlockShared > kSmShared; }
+static_assert(3 * (kLeastTmemBlock + kBlockShared) > kSmShared, "three blocks would fit an SM");
+
 // Sets the calling thread's plan-less error string (cep_last_error(NULL)) and returns `code`.
 int record_error(int code, const char* fmt, ...);
 

@@ -38,6 +38,7 @@ struct __align__(8) Barriers {
 };
 constexpr int kSmemBytes = kStages * (A_STAGE + B_STAGE) + 1024 /*alignment slack*/ + 256;
 static_assert(sizeof(Barriers) <= 256, "barrier block");
+static_assert(alone_on_its_sm(kSmemBytes), "takes all of the tensor memory");
 
 using namespace ptx;
 
@@ -277,6 +278,7 @@ struct TileReader {
 };
 constexpr int kPairSmemBytes = kPairStages * (A_STAGE + PB_STAGE) + (kMaxExperts + 1) * 4 + 1024 + 256;
 static_assert(sizeof(PairBarriers) <= 256, "barrier block");
+static_assert(alone_on_its_sm(kPairSmemBytes), "takes all of the tensor memory");
 
 // kGather: the activation operand is not the permuted copy but the caller's token tensor itself; tm_a then
 // describes that tensor with one-row boxes, src_row[r] is the tensor row that physical row r holds, and the

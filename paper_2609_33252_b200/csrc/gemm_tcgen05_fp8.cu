@@ -74,6 +74,7 @@ struct __align__(8) Bars {
   int abort_flag;
 };
 static_assert(sizeof(Bars) <= kBarBytes, "barrier block");
+static_assert(alone_on_its_sm(Geo<true>::kSmemBytes) && alone_on_its_sm(Geo<false>::kSmemBytes), "takes all of the tensor memory");
 static_assert(BKB == 128 && Geo<true>::kStages % 2 == 0 && Geo<false>::kStages % 2 == 0, "a stage always pairs with the same scratch buffer");
 
 // What the scheduler thread publishes per tile, so that no other role has to search the tile table or

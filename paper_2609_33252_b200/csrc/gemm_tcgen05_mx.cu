@@ -72,6 +72,7 @@ struct __align__(8) Bars {
   int abort_flag;
 };
 static_assert(sizeof(Bars) <= 256, "barrier block");
+static_assert(alone_on_its_sm(kSmemBytes), "takes all of the tensor memory");
 
 struct Ring {
   int slot = 0; uint32_t phase = 0;

@@ -40,6 +40,7 @@ struct __align__(8) Barriers {
 };
 static_assert(sizeof(Barriers) <= 512, "barrier block");
 constexpr int kSmem = kStages * 2 * kHalf + 512 + 1024;
+static_assert(alone_on_its_sm(kSmem), "takes all of the tensor memory");
 static_assert(kSmem <= 227 * 1024 && 128 * kPitch * 4 <= kStages * 2 * kHalf, "shared memory");
 
 // The tiles of a CTA pair, in the order every role of it walks them: from the ring of ids that the leader's warp 6 fills in

@@ -31,7 +31,6 @@ using namespace ptx;
 
 constexpr int kSmallThreads = 192;
 constexpr int kSmallMaxStages = 12;
-constexpr int kTmemCols = 512;                         // tensor memory of an SM
 constexpr int kBatch = 2;                              // (64 tokens, 24 adapters: 36.3 us with two, 37.2 with four)
 constexpr int kMaxSplits = 8;                          // CTAs of a portable cluster
 constexpr int kMostF32 = 64;                           // token columns of a tile with fp32 outputs
@@ -39,6 +38,18 @@ constexpr int kLongestChain = 16;                      // K steps of a chain of 
 constexpr int kWStage = 128 * kKBytes;                 // 16 KiB of weight
 constexpr int kSmallRing = 200 * 1024;
 constexpr int kSharedRing = 136 * 1024;               // the same beside a block of the down projection
+constexpr int stage_bytes_for(int npad) { return kWStage + npad * kKBytes; }
+constexpr int stages_for(int ring, int npad) { return ring / stage_bytes_for(npad) < kSmallMaxStages ? ring / stage_bytes_for(npad) : kSmallMaxStages; }
+constexpr int smem_for(int ring, int npad) { return 1024 + stages_for(ring, npad) * stage_bytes_for(npad) + 512; }
+constexpr int least_smem(int ring) {
+  int least = smem_for(ring, 16);
+  for (int npad = 32; npad <= kSmallTok; npad += 16) least = smem_for(ring, npad) < least ? smem_for(ring, npad) : least;
+  return least;
+}
+// With adapters and few tokens the ring leaves room for a block of the down projection, so that both run at once, and takes
+// half of the tensor memory; a block that needs more of that takes the whole of the SM's shared memory instead.
+constexpr int kSharedColumns = kSmTmemColumns / 2;
+static_assert(least_smem(kSharedRing) >= kLeastTmemBlock && alone_on_its_sm(least_smem(kSmallRing)), "blocks that share an SM");
 struct __align__(8) SmallBarriers {
   uint64_t full[kSmallMaxStages], empty[kSmallMaxStages], ready[kSmallMaxStages], sfull[kSmallMaxStages], acc_full, acc_empty;
   uint32_t tmem_base;
@@ -422,18 +433,13 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   const int steps = p.num_kb / p.splits;               // K steps a CTA has at least
   // Chains of kSlabSteps K steps, or of up to kLongestChain where the accumulators then suffice.
   int chains = a.out_f32 ? (steps + kSlabSteps - 1) / kSlabSteps : 1;
-  int n_acc = kTmemCols / p.npad;
+  int n_acc = kSmTmemColumns / p.npad;
   if (chains <= n_acc) n_acc = chains;
   else if ((p.num_kb + p.splits - 1) / p.splits <= n_acc * kLongestChain) chains = n_acc;
-  const int stage = kWStage + p.npad * kKBytes;
   int tmem_cols = 32;
   while (tmem_cols < n_acc * p.npad) tmem_cols *= 2;
-  // With adapters and few tokens the ring leaves room for a block of the down projection (128 columns of tensor memory), so
-  // that both run at once; an allocation that it might have to wait for takes the whole of the SM's shared memory instead.  So
-  // no block ever waits for tensor memory with another plan's block on its SM: two clusters could wait for each other.
-  const int ring = a.bank && lora_beside(a.T) && tmem_cols <= 256 ? kSharedRing : kSmallRing;
-  int stages = ring / stage;
-  if (stages > kSmallMaxStages) stages = kSmallMaxStages;
+  const int ring = a.bank && lora_beside(a.T) && tmem_cols <= kSharedColumns ? kSharedRing : kSmallRing;
+  const int stages = stages_for(ring, p.npad);
   const size_t elt = a.out_f32 ? 4 : 2;
   const int vec_ok = reinterpret_cast<uintptr_t>(a.y) % (4 * elt) == 0 && a.y_stride % 4 == 0;
   cudaLaunchConfig_t cfg = {};
@@ -443,7 +449,7 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.gridDim = dim3(p.n_tiles, p.splits, p.t_tiles); cfg.blockDim = dim3(kSmallThreads, 1, 1);
-  cfg.dynamicSmemBytes = 1024 + (size_t)stages * stage + 512; cfg.stream = s; cfg.attrs = attr;
+  cfg.dynamicSmemBytes = smem_for(ring, p.npad); cfg.stream = s; cfg.attrs = attr;
   cfg.numAttrs = 2;
   const CUtensorMap& w = reinterpret_cast<const CUtensorMap&>(tm_w);
   const CUtensorMap& x = reinterpret_cast<const CUtensorMap&>(tm_x);

@@ -347,6 +347,9 @@ __global__ void lora_publish_kernel(int rank, float scale, int slot, int32_t* ba
 }
 
 constexpr int kShortSmem = 76 * 1024, kLongSmem = 97 * 1024;     // beside the projection's blocks; two blocks per SM
+constexpr int kShortAcc = 8, kLongAcc = 16;                      // chunks of 16 columns in all accumulators of a block
+static_assert(kShortSmem >= kLeastTmemBlock && kLongSmem >= kLeastTmemBlock && kLongAcc * kLoraChunk <= kSmTmemColumns / 2 &&
+              kShortAcc * kLoraChunk <= kSmTmemColumns / 2, "blocks that share an SM");
 
 }  // namespace
 
@@ -376,7 +379,7 @@ cudaError_t launch_lora_shrink(const GemmTensorMap& tm_x, const GemmTensorMap& t
   const bool beside = lora_beside(T);
   int chunks = beside ? 4 : 8;
   const int smem = beside ? kShortSmem : kLongSmem;
-  const int acc_chunks = beside ? 8 : 16;              // of 16 columns in all accumulators: two blocks share an SM's tensor memory
+  const int acc_chunks = beside ? kShortAcc : kLongAcc;
   const int x_stage = T < kRows ? (T + box - 1) / box * box * 128 : kXStage;
   const int tiles = (T + kRows - 1) / kRows, steps = (K + 63) / 64;
   // passes a tile can need

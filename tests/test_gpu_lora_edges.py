@@ -136,3 +136,26 @@ def test_fp32_long_sums_with_adapters_over_wide_outputs():
         assert ((got - y).norm() / y.norm()).item() <= EXACT + EXACT_ADAPTERS
         for _ in range(5):
             assert torch.equal(c.layer.run(x, ids).double(), got)
+
+
+@pytest.mark.parametrize("pair", [(0, 1), (0, 2), (1, 3), (2, 3), (1, 2), (0, 1, 2, 3)])
+def test_plans_side_by_side(pair):
+    # several plans on a stream each: blocks of different plans share SMs, shared and tensor memory; every result is the one
+    # the plan gives alone
+    shapes = [(64, 2048, 4096, (64, 16, 32) * 4, "bf16"), (100, 2048, 1024, (16,) * 8, "fp32"), (600, 1024, 2048, (32,) * 6, "bf16"),
+              (2048, 1024, 1024, (64, 8), "fp32")]
+    plans = []
+    for i in pair:
+        T, K, N, ranks, out = shapes[i]
+        c = Case(K, N, ranks=ranks, max_tokens=T, out=out, seed=10 * i)
+        x, ids = rand((T, K), i), ids_of(T, len(ranks), i)
+        plans.append((c, x, ids, c.check(x, ids), torch.cuda.Stream(), []))
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for c, x, ids, want, stream, got in plans:
+            got.append(c.layer.run(x, ids, stream=stream))
+    torch.cuda.synchronize()
+    for c, x, ids, want, stream, got in plans:
+        assert c.layer.status() == 0
+        for y in got:
+            assert torch.equal(y, want)
