@@ -38,7 +38,7 @@ class MoEBlock:
         self.logits = empty(max_tokens, E, dtype=torch.float32)
         self.ids = empty(max_tokens, top_k, dtype=torch.int32)
         self.weights = empty(max_tokens, top_k, dtype=torch.float32)
-        self.done, self.last_stream = torch.cuda.Event(), None       # the end of the last call, where it ran
+        self.done = torch.cuda.Event()                       # the end of the last call
         self.codes = self.scales = None
         if dtype != cep.CEP_BF16:
             self.codes = empty(max_tokens, H, dtype=torch.float8_e4m3fn)
@@ -73,12 +73,10 @@ class MoEBlock:
         if attention.shape[0] == 0:                          # (empty tensors have no address, which the layer's calls refuse)
             return out
         stream = torch.cuda.current_stream(attention.device)
-        if self.last_stream is not None and self.last_stream != stream:
-            stream.wait_event(self.done)
+        stream.wait_event(self.done)                         # (before the first call: nothing to wait for)
         for _, call in self.steps(attention, residual, adapter_ids, out, n_chunks):
             call()
         self.done.record(stream)
-        self.last_stream = stream
         return out
 
     def close(self):

@@ -18,7 +18,7 @@ struct cep_lora_plan {
   int32_t* ids; int32_t* n_chunks; int32_t* chunks;
   float* s;
   // The plan's last enqueued work.  Work on another stream waits for it: the workspace and the bank are shared.
-  cudaEvent_t last; cudaStream_t last_stream; bool have_last;
+  cudaEvent_t last; unsigned long long last_stream; bool have_last;    // (by id: a handle can come back as another stream's)
 };
 
 namespace {
@@ -81,7 +81,9 @@ int enter(cep_lora_plan* p, cudaStream_t s, bool* capturing) {
   e = cudaStreamIsCapturing(s, &st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: cudaStreamIsCapturing failed: %s", cudaGetErrorString(e));
   *capturing = st != cudaStreamCaptureStatusNone;
-  if (!*capturing && p->have_last && p->last_stream != s) {
+  unsigned long long id = 0;
+  if (!*capturing && (e = cudaStreamGetId(s, &id)) != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: cudaStreamGetId failed: %s", cudaGetErrorString(e));
+  if (!*capturing && p->have_last && p->last_stream != id) {
     e = cudaStreamWaitEvent(s, p->last, 0);
     if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: cudaStreamWaitEvent failed: %s", cudaGetErrorString(e));
   }
@@ -90,8 +92,9 @@ int enter(cep_lora_plan* p, cudaStream_t s, bool* capturing) {
 int leave(cep_lora_plan* p, cudaStream_t s, bool capturing) {
   if (capturing) return CEP_OK;
   cudaError_t e = cudaEventRecord(p->last, s);
+  if (e == cudaSuccess) e = cudaStreamGetId(s, &p->last_stream);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "lora: cudaEventRecord failed: %s", cudaGetErrorString(e));
-  p->last_stream = s; p->have_last = true;
+  p->have_last = true;
   return CEP_OK;
 }
 

@@ -159,3 +159,26 @@ def test_plans_side_by_side(pair):
         assert c.layer.status() == 0
         for y in got:
             assert torch.equal(y, want)
+
+
+def test_streams_that_come_and_go():
+    # the driver may give a new stream the handle of one that was destroyed with work under way: still another stream
+    import ctypes
+    cudart = ctypes.CDLL(next(l.split()[-1] for l in open("/proc/self/maps") if "libcudart" in l))
+    c = Case(2048, 2048, ranks=(16, 32), max_tokens=600)
+    x, ids = [rand((600, 2048), s) for s in (1, 2)], [ids_of(600, 2, s) for s in (3, 4)]
+    want = [c.check(x[i], ids[i]) for i in range(2)]
+    outs = [torch.empty_like(want[0]) for _ in range(40)]
+    torch.cuda.synchronize()
+    seen = set()
+    for i, out in enumerate(outs):
+        handle = ctypes.c_void_p()
+        assert cudart.cudaStreamCreateWithFlags(ctypes.byref(handle), 1) == 0
+        seen.add(handle.value)
+        cep.lora_project(c.layer.plan, x[i % 2], ids[i % 2], out, stream=handle.value)
+        assert cudart.cudaStreamDestroy(handle) == 0
+    torch.cuda.synchronize()
+    assert c.layer.status() == 0
+    for i, out in enumerate(outs):
+        assert torch.equal(out, want[i % 2]), (i, len(seen))
+    print("%d handles" % len(seen))
