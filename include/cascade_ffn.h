@@ -253,7 +253,8 @@ typedef struct {
  *                 (CEP_FP8_E4M3_BLOCK128); or uint8 ue8m0 [T, ceil(H/32)], the smallest power of two that brings the
  *                 block's largest magnitude to <= 448 (CEP_MXFP4_E4M3).  The last block of a row may be short.
  * codes are taken from the unrounded y.  A row that holds a NaN or an infinity comes out as NaN (infinite h) or all
- * NaN codes; a sum of squares beyond the fp32 range counts as infinite.  Other than the two exact aliases named above,
+ * NaN codes; a sum of squares beyond the fp32 range counts as infinite, and so does a product h * weight, which is formed
+ * before the division by the root.  Other than the two exact aliases named above,
  * outputs may not overlap inputs.  Rows that all start on 16-byte boundaries with H a multiple of 8 take the wide path.
  * Enqueued on `stream`.
  */
