@@ -566,7 +566,8 @@ class LoRAProjection:
     workspace and adapter bank of one plan, and keeps the weight alive.
 
     weight bf16 [N,K] (the layout of a linear layer's weight), used in place.  ``load_adapter`` fills a slot; ``run``
-    takes the slot of every token.  max_adapters = 0 gives the plain projection (with out_elem=CEP_ELEM_FP32 the
+    takes the slot of every token.  The weight's device has to be the current one, here and in every call.  max_adapters = 0
+    gives the plain projection (with out_elem=CEP_ELEM_FP32 the
     router's logits).
     """
 

@@ -4,7 +4,7 @@
 // The work is 2 T r K operations against 2 T K bytes of x: at most r operations per byte, so memory (long batches) or
 // latency (a few tokens) bounds it.  A block takes 128 consecutive tokens as the M side of a matrix product whose N side is
 // the rows of every adapter among them, 16 ranks at a time: x is read once however many adapters the tokens have (up to
-// 64 or 128 ranks a pass; more take further passes), and of the product each token keeps the columns of its own adapter.
+// 64 or 128 ranks a pass, for fp32 outputs and a long K fewer; more take further passes), and of the product each token keeps the columns of its own adapter.
 // Operands come by TMA, accumulators are fp32 in tensor memory.  While there are few token tiles, K is split over the CTAs
 // of a cluster, which add their partial sums in order through shared memory, so results do not depend on timing.
 //
