@@ -94,14 +94,15 @@ __device__ __forceinline__ void add_splits(uint32_t base, int splits, int first,
 }
 
 // Grid (column tiles, K splits, token tiles of `tok`).  npad: token columns of the MMA, a multiple of 16.  chains: accumulation
-// chains that share the CTA's K steps, in turn in n_acc accumulators of npad columns.
-template <typename OT>
+// chains that share the CTA's K steps, in turn in n_acc accumulators of npad columns.  kEmpty: more chains than accumulators;
+// the epilogue's warps then carry sums beside their rows of s, and with those registers the block would leave no room for one of
+// the down projection (128 tokens of 7168 -> 2048 with eight adapters 30.7 us, without 25.0), so that is a kernel of its own.
+template <typename OT, bool kEmpty>
 __global__ void __launch_bounds__(kSmallThreads, 1)
 project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
                      const __grid_constant__ CUtensorMap tm_up, int T, int N, int num_kb, int tok, int npad, int stages, int n_acc, int chains, int tmem_cols, const LoraArgs la,
                      OT* __restrict__ y, int64_t y_stride, int vec_ok, int32_t* __restrict__ status) {
   constexpr int kStep = UpStep<OT>::kChunks, kTerms = UpStep<OT>::kTerms;
-  constexpr bool kF32 = sizeof(OT) == 4;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const int x_stage = npad * kKBytes, stage_bytes = kWStage + x_stage;
@@ -193,7 +194,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
         tc_fence_after();
         if (kb == chain_end) {
           ++chain; chain_end = kb0 + (int)((long long)(kb1 - kb0) * (chain + 1) / chains); first = 1;
-          if (++acc == n_acc) {                          // all in use
+          if (++acc == n_acc && kEmpty) {                // all in use
             acc = 0;
             tc_commit(smem_u32(&bars->acc_full));
             if (!mbar_wait(smem_u32(&bars->acc_empty), emptied, abort_flag, status)) { ok = false; break; }
@@ -241,34 +242,35 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     const int cols = min(tok, T - t0);                 // token columns that exist
     const uint32_t taddr = tmem + ((uint32_t)(lane_grp * 32) << 16);
     bool ok = true;
-    float sum[kF32 ? kMostF32 : 1];                    // fp32: the sum of the chains, a column per token
-    auto add_accumulators = [&](int n) {
+    // Columns c..c+15 of this lane: d = accumulator a, or d += it.
+    auto take_accumulator = [&](int a, int c, float (&d)[16], bool add) {
+      __syncwarp();                                    // the load is warp-collective
+      uint32_t e[16];
+      tc_ld16(taddr + a * npad + c, e);
+      tc_wait_ld();
 #pragma unroll
-      for (int c = 0; c < (kF32 ? kMostF32 : 0); c += 16) {
-        if (c >= cols) break;
-        for (int a = 0; a < n; ++a) {
-          __syncwarp();                                // the load is warp-collective
-          uint32_t d[16];
-          tc_ld16(taddr + a * npad + c, d);
-          tc_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sum[kF32 ? c + i : 0] += __uint_as_float(d[i]);
-        }
-      }
+      for (int i = 0; i < 16; ++i) d[i] = add ? d[i] + __uint_as_float(e[i]) : __uint_as_float(e[i]);
     };
+    constexpr int kSums = kEmpty ? kMostF32 / 16 : 1;
+    float sum[kSums][16];                              // kEmpty: the sum of the chains before the last accumulators'
     uint32_t full = 0;
     int left = chains;                                 // not yet added
     if (!la.has && tid == 0) pdl_release();
-    if constexpr (kF32) {
+    if constexpr (kEmpty) {
 #pragma unroll
-      for (int c = 0; c < kMostF32; ++c) sum[c] = 0.f;
+      for (int q = 0; q < kSums; ++q)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[q][i] = 0.f;
       for (; left > n_acc; left -= n_acc) {
         ok = ok && mbar_wait_relaxed(smem_u32(&bars->acc_full), full, abort_flag, status);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         full ^= 1u;
         tc_fence_after();
-        add_accumulators(n_acc);
+#pragma unroll
+        for (int q = 0; q < kSums; ++q)
+          if (q * 16 < cols)
+            for (int a = 0; a < n_acc; ++a) take_accumulator(a, q * 16, sum[q], true);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars->acc_empty));
@@ -281,7 +283,7 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
       const int cap = tok * kLoraMaxChunks;
       int2 e = list_step<kStep>(list, (split + lane * splits) * kStep, cap);      // lane i: the i-th of the next 32 steps
       const int total = __ldcg(la.n_chunks + blockIdx.z);
-      SRow<4, kTerms> row;
+      SRow<kEmpty ? 1 : 4, kTerms> row;
       row.fetch(la, tid < npad && t0 + tid < T ? t0 + tid : -1);
       int stage = (kb1 - kb0) % stages;                // where the K steps end
       uint32_t phase = 0;                              // one parity bit per stage
@@ -314,21 +316,19 @@ project_small_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_cons
     float* mine = reinterpret_cast<float*>(smem) + lane_grp * 32 + lane;       // [token][128] sums, in the ring: every load has been consumed
     if (all) {
       tc_fence_after();
-      if constexpr (kF32) {
-        add_accumulators(left);
+      auto finish = [&](int c, float (&d)[16]) {
+        take_accumulator(0, c, d, kEmpty);
+        for (int a = 1; a < left; ++a) take_accumulator(a, c, d, true);
 #pragma unroll
-        for (int c = 0; c < kMostF32; ++c)
-          if (c < cols) mine[c * 128] = sum[c];
+        for (int i = 0; i < 16; ++i)
+          if (c + i < cols) mine[(c + i) * 128] = d[i];
+      };
+      if constexpr (kEmpty) {
+#pragma unroll
+        for (int q = 0; q < kSums; ++q)
+          if (q * 16 < cols) finish(q * 16, sum[q]);
       } else {
-        for (int c = 0; c < cols; c += 16) {
-          __syncwarp();                                // the load is warp-collective
-          uint32_t d[16];
-          tc_ld16(taddr + c, d);
-          tc_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (c + i < cols) mine[(c + i) * 128] = __uint_as_float(d[i]);
-        }
+        for (int c = 0; c < cols; c += 16) finish(c, sum[0]);
       }
     }
   }
@@ -387,8 +387,9 @@ cudaError_t project_small_setup(int dev) {
   if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
   int* clusters = g_clusters[dev];
   if (clusters[0]) return cudaSuccess;
-  cudaError_t e = cudaFuncSetAttribute(project_small_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(project_small_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
+  cudaError_t e = cudaFuncSetAttribute(project_small_kernel<__nv_bfloat16, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(project_small_kernel<float, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(project_small_kernel<float, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallRing + 2048);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
@@ -398,7 +399,7 @@ cudaError_t project_small_setup(int dev) {
   for (int c = 1; c <= kMaxSplits; ++c) {
     attr[0].val.clusterDim.y = (unsigned)c;
     cfg.gridDim = dim3(kSms, c, 1);
-    e = cudaOccupancyMaxActiveClusters(&clusters[c], project_small_kernel<__nv_bfloat16>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&clusters[c], project_small_kernel<__nv_bfloat16, false>, &cfg);
     if (e != cudaSuccess) return e;
   }
   clusters[0] = 1;
@@ -456,9 +457,9 @@ cudaError_t launch_project_small(const ProjectArgs& a, const GemmTensorMap& tm_w
   const CUtensorMap& u = reinterpret_cast<const CUtensorMap&>(tm_up);
   const LoraArgs la = lora_args(a);
   if (a.out_f32)
-    return cudaLaunchKernelEx(&cfg, project_small_kernel<float>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, chains, tmem_cols, la, (float*)a.y, a.y_stride,
+    return cudaLaunchKernelEx(&cfg, chains > n_acc ? project_small_kernel<float, true> : project_small_kernel<float, false>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, chains, tmem_cols, la, (float*)a.y, a.y_stride,
                               vec_ok, a.status);
-  return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, chains, tmem_cols, la,
+  return cudaLaunchKernelEx(&cfg, project_small_kernel<__nv_bfloat16, false>, w, x, u, a.T, a.N, p.num_kb, p.tok, p.npad, stages, n_acc, chains, tmem_cols, la,
                             (__nv_bfloat16*)a.y, a.y_stride, vec_ok, a.status);
 }
 
