@@ -98,7 +98,8 @@ typedef enum {
 /* Element type of a plain (unquantised) tensor. */
 typedef enum {
   CEP_ELEM_BF16 = 0,
-  CEP_ELEM_FP32 = 1
+  CEP_ELEM_FP32 = 1,
+  CEP_ELEM_E4M3 = 2            /* key and value caches only                                     */
 } cep_elem;
 
 #define CEP_MAX_CHUNKS_PER_INVOCATION 32   /* a batch is launched early when it holds this many */
@@ -317,6 +318,122 @@ CEP_API int lora_project(cep_lora_plan* plan, const void* x, int64_t x_stride, i
 CEP_API int lora_status(cep_lora_plan* plan);
 CEP_API int lora_plan_destroy(cep_lora_plan* plan);
 
+/* Sizes and strides (in elements) of attn_append.  The strides of a cache: page, position in the page, kv head. */
+typedef struct {
+  int32_t n_tokens;            /* T >= 0; 0 does nothing                                        */
+  int32_t n_heads;             /* heads of q; 0: q is not given                                 */
+  int32_t n_kv_heads;
+  int32_t head_dim;            /* D, even, 2..1024                                              */
+  int32_t rotary_dim;          /* R, even, 0..D: the columns that are rotated                   */
+  int32_t interleaved;         /* 0: column i turns with i + R/2; 1: 2i with 2i + 1             */
+  int32_t cache_elem;          /* CEP_ELEM_BF16 or CEP_ELEM_E4M3                                */
+  int32_t page_size;           /* positions per page, a power of two                            */
+  int64_t n_pages;
+  int64_t q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int64_t k_cache_stride[3], v_cache_stride[3];
+} cep_append_desc;
+
+/*
+ * New tokens on their way into attention: the heads of q and k are rotated by their tokens' positions, k and v are written
+ * to their places in a paged cache.  Needs no plan.  With angle = position * inv_freq[i], for the pair (a, b) of columns i:
+ *   a' = a cos(angle) - b sin(angle);   b' = a sin(angle) + b cos(angle);   columns from R on are copied
+ * in fp32 (the angle's whole turns are taken off in fp64, so far positions are as exact as near ones), rounded once.
+ *   q             [device] bf16 [T, n_heads, D] or NULL;  k, v [device] bf16 [T, n_kv_heads, D]
+ *   positions     [device] int32 [T]
+ *   slots         [device] int64 [T] page * page_size + position in the page; -1: k and v of the token are not written
+ *   inv_freq      [device] fp32 [R/2]
+ *   q_out         [device] out bf16 [T, n_heads, D]; may be q itself
+ *   k_cache, v_cache  [device] bf16 or e4m3 [n_pages, page_size, n_kv_heads, D]; nothing but the slots is written
+ *   k_scale, v_scale  [device] fp32 [n_kv_heads] or NULL (all ones): codes are x / scale, to nearest even, saturating
+ *                 (CEP_ELEM_E4M3 only)
+ *   status        [device] int32 or NULL: set to 1 where a slot other than -1 lies outside the cache (it is not written);
+ *                 never cleared
+ * The slots of one call are distinct (which token's values a slot named twice ends up with is open).  Heads that all start
+ * on 16-byte boundaries (8 in an e4m3 cache) with D - R a multiple of 8 and R one of 16 take the wide path.
+ * Enqueued on `stream`.
+ */
+CEP_API int attn_append(const cep_append_desc* desc, const void* q, const void* k, const void* v, const int32_t* positions, const int64_t* slots,
+                        const float* inv_freq, void* q_out, void* k_cache, void* v_cache, const float* k_scale, const float* v_scale,
+                        int32_t* status, void* stream);
+
+/*
+ * Attention of a batch of sequences, many of which begin with the same keys (a system prompt, a tool description):
+ *   out[t, h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q[t, h] . k_j)
+ * over the prefix of the sequence's group, then the sequence's own keys (causal: up to the token itself).  The new tokens'
+ * keys are in the cache already (attn_append).  A prefix is read once for all of a group's short sequences together.
+ */
+typedef struct cep_attn_plan cep_attn_plan;
+
+typedef struct {
+  int32_t n_heads;             /* a multiple of n_kv_heads: heads h * n_heads / n_kv_heads ... share kv head h; at most 128 each */
+  int32_t n_kv_heads;
+  int32_t head_dim;            /* D, up to 128; multiple of 8 (e4m3 caches: 16)                 */
+  int32_t page_size;           /* 16, 32, 64, 128 or 256                                        */
+  int32_t n_pages;
+  int32_t cache_elem;          /* CEP_ELEM_BF16 or CEP_ELEM_E4M3                                */
+  int32_t max_tokens;          /* upper bound on tokens per call                                */
+  int32_t max_seqs;            /* on sequences, 1..1024                                         */
+  int32_t max_prefixes;        /* on groups, 0..256                                             */
+  float scale;                 /* > 0                                                           */
+  int64_t k_stride[3], v_stride[3];   /* page, position, head; in elements, multiples of 16 bytes */
+} cep_attn_config;
+
+/* One call's sizes and strides (in elements). */
+typedef struct {
+  int32_t n_tokens;            /* T, rows of q and out                                          */
+  int32_t n_seqs;              /* B                                                             */
+  int32_t n_prefixes;          /* G                                                             */
+  int32_t causal;              /* 0: every token sees all kv_len own keys                       */
+  int32_t table_width, prefix_width;          /* pages per row of page_table, prefix_pages      */
+  int64_t table_stride, prefix_stride;
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride, lse_token_stride;
+} cep_attn_batch;
+
+/* Bytes of device workspace.  [host] out. */
+CEP_API int attn_plan_workspace_bytes(const cep_attn_config* cfg, size_t* bytes);
+
+/*
+ * `k_cache`, `v_cache` [device] [n_pages, page_size, n_kv_heads, D], 16-byte aligned; `k_scale`, `v_scale` [device] fp32
+ * [n_kv_heads], positive, or NULL (all ones): a key is its stored value times its head's scale.  `workspace` [device], 256-byte
+ * aligned.  All stay owned by the caller and must outlive the plan.  Must be called with the target device current (memory of
+ * another device is refused); clears the status word on `stream`, which may not be under capture (CEP_ERR_STATE).  A plan is
+ * not thread-safe.  Its calls may go to different streams: each waits for the plan's previous work (inside a stream capture
+ * the caller orders; graphs of one plan share its workspace and may not run at the same time).
+ */
+CEP_API int attn_plan(const cep_attn_config* cfg, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                      void* workspace, size_t workspace_bytes, void* stream, cep_attn_plan** out);
+
+/*
+ *   q             [device] bf16 [T, n_heads, D]; heads on 16-byte boundaries
+ *   q_start       [device] int32 [B+1] first token of each sequence, never falling; tokens outside q_start[0]..q_start[B] are
+ *                 left as they are in out and lse
+ *   kv_len        [device] int32 [B] own keys, the new tokens' among them: token i of n stands at own position kv_len - n + i
+ *   page_table    [device] int32 [B, table_width] pages of each sequence's own keys
+ *   prefix_start  [device] int32 [G+1] first sequence of each group, never falling; sequences outside prefix_start[0]..
+ *                 prefix_start[G] have no prefix.  NULL: one group of all sequences (G <= 1)
+ *   prefix_len    [device] int32 [G] keys of each group's prefix
+ *   prefix_pages  [device] int32 [G, prefix_width]
+ *   out           [device] out bf16 [T, n_heads, D]; may not overlap q
+ *   lse           [device] out fp32 [T, n_heads] or NULL: log of the sum of exp(scale q.k) (natural)
+ * A token that sees no key gets zeros and -infinity.  What lies behind the last key in a page is not looked at, and may be
+ * anything; a key or value that is not finite reaches the tokens that see it and, where one of these belongs to the same
+ * sequence and call, may reach the sequence's earlier tokens of the call.  fp32 from the products on; weights enter the product with V as bf16,
+ * out is rounded once.  Results do not depend on timing.  All lengths are read on the device: a captured call replays with
+ * other lengths (within n_tokens, n_seqs).  What does not fit is cut to what does and reported by attn_status.
+ * Enqueued on `stream`.
+ */
+CEP_API int attn_prefix(cep_attn_plan* plan, const cep_attn_batch* batch, const void* q, const int32_t* q_start, const int32_t* kv_len,
+                        const int32_t* page_table, const int32_t* prefix_start, const int32_t* prefix_len, const int32_t* prefix_pages,
+                        void* out, float* lse, void* stream);
+
+/* Waits for the plan's work and returns what its kernels reported since the last call of this function: CEP_OK,
+ * CEP_ERR_DEVICE_TIMEOUT, CEP_ERR_CAPACITY (a start that falls or a length that the call has no room for) or
+ * CEP_ERR_BAD_ROUTING (a page outside the cache; its keys and values counted as zeros).  Calls that were captured and replayed
+ * are not waited for: the caller synchronises with a replay first.  Off the hot path. */
+CEP_API int attn_status(cep_attn_plan* plan);
+CEP_API int attn_plan_destroy(cep_attn_plan* plan);
+
 /*
  * A replica's routed tokens have arrived (Section 3.2: per-replica completion signal).
  *   chunk_id       0..n_chunks_expected-1, each exactly once, any order
@@ -512,6 +629,16 @@ CEP_API int cep_debug_wait_timeout(cep_plan* plan, int32_t limit_ms, void* strea
  * n_damaged [host out] = number of gaps that changed; 0 means no kernel wrote past the end of a region.
  */
 CEP_API int cep_debug_check_guards(cep_plan* plan, int32_t* n_damaged);
+/*
+ * Host-only: how attn_prefix cuts a batch with these [host] lengths into shares for n_ctas CTAs.  parts [host out, max_parts
+ * rows of 12]: CTA, kind (0 a group's prefix, 1 a short sequence's own keys, 2 both), sequence or -1, group or -1, kv head,
+ * first token (of the group's short ones, or of the sequence), tokens, first step, step behind the last, steps of the item,
+ * first partial row (-1: the rows are final), cost of the item.  part_rows: rows that the workspace has.  Returns the number
+ * of parts, or a negative cep_status.
+ */
+CEP_API int cep_debug_attn_schedule(const cep_attn_config* cfg, int32_t n_tokens, int32_t n_seqs, int32_t n_prefixes, int32_t causal, int32_t n_ctas,
+                                    const int32_t* q_start, const int32_t* kv_len, const int32_t* prefix_start, const int32_t* prefix_len,
+                                    int64_t* parts, int32_t max_parts, int64_t* part_rows);
 CEP_API int cep_debug_schedule(const int64_t* pairs, int32_t n_chunks, int32_t mode, int64_t theta,
                        int32_t* invocation_of_chunk);
 

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libcascade_ffn.so")
 
 CEP_BF16, CEP_FP8_E4M3_BLOCK128, CEP_MXFP4_E4M3 = 0, 1, 2
 DTYPE_OF = {"bf16": CEP_BF16, "fp8": CEP_FP8_E4M3_BLOCK128, "mxfp4": CEP_MXFP4_E4M3}   # workload dtype names
-CEP_ELEM_BF16, CEP_ELEM_FP32 = 0, 1
+CEP_ELEM_BF16, CEP_ELEM_FP32, CEP_ELEM_E4M3 = 0, 1, 2
 CEP_MODE_SYNC, CEP_MODE_ASYNC, CEP_MODE_STREAMFFN = 0, 1, 2
 CEP_GEMM_TCGEN05, CEP_GEMM_SIMT, CEP_GEMM_TCGEN05_1CTA = 0, 1, 2
 STATUS_NAMES = {0: "CEP_OK", -1: "CEP_ERR_ARG", -2: "CEP_ERR_STATE", -3: "CEP_ERR_WORKSPACE",
@@ -29,7 +29,8 @@ EXPORTS = ["moe_plan_workspace_bytes", "moe_packed_weight_bytes", "moe_plan", "m
            "cep_debug_decode_tile", "cep_debug_schedule", "layout_indices_noalloc", "cep_debug_wait_timeout", "ffn_set_addend", "moe_route", "cep_debug_check_guards", "ffn_wait_invocation",
            "ffn_set_active_streams", "cep_calibrate", "ffn_query_call", "cep_calibrate_routed", "moe_norm",
            "lora_plan_workspace_bytes", "lora_bank_bytes", "lora_plan", "lora_load_adapter", "lora_project", "lora_status",
-           "lora_plan_destroy"]
+           "lora_plan_destroy", "attn_append", "attn_plan_workspace_bytes", "attn_plan", "attn_prefix", "attn_status", "attn_plan_destroy",
+           "cep_debug_attn_schedule"]
 
 
 class CepConfig(ctypes.Structure):
@@ -52,6 +53,25 @@ class NormDesc(ctypes.Structure):
 class LoraConfig(ctypes.Structure):
     _fields_ = [("in_features", ctypes.c_int32), ("out_features", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
                 ("max_adapters", ctypes.c_int32), ("max_rank", ctypes.c_int32), ("out_elem", ctypes.c_int32)]
+
+
+class AppendDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_tokens", "n_heads", "n_kv_heads", "head_dim", "rotary_dim", "interleaved", "cache_elem", "page_size")] + \
+               [(n, ctypes.c_int64) for n in ("n_pages", "q_token_stride", "q_head_stride", "q_out_token_stride", "q_out_head_stride", "k_token_stride",
+                                              "k_head_stride", "v_token_stride", "v_head_stride")] + \
+               [("k_cache_stride", ctypes.c_int64 * 3), ("v_cache_stride", ctypes.c_int64 * 3)]
+
+
+class AttnConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "cache_elem", "max_tokens", "max_seqs",
+                                              "max_prefixes")] + \
+               [("scale", ctypes.c_float), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+
+
+class AttnBatch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_tokens", "n_seqs", "n_prefixes", "causal", "table_width", "prefix_width")] + \
+               [(n, ctypes.c_int64) for n in ("table_stride", "prefix_stride", "q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride",
+                                              "lse_token_stride")]
 
 
 class InvocationInfo(ctypes.Structure):
@@ -137,6 +157,13 @@ def load_library(build_if_missing: bool = True):
         "lora_project": (ctypes.c_int, [vp, vp, i64, i32, vp, vp, i64, vp]),
         "lora_status": (ctypes.c_int, [vp]),
         "lora_plan_destroy": (ctypes.c_int, [vp]),
+        "attn_append": (ctypes.c_int, [vp] * 14),
+        "attn_plan_workspace_bytes": (ctypes.c_int, [vp, ctypes.POINTER(sz)]),
+        "attn_plan": (ctypes.c_int, [vp, vp, vp, vp, vp, vp, sz, vp, ctypes.POINTER(vp)]),
+        "attn_prefix": (ctypes.c_int, [vp] * 12),
+        "attn_status": (ctypes.c_int, [vp]),
+        "attn_plan_destroy": (ctypes.c_int, [vp]),
+        "cep_debug_attn_schedule": (ctypes.c_int, [vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp]),
         "layout_indices_noalloc": (ctypes.c_int, [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -362,6 +389,137 @@ def lora_status(plan) -> int:
 
 def lora_plan_destroy(plan):
     _check(lib().lora_plan_destroy(plan))
+
+
+_APPEND_DESC = struct.Struct("8i15q")                  # AppendDesc, packed in one call
+_ATTN_BATCH = struct.Struct("6i7q")                    # AttnBatch
+
+
+def _heads(t, name, shape, dtype, dev):
+    """(token stride, head stride) of a [T, heads, D] tensor on device `dev` with contiguous heads."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise CepError(-1, "%s must be a %s CUDA tensor %s on the current device" % (name, dtype, list(shape)))
+    st = t.stride()
+    if st[2] != 1:
+        raise CepError(-1, "the heads of %s must be contiguous" % name)
+    return st
+
+
+def _vector(t, name, n, dtype, dev):
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != dev or not t.is_contiguous():
+        raise CepError(-1, "%s must be a contiguous CUDA tensor [%d] of %s on the current device" % (name, n, dtype))
+    return t.data_ptr()
+
+
+def _page_rows(t, name, n, dtype, dev):
+    """(width, row stride) of an int32 [n, width] page table."""
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != n or t.get_device() != dev or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise CepError(-1, "%s must be an int32 CUDA tensor [%d, width] on the current device with contiguous rows" % (name, n))
+    return t.shape[1], t.stride(0)
+
+
+def attn_append(k, v, positions, slots, inv_freq, k_cache, v_cache, q=None, q_out=None, interleaved: bool = False, k_scale=None, v_scale=None,
+                status=None, stream=None):
+    """Rotates the heads of q and k by their tokens' positions and writes k and v to their slots of a paged cache (see the header).
+
+    k, v bf16 [T,Hkv,D]; q bf16 [T,Hq,D] or None; positions int32 [T]; slots int64 [T] (-1: not written); inv_freq fp32 [R/2];
+    k_cache, v_cache bf16 or float8_e4m3fn [pages, page_size, Hkv, D], any strides with contiguous heads; k_scale, v_scale fp32 [Hkv]
+    (e4m3); status int32 [1], set to 1 where a slot lies outside the cache.  Returns the rotated q in q_out (allocated if not given;
+    may be q).  Tensors are recorded on a `stream` that is given."""
+    torch = _torch_module or _torch()
+    dev = torch._C._cuda_getDevice()
+    bf16 = torch.bfloat16
+    if k.dim() != 3 or k_cache.dim() != 4:
+        raise CepError(-1, "k must be [T, heads, D], k_cache [pages, page_size, heads, D]")
+    T, Hk, D = k.shape
+    ks, vs = _heads(k, "k", k.shape, bf16, dev), _heads(v, "v", k.shape, bf16, dev)
+    Hq, qp, op, qs, os_ = 0, None, None, (0, 0), (0, 0)
+    if q is not None:
+        Hq = q.shape[1] if q.dim() == 3 else -1
+        qs = _heads(q, "q", (T, Hq, D), bf16, dev)
+        if q_out is None:
+            if stream is None:
+                q_out = torch.empty((T, Hq, D), dtype=bf16, device=q.device)
+            else:
+                with _allocating_on(stream):
+                    q_out = torch.empty((T, Hq, D), dtype=bf16, device=q.device)
+        os_ = qs if q_out is q else _heads(q_out, "q_out", (T, Hq, D), bf16, dev)
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise CepError(-1, "q_out without q")
+    shape = k_cache.shape
+    e4m3 = k_cache.dtype is torch.float8_e4m3fn
+    if not e4m3 and k_cache.dtype is not bf16:
+        raise CepError(-1, "k_cache has dtype %s" % k_cache.dtype)
+    kcs, vcs = k_cache.stride(), v_cache.stride()
+    if (v_cache.dtype is not k_cache.dtype or v_cache.shape != shape or shape[2] != Hk or shape[3] != D or k_cache.get_device() != dev or
+            v_cache.get_device() != dev or kcs[3] != 1 or vcs[3] != 1):
+        raise CepError(-1, "k_cache and v_cache must be CUDA tensors [pages, page_size, %d, %d] of one type on the current device, with contiguous heads" % (Hk, D))
+    pp, sp = _vector(positions, "positions", T, torch.int32, dev), _vector(slots, "slots", T, torch.int64, dev)
+    fp = _vector(inv_freq, "inv_freq", inv_freq.numel(), torch.float32, dev)
+    kp = None if k_scale is None else _vector(k_scale, "k_scale", Hk, torch.float32, dev)
+    vp = None if v_scale is None else _vector(v_scale, "v_scale", Hk, torch.float32, dev)
+    tp = None if status is None else _vector(status, "status", 1, torch.int32, dev)
+    rc = (_lib or lib()).attn_append(
+        _APPEND_DESC.pack(T, Hq, Hk, D, 2 * inv_freq.shape[0], 1 if interleaved else 0, CEP_ELEM_E4M3 if e4m3 else CEP_ELEM_BF16, shape[1], shape[0], qs[0], qs[1],
+                          os_[0], os_[1], ks[0], ks[1], vs[0], vs[1], kcs[0], kcs[1], kcs[2], vcs[0], vcs[1], vcs[2]),
+        qp, k.data_ptr(), v.data_ptr(), pp, sp, fp, op, k_cache.data_ptr(), v_cache.data_ptr(), kp, vp, tp,
+        torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream_handle(stream))
+    if rc:
+        _check(rc)
+    if stream is not None:
+        _record(stream, q, k, v, positions, slots, inv_freq, q_out, k_cache, v_cache, k_scale, v_scale, status)
+    return q_out
+
+
+def attn_plan_workspace_bytes(cfg: AttnConfig) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().attn_plan_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+    return n.value
+
+
+def attn_plan(cfg: AttnConfig, k_cache, v_cache, k_scale, v_scale, workspace, stream=None) -> int:
+    """All tensors CUDA; workspace torch uint8.  Returns the plan handle."""
+    h = ctypes.c_void_p()
+    _check(lib().attn_plan(ctypes.byref(cfg), k_cache.data_ptr(), v_cache.data_ptr(), _dptr(k_scale), _dptr(v_scale), workspace.data_ptr(), workspace.numel(),
+                           _stream_handle(stream), ctypes.byref(h)))
+    return h.value
+
+
+def attn_prefix(plan, batch: bytes, q, q_start, kv_len, page_table, prefix_start, prefix_len, prefix_pages, out, lse, stream=None):
+    """batch: an AttnBatch or its bytes; the others CUDA tensors (see the header)."""
+    rc = (_lib or lib()).attn_prefix(plan, batch if isinstance(batch, bytes) else ctypes.addressof(batch), q.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),
+                                     page_table.data_ptr(), _dptr(prefix_start), _dptr(prefix_len), _dptr(prefix_pages), out.data_ptr(), _dptr(lse),
+                                     _current_stream() if stream is None else _stream_handle(stream))
+    if rc:
+        _check(rc)
+
+
+def attn_status(plan) -> int:
+    return lib().attn_status(plan)
+
+
+def attn_plan_destroy(plan):
+    _check(lib().attn_plan_destroy(plan))
+
+
+def cep_debug_attn_schedule(cfg: AttnConfig, q_start, kv_len, prefix_start=None, prefix_len=(), causal: bool = True, n_ctas: int = 148):
+    """(parts as dicts, partial rows that the workspace has) of a batch with these host lengths (see the header)."""
+    import numpy as np
+    ints = lambda v: np.ascontiguousarray(v, dtype=np.int32)
+    qs, kl, pl = ints(q_start), ints(kv_len), ints(prefix_len)
+    ps = None if prefix_start is None else ints(prefix_start)
+    ptr = lambda a: None if a is None else a.ctypes.data
+    rows = ctypes.c_int64()
+    call = lambda parts, n: lib().cep_debug_attn_schedule(ctypes.byref(cfg), int(qs[-1]), len(kl), len(pl), int(causal), n_ctas, ptr(qs), ptr(kl), ptr(ps), ptr(pl),
+                                                          parts.ctypes.data, n, ctypes.addressof(rows))
+    n = call(np.zeros((1, 12), np.int64), 0)
+    if n < 0:
+        _check(n)
+    parts = np.zeros((max(n, 1), 12), np.int64)
+    call(parts, n)
+    names = ("cta", "kind", "seq", "group", "head", "token", "tokens", "first", "end", "steps", "row", "cost")
+    return [dict(zip(names, map(int, r))) for r in parts[:n]], rows.value
 
 
 def ffn_submit_chunk(plan, chunk_id: int, token_offset: int, n_tokens: int, tokens, token_scales, topk_ids,
@@ -636,6 +794,100 @@ class LoRAProjection:
     def close(self):
         if getattr(self, "plan", None):
             lora_plan_destroy(self.plan)
+            self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class PrefixAttention:
+    """Attention of batches whose sequences share prefixes, over a paged cache of keys and values that it keeps alive: owns the
+    torch-allocated workspace of one plan.
+
+    k_cache, v_cache bf16 or float8_e4m3fn [pages, page_size, Hkv, D] (any strides with contiguous heads), used in place; k_scale,
+    v_scale fp32 [Hkv] or None (all ones): a key is its stored value times its head's scale; scale: of the scores, 1/sqrt(D) by
+    default.  The caches' device has to be the current one, here and in every call.
+    """
+
+    def __init__(self, k_cache, v_cache, n_heads, max_tokens, max_seqs, max_prefixes=1, k_scale=None, v_scale=None, scale=None, stream=None):
+        import torch
+        dev = torch.cuda.current_device()                # the plan is made for this one
+        shape = k_cache.shape
+        elem = {torch.bfloat16: CEP_ELEM_BF16, torch.float8_e4m3fn: CEP_ELEM_E4M3}.get(k_cache.dtype)
+        if (len(shape) != 4 or elem is None or not k_cache.is_cuda or v_cache.shape != shape or v_cache.dtype != k_cache.dtype or k_cache.stride(3) != 1 or
+                v_cache.stride(3) != 1):
+            raise CepError(-1, "k_cache and v_cache must be bf16 or float8_e4m3fn CUDA tensors [pages, page_size, heads, D] of one shape with contiguous heads")
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t is not None and t.get_device() != dev:
+                raise CepError(-1, "%s is on device %d, device %d is current" % (name, t.get_device(), dev))
+        if getattr(stream, "device", None) is not None and stream.device.index != dev:
+            raise CepError(-1, "the stream is of device %s, device %d is current" % (stream.device.index, dev))
+        pages, page_size, Hk, D = shape
+        for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            if t is not None:
+                _vector(t, name, Hk, torch.float32, dev)
+        self.k_cache, self.v_cache, self.k_scale, self.v_scale = k_cache, v_cache, k_scale, v_scale
+        self.n_heads, self.head_dim, self.device_index = n_heads, D, dev
+        self.cfg = AttnConfig(n_heads, Hk, D, page_size, pages, elem, max_tokens, max_seqs, max_prefixes, D ** -0.5 if scale is None else scale,
+                              (ctypes.c_int64 * 3)(*k_cache.stride()[:3]), (ctypes.c_int64 * 3)(*v_cache.stride()[:3]))
+        nb = attn_plan_workspace_bytes(self.cfg)
+        with _allocating_on(stream):                     # (attn_plan clears the status word on `stream`)
+            self.workspace = torch.empty(nb, dtype=torch.uint8, device=k_cache.device)
+        self.plan = attn_plan(self.cfg, k_cache, v_cache, k_scale, v_scale, self.workspace, stream)
+
+    def run(self, q, q_start, kv_len, page_table, prefix_start=None, prefix_len=None, prefix_pages=None, causal=True, out=None, lse=None, stream=None):
+        """q bf16 [T,Hq,D] (heads may be strided), q_start int32 [B+1], kv_len int32 [B], page_table int32 [B,W]; prefixes: prefix_len
+        int32 [G], prefix_pages int32 [G,Wp], prefix_start int32 [G+1] first sequence of each group (None: one group of all).  Returns out
+        [T,Hq,D] (allocated if not given); lse fp32 [T,Hq] is filled if given.  Tensors are recorded on a `stream` that is given."""
+        torch = _torch()
+        dev, i32 = self.device_index, torch.int32
+        T = q.shape[0]
+        shape = (T, self.n_heads, self.head_dim)
+        qs = _heads(q, "q", shape, torch.bfloat16, dev)
+        B = kv_len.shape[0] if kv_len.dim() == 1 else -1
+        _vector(q_start, "q_start", B + 1, i32, dev)
+        _vector(kv_len, "kv_len", B, i32, dev)
+        G = W2 = s2 = 0
+        if prefix_len is not None:
+            G = prefix_len.numel()
+            _vector(prefix_len, "prefix_len", G, i32, dev)
+            if prefix_pages is None:
+                raise CepError(-1, "prefix_len without prefix_pages")
+            W2, s2 = _page_rows(prefix_pages, "prefix_pages", G, i32, dev)
+            if prefix_start is not None:
+                _vector(prefix_start, "prefix_start", G + 1, i32, dev)
+            elif G > 1:
+                raise CepError(-1, "%d prefixes need prefix_start" % G)
+        elif prefix_start is not None or prefix_pages is not None:
+            raise CepError(-1, "prefix_start or prefix_pages without prefix_len")
+        W, s1 = _page_rows(page_table, "page_table", B, i32, dev)
+        if out is None:
+            if stream is None:
+                out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+            else:
+                with _allocating_on(stream):
+                    out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        os_ = _heads(out, "out", shape, torch.bfloat16, dev)
+        ls = 0
+        if lse is not None:
+            if lse.dtype is not torch.float32 or lse.shape != shape[:2] or lse.get_device() != dev or (self.n_heads > 1 and lse.stride(1) != 1):
+                raise CepError(-1, "lse must be a float32 tensor %s on the caches' device with contiguous rows" % list(shape[:2]))
+            ls = lse.stride(0)
+        attn_prefix(self.plan, _ATTN_BATCH.pack(T, B, G, 1 if causal else 0, W, W2, s1, s2, qs[0], qs[1], os_[0], os_[1], ls), q, q_start, kv_len, page_table,
+                    prefix_start, prefix_len, prefix_pages, out, lse, stream)
+        if stream is not None:
+            _record(stream, q, q_start, kv_len, page_table, prefix_start, prefix_len, prefix_pages, out, lse)
+        return out
+
+    def status(self) -> int:
+        return attn_status(self.plan)
+
+    def close(self):
+        if getattr(self, "plan", None):
+            attn_plan_destroy(self.plan)
             self.plan = None
 
     def __del__(self):
