@@ -631,9 +631,9 @@ CEP_API int cep_debug_wait_timeout(cep_plan* plan, int32_t limit_ms, void* strea
 CEP_API int cep_debug_check_guards(cep_plan* plan, int32_t* n_damaged);
 /*
  * Host-only: how attn_prefix cuts a batch with these [host] lengths into shares for n_ctas CTAs.  parts [host out, max_parts
- * rows of 12]: CTA, kind (0 a group's prefix, 1 a short sequence's own keys, 2 both), sequence or -1, group or -1, kv head,
+ * rows of 13]: CTA, kind (0 a group's prefix, 1 a short sequence's own keys, 2 both), sequence or -1, group or -1, kv head,
  * first token (of the group's short ones, or of the sequence), tokens, first step, step behind the last, steps of the item,
- * first partial row (-1: the rows are final), cost of the item.  part_rows: rows that the workspace has.  Returns the number
+ * first partial row (-1: the rows are final), cost of the item, partial results.  part_rows: rows that the workspace has.  Returns the number
  * of parts, or a negative cep_status.
  */
 CEP_API int cep_debug_attn_schedule(const cep_attn_config* cfg, int32_t n_tokens, int32_t n_seqs, int32_t n_prefixes, int32_t causal, int32_t n_ctas,

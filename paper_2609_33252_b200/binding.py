@@ -513,12 +513,12 @@ def cep_debug_attn_schedule(cfg: AttnConfig, q_start, kv_len, prefix_start=None,
     rows = ctypes.c_int64()
     call = lambda parts, n: lib().cep_debug_attn_schedule(ctypes.byref(cfg), int(qs[-1]), len(kl), len(pl), int(causal), n_ctas, ptr(qs), ptr(kl), ptr(ps), ptr(pl),
                                                           parts.ctypes.data, n, ctypes.addressof(rows))
-    n = call(np.zeros((1, 12), np.int64), 0)
+    n = call(np.zeros((1, 13), np.int64), 0)
     if n < 0:
         _check(n)
-    parts = np.zeros((max(n, 1), 12), np.int64)
+    parts = np.zeros((max(n, 1), 13), np.int64)
     call(parts, n)
-    names = ("cta", "kind", "seq", "group", "head", "token", "tokens", "first", "end", "steps", "row", "cost")
+    names = ("cta", "kind", "seq", "group", "head", "token", "tokens", "first", "end", "steps", "row", "cost", "results")
     return [dict(zip(names, map(int, r))) for r in parts[:n]], rows.value
 
 

@@ -262,8 +262,11 @@ int cep_debug_attn_schedule(const cep_attn_config* c, int32_t n_tokens, int32_t 
     s.group[b] = -1;
     for (int g = 0; g < p.G; ++g) if (s.gfirst[g] <= b && b < s.gfirst[g + 1]) s.group[b] = g;
   }
-  s.scum[0] = 0;
-  for (int b = 0; b < p.B; ++b) s.scum[b + 1] = s.scum[b] + (attn_is_short(p, s, b) ? s.q0[b + 1] - s.q0[b] : 0);
+  s.scum[0] = s.pcum[0] = 0;
+  for (int b = 0; b < p.B; ++b) {
+    s.scum[b + 1] = s.scum[b] + (attn_is_short(p, s, b) ? s.q0[b + 1] - s.q0[b] : 0);
+    s.pcum[b + 1] = s.pcum[b] + (attn_has_rows(p, s, b) ? s.q0[b + 1] - s.q0[b] : 0);
+  }
   s.grt[0] = 0;
   for (int g = 0; g < p.G; ++g) s.grt[g + 1] = s.grt[g] + attn_div_up(s.scum[s.gfirst[g + 1]] - s.scum[s.gfirst[g]], 2 * p.tps);
   s.cost[0] = 0;
@@ -278,10 +281,11 @@ int cep_debug_attn_schedule(const cep_attn_config* c, int32_t n_tokens, int32_t 
       const int s0 = attn_steps_before(k, it.n, x0), s1 = attn_steps_before(k, it.n, x1);
       if (s0 >= s1) continue;
       if (n < max_parts) {
-        int64_t* r = parts + 12ll * n;
+        int64_t* r = parts + 13ll * n;
         r[0] = cta; r[1] = it.kind; r[2] = it.b; r[3] = it.g; r[4] = it.head; r[5] = it.tok; r[6] = it.n_tok; r[7] = s0; r[8] = s1; r[9] = it.n;
-        r[10] = it.kind == kAttnJoint && s0 == 0 && s1 == it.n ? -1 : attn_part_row(it, cta, s0);
+        r[10] = attn_is_whole(it, s0, s1) ? -1 : attn_part_row(it, cta, s0);
         r[11] = k.w;
+        r[12] = attn_part_count(it, s0, s1);
       }
       ++n;
     }

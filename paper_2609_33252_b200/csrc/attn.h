@@ -6,6 +6,9 @@
 //                 row tile instead of once per sequence
 //   own items     a short sequence against its own keys
 //   joint items   a sequence that fills row tiles by itself (or has no one to share with): prefix, then own keys
+// Two row tiles' items occupy both warpgroups of a CTA; items of one row tile are taken by the warpgroups in turn, step by step, so
+// that a CTA's part of such an item leaves up to two partial results.
+//
 // The items lie on one axis of estimated cost, which is cut into equal shares, one per CTA; a cut inside an item falls on a
 // step.  A row whose keys ended up in several places is put together from partial results (sums, maxima) by a second kernel,
 // in the order of the cuts: nothing depends on timing.
@@ -35,11 +38,12 @@ struct AttnShape {
 struct AttnSched {
   int32_t* q0;                               // [B+1] first token of each sequence
   int32_t* kv;                               // [B] own keys
-  int32_t* group;                            // [B] -1: no prefix
   int32_t* scum;                             // [B+1] tokens of short sequences before this one
+  int32_t* pcum;                             // [B+1] tokens of sequences with partial rows of their own before this one
   int32_t* gfirst;                           // [G+1] first sequence of each group
   int32_t* glen;                             // [G] prefix keys
   int32_t* grt;                              // [G+1] group items of a kv head before this group
+  int16_t* group;                            // [B] -1: no prefix
   long long* cost;                           // [G+B+1] cost before each entity (a group or a sequence)
   long long share;                           // of one CTA
 };
@@ -50,15 +54,16 @@ __host__ __device__ inline AttnSched attn_carve(void* base, int B, int G) {
   int32_t* p = reinterpret_cast<int32_t*>(s.cost + G + B + 1);
   s.q0 = p; p += B + 1;
   s.kv = p; p += B;
-  s.group = p; p += B;
   s.scum = p; p += B + 1;
+  s.pcum = p; p += B + 1;
   s.gfirst = p; p += G + 1;
   s.glen = p; p += G;
-  s.grt = p;
+  s.grt = p; p += G + 1;
+  s.group = reinterpret_cast<int16_t*>(p);
   s.share = 0;
   return s;
 }
-__host__ __device__ constexpr int attn_sched_words(int B, int G) { return 2 * (G + B + 1) + (4 * B + 2 + 3 * G + 2 + 1) / 2 * 2; }   // 4-byte words, an even number
+__host__ __device__ constexpr int attn_sched_words(int B, int G) { return 2 * (G + B + 1) + (4 * B + 3 + 3 * G + 2 + (B + 1) / 2 + 1) / 2 * 2; }   // 4-byte words, an even number
 constexpr int kAttnSchedBytes = attn_sched_words(kAttnMaxSeqs, kAttnMaxPrefixes) * 4;
 
 __host__ __device__ inline int attn_div_up(int a, int b) { return (a + b - 1) / b; }
@@ -68,6 +73,9 @@ __host__ __device__ inline bool attn_is_short(const AttnShape& p, const AttnSche
   const int n = s.q0[b + 1] - s.q0[b], g = s.group[b];
   return g >= 0 && n > 0 && n <= 2 * p.tps && s.glen[g] > 0 && s.gfirst[g + 1] - s.gfirst[g] >= 2;
 }
+
+// Sequences of up to two row tiles have partial rows of their own; longer ones use those of the CTAs whose cut goes through them.
+__host__ __device__ inline bool attn_has_rows(const AttnShape& p, const AttnSched& s, int b) { return s.q0[b + 1] - s.q0[b] <= 2 * p.tps; }
 
 // An entity's items per kv head, and what item r (0-based) of them costs: a + slope * (r + 1).
 struct AttnEntity { int items; long long a, slope; };
@@ -153,7 +161,8 @@ enum AttnKind { kAttnGroup = 0, kAttnOwn = 1, kAttnJoint = 2 };
 struct AttnItem {
   int kind, b, g, head;                      // sequence (-1 for a group item), group (-1: none)
   int tok;                                   // first token: among the group's short tokens, or in the sequence
-  int n_tok;                                 // tokens; more than tps: two row tiles
+  int n_tok;                                 // tokens
+  bool dual;                                 // two row tiles (the second may be empty in an entity's last item)
   int ahead, own;                            // prefix keys, own keys that the item's last token sees
   int n_ahead, n;                            // steps over the prefix, all steps
   long long rows;                            // first partial row
@@ -168,17 +177,19 @@ __host__ __device__ inline AttnItem attn_item(const AttnShape& p, const AttnSche
     it.tok = k.r * tile_tokens;
     const int n = s.scum[s.gfirst[k.e + 1]] - s.scum[s.gfirst[k.e]];
     it.n_tok = n - it.tok < tile_tokens ? n - it.tok : tile_tokens;
+    it.dual = n > p.tps;
     it.ahead = s.glen[k.e]; it.own = 0;
     it.rows = ((long long)p.Hkv * s.grt[k.e] + (long long)k.head * k.x.items + k.r) * tile_rows;
   } else {
     it.b = k.e - p.G;
     const int n = s.q0[it.b + 1] - s.q0[it.b], kv = s.kv[it.b];
     it.g = s.group[it.b];
+    it.dual = n > p.tps;
+    it.rows = group_rows + 2ll * s.pcum[it.b] * p.Hq + (attn_has_rows(p, s, it.b) ? 2ll * k.head * n * p.Gh : 0);
     if (attn_is_short(p, s, it.b)) {
       it.kind = kAttnOwn;
       it.tok = 0; it.n_tok = n;
       it.ahead = 0; it.own = kv;
-      it.rows = group_rows + (long long)s.scum[it.b] * p.Hq + (long long)k.head * n * p.Gh;
     } else {
       it.kind = kAttnJoint;
       it.tok = k.r * tile_tokens;
@@ -186,7 +197,6 @@ __host__ __device__ inline AttnItem attn_item(const AttnShape& p, const AttnSche
       it.ahead = it.g >= 0 ? s.glen[it.g] : 0;
       const int seen = p.causal ? kv - n + it.tok + it.n_tok : kv;
       it.own = seen < 0 ? 0 : seen < kv ? seen : kv;
-      it.rows = group_rows + (long long)s.scum[it.b] * p.Hq;
     }
   }
   it.n_ahead = attn_div_up(it.ahead, kAttnTile);
@@ -200,15 +210,19 @@ __host__ __device__ inline int attn_steps_before(const AttnWalk& k, int n, long 
   if (x >= k.at + k.w) return n;
   return (int)(((x - k.at) * n + k.w - 1) / k.w);
 }
-// First partial row of what CTA c has of an item, steps from s0 on.
+// First partial row of what CTA c has of an item, steps from s0 on; and how many partial results that is, tok rows apart.
 __host__ __device__ inline long long attn_part_row(const AttnItem& it, int c, int s0) {
   return it.rows + (long long)c * kAttnSplitRows + (s0 == 0 ? kAttnSplitRows / 2 : 0);
 }
+__host__ __device__ inline int attn_part_count(const AttnItem& it, int s0, int s1) { return it.dual || s1 - s0 == 1 ? 1 : 2; }
+__host__ __device__ inline bool attn_is_whole(const AttnItem& it, int s0, int s1) {
+  return it.kind == kAttnJoint && s1 - s0 == it.n && attn_part_count(it, s0, s1) == 1;
+}
 __host__ __device__ inline long long attn_max_part_rows(int max_tokens, int max_seqs, int max_prefixes, int Hq, int Hkv, int n_ctas) {
   const int Gh = Hq / Hkv, tps = kAttnTile / Gh;
-  long long most = (long long)max_seqs * 2 * tps;                      // tokens of short sequences
+  long long most = (long long)max_seqs * 2 * tps;                      // tokens of sequences with rows of their own
   if (most > max_tokens) most = max_tokens;
-  return most * Hq + (long long)Hkv * (most / (2 * tps) + max_prefixes) * 2 * tps * Gh + (long long)(n_ctas + 1) * kAttnSplitRows;
+  return 2 * most * Hq + (long long)Hkv * (most / (2 * tps) + max_prefixes) * 2 * tps * Gh + (long long)(n_ctas + 1) * kAttnSplitRows;
 }
 
 // The cost that each CTA gets: equal shares, and no less than two steps, which two warpgroups take at the same time.

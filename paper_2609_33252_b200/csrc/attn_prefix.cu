@@ -5,8 +5,9 @@
 // fetched page by page by TMA into a ring that K and V tiles share, S = Q K^T and O += P V run on the tensor core with S, P and
 // O in tensor memory (P takes S's place).  Each thread of a warpgroup owns one row of S: maximum and sum need no exchange.
 //   two row tiles: both warpgroups use every key tile, the tensor core works for one while the other takes its exponentials
-//   one row tile (decoding): the warpgroups take the key tiles in turn, with a maximum, sum and O of their own, joined at the
-//     end through shared memory
+//   one row tile (decoding): the warpgroups take the key tiles in turn, with a Q, maximum, sum and O of their own
+// The CTA's items form one stream of key tiles, so that loads, products and row work of neighbouring items overlap; the thread
+// that issues the products serves whichever warpgroup is ready.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -20,7 +21,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kItemWarp = 10, kCodeWarp = 12;     // (kCodeWarp and the next three: e4m3 only)
-constexpr int kItemSlots = 4;
+constexpr int kItemSlots = 8;                               // items between the warp that walks the schedule and the slowest reader
 constexpr int kMaxShared = 227 * 1024;
 constexpr int kHalfBytes = kAttnTile * 128;                 // 128 rows of 64 bf16: what a 128-byte swizzled box column is
 
@@ -32,7 +33,7 @@ template <int DP, bool E4M3> struct Layout {
   static constexpr int tile_bytes = halves * kHalfBytes;    // a K, V or Q tile
   static constexpr int stages = (E4M3 ? 96 : 128) * 1024 / tile_bytes;
   static constexpr int code_bytes = kAttnTile * DP, max_codes = 8;
-  static constexpr int q = 0, ring = 2 * tile_bytes, misc = ring + stages * tile_bytes, codes = misc + 3072, align = 1024;
+  static constexpr int q = 0, ring = 2 * tile_bytes, misc = ring + stages * tile_bytes, codes = misc + 2048, align = 1024;
   // tiles of codes beside a schedule of `words` words: at least two, for the largest
   __host__ __device__ static constexpr int code_slots(int words) {
     return E4M3 ? ((kMaxShared - align - codes - words * 4) / code_bytes < max_codes ? (kMaxShared - align - codes - words * 4) / code_bytes : max_codes) : 0;
@@ -50,45 +51,15 @@ static_assert(layout_ok<64, false>() && layout_ok<128, false>() && layout_ok<64,
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
-        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
                  "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                : "memory");
 }
-// Columns of S at or behind `see` count for nothing.
-__device__ __forceinline__ void hide(uint32_t (&r)[32], int see) {
-  if (see < 32) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) r[i] = i < see ? r[i] : 0xff800000u;
-  }
-}
-// Four e4m3 codes as four bf16.  A code's exponent and mantissa, moved to bf16's places, read as the value times 2^-120 (the
-// exponents' offsets are 7 and 127), subnormals too; NaN is the one code that needs a look.
+// Four e4m3 codes as four fp16, exactly.
 __device__ __forceinline__ void decode4(uint32_t x, uint32_t& lo, uint32_t& hi) {
-  auto two = [](uint32_t h) {                              // codes in the upper bytes of both halves
-    const uint32_t bits = (h & 0x80008000u) | ((h >> 4) & 0x07f007f0u);
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(bits), "r"(0x7b807b80u));      // 2^120
-    return r;
-  };
-  const uint32_t a = __byte_perm(x, 0, 0x1404), b = __byte_perm(x, 0, 0x3424);
-  lo = two(a); hi = two(b);
-  if (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) {
-    if ((a & 0x7f00u) == 0x7f00u) lo |= 0x7fc0u;
-    if ((a & 0x7f000000u) == 0x7f000000u) lo |= 0x7fc00000u;
-    if ((b & 0x7f00u) == 0x7f00u) hi |= 0x7fc0u;
-    if ((b & 0x7f000000u) == 0x7f000000u) hi |= 0x7fc00000u;
-  }
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(x));
 }
 // A from tensor memory (lane = row, two bf16 per 32-bit column), B from shared memory
 __device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -113,81 +84,106 @@ constexpr uint32_t kTransposeB = 1u << 16;           // instruction descriptor: 
 
 
 // ---------------------------------------------------------------- the schedule
-// Exclusive scan of n values over the block with `op`; put(i, before, through); returns the total.
-template <typename V, typename Op, typename Get, typename Put>
-__device__ __forceinline__ V block_scan(int n, V identity, Op op, Get get, Put put, V* warp_totals) {
+// Exclusive scan of n pairs over the block: put(i, before); returns the totals.
+struct Pair { long long a; int b; };
+template <typename Get, typename Put>
+__device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_totals) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
-  V carry = identity;
+  Pair carry{0, 0};
   for (int base = 0; base < n; base += blockDim.x) {
     const int i = base + tid;
-    V v = i < n ? get(i) : identity;
-#pragma unroll
+    Pair v{0, 0};
+    if (i < n) v = get(i);
+    const Pair own = v;
+#pragma unroll 1
     for (int d = 1; d < 32; d <<= 1) {
-      const V o = __shfl_up_sync(0xffffffffu, v, d);
-      if (lane >= d) v = op(o, v);
+      const long long a = __shfl_up_sync(0xffffffffu, v.a, d);
+      const int b = __shfl_up_sync(0xffffffffu, v.b, d);
+      if (lane >= d) { v.a += a; v.b += b; }
     }
     if (lane == 31) warp_totals[warp] = v;
-    V before = __shfl_up_sync(0xffffffffu, v, 1);
-    if (lane == 0) before = identity;
     __syncthreads();
-    V ahead = carry;
-    for (int w = 0; w < warp; ++w) ahead = op(ahead, warp_totals[w]);
-    for (int w = 0; w < n_warps; ++w) carry = op(carry, warp_totals[w]);
-    if (i < n) put(i, op(ahead, before), op(ahead, v));
+    Pair w{0, 0};
+    if (lane < n_warps) w = warp_totals[lane];
+    const Pair ahead = carry;
+    Pair mine = ahead;
+#pragma unroll 1
+    for (int d = 16; d; d >>= 1) {                          // sums over the warps before this one, and over all
+      const long long a = __shfl_xor_sync(0xffffffffu, w.a, d);
+      const int b = __shfl_xor_sync(0xffffffffu, w.b, d);
+      w.a += a; w.b += b;
+    }
+    carry.a += w.a; carry.b += w.b;
+    Pair x{0, 0};
+    if (lane < warp) x = warp_totals[lane];
+#pragma unroll 1
+    for (int d = 16; d; d >>= 1) {
+      const long long a = __shfl_xor_sync(0xffffffffu, x.a, d);
+      const int b = __shfl_xor_sync(0xffffffffu, x.b, d);
+      x.a += a; x.b += b;
+    }
+    mine.a += x.a + v.a - own.a; mine.b += x.b + v.b - own.b;
+    if (i < n) put(i, mine);
     __syncthreads();
   }
   return carry;
 }
 
+// Starts that fall are held at the largest before them (this is not what a correct call needs: one thread).
+__device__ __forceinline__ void never_fall(int32_t* v, int n) {
+  for (int i = 1; i < n; ++i) if (v[i] < v[i - 1]) v[i] = v[i - 1];
+}
+
 // Every CTA computes the whole schedule from the lengths.  What does not fit the call is cut to what does and reported.
-__device__ void build_schedule(const AttnArgs& a, AttnSched& s, long long* scratch) {
+__device__ __forceinline__ void build_schedule(const AttnArgs& a, AttnSched& s, Pair* scratch) {
   const AttnShape& p = a.p;
   const int tid = threadIdx.x, nt = blockDim.x;
-  int bad = 0;
-  auto larger = [](int x, int y) { return x > y ? x : y; };
-  auto clamp = [](int v, int hi) { return v < 0 ? 0 : v > hi ? hi : v; };
-  int* totals = reinterpret_cast<int*>(scratch);
-  // first tokens and first sequences never fall
-  block_scan<int>(p.B + 1, 0, larger, [&](int i) { const int v = a.q_start[i], c = clamp(v, p.T); bad |= v != c; return c; },
-                  [&](int i, int before, int v) { bad |= before > a.q_start[i]; s.q0[i] = v; }, totals);
-  if (p.G)
-    block_scan<int>(p.G + 1, 0, larger, [&](int i) { const int v = a.prefix_start ? a.prefix_start[i] : i ? p.B : 0, c = clamp(v, p.B); bad |= v != c; return c; },
-                    [&](int i, int before, int v) { bad |= a.prefix_start && before > a.prefix_start[i]; s.gfirst[i] = v; }, totals);
-  else if (tid == 0) s.gfirst[0] = 0;
-  for (int g = tid; g < p.G; g += nt) { const int v = a.prefix_len[g]; s.glen[g] = clamp(v, p.prefix_cap); bad |= s.glen[g] != v; }
-  for (int b = tid; b < p.B; b += nt) { const int v = a.kv_len[b]; s.kv[b] = clamp(v, p.own_cap); bad |= s.kv[b] != v; }
-  __syncthreads();
-  for (int b = tid; b < p.B; b += nt) {
-    int g = -1;
-    if (p.G && b >= s.gfirst[0] && b < s.gfirst[p.G]) {                // the last group that starts at or before b
-      int lo = 0, hi = p.G;
-      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s.gfirst[mid] <= b) lo = mid; else hi = mid; }
-      g = lo;
-    }
-    s.group[b] = g;
+  int bad = 0, falls = 0;
+  auto take = [&](int v, int hi) { const int c = v < 0 ? 0 : v > hi ? hi : v; bad |= c != v; return c; };
+  for (int i = tid; i <= p.B; i += nt) {
+    const int v = a.q_start[i];
+    if (i < p.B) { falls |= a.q_start[i + 1] < v; s.kv[i] = take(a.kv_len[i], p.own_cap); }
+    s.q0[i] = take(v, p.T);
   }
+  for (int i = tid; i <= p.G; i += nt) {
+    if (i < p.G) s.glen[i] = take(a.prefix_len[i], p.prefix_cap);
+    if (!a.prefix_start) { s.gfirst[i] = i && p.G ? p.B : 0; continue; }
+    const int v = a.prefix_start[i];
+    if (i < p.G) falls |= a.prefix_start[i + 1] < v;
+    s.gfirst[i] = take(v, p.B);
+  }
+  if (__syncthreads_or(falls)) {
+    bad = 1;
+    if (tid == 0) { never_fall(s.q0, p.B + 1); never_fall(s.gfirst, p.G + 1); }
+    __syncthreads();
+  }
+  const Pair places = block_scan(p.B,
+      [&](int b) {
+        int g = -1;
+        if (b >= s.gfirst[0] && b < s.gfirst[p.G]) {       // the last group that starts at or before b
+          int lo = 0, hi = p.G;
+          while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s.gfirst[mid] <= b) lo = mid; else hi = mid; }
+          g = lo;
+        }
+        s.group[b] = (int16_t)g;
+        const int n = s.q0[b + 1] - s.q0[b];
+        return Pair{attn_has_rows(p, s, b) ? n : 0, attn_is_short(p, s, b) ? n : 0};
+      },
+      [&](int b, const Pair& before) { s.pcum[b] = (int)before.a; s.scum[b] = before.b; }, scratch);
+  if (tid == 0) { s.pcum[p.B] = (int)places.a; s.scum[p.B] = places.b; }
   __syncthreads();
-  auto add = [](int x, int y) { return x + y; };
-  const int n_short = block_scan<int>(p.B, 0, add, [&](int b) { return attn_is_short(p, s, b) ? s.q0[b + 1] - s.q0[b] : 0; },
-                                      [&](int b, int before, int) { s.scum[b] = before; }, totals);
-  if (tid == 0) s.scum[p.B] = n_short;
-  __syncthreads();
-  const int n_tiles = block_scan<int>(p.G, 0, add, [&](int g) { return attn_div_up(s.scum[s.gfirst[g + 1]] - s.scum[s.gfirst[g]], 2 * p.tps); },
-                                      [&](int g, int before, int) { s.grt[g] = before; }, totals);
-  if (tid == 0) s.grt[p.G] = n_tiles;
-  __syncthreads();
-  const long long total = block_scan<long long>(p.G + p.B, 0ll, [](long long x, long long y) { return x + y; },
-      [&](int e) { const AttnEntity x = attn_entity(p, s, e); return p.Hkv * attn_items_cost(x, x.items); },
-      [&](int e, long long before, long long) { s.cost[e] = before; }, scratch);
-  if (tid == 0) s.cost[p.G + p.B] = total;
-  s.share = attn_share(p, total);
+  const Pair total = block_scan(p.G + p.B,
+      [&](int e) { const AttnEntity x = attn_entity(p, s, e); return Pair{p.Hkv * attn_items_cost(x, x.items), e < p.G ? x.items : 0}; },
+      [&](int e, const Pair& before) { s.cost[e] = before.a; if (e < p.G) s.grt[e] = before.b; }, scratch);
+  if (tid == 0) { s.cost[p.G + p.B] = total.a; s.grt[p.G] = total.b; }
+  s.share = attn_share(p, total.a);
   if (bad) atomicExch(&a.status[kStBoundsViolation], 1);
   __syncthreads();
 }
 
-// The sequence among whose short tokens number `i` of all short tokens is.
-__device__ __forceinline__ int short_sequence(const AttnSched& s, int lo, int hi, int i) {
-  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s.scum[mid] <= i) lo = mid; else hi = mid; }
+// The sequence (lo <= b < hi) with before[b] <= i < before[b + 1].
+__device__ __forceinline__ int sequence_of(const int32_t* before, int lo, int hi, int i) {
+  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (before[mid] <= i) lo = mid; else hi = mid; }
   return lo;
 }
 
@@ -199,14 +195,34 @@ struct alignas(16) Work {
   int32_t seen;                              // own keys that the first token sees
   int32_t b, g;
   int32_t lo, hi;                            // group: its sequences
-  int32_t whole;                             // nothing to join: the rows are final
+  int32_t flags;                             // 1: two row tiles; 2: the rows are final
   long long prow;                            // first partial row
 };
 static_assert(sizeof(Work) == 64, "");
+enum { kDual = 1, kWhole = 2 };
 
-// Places in the ring, in the order in which the tensor core needs them: K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
-__device__ __forceinline__ uint32_t pos_k(uint32_t base, int j) { return base + (j ? 2 * j - 1 : 0); }
-__device__ __forceinline__ uint32_t pos_v(uint32_t base, int j, int n) { return base + (j == n - 1 ? 2 * n - 1 : 2 * j + 2); }
+// The CTA's key tiles are numbered through, t = 0, 1, ...  Places in the ring, in the order in which the tensor core needs them:
+// K0 K1 V0 K2 V1 K3 V2 ...
+__device__ __forceinline__ uint32_t pos_k(uint32_t t) { return t ? 2 * t - 1 : 0; }
+__device__ __forceinline__ uint32_t pos_v(uint32_t t) { return 2 * t + 2; }
+// Of an item whose first tile is t0, a warpgroup has all tiles (two row tiles) or those with its parity.
+__device__ __forceinline__ int first_step(uint32_t t0, bool dual, int wg) { return dual ? 0 : (int)((t0 + wg) & 1); }
+
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+
+// Two fp32 values in one 64-bit register pair: one instruction multiplies and adds both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair2(float lo, float hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ void unpair2(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { uint32_t r; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
 
 // ---------------------------------------------------------------- the kernel
 template <int DP, bool E4M3>
@@ -217,13 +233,12 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t sbase = smem_u32(smem);
   const uint32_t bar0 = sbase + L::misc;
-  const uint32_t full = bar0, empty = bar0 + 64, s_full = bar0 + 128, p_ready = bar0 + 144, o_done = bar0 + 160, q_ready = bar0 + 176, rows_meet = bar0 + 184,
-                 w_full = bar0 + 192, w_empty = bar0 + 224, code_full = bar0 + 256, code_empty = bar0 + 320;
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::misc + 384);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::misc + 388);
-  long long* scratch = reinterpret_cast<long long*>(smem + L::misc + 512);             // a block's warps' totals
-  const Work* work = reinterpret_cast<const Work*>(smem + L::misc + 640);
-  float2* exchange = reinterpret_cast<float2*>(smem + L::misc + 1024);                 // [128] maximum and sum of the other warpgroup's rows
+  const uint32_t full = bar0, empty = bar0 + 64, s_full = bar0 + 128, p_ready = bar0 + 144, o_done = bar0 + 160, q_ready = bar0 + 176,
+                 w_full = bar0 + 192, w_empty = bar0 + 256, code_full = bar0 + 320, code_empty = bar0 + 384;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::misc + 448);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::misc + 452);
+  Pair* scratch = reinterpret_cast<Pair*>(smem + L::misc + 512);                       // a block's warps' totals
+  const Work* work = reinterpret_cast<const Work*>(smem + L::misc + 1024);
   const int words = attn_sched_words(a.p.B, a.p.G), n_codes = L::code_slots(words);
   uint8_t* sched_at = smem + L::codes + n_codes * L::code_bytes;
 
@@ -231,10 +246,9 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   if (tid == 0) {
     for (int i = 0; i < L::stages; ++i) { mbar_init(full + 8 * i, E4M3 ? 4 : 1); mbar_init(empty + 8 * i, 1); }
     for (int i = 0; i < n_codes; ++i) { mbar_init(code_full + 8 * i, 1); mbar_init(code_empty + 8 * i, 4); }
-    for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(o_done + 8 * i, 1); }
-    mbar_init(q_ready, 8);
-    mbar_init(rows_meet, 8);
-    for (int i = 0; i < kItemSlots; ++i) { mbar_init(w_full + 8 * i, 1); mbar_init(w_empty + 8 * i, E4M3 ? 14 : 10); }
+    for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(o_done + 8 * i, 1); mbar_init(q_ready + 8 * i, 4); }
+    // readers of an item: the loading warp, the products of each warpgroup, eight row warps, four decoding warps
+    for (int i = 0; i < kItemSlots; ++i) { mbar_init(w_full + 8 * i, 1); mbar_init(w_empty + 8 * i, E4M3 ? 15 : 11); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -252,15 +266,9 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   const AttnShape& p = a.p;
   AttnSched s = attn_carve(sched_at, p.B, p.G);
   build_schedule(a, s, scratch);
-  if (blockIdx.x == 0) {                                    // for the kernel that joins partial results
-    int32_t* dst = static_cast<int32_t*>(a.sched);
-    const int32_t* src = reinterpret_cast<const int32_t*>(sched_at);
-    for (int i = tid; i < words; i += L::threads) dst[i] = src[i];
-  }
 
-  const long long x0 = (long long)blockIdx.x * s.share, x1 = x0 + s.share;
-  uint32_t ring = 0, turn = 0;                              // places of the ring and items used so far
-  // the next item; every warp that took it gives it back after its last look
+  // the next item; every reader gives it back after its last look
+  uint32_t turn = 0;
   auto take = [&]() -> const Work& {
     mbar_wait(w_full + 8 * (turn % kItemSlots), (turn / kItemSlots) & 1, abort_flag, a.status);
     return work[turn % kItemSlots];
@@ -270,83 +278,101 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     if (lane == 0) mbar_arrive(w_empty + 8 * (turn % kItemSlots));
     ++turn;
   };
+  // a key tile of an item: where its keys begin, and how many there are from there on
+  auto keys_of = [](const Work& it, int j, int& key0) {
+    const int step = it.s0 + j;
+    const bool in_ahead = step < it.n_ahead;
+    key0 = (in_ahead ? step : step - it.n_ahead) * kAttnTile;
+    return (in_ahead ? it.ahead : it.own) - key0;
+  };
 
   if (warp == kLoadWarp) {
     // ------------------------------------------------------ keys and values, page by page
     const int page = 1 << a.page_shift, box = page < kAttnTile ? page : kAttnTile, box_shift = page < kAttnTile ? a.page_shift : 7;
+    const int places = E4M3 ? n_codes : L::stages;
     int bad = 0;
     bool alive = true;
     uint32_t issued = 0;
-    while (alive) {
-      const Work it = take();
-      if (it.n == 0) break;
-      give_back();
-      const int s0 = it.s0, n = it.n;
-      const int32_t* own_table = it.b >= 0 ? a.page_table + (long long)it.b * a.table_stride : nullptr;
-      const int32_t* ahead_table = it.g >= 0 ? a.prefix_pages + (long long)it.g * a.prefix_stride : nullptr;
-      // a lane's page of a step (up to 8), or -1 where the step has no keys any more
-      auto page_of = [&](int j) -> int {
-        const int step = s0 + j;
-        const bool in_ahead = step < it.n_ahead;
-        const int key = (in_ahead ? step : step - it.n_ahead) * kAttnTile + (lane << box_shift), keys = in_ahead ? it.ahead : it.own;
-        if (j >= n || lane >= (kAttnTile >> box_shift) || key >= keys) return -1;
-        int pg = (in_ahead ? ahead_table : own_table)[key >> a.page_shift];
-        if (pg < 0 || pg >= a.n_pages) { bad = 1; pg = a.n_pages; }                    // (reads zeros)
-        return pg;
-      };
-      auto load = [&](uint32_t pos, const CUtensorMap* tm, int j, int pg) {
-        const int places = E4M3 ? n_codes : L::stages, st = pos % places;
-        const uint32_t landed = (E4M3 ? code_full : full) + 8 * st, free = (E4M3 ? code_empty : empty) + 8 * st;
-        alive = __all_sync(0xffffffffu, mbar_wait(free, ((pos / places) & 1) ^ 1, abort_flag, a.status));
-        if (!alive) return;
-        issued = pos + 1;
-        const int step = s0 + j, in_page = ((step < it.n_ahead ? step : step - it.n_ahead) * kAttnTile) & (page - 1);
-        const int pages = __popc(__ballot_sync(0xffffffffu, pg >= 0));
-        if (lane == 0) mbar_expect_tx(landed, pages * box * (E4M3 ? DP : 128 * L::halves));
-        __syncwarp();
-        if (pg >= 0) {
-          if (E4M3) {
-            tma_load_4d(sbase + L::codes + st * L::code_bytes + (lane << box_shift) * DP, tm, 0, in_page, it.head, pg, landed);
-          } else {
-#pragma unroll
-            for (int h = 0; h < L::halves; ++h)
-              tma_load_4d(sbase + L::ring + st * L::tile_bytes + h * kHalfBytes + ((lane << box_shift) * 128), tm, h * 64, in_page, it.head, pg, landed);
-          }
-        }
-        __syncwarp();
-      };
-      int cur = page_of(0), next = page_of(1);
-      load(pos_k(ring, 0), &tm_k, 0, cur);
-      for (int j = 0; j < n && alive; ++j) {
-        const int after = page_of(j + 2);
-        if (j + 1 < n) load(pos_k(ring, j + 1), &tm_k, j + 1, next);
-        if (alive) load(pos_v(ring, j, n), &tm_v, j, cur);
-        cur = next; next = after;
+    Work it;
+    int j = 0;
+    // What a lane has to fetch of the tile (item `it`, step j): its page (-1: none) and the rest.
+    struct Fetch { int page, in_page, head; };
+    auto look = [&]() -> Fetch {
+      int key0;
+      const int keys = keys_of(it, j, key0), key = lane << box_shift;
+      Fetch f{-1, key0 & (page - 1), it.head};
+      if (lane < (kAttnTile >> box_shift) && key < keys) {
+        const int32_t* table = it.s0 + j < it.n_ahead ? a.prefix_pages + (long long)it.g * a.prefix_stride : a.page_table + (long long)it.b * a.table_stride;
+        f.page = table[(key0 + key) >> a.page_shift];
+        if (f.page < 0 || f.page >= a.n_pages) { bad = 1; f.page = a.n_pages; }        // (reads zeros)
       }
-      ring += 2 * n;
+      return f;
+    };
+    auto load = [&](uint32_t pos, const CUtensorMap* tm, const Fetch& f) {
+      const int st = pos % places;
+      const uint32_t landed = (E4M3 ? code_full : full) + 8 * st, free = (E4M3 ? code_empty : empty) + 8 * st;
+      alive = __all_sync(0xffffffffu, mbar_wait(free, ((pos / places) & 1) ^ 1, abort_flag, a.status));
+      if (!alive) return;
+      issued = pos + 1;
+      const int pages = __popc(__ballot_sync(0xffffffffu, f.page >= 0));
+      if (lane == 0) mbar_expect_tx(landed, pages * box * (E4M3 ? DP : 128 * L::halves));
+      __syncwarp();
+      if (f.page >= 0) {
+        if (E4M3) {
+          tma_load_4d(sbase + L::codes + st * L::code_bytes + (lane << box_shift) * DP, tm, 0, f.in_page, f.head, f.page, landed);
+        } else {
+#pragma unroll
+          for (int h = 0; h < L::halves; ++h)
+            tma_load_4d(sbase + L::ring + st * L::tile_bytes + h * kHalfBytes + ((lane << box_shift) * 128), tm, h * 64, f.in_page, f.head, f.page, landed);
+        }
+      }
+      __syncwarp();
+    };
+    auto next_tile = [&]() -> bool {                        // moves on to the next tile, if there is one
+      if (++j < it.n) return true;
+      it = take();
+      if (__any_sync(0xffffffffu, it.n == 0 || *abort_flag)) return false;
+      give_back();
+      j = 0;
+      return true;
+    };
+    it.n = 0;
+    bool more = next_tile();
+    Fetch next, last;
+    if (more) next = look();
+    uint32_t t = 0;
+    while (more && alive) {
+      const Fetch now = next;
+      more = next_tile();
+      if (more) next = look();                              // (its page ids arrive while this tile waits for its place)
+      load(pos_k(t), &tm_k, now);
+      if (t && alive) load(pos_v(t - 1), &tm_v, last);
+      last = now;
+      ++t;
     }
+    if (t && alive) load(pos_v(t - 1), &tm_v, last);
     if (bad) atomicExch(&a.status[kStBadRouting], 1);
     if (!alive) {                                           // copies in flight land before the block's memory is given up
       const unsigned long long t0 = globaltimer();
-      const uint32_t places = E4M3 ? n_codes : L::stages;
-      for (uint32_t pos = issued > places ? issued - places : 0; pos < issued; ++pos)
+      for (uint32_t pos = issued > (uint32_t)places ? issued - places : 0; pos < issued; ++pos)
         while (!mbar_try_wait((E4M3 ? code_full : full) + 8 * (pos % places), (pos / places) & 1) && globaltimer() - t0 < 100000000ull) {}
     }
   } else if (warp == kItemWarp) {
     // ------------------------------------------------------ the CTA's share of the schedule, item by item
     if (lane == 0) {
+      const long long x0 = (long long)blockIdx.x * s.share, x1 = x0 + s.share;
       AttnWalk k = attn_walk_at(p, s, x0);
       Work* out = const_cast<Work*>(work);
       for (;;) {
         Work w;
-        w.n = 0; w.n_tok = 0;
+        w.n = 0;
         for (; !k.done && k.at < x1 && w.n == 0; attn_walk_next(p, s, &k)) {
           const AttnItem it = attn_item(p, s, k);
           const int s0 = attn_steps_before(k, it.n, x0), s1 = attn_steps_before(k, it.n, x1);
           w.n = s1 - s0; w.s0 = s0;
           if (w.n == 0) continue;
           w.head = it.head; w.n_tok = it.n_tok; w.ahead = it.ahead; w.own = it.own; w.n_ahead = it.n_ahead; w.b = it.b; w.g = it.g;
-          w.whole = it.kind == kAttnJoint && w.n == it.n;
+          w.flags = (it.dual ? kDual : 0) | (attn_is_whole(it, s0, s1) ? kWhole : 0);
           w.prow = attn_part_row(it, blockIdx.x, s0);
           if (it.kind == kAttnGroup) {
             w.lo = s.gfirst[it.g]; w.hi = s.gfirst[it.g + 1];
@@ -357,7 +383,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             w.seen = s.kv[it.b] - (s.q0[it.b + 1] - s.q0[it.b]) + it.tok + 1;
           }
         }
-        if (!mbar_wait(w_empty + 8 * (turn % kItemSlots), ((turn / kItemSlots) & 1) ^ 1, abort_flag, a.status)) w.n = 0;
+        if (!mbar_wait(w_empty + 8 * (turn % kItemSlots), ((turn / kItemSlots) & 1) ^ 1, abort_flag, a.status)) break;
         out[turn % kItemSlots] = w;
         mbar_arrive(w_full + 8 * (turn % kItemSlots));
         ++turn;
@@ -365,348 +391,358 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       }
     }
     __syncwarp();
+    if (blockIdx.x == 0) {                                  // the schedule, for the kernel that joins partial results
+      int32_t* dst = static_cast<int32_t*>(a.sched);
+      const int32_t* src = reinterpret_cast<const int32_t*>(sched_at);
+      for (int i = lane; i < words; i += 32) dst[i] = src[i];
+    }
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------ tensor core, one thread
     if (lane == 0) {
-      constexpr uint32_t idesc_s = make_idesc_bf16(128, 128), idesc_o = make_idesc_bf16(128, DP) | kTransposeB;
-      bool alive = true;
-      uint32_t items = 0, p_phase[2] = {0, 0};
-      auto wait_stage = [&](uint32_t pos) { alive = alive && mbar_wait(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status); tc_fence_after(); };
-      auto wait_p = [&](int w) { alive = alive && mbar_wait(p_ready + 8 * w, p_phase[w] & 1, abort_flag, a.status); ++p_phase[w]; tc_fence_after(); };
-      auto free_stage = [&](uint32_t pos) { tc_commit(empty + 8 * (pos % L::stages)); };
-      auto qk = [&](int w, int q_tile, uint32_t pos) {
-        const uint64_t qd = make_smem_desc(sbase + L::q + q_tile * L::tile_bytes);
-        const uint64_t kd = make_smem_desc(sbase + L::ring + (pos % L::stages) * L::tile_bytes);
+      constexpr uint32_t type = E4M3 ? (1u << 7) | (1u << 10) : 0u;         // codes are decoded to fp16, whose type bits are 0 (bf16: 1)
+      constexpr uint32_t idesc_s = make_idesc_bf16(128, 128) ^ type, idesc_o = (make_idesc_bf16(128, DP) | kTransposeB) ^ type;
+      // Each warpgroup's place in the stream: what it needs next is an item, a tile's Q K^T or its P V.
+      enum { kItem, kScores, kProduct, kEnd };
+      struct Side { uint32_t turn, t0; int n, j, state; bool dual; uint32_t q_phase, p_phase; } side[2];
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
-          const uint64_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;
-          tc_mma_f16(tmem + w * 128, qd + off, kd + off, idesc_s, i > 0);
-        }
-        tc_commit(s_full + 8 * w);
+      for (int w = 0; w < 2; ++w) side[w] = Side{0, 0, 0, 0, kItem, false, 0, 0};
+      uint32_t half_used = 0;                               // stages that one of a pair of warpgroups is through with
+      auto free_stage = [&](bool dual, int st) {
+        if (dual && !(half_used >> st & 1)) { half_used |= 1u << st; return; }
+        half_used &= ~(1u << st);
+        tc_commit(empty + 8 * st);
       };
-      auto pv = [&](int w, uint32_t pos, bool first) {
-        const uint64_t vd = make_v_desc(sbase + L::ring + (pos % L::stages) * L::tile_bytes);
+      unsigned long long since = globaltimer();
+      uint32_t idle = 0;
+      while (side[0].state != kEnd || side[1].state != kEnd) {
+        bool moved = false;
 #pragma unroll
-        for (int i = 0; i < kAttnTile / 16; ++i)
-          tc_mma_f16_ts(tmem + 256 + w * 128, tmem + w * 128 + i * 8, vd + ((i * 16 * 128) >> 4), idesc_o, !first || i > 0);
-      };
-      while (alive) {
-        const Work& it = take();
-        const int n = it.n;
-        const bool dual = it.n_tok > p.tps;
-        if (n == 0) break;
-        mbar_arrive(w_empty + 8 * (turn % kItemSlots));
-        ++turn;
-        alive = alive && mbar_wait(q_ready, items & 1, abort_flag, a.status);
-        ++items;
-        tc_fence_after();
-        if (dual) {
-          wait_stage(pos_k(ring, 0));
-          if (!alive) break;
-          qk(0, 0, pos_k(ring, 0));
-          qk(1, 1, pos_k(ring, 0));
-          free_stage(pos_k(ring, 0));
-          for (int j = 0; j < n; ++j) {
-            const bool more = j + 1 < n;
-            const uint32_t pv_at = pos_v(ring, j, n), pk_at = pos_k(ring, j + 1);
-            wait_p(0);
-            if (more) wait_stage(pk_at);                    // (loaded before this step's V)
-            wait_stage(pv_at);
-            if (!alive) break;
-            pv(0, pv_at, j == 0);
-            if (more) qk(0, 0, pk_at); else tc_commit(o_done);
-            wait_p(1);
-            if (!alive) break;
-            pv(1, pv_at, j == 0);
-            free_stage(pv_at);
-            if (more) { qk(1, 1, pk_at); free_stage(pk_at); } else tc_commit(o_done + 8);
+        for (int w = 0; w < 2; ++w) {
+          Side& x = side[w];
+          if (x.state == kProduct) {
+            const uint32_t t = x.t0 + x.j, pos = pos_v(t);
+            const int st = pos % L::stages;
+            if (mbar_test(p_ready + 8 * w, x.p_phase & 1) && mbar_test(full + 8 * st, (pos / L::stages) & 1)) {
+              tc_fence_after();
+              ++x.p_phase;
+              const bool first = x.j < (x.dual ? 1 : 2);
+              const uint64_t vd = make_v_desc(sbase + L::ring + st * L::tile_bytes);
+#pragma unroll
+              for (int i = 0; i < kAttnTile / 16; ++i)
+                tc_mma_f16_ts(tmem + 256 + w * 128, tmem + w * 128 + i * 8, vd + ((i * 16 * 128) >> 4), idesc_o, !first || i > 0);
+              free_stage(x.dual, st);
+              x.j += x.dual ? 1 : 2;
+              x.state = kScores;
+              if (x.j >= x.n) {
+                tc_commit(o_done + 8 * w);
+                x.t0 += x.n;
+                x.state = kItem;
+              }
+              moved = true;
+            }
           }
-        } else {
-          for (int j = 0; j < 2 && j < n; ++j) {
-            wait_stage(pos_k(ring, j));
-            if (!alive) break;
-            qk(j, 0, pos_k(ring, j));
-            free_stage(pos_k(ring, j));
+          if (x.state == kItem && mbar_test(w_full + 8 * (x.turn % kItemSlots), (x.turn / kItemSlots) & 1)) {
+            const Work& it = work[x.turn % kItemSlots];
+            x.n = it.n;
+            x.dual = it.flags & kDual;
+            if (x.n == 0) {
+              x.state = kEnd;
+            } else {
+              mbar_arrive(w_empty + 8 * (x.turn % kItemSlots));
+              ++x.turn;
+              x.j = first_step(x.t0, x.dual, w);
+              if (x.j < x.n) x.state = kScores; else x.t0 += x.n;
+            }
+            moved = true;
           }
-          for (int j = 0; j < n && alive; ++j) {
-            const int w = j & 1;
-            wait_p(w);
-            wait_stage(pos_v(ring, j, n));
-            if (!alive) break;
-            pv(w, pos_v(ring, j, n), j < 2);
-            free_stage(pos_v(ring, j, n));
-            if (j + 2 >= n) { tc_commit(o_done + 8 * w); continue; }
-            wait_stage(pos_k(ring, j + 2));
-            if (!alive) break;
-            qk(w, 0, pos_k(ring, j + 2));
-            free_stage(pos_k(ring, j + 2));
+          if (x.state == kScores) {
+            const uint32_t t = x.t0 + x.j, pos = pos_k(t);
+            const int st = pos % L::stages;
+            const bool first = x.j < (x.dual ? 1 : 2);
+            if ((!first || mbar_test(q_ready + 8 * w, x.q_phase & 1)) && mbar_test(full + 8 * st, (pos / L::stages) & 1)) {
+              tc_fence_after();
+              x.q_phase += first;
+              const uint64_t qd = make_smem_desc(sbase + L::q + w * L::tile_bytes);
+              const uint64_t kd = make_smem_desc(sbase + L::ring + st * L::tile_bytes);
+#pragma unroll
+              for (int i = 0; i < DP / 16; ++i) {
+                const uint64_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;
+                tc_mma_f16(tmem + w * 128, qd + off, kd + off, idesc_s, i > 0);
+              }
+              tc_commit(s_full + 8 * w);
+              free_stage(x.dual, st);
+              x.state = kProduct;
+              moved = true;
+            }
           }
         }
-        ring += 2 * n;
+        if (moved) { idle = 0; continue; }
+        if ((++idle & 1023u) == 0u) {                       // (a wait with a limit, as everywhere)
+          if (*abort_flag) break;
+          if (idle == 1024u) since = globaltimer();
+          else if (globaltimer() - since > kWaitLimitNs) { *abort_flag = 1; atomicExch(&a.status[kStTimeout], 1); break; }
+        }
       }
     }
     __syncwarp();
   } else if (E4M3 && warp >= kCodeWarp) {
-    // ------------------------------------------------------ codes to bf16, which holds every e4m3 value
+    // ------------------------------------------------------ codes to fp16, which holds every e4m3 value
     const int ct = tid & 127;
     bool alive = true;
+    auto decode = [&](uint32_t pos, int keys) {
+      const int st = pos % L::stages, slot = pos % n_codes;
+      const bool ok = mbar_wait(code_full + 8 * slot, (pos / n_codes) & 1, abort_flag, a.status) &&
+                      mbar_wait(empty + 8 * st, ((pos / L::stages) & 1) ^ 1, abort_flag, a.status);
+      alive = __all_sync(0xffffffffu, ok);
+      if (!alive) return;
+      const uint8_t* src = smem + L::codes + slot * L::code_bytes;
+      uint8_t* dst = smem + L::ring + st * L::tile_bytes;
+      constexpr int per_row = DP / 16, batch = 4;          // 16 codes at a time
+#pragma unroll 1
+      for (int u = 0; u < kAttnTile * per_row / 128; u += batch) {
+        uint4 v[batch];
+#pragma unroll
+        for (int i = 0; i < batch; ++i) v[i] = *reinterpret_cast<const uint4*>(src + ((u + i) * 128 + ct) * 16);
+#pragma unroll
+        for (int i = 0; i < batch; ++i) {
+          const int id = (u + i) * 128 + ct, row = id / per_row, c = id % per_row;
+          if (row >= keys) v[i] = make_uint4(0, 0, 0, 0);  // what lies behind the last key may be anything: its weight 0 needs a finite value
+          uint4 lo, hi;
+          decode4(v[i].x, lo.x, lo.y); decode4(v[i].y, lo.z, lo.w);
+          decode4(v[i].z, hi.x, hi.y); decode4(v[i].w, hi.z, hi.w);
+          uint8_t* at = dst + (c >> 2) * kHalfBytes + row * 128;
+          const int first = (((c & 3) * 2) ^ (row & 7)) << 4, flip = (c & 4) << 2;      // (the other order where c & 4: then the halves' stores share no bank)
+          *reinterpret_cast<uint4*>(at + (first ^ flip)) = flip ? hi : lo;
+          *reinterpret_cast<uint4*>(at + (first ^ 16 ^ flip)) = flip ? lo : hi;
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(code_empty + 8 * slot); mbar_arrive(full + 8 * st); }
+    };
+    uint32_t t = 0;
+    int before = 0;
     while (alive) {
       const Work it = take();
-      if (__any_sync(0xffffffffu, it.n == 0)) break;
+      if (__any_sync(0xffffffffu, it.n == 0 || *abort_flag)) break;
       give_back();
-      for (int i = 0; i < 2 * it.n && alive; ++i) {
-        const uint32_t pos = ring + i;
-        const int j = i == 0 ? 0 : i == 2 * it.n - 1 ? it.n - 1 : (i & 1) ? (i + 1) >> 1 : (i >> 1) - 1;             // the order of pos_k and pos_v
-        const int step = it.s0 + j, keys = (step < it.n_ahead ? it.ahead - step * kAttnTile : it.own - (step - it.n_ahead) * kAttnTile);
-        const int st = pos % L::stages, slot = pos % n_codes;
-        const bool ok = mbar_wait(code_full + 8 * slot, (pos / n_codes) & 1, abort_flag, a.status) &&
-                        mbar_wait(empty + 8 * st, ((pos / L::stages) & 1) ^ 1, abort_flag, a.status);
-        alive = __all_sync(0xffffffffu, ok);
-        if (!alive) break;
-        const uint8_t* src = smem + L::codes + slot * L::code_bytes;
-        uint8_t* dst = smem + L::ring + st * L::tile_bytes;
-        constexpr int per_row = DP / 16;                   // 16 codes at a time
-#pragma unroll
-        for (int u = 0; u < kAttnTile * per_row / 128; ++u) {
-          const int id = u * 128 + ct, row = id / per_row, c = id % per_row;
-          uint4 v = *reinterpret_cast<const uint4*>(src + id * 16);
-          if (row >= keys) v = make_uint4(0, 0, 0, 0);     // what lies behind the last key may be anything: its weight 0 needs a finite value
-          uint4 lo, hi;
-          decode4(v.x, lo.x, lo.y); decode4(v.y, lo.z, lo.w);
-          decode4(v.z, hi.x, hi.y); decode4(v.w, hi.z, hi.w);
-          uint8_t* at = dst + (c >> 2) * kHalfBytes + row * 128;
-          const int first = (((c & 3) * 2) ^ (row & 7)) << 4, second = first ^ 16;
-          if (c & 4) {                                     // (the other order: both halves' stores share no bank)
-            *reinterpret_cast<uint4*>(at + second) = hi;
-            *reinterpret_cast<uint4*>(at + first) = lo;
-          } else {
-            *reinterpret_cast<uint4*>(at + first) = lo;
-            *reinterpret_cast<uint4*>(at + second) = hi;
-          }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) { mbar_arrive(code_empty + 8 * slot); mbar_arrive(full + 8 * st); }
+      for (int j = 0; j < it.n && alive; ++j) {
+        int key0;
+        const int keys = keys_of(it, j, key0);
+        decode(pos_k(t), keys);
+        if (t && alive) decode(pos_v(t - 1), before);
+        before = keys;
+        ++t;
       }
-      ring += 2 * it.n;
     }
+    if (t && alive) decode(pos_v(t - 1), before);
   } else if (warp < kMmaWarp) {
     // ------------------------------------------------------ rows: softmax, corrections, results
     // (After a wait that was given up an item's steps run on with what is there: what a warp does must not differ by lane.)
     const int wg = warp >> 2, row = tid & 127, row_tok = row / p.Gh, row_head = row - row_tok * p.Gh;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
     const uint32_t t_s = tmem + lanes + wg * 128, t_o = tmem + lanes + 256 + wg * 128;
-    uint32_t s_phase = 0, o_phase = 0, m_phase = 0;
-    auto meet = [&]() {                                     // both warpgroups
-      __syncwarp();
-      if (lane == 0) mbar_arrive(rows_meet);
-      mbar_wait(rows_meet, m_phase & 1, abort_flag, a.status);
-      ++m_phase;
-    };
-    for (;;) {
-      const Work& it = take();
-      const int n = it.n;
-      if (__any_sync(0xffffffffu, n == 0 || *abort_flag)) break;
-      const int s0 = it.s0, n_ahead = it.n_ahead, ahead = it.ahead, own = it.own, kvh = it.head;
-      const bool dual = it.n_tok > p.tps, whole = it.whole;
-      const int tt = (dual ? wg * p.tps : 0) + row_tok;     // token of the item
-      const bool mine = row_tok < p.tps && tt < it.n_tok;
-      const bool active = __any_sync(0xffffffffu, mine);
-      int token = it.tok + tt, own_seen = own;
-      if (mine) {
-        if (it.hi > 0) {
-          const int b = short_sequence(s, it.lo, it.hi, token);
-          token = s.q0[b] + (token - s.scum[b]);
-        } else if (p.causal) {
-          own_seen = it.seen + tt;
+    uint32_t s_phase = 0, o_phase = 0, t0 = 0;
+    // This thread's row of an item.
+    struct Row { int n, j, s0, n_ahead, ahead, own, seen, head, token; bool dual, whole, mine, active; uint32_t t0; long long prow; float sl2; };
+    // The next item that this warpgroup has a part in: its row of Q goes to shared memory (nothing reads the last item's any more)
+    auto next_item = [&](Row& r) -> bool {
+      for (;;) {
+        const Work& it = take();
+        const int n = it.n;
+        if (__any_sync(0xffffffffu, n == 0 || *abort_flag)) return false;
+        const bool dual = it.flags & kDual;
+        const int j = first_step(t0, dual, wg);
+        if (j >= n) { give_back(); t0 += n; continue; }
+        r.n = n; r.j = j; r.t0 = t0; r.dual = dual; r.whole = it.flags & kWhole;
+        r.s0 = it.s0; r.n_ahead = it.n_ahead; r.ahead = it.ahead; r.own = it.own;
+        const int tt = (dual ? wg * p.tps : 0) + row_tok, kvh = it.head;      // token of the item
+        r.mine = row_tok < p.tps && tt < it.n_tok;
+        r.token = it.tok + tt;
+        r.seen = it.own;
+        if (r.mine) {
+          if (it.hi > 0) {
+            const int b = sequence_of(s.scum, it.lo, it.hi, r.token);
+            r.token = s.q0[b] + (r.token - s.scum[b]);
+          } else if (p.causal) {
+            r.seen = it.seen + tt;
+          }
         }
-      }
-      const int head = kvh * p.Gh + row_head;
-      const long long prow = it.prow + (long long)tt * p.Gh + row_head;
-      give_back();
-      // Q into shared memory, columns beyond D as zeros (rows of nobody stay as they are: rows do not mix)
-      if (mine && (dual || wg == 0)) {
-        const uint16_t* src = a.q + (long long)token * a.q_tok + (long long)head * a.q_head;
-        uint8_t* dst = smem + L::q + (dual ? wg : 0) * L::tile_bytes + row * 128;
+        r.head = kvh * p.Gh + row_head;
+        // partial rows: those of the item's tokens; where the warpgroups take turns, once for the one with the first tile and once for the other
+        r.prow = it.prow + (long long)(tt + (dual ? 0 : j * it.n_tok)) * p.Gh + row_head;
+        t0 += n;
+        give_back();
+        r.active = __any_sync(0xffffffffu, r.mine);
+        r.sl2 = a.scale_log2 * (a.k_scale ? a.k_scale[kvh] : 1.f);
+        if (r.mine) {
+          const uint16_t* src = a.q + (long long)r.token * a.q_tok + (long long)r.head * a.q_head;
+          uint8_t* dst = smem + L::q + wg * L::tile_bytes + row * 128;
+          uint4 v[DP / 8];                                  // columns beyond D as zeros (rows of nobody stay as they are: rows do not mix)
 #pragma unroll
-        for (int c = 0; c < DP / 8; ++c) {
-          const uint4 v = c * 8 < a.D ? __ldg(reinterpret_cast<const uint4*>(src + c * 8)) : make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(dst + (c >> 3) * kHalfBytes + (((c & 7) ^ (row & 7)) << 4)) = v;
+          for (int c = 0; c < DP / 8; ++c) v[c] = c * 8 < a.D ? __ldg(reinterpret_cast<const uint4*>(src + c * 8)) : make_uint4(0, 0, 0, 0);
+          if (E4M3) {
+            // As fp16, times the power of two that brings the row's largest value to 2^14 (exact; what falls below fp16's range then is
+            // 2^-38 of the largest).  The scores are taken back by sl2.
+            uint32_t top = 0;
+#pragma unroll
+            for (int c = 0; c < DP / 8; ++c) {
+              const uint32_t w4[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) top = max(top, max(w4[i] & 0x7fffu, w4[i] >> 16 & 0x7fffu));
+            }
+            const int e = (int)(top >> 7);                  // biased exponent of the largest
+            const int shift = e == 0 || e == 255 ? 0 : min(100, 127 + 14 - e);
+            const float up = __int_as_float((127 + shift) << 23);
+            r.sl2 *= __int_as_float((127 - shift) << 23);
+#pragma unroll
+            for (int c = 0; c < DP / 8; ++c) {
+              auto half2 = [&](uint32_t w2) { return pack_f16(__uint_as_float(w2 << 16) * up, __uint_as_float(w2 & 0xffff0000u) * up); };
+              v[c] = make_uint4(half2(v[c].x), half2(v[c].y), half2(v[c].z), half2(v[c].w));
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < DP / 8; ++c) *reinterpret_cast<uint4*>(dst + (c >> 3) * kHalfBytes + (((c & 7) ^ (row & 7)) << 4)) = v[c];
         }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_ready + 8 * wg);
+        return true;
       }
-      fence_proxy_async_smem();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_ready);
-
-      const float sl2 = a.scale_log2 * (a.k_scale ? a.k_scale[kvh] : 1.f);
+    };
+    Row r, next;
+    bool more = next_item(next);
+    while (more) {
+      r = next;
       float m = -CUDART_INF_F, l = 0.f;                     // maximum that the sums refer to (unscaled), sum
       bool any = false;                                     // O holds something
-      for (int j = dual ? 0 : wg; j < n; j += dual ? 1 : 2) {
-        const int step = s0 + j;
-        const bool in_ahead = step < n_ahead;
-        const int key0 = (in_ahead ? step : step - n_ahead) * kAttnTile, keys = (in_ahead ? ahead : own) - key0;
+#pragma unroll 1
+      for (int j = r.j; j < r.n; j += r.dual ? 1 : 2) {
+        const int step = r.s0 + j;
+        const bool in_ahead = step < r.n_ahead;
+        const int key0 = (in_ahead ? step : step - r.n_ahead) * kAttnTile, keys = (in_ahead ? r.ahead : r.own) - key0;
         mbar_wait(s_full + 8 * wg, s_phase & 1, abort_flag, a.status);
         ++s_phase;
         tc_fence_after();
         if (!E4M3 && keys < kAttnTile) {                    // what lies behind the last key may be anything: its weight 0 needs a finite value.
           // (Not before S: only then has this stage's use before last ended, and the parity tells the uses apart.)
-          const uint32_t pos = pos_v(ring, j, n);
+          const uint32_t pos = pos_v(r.t0 + j);
           mbar_wait(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status);
           uint8_t* v = smem + L::ring + (pos % L::stages) * L::tile_bytes;
           const int from = keys < 0 ? 0 : keys;
-#pragma unroll
           for (int h = 0; h < L::halves; ++h)
             for (int i = from * 8 + (tid & 127); i < kAttnTile * 8; i += 128) *reinterpret_cast<uint4*>(v + h * kHalfBytes + i * 16) = make_uint4(0, 0, 0, 0);
           fence_proxy_async_smem();
         }
-        if (active) {
-          const int see = in_ahead ? keys : (own_seen - key0 < keys ? own_seen - key0 : keys);
-          float m_new = m;
+        if (r.active) {
+          // S is held in registers where there are enough, else read twice.
+          constexpr int held = E4M3 ? 1 : 4;
+          uint32_t x[held][32];
+          const int see = in_ahead ? keys : (r.seen - key0 < keys ? r.seen - key0 : keys);
+          const bool hide = __any_sync(0xffffffffu, see < kAttnTile);
+          auto mask = [&](int c) {
+            if (hide) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[c % held][i] = c * 32 + i < see ? x[c % held][i] : 0xff800000u;
+            }
+          };
+          if (held == 4) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tc_ld32(t_s + c * 32, x[c % held]);
+            tc_wait_ld();
+          }
+          float top[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            uint32_t r[32];
-            tc_ld32(t_s + c * 32, r);
-            tc_wait_ld();
-            hide(r, see - c * 32);
-            float top = __uint_as_float(r[0]);
+            if (held == 1) { tc_ld32(t_s + c * 32, x[0]); tc_wait_ld(); }
+            mask(c);
+            uint32_t (&y)[32] = x[c % held];
+            top[c] = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
 #pragma unroll
-            for (int i = 1; i < 31; i += 2) top = max3(top, __uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-            m_new = max3(m_new, top, __uint_as_float(r[31]));
+            for (int i = 2; i < 32; i += 2) top[c] = max3(top[c], __uint_as_float(y[i]), __uint_as_float(y[i + 1]));
           }
-          // The sums keep referring to an older maximum until weights could pass 2^8: fp32 and bf16 carry that exactly as well.
-          const bool raise = m_new > m && (m_new - m) * sl2 > 8.f;
+          const float m_new = max3(max3(m, top[0], top[1]), top[2], top[3]);
+          // The sums keep referring to an older maximum until weights could pass 2^8: fp32 and the weights' type carry that exactly as well.
+          const bool raise = m_new > m && (m_new - m) * r.sl2 > 8.f;
           if (!any) {
             m = m_new;
           } else if (__any_sync(0xffffffffu, raise)) {
-            const float f = raise ? ex2((m - m_new) * sl2) : 1.f;
+            const float f = raise ? ex2((m - m_new) * r.sl2) : 1.f;
             if (raise) { m = m_new; l *= f; }
-#pragma unroll
-            for (int c = 0; c < DP / 32; ++c) {
-              uint32_t o[32];
-              tc_ld32(t_o + c * 32, o);
+#pragma unroll 1
+            for (int c = 0; c < DP / 16; ++c) {
+              uint32_t o[16];
+              tc_ld16(t_o + c * 16, o);
               tc_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tc_st32(t_o + c * 32, o);
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tc_st16(t_o + c * 16, o);
             }
             tc_wait_st();
           }
           any = true;
-          const float shift = m == -CUDART_INF_F ? 0.f : m * sl2;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          const float shift = m == -CUDART_INF_F ? 0.f : -m * r.sl2;
+          const f32x2 scale2 = pair2(r.sl2, r.sl2), shift2 = pair2(shift, shift);
+          f32x2 sum[2] = {0, 0};
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            uint32_t r[32], w[16];
-            tc_ld32(t_s + c * 32, r);
-            tc_wait_ld();
-            hide(r, see - c * 32);
+            if (held == 1) { tc_ld32(t_s + c * 32, x[0]); tc_wait_ld(); mask(c); }
+            uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float p0 = ex2(fmaf(__uint_as_float(r[2 * i]), sl2, -shift)), p1 = ex2(fmaf(__uint_as_float(r[2 * i + 1]), sl2, -shift));
-              sum[i & 1] += p0; sum[2 + (i & 1)] += p1;
-              w[i] = pack_bf16(p0, p1);
+              float p0, p1;
+              unpair2(fma2(pair2(__uint_as_float(x[c % held][2 * i]), __uint_as_float(x[c % held][2 * i + 1])), scale2, shift2), p0, p1);
+              p0 = ex2(p0); p1 = ex2(p1);
+              sum[i & 1] = add2(sum[i & 1], pair2(p0, p1));
+              w[i] = E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
             }
             tc_st16(t_s + c * 16, w);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          float s0, s1;
+          unpair2(add2(sum[0], sum[1]), s0, s1);
+          l += s0 + s1;
           tc_wait_st();
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(p_ready + 8 * wg);
       }
+      more = next_item(next);                               // (its Q arrives while the last product runs)
 
       // ---- the item's result
-      const bool worked = dual || wg < n;                   // (of one step, the second warpgroup has none)
-      if (worked) { mbar_wait(o_done + 8 * wg, o_phase & 1, abort_flag, a.status); ++o_phase; tc_fence_after(); }
-      const float m2 = m == -CUDART_INF_F ? m : m * sl2;
-      // 32 columns of O at a time
-      auto finish = [&](float m2, float l, auto get) {
-        if (whole) {
-          const float inv = l > 0.f ? (a.v_scale ? a.v_scale[kvh] : 1.f) / l : l;        // (a NaN stays)
-          uint16_t* dst = a.out + (long long)token * a.out_tok + (long long)head * a.out_head;
-#pragma unroll
-          for (int c = 0; c < DP / 32; ++c) {
-            float o[32];
-            get(c, o);
-            if (mine) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 8)
-                if (c * 32 + i < a.D) {
-                  uint4 v;
-                  v.x = l == 0.f ? 0u : pack_bf16(o[i] * inv, o[i + 1] * inv); v.y = l == 0.f ? 0u : pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
-                  v.z = l == 0.f ? 0u : pack_bf16(o[i + 4] * inv, o[i + 5] * inv); v.w = l == 0.f ? 0u : pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
-                  *reinterpret_cast<uint4*>(dst + c * 32 + i) = v;
-                }
-            }
-          }
-          if (mine && a.lse) a.lse[(long long)token * a.lse_tok + head] = (m2 + __log2f(l)) * 0.6931471805599453f;
-        } else {
-          float* dst = a.part_o + prow * DP;
-#pragma unroll
-          for (int c = 0; c < DP / 32; ++c) {
-            float o[32];
-            get(c, o);
-            if (mine) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(dst + c * 32 + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-            }
-          }
-          if (mine) a.part_ml[prow] = make_float2(m2, l);
-        }
-      };
-      if (dual) {
-        if (active) finish(m2, l, [&](int c, float (&o)[32]) {
-          uint32_t r[32];
-          tc_ld32(t_o + c * 32, r);
+      mbar_wait(o_done + 8 * wg, o_phase & 1, abort_flag, a.status);
+      ++o_phase;
+      tc_fence_after();
+      if (r.active) {
+        const float m2 = m == -CUDART_INF_F ? m : m * r.sl2;
+        const int kvh = r.head / p.Gh;
+        const float inv = l > 0.f ? (a.v_scale ? a.v_scale[kvh] : 1.f) / l : l;        // (a NaN stays)
+        uint16_t* dst = a.out + (long long)r.token * a.out_tok + (long long)r.head * a.out_head;
+        float* part = a.part_o + r.prow * DP;
+#pragma unroll 1
+        for (int c = 0; c < DP / 32; ++c) {
+          uint32_t o[32];
+          tc_ld32(t_o + c * 32, o);
           tc_wait_ld();
+          if (r.mine && r.whole) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(r[i]);
-        });
-        // (the other warpgroup may still read its Q: each overwrites its own only)
-      } else {
-        // the second warpgroup's O goes through the memory of Q, which nothing reads any more
-        constexpr int chunks = DP / 4;
-        float4* pool = reinterpret_cast<float4*>(smem + L::q) + row * chunks;
-        meet();
-        if (wg == 1) {
-          if (active && worked) {
+            for (int i = 0; i < 32; i += 8)
+              if (c * 32 + i < a.D) {
+                uint32_t w[4];
 #pragma unroll
-            for (int c = 0; c < DP / 32; ++c) {
-              uint32_t r[32];
-              tc_ld32(t_o + c * 32, r);
-              tc_wait_ld();
+                for (int q = 0; q < 4; ++q) w[q] = l == 0.f ? 0u : pack_bf16(__uint_as_float(o[i + 2 * q]) * inv, __uint_as_float(o[i + 2 * q + 1]) * inv);
+                *reinterpret_cast<uint4*>(dst + c * 32 + i) = make_uint4(w[0], w[1], w[2], w[3]);
+              }
+          } else if (r.mine) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                pool[(c * 8 + i) ^ (row & (chunks - 1))] = make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]), __uint_as_float(r[4 * i + 2]),
-                                                                       __uint_as_float(r[4 * i + 3]));
-            }
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(part + c * 32 + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
           }
-          exchange[row] = make_float2(m2, l);
         }
-        meet();
-        if (wg == 0 && active) {
-          const float2 other = exchange[row];
-          const bool two = n > 1;
-          const float mm = two ? fmaxf(m2, other.x) : m2, base = mm == -CUDART_INF_F ? 0.f : mm;
-          const float f0 = two ? ex2(m2 - base) : 1.f, f1 = two ? ex2(other.x - base) : 0.f;
-          finish(mm, two ? l * f0 + other.y * f1 : l, [&](int c, float (&o)[32]) {
-            uint32_t r[32];
-            tc_ld32(t_o + c * 32, r);
-            tc_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float4 x = two ? pool[(c * 8 + i) ^ (row & (chunks - 1))] : make_float4(0.f, 0.f, 0.f, 0.f);
-              o[4 * i] = __uint_as_float(r[4 * i]) * f0 + x.x * f1; o[4 * i + 1] = __uint_as_float(r[4 * i + 1]) * f0 + x.y * f1;
-              o[4 * i + 2] = __uint_as_float(r[4 * i + 2]) * f0 + x.z * f1; o[4 * i + 3] = __uint_as_float(r[4 * i + 3]) * f0 + x.w * f1;
-            }
-          });
-        }
-        meet();
+        if (r.mine && !r.whole) a.part_ml[r.prow] = make_float2(m2, l);
+        if (r.mine && r.whole && a.lse) a.lse[(long long)r.token * a.lse_tok + r.head] = (m2 + __log2f(l)) * 0.6931471805599453f;
       }
       tc_fence_before();
-      ring += 2 * n;
     }
   }
   tc_fence_before();
@@ -723,13 +759,16 @@ template <int DP>
 __device__ __forceinline__ void join_item(const AttnArgs& a, const AttnSched& s, const AttnWalk& k, const AttnItem& it, int row, float& m, float& l, float4& o) {
   const int lane = threadIdx.x & 31;
   const int c_lo = (int)(k.at / s.share), c_hi = (int)((k.at + k.w - 1) / s.share);
-  for (int c0 = c_lo; c0 <= c_hi; c0 += 32) {
-    const int c = c0 + lane;
+  for (int c0 = c_lo; c0 <= c_hi; c0 += 16) {               // a lane for each of a CTA's two results
+    const int c = c0 + (lane >> 1);
     long long at = -1;
     float2 ml = make_float2(-CUDART_INF_F, 0.f);
     if (c <= c_hi) {
       const int s0 = attn_steps_before(k, it.n, c * s.share), s1 = attn_steps_before(k, it.n, (c + 1) * s.share);
-      if (s0 < s1) { at = attn_part_row(it, c, s0) + row; ml = a.part_ml[at]; }
+      if (s0 < s1 && (lane & 1) < attn_part_count(it, s0, s1)) {
+        at = attn_part_row(it, c, s0) + (lane & 1) * it.n_tok * a.p.Gh + row;
+        ml = a.part_ml[at];
+      }
     }
     float top = ml.x;
 #pragma unroll
@@ -784,38 +823,42 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
   }
   AttnSched s = attn_carve(join_smem, p.B, p.G);
   s.share = attn_share(p, s.cost[p.G + p.B]);
-  // tokens of short sequences: their group's prefix, then their own keys
-  const int n_rows = s.scum[p.B] * p.Hq;                    // (at most 2^31: checked by the plan)
+  // tokens of sequences with partial rows of their own: their group's prefix and their own keys, or both in one item
+  const int n_rows = s.pcum[p.B] * p.Hq;                    // (below 2^31: checked by the plan)
   for (int u = blockIdx.x * warps + warp; u < n_rows; u += gridDim.x * warps) {
-    const int i = u / p.Hq, head = u - i * p.Hq, b = short_sequence(s, 0, p.B, i), g = s.group[b];
+    const int i = u / p.Hq, head = u - i * p.Hq, b = sequence_of(s.pcum, 0, p.B, i), g = s.group[b], t = i - s.pcum[b];
     const int kvh = head / p.Gh, rh = head - kvh * p.Gh;
     float m = -CUDART_INF_F, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     AttnWalk k;
     k.done = false;
-    k.e = g; k.head = kvh;
-    k.x = attn_entity(p, s, g);
-    const int in_group = i - s.scum[s.gfirst[g]];
-    k.r = in_group / (2 * p.tps);
-    k.w = k.x.a;
-    k.at = s.cost[g] + (long long)(kvh * k.x.items + k.r) * k.x.a;
-    join_item<DP>(a, s, k, attn_item(p, s, k), (in_group - k.r * 2 * p.tps) * p.Gh + rh, m, l, o);
-    if (s.kv[b] > 0) {
-      k.e = p.G + b; k.r = 0;
+    k.head = kvh;
+    const bool shares = attn_is_short(p, s, b);
+#pragma unroll 1
+    for (int part = shares ? 0 : 1; part < 2; ++part) {
+      k.e = part ? p.G + b : g;
       k.x = attn_entity(p, s, k.e);
-      k.w = k.x.a;
-      k.at = s.cost[k.e] + kvh * k.x.a;
-      join_item<DP>(a, s, k, attn_item(p, s, k), (i - s.scum[b]) * p.Gh + rh, m, l, o);
+      if (k.x.items == 0) continue;                         // (no own keys)
+      const int at = part ? t : s.scum[b] - s.scum[s.gfirst[g]] + t;     // token among the entity's
+      k.r = at / (2 * p.tps);
+      k.w = k.x.a + k.x.slope * (k.r + 1);
+      k.at = s.cost[k.e] + kvh * attn_items_cost(k.x, k.x.items) + attn_items_cost(k.x, k.r);
+      const AttnItem it = attn_item(p, s, k);
+      if (!shares) {                                        // final already?
+        const int c = (int)(k.at / s.share);
+        if (attn_is_whole(it, attn_steps_before(k, it.n, c * s.share), attn_steps_before(k, it.n, (c + 1) * s.share))) { k.done = true; break; }
+      }
+      join_item<DP>(a, s, k, it, (at - k.r * 2 * p.tps) * p.Gh + rh, m, l, o);
     }
-    write_row<DP>(a, s.q0[b] + (i - s.scum[b]), head, m, l, o);
+    if (!k.done) write_row<DP>(a, s.q0[b] + t, head, m, l, o);
   }
-  // joint items that a cut between two CTAs' shares went through: found at their first cut
+  // longer sequences' items that a cut between two CTAs' shares went through: found at their first cut
   for (int c = 1 + blockIdx.x; c < p.n_ctas; c += gridDim.x) {
     const long long x = c * s.share;
     const AttnWalk k = attn_walk_at(p, s, x);
     if (k.done) break;
     const AttnItem it = attn_item(p, s, k);
-    if (it.kind != kAttnJoint) continue;
+    if (it.kind != kAttnJoint || attn_has_rows(p, s, it.b)) continue;
     const int before = attn_steps_before(k, it.n, x);
     if (before == 0 || before == it.n || attn_steps_before(k, it.n, x - s.share) > 0) continue;
     for (int r = warp; r < it.n_tok * p.Gh; r += warps) {

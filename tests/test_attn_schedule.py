@@ -36,7 +36,8 @@ def check(heads, kv_heads, q_len, kv_len, prefix_start, prefix_len, causal, n_ct
         items.setdefault(key, []).append(p)
         assert 0 < p["tokens"] <= tile and 0 <= p["head"] < kv_heads
         if p["row"] >= 0:
-            places.append((p["row"], p["row"] + p["tokens"] * Gh))
+            places.append((p["row"], p["row"] + p["results"] * p["tokens"] * Gh))
+            assert p["results"] in (1, 2) and p["results"] * p["tokens"] <= tile
         else:
             assert p["kind"] == 2
         cost[p["cta"]] = cost.get(p["cta"], 0) + p["cost"] * (p["end"] - p["first"]) / p["steps"]
@@ -71,7 +72,7 @@ def check(heads, kv_heads, q_len, kv_len, prefix_start, prefix_len, causal, n_ct
         assert all(p["tokens"] == want[key][0] and p["steps"] == want[key][1] for p in ps)
         assert ps[0]["first"] == 0 and ps[-1]["end"] == want[key][1]
         assert all(a["end"] == b["first"] and a["cta"] < b["cta"] for a, b in zip(ps, ps[1:]))
-        assert (len(ps) == 1 and key[0] == 2) == (ps[0]["row"] < 0)
+        assert (len(ps) == 1 and key[0] == 2 and ps[0]["results"] == 1) == (ps[0]["row"] < 0)
     return cost
 
 
