@@ -35,7 +35,8 @@ int check_config(const cep_attn_config* c) {
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128 && c->page_size != 256)
     return record_error(CEP_ERR_UNSUPPORTED, "attn: page_size must be 16, 32, 64, 128 or 256");
   if (c->n_pages <= 0) return record_error(CEP_ERR_ARG, "attn: n_pages must be positive");
-  if (c->max_tokens <= 0 || (long long)c->max_tokens * c->n_heads > 0x7fffffffll) return record_error(CEP_ERR_ARG, "attn: max_tokens must be positive, max_tokens * n_heads below 2^31");
+  if (c->max_tokens <= 0 || c->max_tokens > (1 << 22) || (long long)c->max_tokens * c->n_heads > 0x7fffffffll)
+    return record_error(CEP_ERR_ARG, "attn: max_tokens must be in 1..2^22, max_tokens * n_heads below 2^31");
   if (c->max_seqs <= 0 || c->max_seqs > kAttnMaxSeqs) return record_error(CEP_ERR_ARG, "attn: max_seqs must be in 1..%d", kAttnMaxSeqs);
   if (c->max_prefixes < 0 || c->max_prefixes > kAttnMaxPrefixes) return record_error(CEP_ERR_ARG, "attn: max_prefixes must be in 0..%d", kAttnMaxPrefixes);
   if (!(c->scale > 0.f) || c->scale > 3.402823466e38f) return record_error(CEP_ERR_ARG, "attn: the scale must be finite and positive");
@@ -195,8 +196,8 @@ int attn_prefix(cep_attn_plan* p, const cep_attn_batch* b, const void* q, const 
   const int rc = enter(p, st, &capturing);
   if (rc) return rc;
   AttnArgs a{};
-  a.p = AttnShape{b->n_tokens, b->n_seqs, b->n_prefixes, c.n_heads, c.n_kv_heads, c.n_heads / c.n_kv_heads, kAttnTile / (c.n_heads / c.n_kv_heads), b->causal != 0,
-                  b->table_width * c.page_size, b->prefix_width * c.page_size, p->n_ctas};
+  a.p = attn_shape(b->n_tokens, b->n_seqs, b->n_prefixes, c.n_heads, c.n_kv_heads, b->causal != 0, (long long)b->table_width * c.page_size,
+                   (long long)b->prefix_width * c.page_size, p->n_ctas);
   a.D = c.head_dim;
   while ((1 << a.page_shift) < c.page_size) ++a.page_shift;
   a.n_pages = c.n_pages;
@@ -248,9 +249,11 @@ int cep_debug_attn_schedule(const cep_attn_config* c, int32_t n_tokens, int32_t 
     return record_error(CEP_ERR_ARG, "attn: a schedule needs lengths, room and a positive grid");
   if (n_tokens > c->max_tokens || n_seqs > c->max_seqs || n_prefixes > c->max_prefixes || n_ctas > kAttnMaxCtas)
     return record_error(CEP_ERR_CAPACITY, "attn: more than the plan was made for");
-  const int Gh = c->n_heads / c->n_kv_heads;
-  const AttnShape p{n_tokens, n_seqs, n_prefixes, c->n_heads, c->n_kv_heads, Gh, kAttnTile / Gh, causal != 0, 1 << 30, 1 << 30, n_ctas};
-  long long* store = new (std::nothrow) long long[kAttnSchedBytes / 8 + 1];
+  long long own_cap = 0, prefix_cap = 0;
+  for (int i = 0; i < n_seqs; ++i) own_cap = std::max<long long>(own_cap, kv_len[i]);
+  for (int i = 0; i < n_prefixes; ++i) prefix_cap = std::max<long long>(prefix_cap, prefix_len[i]);
+  const AttnShape p = attn_shape(n_tokens, n_seqs, n_prefixes, c->n_heads, c->n_kv_heads, causal != 0, own_cap, prefix_cap, n_ctas);
+  int32_t* store = new (std::nothrow) int32_t[kAttnSchedBytes / 4];
   if (!store) return record_error(CEP_ERR_ARG, "attn: out of host memory");
   AttnSched s = attn_carve(store, p.B, p.G);
   for (int i = 0; i <= p.B; ++i) s.q0[i] = std::max(i ? s.q0[i - 1] : 0, std::min(std::max(q_start[i], 0), p.T));
@@ -268,14 +271,14 @@ int cep_debug_attn_schedule(const cep_attn_config* c, int32_t n_tokens, int32_t 
     s.pcum[b + 1] = s.pcum[b] + (attn_has_rows(p, s, b) ? s.q0[b + 1] - s.q0[b] : 0);
   }
   s.grt[0] = 0;
-  for (int g = 0; g < p.G; ++g) s.grt[g + 1] = s.grt[g] + attn_div_up(s.scum[s.gfirst[g + 1]] - s.scum[s.gfirst[g]], 2 * p.tps);
+  for (int g = 0; g < p.G; ++g) s.grt[g + 1] = s.grt[g] + attn_tiles(p, s.scum[s.gfirst[g + 1]] - s.scum[s.gfirst[g]]);
   s.cost[0] = 0;
   for (int e = 0; e < p.G + p.B; ++e) { const AttnEntity x = attn_entity(p, s, e); s.cost[e + 1] = s.cost[e] + p.Hkv * attn_items_cost(x, x.items); }
   s.share = attn_share(p, s.cost[p.G + p.B]);
   *part_rows = attn_max_part_rows(c->max_tokens, c->max_seqs, c->max_prefixes, c->n_heads, c->n_kv_heads, kAttnMaxCtas);
   int n = 0;
   for (int cta = 0; cta < n_ctas; ++cta) {
-    const long long x0 = cta * s.share, x1 = x0 + s.share;
+    const int x0 = cta * s.share, x1 = x0 + s.share;
     for (AttnWalk k = attn_walk_at(p, s, x0); !k.done && k.at < x1; attn_walk_next(p, s, &k)) {
       const AttnItem it = attn_item(p, s, k);
       const int s0 = attn_steps_before(k, it.n, x0), s1 = attn_steps_before(k, it.n, x1);

@@ -14,6 +14,8 @@
 // in the order of the cuts: nothing depends on timing.
 #pragma once
 #include "cep_common.h"
+#include <math.h>
+
 #include "gemm_tcgen05.h"
 
 namespace cep {
@@ -22,8 +24,8 @@ constexpr int kAttnTile = 128;               // keys of a step, rows of a row ti
 constexpr int kAttnMaxSeqs = 1024, kAttnMaxPrefixes = 256;
 constexpr int kAttnMaxCtas = 148;
 constexpr int kAttnSplitRows = 2 * 2 * kAttnTile;                      // partial rows that a CTA's two cut items may need
-// Estimated cost of a key for one row tile's pair of warpgroups and for two row tiles, and of an item beside its keys.
-constexpr int kAttnCostSingle = 10, kAttnCostDual = 16, kAttnCostItem = 2400;
+// Estimated cost of four keys for one row tile (taken by the warpgroups in turn) and for two, and of an item beside its keys.
+constexpr int kAttnCostSingle = 2, kAttnCostDual = 3, kAttnCostItem = 112;
 
 struct AttnShape {
   int T, B, G;                               // tokens, sequences, groups
@@ -32,6 +34,9 @@ struct AttnShape {
   int causal;
   int own_cap, prefix_cap;                   // keys that the page tables have room for
   int n_ctas;
+  float per_cta;                             // 1 / n_ctas
+  int cost_shift;                            // keeps the sum of all costs below 2^31
+  uint32_t tile_magic;                       // division by 2 tps: (x * tile_magic) >> 32
 };
 
 // The schedule of one call, in shared or in global memory.  
@@ -44,14 +49,14 @@ struct AttnSched {
   int32_t* glen;                             // [G] prefix keys
   int32_t* grt;                              // [G+1] group items of a kv head before this group
   int16_t* group;                            // [B] -1: no prefix
-  long long* cost;                           // [G+B+1] cost before each entity (a group or a sequence)
-  long long share;                           // of one CTA
+  int32_t* cost;                             // [G+B+1] cost before each entity (a group or a sequence)
+  int32_t share;                             // of one CTA
 };
-// The arrays of a schedule carved from `base` (8-byte aligned).
+// The arrays of a schedule carved from `base`.
 __host__ __device__ inline AttnSched attn_carve(void* base, int B, int G) {
   AttnSched s;
-  s.cost = static_cast<long long*>(base);
-  int32_t* p = reinterpret_cast<int32_t*>(s.cost + G + B + 1);
+  int32_t* p = static_cast<int32_t*>(base);
+  s.cost = p; p += G + B + 1;
   s.q0 = p; p += B + 1;
   s.kv = p; p += B;
   s.scum = p; p += B + 1;
@@ -63,10 +68,25 @@ __host__ __device__ inline AttnSched attn_carve(void* base, int B, int G) {
   s.share = 0;
   return s;
 }
-__host__ __device__ constexpr int attn_sched_words(int B, int G) { return 2 * (G + B + 1) + (4 * B + 3 + 3 * G + 2 + (B + 1) / 2 + 1) / 2 * 2; }   // 4-byte words, an even number
+__host__ __device__ constexpr int attn_sched_words(int B, int G) { return G + B + 1 + 4 * B + 3 + 3 * G + 2 + (B + 1) / 2; }      // 4-byte words
 constexpr int kAttnSchedBytes = attn_sched_words(kAttnMaxSeqs, kAttnMaxPrefixes) * 4;
 
-__host__ __device__ inline int attn_div_up(int a, int b) { return (a + b - 1) / b; }
+__host__ __device__ inline int attn_key_tiles(int keys) { return (keys + kAttnTile - 1) / kAttnTile; }
+
+__host__ __device__ inline int attn_tiles(const AttnShape& p, int tokens) {     // of 2 tps tokens
+#ifdef __CUDA_ARCH__
+  return __umulhi((uint32_t)(tokens + 2 * p.tps - 1), p.tile_magic);
+#else
+  return (int)((uint64_t)(uint32_t)(tokens + 2 * p.tps - 1) * p.tile_magic >> 32);
+#endif
+}
+// a / b without the long division: an estimate, put right by products.
+__host__ __device__ inline int attn_div(int a, int b) {
+  int q = (int)((float)a / (float)b);
+  while ((long long)q * b > a) --q;
+  while ((long long)(q + 1) * b <= a) ++q;
+  return q;
+}
 
 // Tokens that a group's prefix is shared by: sequences short enough to leave a row tile's rows empty, in a group of two or more.
 __host__ __device__ inline bool attn_is_short(const AttnShape& p, const AttnSched& s, int b) {
@@ -78,70 +98,74 @@ __host__ __device__ inline bool attn_is_short(const AttnShape& p, const AttnSche
 __host__ __device__ inline bool attn_has_rows(const AttnShape& p, const AttnSched& s, int b) { return s.q0[b + 1] - s.q0[b] <= 2 * p.tps; }
 
 // An entity's items per kv head, and what item r (0-based) of them costs: a + slope * (r + 1).
-struct AttnEntity { int items; long long a, slope; };
+struct AttnEntity { int items, a, slope; };
 __host__ __device__ inline AttnEntity attn_entity(const AttnShape& p, const AttnSched& s, int e) {
-  AttnEntity x;
-  x.slope = 0;
+  int n, keys, slope = 0;
+  bool some = true;
   if (e < p.G) {
-    const int n = s.scum[s.gfirst[e + 1]] - s.scum[s.gfirst[e]];
-    x.items = attn_div_up(n, 2 * p.tps);
-    x.a = kAttnCostItem + (long long)(n > p.tps ? kAttnCostDual : kAttnCostSingle) * s.glen[e];
-    return x;
+    n = s.scum[s.gfirst[e + 1]] - s.scum[s.gfirst[e]];
+    keys = s.glen[e];
+  } else {
+    const int b = e - p.G, g = s.group[b], kv = s.kv[b];
+    n = s.q0[b + 1] - s.q0[b];
+    keys = kv;
+    if (attn_is_short(p, s, b)) {
+      some = kv > 0;
+    } else {
+      if (p.causal) { keys = kv > n ? kv - n : 0; slope = 1; }
+      if (g >= 0) keys += s.glen[g];
+    }
   }
-  const int b = e - p.G, n = s.q0[b + 1] - s.q0[b], kv = s.kv[b];
-  const long long unit = n > p.tps ? kAttnCostDual : kAttnCostSingle;
-  if (attn_is_short(p, s, b)) {
-    x.items = kv > 0;
-    x.a = kAttnCostItem + unit * kv;
-    return x;
-  }
-  x.items = attn_div_up(n, 2 * p.tps);
-  const int g = s.group[b], ahead = g >= 0 ? s.glen[g] : 0;
-  x.a = kAttnCostItem + unit * ((long long)ahead + (p.causal ? (kv > n ? kv - n : 0) : kv));
-  if (p.causal) x.slope = unit * 2 * p.tps;
+  const int unit = n > p.tps ? kAttnCostDual : kAttnCostSingle;
+  AttnEntity x;
+  x.items = some ? attn_tiles(p, n) : 0;
+  x.a = (int)((kAttnCostItem + (long long)unit * (keys >> 2)) >> p.cost_shift) + 1;
+  x.slope = slope ? unit * 2 * p.tps >> (2 + p.cost_shift) : 0;
   return x;
 }
-__host__ __device__ inline long long attn_items_cost(const AttnEntity& x, long long r) { return r * x.a + x.slope * (r * (r + 1) / 2); }
+__host__ __device__ inline int attn_items_cost(const AttnEntity& x, int r) { return r * x.a + (x.slope ? x.slope * (int)(((long long)r * (r + 1)) >> 1) : 0); }
 
 // Where a CTA's walk over its items stands.
 struct AttnWalk {
   int e, head, r;                            // entity, kv head, item of these
-  long long at, w;                           // cost before the item, of the item
+  int at, w;                                 // cost before the item, of the item
   AttnEntity x;
   bool done;
 };
-__host__ __device__ inline void attn_walk_entity(const AttnShape& p, const AttnSched& s, AttnWalk* k) {
-  while (k->e < p.G + p.B && s.cost[k->e + 1] == s.cost[k->e]) ++k->e;       // entities without items
-  k->done = k->e >= p.G + p.B;
-  if (!k->done) k->x = attn_entity(p, s, k->e);
-}
-// The item that the point `x` of the cost axis lies in.
-__host__ __device__ inline AttnWalk attn_walk_at(const AttnShape& p, const AttnSched& s, long long x) {
+// The item that the point `x` of the cost axis lies in, which is in entity `e`.
+__host__ __device__ inline AttnWalk attn_walk_in(const AttnShape& p, const AttnSched& s, int e, int x) {
   AttnWalk k;
-  k.e = 0; k.head = 0; k.r = 0; k.at = 0; k.w = 0;
+  k.e = e; k.done = false;
+  k.x = attn_entity(p, s, e);
+  const int per_head = attn_items_cost(k.x, k.x.items);
+  int rest = x - s.cost[e];
+  k.head = attn_div(rest, per_head);
+  rest -= k.head * per_head;
+  int r;                                     // items_cost(r) <= rest < items_cost(r + 1)
+  if (k.x.slope == 0) {
+    r = attn_div(rest, k.x.a);
+  } else {                                   // the root of slope r^2 / 2 + (a + slope / 2) r = rest, put right by the sums themselves
+    const float h = (float)k.x.a / (float)k.x.slope + 0.5f;
+    r = (int)(sqrtf(h * h + 2.f * (float)rest / (float)k.x.slope) - h);
+    if (r > k.x.items - 1) r = k.x.items - 1;
+    while (r > 0 && attn_items_cost(k.x, r) > rest) --r;
+    while (attn_items_cost(k.x, r + 1) <= rest) ++r;
+  }
+  k.r = r;
+  k.at = x - (rest - attn_items_cost(k.x, r));
+  k.w = k.x.a + k.x.slope * (r + 1);
+  return k;
+}
+__host__ __device__ inline AttnWalk attn_walk_at(const AttnShape& p, const AttnSched& s, int x) {
   const int E = p.G + p.B;
-  k.done = x >= s.cost[E];
-  if (k.done) return k;
+  if (x >= s.cost[E]) { AttnWalk k; k.done = true; return k; }
   int lo = 0, hi = E;                        // cost[lo] <= x < cost[hi]
+#pragma unroll 1
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (s.cost[mid] <= x) lo = mid; else hi = mid;
   }
-  k.e = lo;
-  k.x = attn_entity(p, s, lo);
-  const long long per_head = attn_items_cost(k.x, k.x.items);
-  long long rest = x - s.cost[lo];
-  k.head = (int)(rest / per_head);
-  rest -= k.head * per_head;
-  int a = 0, b = k.x.items;                  // items_cost(a) <= rest < items_cost(b)
-  while (b - a > 1) {
-    const int mid = (a + b) >> 1;
-    if (attn_items_cost(k.x, mid) <= rest) a = mid; else b = mid;
-  }
-  k.r = a;
-  k.at = x - (rest - attn_items_cost(k.x, a));
-  k.w = k.x.a + k.x.slope * (a + 1);
-  return k;
+  return attn_walk_in(p, s, lo, x);
 }
 __host__ __device__ inline void attn_walk_next(const AttnShape& p, const AttnSched& s, AttnWalk* k) {
   k->at += k->w;
@@ -149,9 +173,10 @@ __host__ __device__ inline void attn_walk_next(const AttnShape& p, const AttnSch
     k->r = 0;
     if (++k->head == p.Hkv) {
       k->head = 0;
-      ++k->e;
-      attn_walk_entity(p, s, k);
+      do ++k->e; while (k->e < p.G + p.B && s.cost[k->e + 1] == s.cost[k->e]);       // entities without items
+      k->done = k->e >= p.G + p.B;
       if (k->done) return;
+      k->x = attn_entity(p, s, k->e);
     }
   }
   k->w = k->x.a + k->x.slope * (k->r + 1);
@@ -199,16 +224,18 @@ __host__ __device__ inline AttnItem attn_item(const AttnShape& p, const AttnSche
       it.own = seen < 0 ? 0 : seen < kv ? seen : kv;
     }
   }
-  it.n_ahead = attn_div_up(it.ahead, kAttnTile);
-  it.n = it.n_ahead + attn_div_up(it.own, kAttnTile);
+  it.n_ahead = attn_key_tiles(it.ahead);
+  it.n = it.n_ahead + attn_key_tiles(it.own);
   if (it.n == 0) it.n = 1;                   // rows that see nothing are written all the same
   return it;
 }
 // Steps of the item that lie before the point x.
-__host__ __device__ inline int attn_steps_before(const AttnWalk& k, int n, long long x) {
+__host__ __device__ inline int attn_steps_before(const AttnWalk& k, int n, int x) {
   if (x <= k.at) return 0;
   if (x >= k.at + k.w) return n;
-  return (int)(((x - k.at) * n + k.w - 1) / k.w);
+  // (in fp32: what counts is that it never falls with x, and that all who ask get the same)
+  const int steps = (int)ceilf((float)(x - k.at) * ((float)n / (float)k.w));
+  return steps < n ? steps : n;
 }
 // First partial row of what CTA c has of an item, steps from s0 on; and how many partial results that is, tok rows apart.
 __host__ __device__ inline long long attn_part_row(const AttnItem& it, int c, int s0) {
@@ -226,9 +253,24 @@ __host__ __device__ inline long long attn_max_part_rows(int max_tokens, int max_
 }
 
 // The cost that each CTA gets: equal shares, and no less than two steps, which two warpgroups take at the same time.
-__host__ __device__ inline long long attn_share(const AttnShape& p, long long total) {
-  const long long share = (total + p.n_ctas - 1) / p.n_ctas, least = 2ll * kAttnTile * kAttnCostSingle;
+__host__ __device__ inline int attn_share(const AttnShape& p, int total) {
+  // (fp32 is off by 2^-23 of the sum at most, which is less than one part in 10^4 of a share)
+  int share = (int)((float)total * p.per_cta) + 1 + (total >> 21);
+  const int least = 2 * (kAttnTile / 4) * kAttnCostSingle >> p.cost_shift;
   return share > least ? share : least;
+}
+
+inline AttnShape attn_shape(int T, int B, int G, int Hq, int Hkv, int causal, long long own_cap, long long prefix_cap, int n_ctas) {
+  AttnShape p{};
+  p.T = T; p.B = B; p.G = G; p.Hq = Hq; p.Hkv = Hkv; p.Gh = Hq / Hkv; p.tps = kAttnTile / p.Gh; p.causal = causal;
+  p.own_cap = (int)own_cap; p.prefix_cap = (int)prefix_cap;
+  p.n_ctas = n_ctas; p.per_cta = 1.f / n_ctas;
+  p.tile_magic = (uint32_t)(0x100000000ull / (2 * p.tps) + 1);
+  // more than all items can cost: every item with as many keys as the tables hold, and the slope's rounding
+  const double items = (double)Hkv * ((double)T / (2 * p.tps) + B + G);
+  const double most = items * (kAttnCostItem + 2 + kAttnCostDual * 0.25 * ((double)own_cap + (double)prefix_cap + T + 4 * p.tps));
+  while (ldexp(most, -p.cost_shift) + items > 2.0e9) ++p.cost_shift;
+  return p;
 }
 
 struct AttnArgs {

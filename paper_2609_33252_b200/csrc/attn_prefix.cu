@@ -20,9 +20,10 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kItemWarp = 10, kCodeWarp = 12;     // (kCodeWarp and the next three: e4m3 only)
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kItemWarp = 10, kMmaWarp2 = 11, kCodeWarp = 12;     // (kCodeWarp and the next three: e4m3 only)
 constexpr int kItemSlots = 8;                               // items between the warp that walks the schedule and the slowest reader
 constexpr int kMaxShared = 227 * 1024;
+constexpr int kPolynomial = 0x4a;                            // of eight pairs of weights, which go to the multiply-add units
 constexpr int kHalfBytes = kAttnTile * 128;                 // 128 rows of 64 bf16: what a 128-byte swizzled box column is
 
 // Shared memory: Q of two row tiles, the ring of K and V tiles, barriers and the like, the schedule; in an e4m3 cache's kernel the
@@ -83,13 +84,29 @@ __device__ __forceinline__ uint64_t make_v_desc(uint32_t saddr) {
 constexpr uint32_t kTransposeB = 1u << 16;           // instruction descriptor: B's rows are contiguous along N
 
 
+// The bounded wait of tcgen05_ptx.cuh in few instructions: the kernel's roles share an instruction cache.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  uint32_t spin = 0;
+  unsigned long long t0 = 0;
+#pragma unroll 1
+  while (!mbar_try_wait(bar, parity)) {
+    if ((++spin & 255u) != 0u) continue;
+    const unsigned long long now = globaltimer();
+    if (t0 == 0) t0 = now;
+    if (now - t0 > kWaitLimitNs) { *abort_flag = 1; atomicExch(&status[kStTimeout], 1); }
+    if (*abort_flag) return false;
+  }
+  return true;
+}
+
 // ---------------------------------------------------------------- the schedule
 // Exclusive scan of n pairs over the block: put(i, before); returns the totals.
-struct Pair { long long a; int b; };
+struct Pair { int a, b; };
 template <typename Get, typename Put>
 __device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_totals) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
   Pair carry{0, 0};
+#pragma unroll 1
   for (int base = 0; base < n; base += blockDim.x) {
     const int i = base + tid;
     Pair v{0, 0};
@@ -97,7 +114,7 @@ __device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_t
     const Pair own = v;
 #pragma unroll 1
     for (int d = 1; d < 32; d <<= 1) {
-      const long long a = __shfl_up_sync(0xffffffffu, v.a, d);
+      const int a = __shfl_up_sync(0xffffffffu, v.a, d);
       const int b = __shfl_up_sync(0xffffffffu, v.b, d);
       if (lane >= d) { v.a += a; v.b += b; }
     }
@@ -109,7 +126,7 @@ __device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_t
     Pair mine = ahead;
 #pragma unroll 1
     for (int d = 16; d; d >>= 1) {                          // sums over the warps before this one, and over all
-      const long long a = __shfl_xor_sync(0xffffffffu, w.a, d);
+      const int a = __shfl_xor_sync(0xffffffffu, w.a, d);
       const int b = __shfl_xor_sync(0xffffffffu, w.b, d);
       w.a += a; w.b += b;
     }
@@ -118,7 +135,7 @@ __device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_t
     if (lane < warp) x = warp_totals[lane];
 #pragma unroll 1
     for (int d = 16; d; d >>= 1) {
-      const long long a = __shfl_xor_sync(0xffffffffu, x.a, d);
+      const int a = __shfl_xor_sync(0xffffffffu, x.a, d);
       const int b = __shfl_xor_sync(0xffffffffu, x.b, d);
       x.a += a; x.b += b;
     }
@@ -131,20 +148,24 @@ __device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_t
 
 // Starts that fall are held at the largest before them (this is not what a correct call needs: one thread).
 __device__ __forceinline__ void never_fall(int32_t* v, int n) {
+#pragma unroll 1
   for (int i = 1; i < n; ++i) if (v[i] < v[i - 1]) v[i] = v[i - 1];
 }
 
 // Every CTA computes the whole schedule from the lengths.  What does not fit the call is cut to what does and reported.
-__device__ __forceinline__ void build_schedule(const AttnArgs& a, AttnSched& s, Pair* scratch) {
+// first_entity: where this CTA's share begins (-1: behind the end).
+__device__ __forceinline__ void build_schedule(const AttnArgs& a, AttnSched& s, Pair* scratch, volatile int* first_entity) {
   const AttnShape& p = a.p;
   const int tid = threadIdx.x, nt = blockDim.x;
   int bad = 0, falls = 0;
   auto take = [&](int v, int hi) { const int c = v < 0 ? 0 : v > hi ? hi : v; bad |= c != v; return c; };
+#pragma unroll 1
   for (int i = tid; i <= p.B; i += nt) {
     const int v = a.q_start[i];
     if (i < p.B) { falls |= a.q_start[i + 1] < v; s.kv[i] = take(a.kv_len[i], p.own_cap); }
     s.q0[i] = take(v, p.T);
   }
+#pragma unroll 1
   for (int i = tid; i <= p.G; i += nt) {
     if (i < p.G) s.glen[i] = take(a.prefix_len[i], p.prefix_cap);
     if (!a.prefix_start) { s.gfirst[i] = i && p.G ? p.B : 0; continue; }
@@ -162,6 +183,7 @@ __device__ __forceinline__ void build_schedule(const AttnArgs& a, AttnSched& s, 
         int g = -1;
         if (b >= s.gfirst[0] && b < s.gfirst[p.G]) {       // the last group that starts at or before b
           int lo = 0, hi = p.G;
+#pragma unroll 1
           while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s.gfirst[mid] <= b) lo = mid; else hi = mid; }
           g = lo;
         }
@@ -169,20 +191,26 @@ __device__ __forceinline__ void build_schedule(const AttnArgs& a, AttnSched& s, 
         const int n = s.q0[b + 1] - s.q0[b];
         return Pair{attn_has_rows(p, s, b) ? n : 0, attn_is_short(p, s, b) ? n : 0};
       },
-      [&](int b, const Pair& before) { s.pcum[b] = (int)before.a; s.scum[b] = before.b; }, scratch);
-  if (tid == 0) { s.pcum[p.B] = (int)places.a; s.scum[p.B] = places.b; }
+      [&](int b, const Pair& before) { s.pcum[b] = before.a; s.scum[b] = before.b; }, scratch);
+  if (tid == 0) { s.pcum[p.B] = places.a; s.scum[p.B] = places.b; }
   __syncthreads();
   const Pair total = block_scan(p.G + p.B,
       [&](int e) { const AttnEntity x = attn_entity(p, s, e); return Pair{p.Hkv * attn_items_cost(x, x.items), e < p.G ? x.items : 0}; },
       [&](int e, const Pair& before) { s.cost[e] = before.a; if (e < p.G) s.grt[e] = before.b; }, scratch);
-  if (tid == 0) { s.cost[p.G + p.B] = total.a; s.grt[p.G] = total.b; }
+  if (tid == 0) { s.cost[p.G + p.B] = total.a; s.grt[p.G] = total.b; *first_entity = -1; }
   s.share = attn_share(p, total.a);
+  __syncthreads();
+  const int x0 = blockIdx.x * s.share;
+#pragma unroll 1
+  for (int e = tid; e < p.G + p.B; e += nt)
+    if (s.cost[e] <= x0 && x0 < s.cost[e + 1]) *first_entity = e;
   if (bad) atomicExch(&a.status[kStBoundsViolation], 1);
   __syncthreads();
 }
 
 // The sequence (lo <= b < hi) with before[b] <= i < before[b + 1].
 __device__ __forceinline__ int sequence_of(const int32_t* before, int lo, int hi, int i) {
+#pragma unroll 1
   while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (before[mid] <= i) lo = mid; else hi = mid; }
   return lo;
 }
@@ -208,13 +236,6 @@ __device__ __forceinline__ uint32_t pos_v(uint32_t t) { return 2 * t + 2; }
 // Of an item whose first tile is t0, a warpgroup has all tiles (two row tiles) or those with its parity.
 __device__ __forceinline__ int first_step(uint32_t t0, bool dual, int wg) { return dual ? 0 : (int)((t0 + wg) & 1); }
 
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-
 // Two fp32 values in one 64-bit register pair: one instruction multiplies and adds both.
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pair2(float lo, float hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
@@ -223,6 +244,35 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm(
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { uint32_t r; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
+
+__device__ __forceinline__ float max3_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+
+// 2^x of a pair on the multiply-add units, which have time while the unit that exponentials go to has none: x = n + f, n the nearest
+// whole number (Cody and Waite's reduction: adding 1.5 * 2^23 rounds and leaves n in the low bits), 2^f by the polynomial of degree 4 with constant 1
+// whose largest relative error on [-1/2, 1/2] is least (2.8e-6; a weight's own rounding is 2^-9 or 2^-12).  x up to 127; -127 and
+// below give exactly 0; NaN does not survive.
+__device__ __forceinline__ void ex2_pair(f32x2 x, float& lo, float& hi) {
+  float a, b;
+  unpair2(x, a, b);
+  x = pair2(fmaxf(a, -127.f), fmaxf(b, -127.f));
+  const f32x2 r = add2(x, pair2(12582912.f, 12582912.f)), n = add2(r, pair2(-12582912.f, -12582912.f)), f = fma2(n, pair2(-1.f, -1.f), x);
+  f32x2 y = fma2(f, pair2(0.009585382416844368f, 0.009585382416844368f), pair2(0.05590662732720375f, 0.05590662732720375f));
+  y = fma2(y, f, pair2(0.24024038016796112f, 0.24024038016796112f));
+  y = fma2(y, f, pair2(0.6931241750717163f, 0.6931241750717163f));
+  y = fma2(y, f, pair2(1.f, 1.f));
+  float r0, r1;
+  unpair2(r, r0, r1);
+  unpair2(y, a, b);
+  lo = __int_as_float(__float_as_int(a) + (__float_as_int(r0) << 23));
+  hi = __int_as_float(__float_as_int(b) + (__float_as_int(r1) << 23));
+}
+
+// What tcgen05.ld brought may be used from here on (the wait before this has seen it arrive).
+__device__ __forceinline__ void arrived(uint32_t (&r)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+}
 
 // ---------------------------------------------------------------- the kernel
 template <int DP, bool E4M3>
@@ -234,9 +284,10 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   const uint32_t sbase = smem_u32(smem);
   const uint32_t bar0 = sbase + L::misc;
   const uint32_t full = bar0, empty = bar0 + 64, s_full = bar0 + 128, p_ready = bar0 + 144, o_done = bar0 + 160, q_ready = bar0 + 176,
-                 w_full = bar0 + 192, w_empty = bar0 + 256, code_full = bar0 + 320, code_empty = bar0 + 384;
+                 w_full = bar0 + 192, w_empty = bar0 + 256, code_full = bar0 + 320, code_empty = bar0 + 384, p_half = bar0 + 464;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::misc + 448);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::misc + 452);
+  volatile int* first_entity = reinterpret_cast<volatile int*>(smem + L::misc + 456);
   Pair* scratch = reinterpret_cast<Pair*>(smem + L::misc + 512);                       // a block's warps' totals
   const Work* work = reinterpret_cast<const Work*>(smem + L::misc + 1024);
   const int words = attn_sched_words(a.p.B, a.p.G), n_codes = L::code_slots(words);
@@ -244,9 +295,9 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < L::stages; ++i) { mbar_init(full + 8 * i, E4M3 ? 4 : 1); mbar_init(empty + 8 * i, 1); }
+    for (int i = 0; i < L::stages; ++i) { mbar_init(full + 8 * i, E4M3 ? 4 : 1); mbar_init(empty + 8 * i, 2); }
     for (int i = 0; i < n_codes; ++i) { mbar_init(code_full + 8 * i, 1); mbar_init(code_empty + 8 * i, 4); }
-    for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(o_done + 8 * i, 1); mbar_init(q_ready + 8 * i, 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(p_half + 8 * i, 4); mbar_init(o_done + 8 * i, 1); mbar_init(q_ready + 8 * i, 4); }
     // readers of an item: the loading warp, the products of each warpgroup, eight row warps, four decoding warps
     for (int i = 0; i < kItemSlots; ++i) { mbar_init(w_full + 8 * i, 1); mbar_init(w_empty + 8 * i, E4M3 ? 15 : 11); }
     *abort_flag = 0;
@@ -265,12 +316,12 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   pdl_enter();
   const AttnShape& p = a.p;
   AttnSched s = attn_carve(sched_at, p.B, p.G);
-  build_schedule(a, s, scratch);
+  build_schedule(a, s, scratch, first_entity);
 
   // the next item; every reader gives it back after its last look
   uint32_t turn = 0;
   auto take = [&]() -> const Work& {
-    mbar_wait(w_full + 8 * (turn % kItemSlots), (turn / kItemSlots) & 1, abort_flag, a.status);
+    wait_bar(w_full + 8 * (turn % kItemSlots), (turn / kItemSlots) & 1, abort_flag, a.status);
     return work[turn % kItemSlots];
   };
   auto give_back = [&]() {
@@ -295,35 +346,37 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     uint32_t issued = 0;
     Work it;
     int j = 0;
-    // What a lane has to fetch of the tile (item `it`, step j): its page (-1: none) and the rest.
-    struct Fetch { int page, in_page, head; };
+    // What a lane has to fetch of the tile (item `it`, step j).
+    struct Fetch { int page, in_page, head; bool want; };
     auto look = [&]() -> Fetch {
       int key0;
       const int keys = keys_of(it, j, key0), key = lane << box_shift;
-      Fetch f{-1, key0 & (page - 1), it.head};
-      if (lane < (kAttnTile >> box_shift) && key < keys) {
+      Fetch f{0, key0 & (page - 1), it.head, lane < (kAttnTile >> box_shift) && key < keys};
+      if (f.want) {
         const int32_t* table = it.s0 + j < it.n_ahead ? a.prefix_pages + (long long)it.g * a.prefix_stride : a.page_table + (long long)it.b * a.table_stride;
         f.page = table[(key0 + key) >> a.page_shift];
-        if (f.page < 0 || f.page >= a.n_pages) { bad = 1; f.page = a.n_pages; }        // (reads zeros)
       }
       return f;
     };
     auto load = [&](uint32_t pos, const CUtensorMap* tm, const Fetch& f) {
       const int st = pos % places;
       const uint32_t landed = (E4M3 ? code_full : full) + 8 * st, free = (E4M3 ? code_empty : empty) + 8 * st;
-      alive = __all_sync(0xffffffffu, mbar_wait(free, ((pos / places) & 1) ^ 1, abort_flag, a.status));
+      alive = __all_sync(0xffffffffu, wait_bar(free, ((pos / places) & 1) ^ 1, abort_flag, a.status));
       if (!alive) return;
       issued = pos + 1;
-      const int pages = __popc(__ballot_sync(0xffffffffu, f.page >= 0));
+      const int pages = __popc(__ballot_sync(0xffffffffu, f.want));
+      const bool known = f.page >= 0 && f.page < a.n_pages;
+      const int from = known ? f.page : a.n_pages;          // (behind the last page: reads zeros)
+      bad |= f.want && !known;
       if (lane == 0) mbar_expect_tx(landed, pages * box * (E4M3 ? DP : 128 * L::halves));
       __syncwarp();
-      if (f.page >= 0) {
+      if (f.want) {
         if (E4M3) {
-          tma_load_4d(sbase + L::codes + st * L::code_bytes + (lane << box_shift) * DP, tm, 0, f.in_page, f.head, f.page, landed);
+          tma_load_4d(sbase + L::codes + st * L::code_bytes + (lane << box_shift) * DP, tm, 0, f.in_page, f.head, from, landed);
         } else {
 #pragma unroll
           for (int h = 0; h < L::halves; ++h)
-            tma_load_4d(sbase + L::ring + st * L::tile_bytes + h * kHalfBytes + ((lane << box_shift) * 128), tm, h * 64, f.in_page, f.head, f.page, landed);
+            tma_load_4d(sbase + L::ring + st * L::tile_bytes + h * kHalfBytes + ((lane << box_shift) * 128), tm, h * 64, f.in_page, f.head, from, landed);
         }
       }
       __syncwarp();
@@ -337,20 +390,22 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       return true;
     };
     it.n = 0;
-    bool more = next_tile();
-    Fetch next, last;
-    if (more) next = look();
-    uint32_t t = 0;
-    while (more && alive) {
-      const Fetch now = next;
-      more = next_tile();
-      if (more) next = look();                              // (its page ids arrive while this tile waits for its place)
-      load(pos_k(t), &tm_k, now);
-      if (t && alive) load(pos_v(t - 1), &tm_v, last);
-      last = now;
-      ++t;
+    bool more = true;
+    Fetch next, now, last;
+    next.want = false;
+    // tile t's K, then tile t - 1's V; the page ids of tile t + 1 arrive while tile t waits for its place
+    for (uint32_t t = 0; alive; ++t) {
+      last = now; now = next;
+      const bool have = more;                               // (in the first round: a tile that is none)
+      more = more && next_tile();
+      if (more) next = look();
+      if (t == 0) { if (!more) break; continue; }
+#pragma unroll 1
+      for (int v = 0; v < 2; ++v) {                         // tiles are numbered from 0, rounds from 1
+        if (v == 0 ? have : t > 1) { if (alive) load(v == 0 ? pos_k(t - 1) : pos_v(t - 2), v == 0 ? &tm_k : &tm_v, v == 0 ? now : last); }
+      }
+      if (!have) break;
     }
-    if (t && alive) load(pos_v(t - 1), &tm_v, last);
     if (bad) atomicExch(&a.status[kStBadRouting], 1);
     if (!alive) {                                           // copies in flight land before the block's memory is given up
       const unsigned long long t0 = globaltimer();
@@ -360,8 +415,10 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   } else if (warp == kItemWarp) {
     // ------------------------------------------------------ the CTA's share of the schedule, item by item
     if (lane == 0) {
-      const long long x0 = (long long)blockIdx.x * s.share, x1 = x0 + s.share;
-      AttnWalk k = attn_walk_at(p, s, x0);
+      const int x0 = blockIdx.x * s.share, x1 = x0 + s.share;
+      AttnWalk k;
+      k.done = *first_entity < 0;
+      if (!k.done) k = attn_walk_in(p, s, *first_entity, x0);
       Work* out = const_cast<Work*>(work);
       for (;;) {
         Work w;
@@ -383,7 +440,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             w.seen = s.kv[it.b] - (s.q0[it.b + 1] - s.q0[it.b]) + it.tok + 1;
           }
         }
-        if (!mbar_wait(w_empty + 8 * (turn % kItemSlots), ((turn / kItemSlots) & 1) ^ 1, abort_flag, a.status)) break;
+        if (!wait_bar(w_empty + 8 * (turn % kItemSlots), ((turn / kItemSlots) & 1) ^ 1, abort_flag, a.status)) break;
         out[turn % kItemSlots] = w;
         mbar_arrive(w_full + 8 * (turn % kItemSlots));
         ++turn;
@@ -394,94 +451,68 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     if (blockIdx.x == 0) {                                  // the schedule, for the kernel that joins partial results
       int32_t* dst = static_cast<int32_t*>(a.sched);
       const int32_t* src = reinterpret_cast<const int32_t*>(sched_at);
+#pragma unroll 1
       for (int i = lane; i < words; i += 32) dst[i] = src[i];
     }
-  } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------ tensor core, one thread
+  } else if (warp == kMmaWarp || warp == kMmaWarp2) {
+    // ------------------------------------------------------ tensor core: one thread for each warpgroup's products
+    // (A tcgen05 instruction costs the thread that issues it some 60 cycles, as long as the products here take: one thread for both
+    // would be what bounds the kernel.)
     if (lane == 0) {
       constexpr uint32_t type = E4M3 ? (1u << 7) | (1u << 10) : 0u;         // codes are decoded to fp16, whose type bits are 0 (bf16: 1)
       constexpr uint32_t idesc_s = make_idesc_bf16(128, 128) ^ type, idesc_o = (make_idesc_bf16(128, DP) | kTransposeB) ^ type;
-      // Each warpgroup's place in the stream: what it needs next is an item, a tile's Q K^T or its P V.
-      enum { kItem, kScores, kProduct, kEnd };
-      struct Side { uint32_t turn, t0; int n, j, state; bool dual; uint32_t q_phase, p_phase; } side[2];
-#pragma unroll
-      for (int w = 0; w < 2; ++w) side[w] = Side{0, 0, 0, 0, kItem, false, 0, 0};
-      uint32_t half_used = 0;                               // stages that one of a pair of warpgroups is through with
+      const int w = warp == kMmaWarp2;
+      const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
+      const uint64_t qd = make_smem_desc(sbase + L::q + w * L::tile_bytes);
+      uint32_t t0 = 0, q_phase = 0, p_phase = 0;
+      bool alive = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) { alive = alive && wait_bar(bar, parity & 1, abort_flag, a.status); };
+      // A stage is free when both threads say so; a tile of one warpgroup is none of the other's business.
       auto free_stage = [&](bool dual, int st) {
-        if (dual && !(half_used >> st & 1)) { half_used |= 1u << st; return; }
-        half_used &= ~(1u << st);
         tc_commit(empty + 8 * st);
+        if (!dual) mbar_arrive(empty + 8 * st);
       };
-      unsigned long long since = globaltimer();
-      uint32_t idle = 0;
-      while (side[0].state != kEnd || side[1].state != kEnd) {
-        bool moved = false;
+#pragma unroll 1
+      while (alive) {
+        const Work& it = take();
+        const int n = it.n;
+        const bool dual = it.flags & kDual;
+        if (n == 0 || *abort_flag) break;
+        mbar_arrive(w_empty + 8 * (turn % kItemSlots));
+        ++turn;
+        const int j0 = first_step(t0, dual, w);
+        if (j0 < n) wait(q_ready + 8 * w, q_phase++);
+#pragma unroll 1
+        for (int j = j0; j < n && alive; j += dual ? 1 : 2) {
+          const uint32_t pk = pos_k(t0 + j), pv = pos_v(t0 + j);
+          const int sk = pk % L::stages, sv = pv % L::stages;
+          wait(full + 8 * sk, pk / L::stages);
+          if (!alive) break;
+          tc_fence_after();
+          const uint64_t kd = make_smem_desc(sbase + L::ring + sk * L::tile_bytes);
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          Side& x = side[w];
-          if (x.state == kProduct) {
-            const uint32_t t = x.t0 + x.j, pos = pos_v(t);
-            const int st = pos % L::stages;
-            if (mbar_test(p_ready + 8 * w, x.p_phase & 1) && mbar_test(full + 8 * st, (pos / L::stages) & 1)) {
-              tc_fence_after();
-              ++x.p_phase;
-              const bool first = x.j < (x.dual ? 1 : 2);
-              const uint64_t vd = make_v_desc(sbase + L::ring + st * L::tile_bytes);
+          for (int i = 0; i < DP / 16; ++i) {
+            const uint64_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;
+            tc_mma_f16(t_s, qd + off, kd + off, idesc_s, i > 0);
+          }
+          tc_commit(s_full + 8 * w);
+          free_stage(dual, sk);
+          wait(full + 8 * sv, pv / L::stages);
+          const uint64_t vd = make_v_desc(sbase + L::ring + sv * L::tile_bytes);
+          const uint32_t more = j != j0;
 #pragma unroll
-              for (int i = 0; i < kAttnTile / 16; ++i)
-                tc_mma_f16_ts(tmem + 256 + w * 128, tmem + w * 128 + i * 8, vd + ((i * 16 * 128) >> 4), idesc_o, !first || i > 0);
-              free_stage(x.dual, st);
-              x.j += x.dual ? 1 : 2;
-              x.state = kScores;
-              if (x.j >= x.n) {
-                tc_commit(o_done + 8 * w);
-                x.t0 += x.n;
-                x.state = kItem;
-              }
-              moved = true;
-            }
-          }
-          if (x.state == kItem && mbar_test(w_full + 8 * (x.turn % kItemSlots), (x.turn / kItemSlots) & 1)) {
-            const Work& it = work[x.turn % kItemSlots];
-            x.n = it.n;
-            x.dual = it.flags & kDual;
-            if (x.n == 0) {
-              x.state = kEnd;
-            } else {
-              mbar_arrive(w_empty + 8 * (x.turn % kItemSlots));
-              ++x.turn;
-              x.j = first_step(x.t0, x.dual, w);
-              if (x.j < x.n) x.state = kScores; else x.t0 += x.n;
-            }
-            moved = true;
-          }
-          if (x.state == kScores) {
-            const uint32_t t = x.t0 + x.j, pos = pos_k(t);
-            const int st = pos % L::stages;
-            const bool first = x.j < (x.dual ? 1 : 2);
-            if ((!first || mbar_test(q_ready + 8 * w, x.q_phase & 1)) && mbar_test(full + 8 * st, (pos / L::stages) & 1)) {
-              tc_fence_after();
-              x.q_phase += first;
-              const uint64_t qd = make_smem_desc(sbase + L::q + w * L::tile_bytes);
-              const uint64_t kd = make_smem_desc(sbase + L::ring + st * L::tile_bytes);
+          for (int h = 0; h < 2; ++h) {                     // the first half of the weights is in place before the second
+            wait((h ? p_ready : p_half) + 8 * w, p_phase);
+            if (!alive) break;
+            tc_fence_after();
 #pragma unroll
-              for (int i = 0; i < DP / 16; ++i) {
-                const uint64_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;
-                tc_mma_f16(tmem + w * 128, qd + off, kd + off, idesc_s, i > 0);
-              }
-              tc_commit(s_full + 8 * w);
-              free_stage(x.dual, st);
-              x.state = kProduct;
-              moved = true;
-            }
+            for (int i = 4 * h; i < 4 * h + 4; ++i) tc_mma_f16_ts(t_o, t_s + i * 8, vd + ((i * 16 * 128) >> 4), idesc_o, i ? 1u : more);
           }
+          ++p_phase;
+          free_stage(dual, sv);
+          if (j + (dual ? 1 : 2) >= n) tc_commit(o_done + 8 * w);
         }
-        if (moved) { idle = 0; continue; }
-        if ((++idle & 1023u) == 0u) {                       // (a wait with a limit, as everywhere)
-          if (*abort_flag) break;
-          if (idle == 1024u) since = globaltimer();
-          else if (globaltimer() - since > kWaitLimitNs) { *abort_flag = 1; atomicExch(&a.status[kStTimeout], 1); break; }
-        }
+        t0 += n;
       }
     }
     __syncwarp();
@@ -491,8 +522,8 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     bool alive = true;
     auto decode = [&](uint32_t pos, int keys) {
       const int st = pos % L::stages, slot = pos % n_codes;
-      const bool ok = mbar_wait(code_full + 8 * slot, (pos / n_codes) & 1, abort_flag, a.status) &&
-                      mbar_wait(empty + 8 * st, ((pos / L::stages) & 1) ^ 1, abort_flag, a.status);
+      const bool ok = wait_bar(code_full + 8 * slot, (pos / n_codes) & 1, abort_flag, a.status) &&
+                      wait_bar(empty + 8 * st, ((pos / L::stages) & 1) ^ 1, abort_flag, a.status);
       alive = __all_sync(0xffffffffu, ok);
       if (!alive) return;
       const uint8_t* src = smem + L::codes + slot * L::code_bytes;
@@ -521,25 +552,30 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       if (lane == 0) { mbar_arrive(code_empty + 8 * slot); mbar_arrive(full + 8 * st); }
     };
     uint32_t t = 0;
-    int before = 0;
-    while (alive) {
-      const Work it = take();
-      if (__any_sync(0xffffffffu, it.n == 0 || *abort_flag)) break;
-      give_back();
-      for (int j = 0; j < it.n && alive; ++j) {
-        int key0;
-        const int keys = keys_of(it, j, key0);
-        decode(pos_k(t), keys);
-        if (t && alive) decode(pos_v(t - 1), before);
-        before = keys;
-        ++t;
+    int before = 0, j = 0;
+    bool more = true;
+    Work it;
+    it.n = 0;
+#pragma unroll 1
+    while (more && alive) {
+      if (j == it.n) {
+        it = take();
+        more = !__any_sync(0xffffffffu, it.n == 0 || *abort_flag);
+        if (more) give_back();
+        j = 0;
       }
+      int key0, keys = 0;
+      if (more) keys = keys_of(it, j, key0);
+#pragma unroll 1
+      for (int v = 0; v < 2; ++v)                           // a tile's K, then the tile before's V
+        if ((v == 0 ? more : t > 0) && alive) decode(v == 0 ? pos_k(t) : pos_v(t - 1), v == 0 ? keys : before);
+      before = keys;
+      ++t; ++j;
     }
-    if (t && alive) decode(pos_v(t - 1), before);
   } else if (warp < kMmaWarp) {
     // ------------------------------------------------------ rows: softmax, corrections, results
     // (After a wait that was given up an item's steps run on with what is there: what a warp does must not differ by lane.)
-    const int wg = warp >> 2, row = tid & 127, row_tok = row / p.Gh, row_head = row - row_tok * p.Gh;
+    const int wg = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
     const uint32_t t_s = tmem + lanes + wg * 128, t_o = tmem + lanes + 256 + wg * 128;
     uint32_t s_phase = 0, o_phase = 0, t0 = 0;
@@ -556,6 +592,9 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         if (j >= n) { give_back(); t0 += n; continue; }
         r.n = n; r.j = j; r.t0 = t0; r.dual = dual; r.whole = it.flags & kWhole;
         r.s0 = it.s0; r.n_ahead = it.n_ahead; r.ahead = it.ahead; r.own = it.own;
+        // Two row tiles: the second follows the first.  One: the second warpgroup's rows lie half a tile further, as few rows would
+        // otherwise be the work of one scheduler's warps.
+        const int at = dual ? row : row ^ (wg << 6), row_tok = attn_div(at, p.Gh), row_head = at - row_tok * p.Gh;
         const int tt = (dual ? wg * p.tps : 0) + row_tok, kvh = it.head;      // token of the item
         r.mine = row_tok < p.tps && tt < it.n_tok;
         r.token = it.tok + tt;
@@ -611,107 +650,12 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         return true;
       }
     };
-    Row r, next;
-    bool more = next_item(next);
-    while (more) {
-      r = next;
-      float m = -CUDART_INF_F, l = 0.f;                     // maximum that the sums refer to (unscaled), sum
-      bool any = false;                                     // O holds something
-#pragma unroll 1
-      for (int j = r.j; j < r.n; j += r.dual ? 1 : 2) {
-        const int step = r.s0 + j;
-        const bool in_ahead = step < r.n_ahead;
-        const int key0 = (in_ahead ? step : step - r.n_ahead) * kAttnTile, keys = (in_ahead ? r.ahead : r.own) - key0;
-        mbar_wait(s_full + 8 * wg, s_phase & 1, abort_flag, a.status);
-        ++s_phase;
-        tc_fence_after();
-        if (!E4M3 && keys < kAttnTile) {                    // what lies behind the last key may be anything: its weight 0 needs a finite value.
-          // (Not before S: only then has this stage's use before last ended, and the parity tells the uses apart.)
-          const uint32_t pos = pos_v(r.t0 + j);
-          mbar_wait(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status);
-          uint8_t* v = smem + L::ring + (pos % L::stages) * L::tile_bytes;
-          const int from = keys < 0 ? 0 : keys;
-          for (int h = 0; h < L::halves; ++h)
-            for (int i = from * 8 + (tid & 127); i < kAttnTile * 8; i += 128) *reinterpret_cast<uint4*>(v + h * kHalfBytes + i * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
-        }
-        if (r.active) {
-          // S is held in registers where there are enough, else read twice.
-          constexpr int held = E4M3 ? 1 : 4;
-          uint32_t x[held][32];
-          const int see = in_ahead ? keys : (r.seen - key0 < keys ? r.seen - key0 : keys);
-          const bool hide = __any_sync(0xffffffffu, see < kAttnTile);
-          auto mask = [&](int c) {
-            if (hide) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[c % held][i] = c * 32 + i < see ? x[c % held][i] : 0xff800000u;
-            }
-          };
-          if (held == 4) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tc_ld32(t_s + c * 32, x[c % held]);
-            tc_wait_ld();
-          }
-          float top[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (held == 1) { tc_ld32(t_s + c * 32, x[0]); tc_wait_ld(); }
-            mask(c);
-            uint32_t (&y)[32] = x[c % held];
-            top[c] = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
-#pragma unroll
-            for (int i = 2; i < 32; i += 2) top[c] = max3(top[c], __uint_as_float(y[i]), __uint_as_float(y[i + 1]));
-          }
-          const float m_new = max3(max3(m, top[0], top[1]), top[2], top[3]);
-          // The sums keep referring to an older maximum until weights could pass 2^8: fp32 and the weights' type carry that exactly as well.
-          const bool raise = m_new > m && (m_new - m) * r.sl2 > 8.f;
-          if (!any) {
-            m = m_new;
-          } else if (__any_sync(0xffffffffu, raise)) {
-            const float f = raise ? ex2((m - m_new) * r.sl2) : 1.f;
-            if (raise) { m = m_new; l *= f; }
-#pragma unroll 1
-            for (int c = 0; c < DP / 16; ++c) {
-              uint32_t o[16];
-              tc_ld16(t_o + c * 16, o);
-              tc_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tc_st16(t_o + c * 16, o);
-            }
-            tc_wait_st();
-          }
-          any = true;
-          const float shift = m == -CUDART_INF_F ? 0.f : -m * r.sl2;
-          const f32x2 scale2 = pair2(r.sl2, r.sl2), shift2 = pair2(shift, shift);
-          f32x2 sum[2] = {0, 0};
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (held == 1) { tc_ld32(t_s + c * 32, x[0]); tc_wait_ld(); mask(c); }
-            uint32_t w[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float p0, p1;
-              unpair2(fma2(pair2(__uint_as_float(x[c % held][2 * i]), __uint_as_float(x[c % held][2 * i + 1])), scale2, shift2), p0, p1);
-              p0 = ex2(p0); p1 = ex2(p1);
-              sum[i & 1] = add2(sum[i & 1], pair2(p0, p1));
-              w[i] = E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
-            }
-            tc_st16(t_s + c * 16, w);
-          }
-          float s0, s1;
-          unpair2(add2(sum[0], sum[1]), s0, s1);
-          l += s0 + s1;
-          tc_wait_st();
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready + 8 * wg);
-      }
-      more = next_item(next);                               // (its Q arrives while the last product runs)
-
-      // ---- the item's result
-      mbar_wait(o_done + 8 * wg, o_phase & 1, abort_flag, a.status);
+    Row r{}, next{};
+    float m = 0.f, l = 0.f;                                 // maximum that the sums refer to (unscaled), sum
+    bool first_round = true;
+    // the item's result: its rows, or partial ones
+    auto result = [&]() {
+      wait_bar(o_done + 8 * wg, o_phase & 1, abort_flag, a.status);
       ++o_phase;
       tc_fence_after();
       if (r.active) {
@@ -743,6 +687,129 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         if (r.mine && r.whole && a.lse) a.lse[(long long)r.token * a.lse_tok + r.head] = (m2 + __log2f(l)) * 0.6931471805599453f;
       }
       tc_fence_before();
+    };
+#pragma unroll 1
+    for (;;) {
+      const bool more = next_item(next);                    // (its Q arrives while the last item's last product runs)
+      if (!first_round) result();
+      if (!more) break;
+      first_round = false;
+      r = next;
+      m = -CUDART_INF_F; l = 0.f;
+      bool any = false;                                     // O holds something
+#pragma unroll 1
+      for (int j = r.j; j < r.n; j += r.dual ? 1 : 2) {
+        const int step = r.s0 + j;
+        const bool in_ahead = step < r.n_ahead;
+        const int key0 = (in_ahead ? step : step - r.n_ahead) * kAttnTile, keys = (in_ahead ? r.ahead : r.own) - key0;
+        wait_bar(s_full + 8 * wg, s_phase & 1, abort_flag, a.status);
+        ++s_phase;
+        tc_fence_after();
+        if (!E4M3 && keys < kAttnTile) {                    // what lies behind the last key may be anything: its weight 0 needs a finite value.
+          // (Not before S: only then has this stage's use before last ended, and the parity tells the uses apart.)
+          const uint32_t pos = pos_v(r.t0 + j);
+          wait_bar(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status);
+          uint8_t* v = smem + L::ring + (pos % L::stages) * L::tile_bytes;
+          const int from = keys < 0 ? 0 : keys;
+#pragma unroll 1
+          for (int h = 0; h < L::halves; ++h)
+#pragma unroll 1
+            for (int i = from * 8 + (tid & 127); i < kAttnTile * 8; i += 128) *reinterpret_cast<uint4*>(v + h * kHalfBytes + i * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+        }
+        if (r.active) {
+          const int see = in_ahead ? keys : (r.seen - key0 < keys ? r.seen - key0 : keys);
+          const bool hide = __any_sync(0xffffffffu, see < kAttnTile);
+          // S is held in registers where there are enough, else read twice.  Two of its four parts are on their way at a time.
+          constexpr int held = E4M3 ? 2 : 4;
+          uint32_t x[held][32];
+          auto fetch = [&](int c) { tc_ld32(t_s + c * 32, x[c % held]); };
+          auto have = [&](int c) {
+            arrived(x[c % held]);
+            if (hide) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[c % held][i] = c * 32 + i < see ? x[c % held][i] : 0xff800000u;
+            }
+          };
+          auto largest = [&](int c, float m0) {
+            const uint32_t (&y)[32] = x[c % held];
+            float m1 = __uint_as_float(y[0]);
+#pragma unroll
+            for (int i = 1; i < 17; i += 2) m1 = max3_nan(m1, __uint_as_float(y[i]), __uint_as_float(y[i + 1]));
+#pragma unroll
+            for (int i = 17; i < 31; i += 2) m0 = max3_nan(m0, __uint_as_float(y[i]), __uint_as_float(y[i + 1]));
+            return max3_nan(m0, m1, __uint_as_float(y[31]));
+          };
+          fetch(0); fetch(1);
+          tc_wait_ld();
+          have(0); have(1);
+          if (held == 4) { fetch(2); fetch(3); }
+          float m_new = largest(0, m), m_other = largest(1, m);
+          if (held == 2) { fetch(2); fetch(3); }
+          tc_wait_ld();
+          have(2); have(3);
+          m_new = max_nan(largest(2, m_new), largest(3, m_other));
+          if (held == 2) { fetch(0); fetch(1); }
+          // The sums keep referring to an older maximum until weights could pass 2^8: fp32 and the weights' type carry that exactly as well.
+          // (A NaN raises too: it then is in the sums.)
+          const bool raise = m_new != m && !((m_new - m) * r.sl2 <= 8.f);
+          if (!any) {
+            m = m_new;
+          } else if (__any_sync(0xffffffffu, raise)) {
+            const float f = raise ? ex2((m - m_new) * r.sl2) : 1.f;
+            if (raise) { m = m_new; l *= f; }
+            if (held == 2) tc_wait_ld();
+#pragma unroll 1
+            for (int c = 0; c < DP / 16; ++c) {
+              uint32_t o[16];
+              tc_ld16(t_o + c * 16, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tc_st16(t_o + c * 16, o);
+            }
+            tc_wait_st();
+          }
+          any = true;
+          // no key seen yet: all weights 0; an infinite score: NaN
+          const float shift = m == -CUDART_INF_F ? 0.f : m == CUDART_INF_F ? CUDART_NAN_F : -m * r.sl2;
+          const f32x2 scale2 = pair2(r.sl2, r.sl2), shift2 = pair2(shift, shift);
+          f32x2 sum[2] = {0, 0};
+          if (held == 2) { tc_wait_ld(); have(0); have(1); }
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const f32x2 z = fma2(pair2(__uint_as_float(x[c % held][2 * i]), __uint_as_float(x[c % held][2 * i + 1])), scale2, shift2);
+              float p0, p1;
+              if (kPolynomial >> (i & 7) & 1) {
+                ex2_pair(z, p0, p1);
+              } else {
+                unpair2(z, p0, p1);
+                p0 = ex2(p0); p1 = ex2(p1);
+              }
+              sum[i & 1] = add2(sum[i & 1], pair2(p0, p1));
+              w[i] = E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
+            }
+            if (held == 2 && c == 1) { fetch(2); fetch(3); tc_wait_ld(); have(2); have(3); }
+            tc_st16(t_s + c * 16, w);
+            if (c == 1) {
+              tc_wait_st();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(p_half + 8 * wg);
+            }
+          }
+          float s0, s1;
+          unpair2(add2(sum[0], sum[1]), s0, s1);
+          l += s0 + s1;
+          tc_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) { if (!r.active) mbar_arrive(p_half + 8 * wg); mbar_arrive(p_ready + 8 * wg); }
+      }
     }
   }
   tc_fence_before();
@@ -854,7 +921,7 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
   }
   // longer sequences' items that a cut between two CTAs' shares went through: found at their first cut
   for (int c = 1 + blockIdx.x; c < p.n_ctas; c += gridDim.x) {
-    const long long x = c * s.share;
+    const int x = c * s.share;
     const AttnWalk k = attn_walk_at(p, s, x);
     if (k.done) break;
     const AttnItem it = attn_item(p, s, k);
