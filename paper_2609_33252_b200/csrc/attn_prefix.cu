@@ -23,7 +23,7 @@ using namespace ptx;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kItemWarp = 10, kMmaWarp2 = 11, kCodeWarp = 12;     // (kCodeWarp and the next three: e4m3 only)
 constexpr int kItemSlots = 8;                               // items between the warp that walks the schedule and the slowest reader
 constexpr int kMaxShared = 227 * 1024;
-constexpr int kPolynomial = 0x4a;                            // of eight pairs of weights, which go to the multiply-add units
+constexpr int kPolynomial = 0;                            // of eight pairs of weights, which go to the multiply-add units
 constexpr int kHalfBytes = kAttnTile * 128;                 // 128 rows of 64 bf16: what a 128-byte swizzled box column is
 
 // Shared memory: Q of two row tiles, the ring of K and V tiles, barriers and the like, the schedule; in an e4m3 cache's kernel the
@@ -50,6 +50,7 @@ static_assert(layout_ok<64, false>() && layout_ok<128, false>() && layout_ok<64,
               "all tensor memory: no other block may share the SM");
 
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float ex2_here(float x) { float r; asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
@@ -97,6 +98,12 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
     if (*abort_flag) return false;
   }
   return true;
+}
+
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+  return yes != 0;
 }
 
 // ---------------------------------------------------------------- the schedule
@@ -283,12 +290,13 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t sbase = smem_u32(smem);
   const uint32_t bar0 = sbase + L::misc;
-  const uint32_t full = bar0, empty = bar0 + 64, s_full = bar0 + 128, p_ready = bar0 + 144, o_done = bar0 + 160, q_ready = bar0 + 176,
-                 w_full = bar0 + 192, w_empty = bar0 + 256, code_full = bar0 + 320, code_empty = bar0 + 384, p_half = bar0 + 464;
+  const uint32_t full = bar0, empty = bar0 + 64, s_full = bar0 + 128, o_done = bar0 + 160, q_ready = bar0 + 176,
+                 w_full = bar0 + 192, w_empty = bar0 + 256, code_full = bar0 + 320, code_empty = bar0 + 384, p_ready = bar0 + 464, o_mid = bar0 + 496;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::misc + 448);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::misc + 452);
   volatile int* first_entity = reinterpret_cast<volatile int*>(smem + L::misc + 456);
   Pair* scratch = reinterpret_cast<Pair*>(smem + L::misc + 512);                       // a block's warps' totals
+  const uint32_t ex_turn = bar0 + 768;                                                 // [2][4] a warp of each warpgroup may take its exponentials
   const Work* work = reinterpret_cast<const Work*>(smem + L::misc + 1024);
   const int words = attn_sched_words(a.p.B, a.p.G), n_codes = L::code_slots(words);
   uint8_t* sched_at = smem + L::codes + n_codes * L::code_bytes;
@@ -297,7 +305,9 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   if (tid == 0) {
     for (int i = 0; i < L::stages; ++i) { mbar_init(full + 8 * i, E4M3 ? 4 : 1); mbar_init(empty + 8 * i, 2); }
     for (int i = 0; i < n_codes; ++i) { mbar_init(code_full + 8 * i, 1); mbar_init(code_empty + 8 * i, 4); }
-    for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); mbar_init(p_half + 8 * i, 4); mbar_init(o_done + 8 * i, 1); mbar_init(q_ready + 8 * i, 4); }
+    for (int i = 0; i < 4; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); }
+    for (int i = 0; i < 8; ++i) mbar_init(ex_turn + 8 * i, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(o_mid + 8 * i, 1); mbar_init(o_done + 8 * i, 1); mbar_init(q_ready + 8 * i, 4); }
     // readers of an item: the loading warp, the products of each warpgroup, eight row warps, four decoding warps
     for (int i = 0; i < kItemSlots; ++i) { mbar_init(w_full + 8 * i, 1); mbar_init(w_empty + 8 * i, E4M3 ? 15 : 11); }
     *abort_flag = 0;
@@ -456,11 +466,11 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     }
   } else if (warp == kMmaWarp || warp == kMmaWarp2) {
     // ------------------------------------------------------ tensor core: one thread for each warpgroup's products
-    // (A tcgen05 instruction costs the thread that issues it some 60 cycles, as long as the products here take: one thread for both
-    // would be what bounds the kernel.)
-    if (lane == 0) {
+    // (Elected, not picked by its number: the compiler then knows that one thread issues, and a product of 128 x 128 x 16 takes its 64
+    // cycles of the tensor core; from a thread picked by number every tcgen05 instruction takes 66 of its own, whatever its size.)
+    if (elect_one()) {
       constexpr uint32_t type = E4M3 ? (1u << 7) | (1u << 10) : 0u;         // codes are decoded to fp16, whose type bits are 0 (bf16: 1)
-      constexpr uint32_t idesc_s = make_idesc_bf16(128, 128) ^ type, idesc_o = (make_idesc_bf16(128, DP) | kTransposeB) ^ type;
+      constexpr uint32_t idesc_s = make_idesc_bf16(128, 64) ^ type, idesc_o = (make_idesc_bf16(128, DP) | kTransposeB) ^ type;
       const int w = warp == kMmaWarp2;
       const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
       const uint64_t qd = make_smem_desc(sbase + L::q + w * L::tile_bytes);
@@ -480,37 +490,51 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         if (n == 0 || *abort_flag) break;
         mbar_arrive(w_empty + 8 * (turn % kItemSlots));
         ++turn;
-        const int j0 = first_step(t0, dual, w);
-        if (j0 < n) wait(q_ready + 8 * w, q_phase++);
-#pragma unroll 1
-        for (int j = j0; j < n && alive; j += dual ? 1 : 2) {
-          const uint32_t pk = pos_k(t0 + j), pv = pos_v(t0 + j);
-          const int sk = pk % L::stages, sv = pv % L::stages;
-          wait(full + 8 * sk, pk / L::stages);
-          if (!alive) break;
-          tc_fence_after();
-          const uint64_t kd = make_smem_desc(sbase + L::ring + sk * L::tile_bytes);
+        const int j0 = first_step(t0, dual, w), step = dual ? 1 : 2;
+        // scores of half a tile's keys
+        auto scores = [&](int j, int h) {
+          const int sk = pos_k(t0 + j) % L::stages;
+          const uint64_t kd = make_smem_desc(sbase + L::ring + sk * L::tile_bytes + h * (kHalfBytes / 2));
 #pragma unroll
           for (int i = 0; i < DP / 16; ++i) {
             const uint64_t off = ((i >> 2) * kHalfBytes + (i & 3) * 32) >> 4;
-            tc_mma_f16(t_s, qd + off, kd + off, idesc_s, i > 0);
+            tc_mma_f16(t_s + h * 64, qd + off, kd + off, idesc_s, i > 0);
           }
-          tc_commit(s_full + 8 * w);
-          free_stage(dual, sk);
-          wait(full + 8 * sv, pv / L::stages);
+          tc_commit(s_full + 16 * w + 8 * h);
+          if (h) free_stage(dual, sk);
+        };
+        auto wait_stage = [&](uint32_t pos) { wait(full + 8 * (pos % L::stages), pos / L::stages); tc_fence_after(); };
+        if (j0 < n) {
+          wait(q_ready + 8 * w, q_phase++);
+          wait_stage(pos_k(t0 + j0));
+          if (!alive) break;
+          scores(j0, 0);
+          scores(j0, 1);
+        }
+#pragma unroll 1
+        for (int j = j0; j < n && alive; j += step) {
+          const uint32_t pv = pos_v(t0 + j);
+          const int sv = pv % L::stages;
+          const bool more = j + step < n;
+          wait_stage(pv);
           const uint64_t vd = make_v_desc(sbase + L::ring + sv * L::tile_bytes);
-          const uint32_t more = j != j0;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {                     // the first half of the weights is in place before the second
-            wait((h ? p_ready : p_half) + 8 * w, p_phase);
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {                     // the other half's weights are on their way meanwhile
+            wait(p_ready + 16 * w + 8 * h, p_phase);
             if (!alive) break;
             tc_fence_after();
 #pragma unroll
-            for (int i = 4 * h; i < 4 * h + 4; ++i) tc_mma_f16_ts(t_o, t_s + i * 8, vd + ((i * 16 * 128) >> 4), idesc_o, i ? 1u : more);
+            for (int i = 0; i < 4; ++i)
+              tc_mma_f16_ts(t_o, t_s + h * 64 + i * 8, vd + ((h * 64 + i * 16) * 128 >> 4), idesc_o, i + h ? 1u : (uint32_t)(j != j0));
+            if (h == 0) tc_commit(o_mid + 8 * w); else free_stage(dual, sv);
+            if (more) {
+              if (h == 0) wait_stage(pos_k(t0 + j + step));
+              if (!alive) break;
+              scores(j + step, h);
+            }
           }
           ++p_phase;
-          free_stage(dual, sv);
-          if (j + (dual ? 1 : 2) >= n) tc_commit(o_done + 8 * w);
+          if (!more && alive) tc_commit(o_done + 8 * w);
         }
         t0 += n;
       }
@@ -578,7 +602,8 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     const int wg = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
     const uint32_t t_s = tmem + lanes + wg * 128, t_o = tmem + lanes + 256 + wg * 128;
-    uint32_t s_phase = 0, o_phase = 0, t0 = 0;
+    const uint32_t my_turn = ex_turn + 32 * wg + 8 * (warp & 3), other_turn = ex_turn + 32 * (wg ^ 1) + 8 * (warp & 3);
+    uint32_t s_phase = 0, o_phase = 0, t0 = 0, e_phase = 0;
     // This thread's row of an item.
     struct Row { int n, j, s0, n_ahead, ahead, own, seen, head, token; bool dual, whole, mine, active; uint32_t t0; long long prow; float sl2; };
     // The next item that this warpgroup has a part in: its row of Q goes to shared memory (nothing reads the last item's any more)
@@ -702,113 +727,125 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         const int step = r.s0 + j;
         const bool in_ahead = step < r.n_ahead;
         const int key0 = (in_ahead ? step : step - r.n_ahead) * kAttnTile, keys = (in_ahead ? r.ahead : r.own) - key0;
-        wait_bar(s_full + 8 * wg, s_phase & 1, abort_flag, a.status);
-        ++s_phase;
-        tc_fence_after();
-        if (!E4M3 && keys < kAttnTile) {                    // what lies behind the last key may be anything: its weight 0 needs a finite value.
-          // (Not before S: only then has this stage's use before last ended, and the parity tells the uses apart.)
-          const uint32_t pos = pos_v(r.t0 + j);
-          wait_bar(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status);
-          uint8_t* v = smem + L::ring + (pos % L::stages) * L::tile_bytes;
-          const int from = keys < 0 ? 0 : keys;
+        // Two warps, one of each warpgroup, share a scheduler and its unit for exponentials: left to themselves they fall into step and
+        // want it at the same time, so they take turns.
+        auto take_turn = [&]() {
+          if (r.dual) wait_bar(my_turn, (e_phase & 1) ^ (wg ^ 1), abort_flag, a.status);
+        };
+        auto pass_turn = [&]() {
+          if (!r.dual) return;
+          ++e_phase;
+          if (lane == 0) mbar_arrive(other_turn);
+        };
+        const int see = in_ahead ? keys : (r.seen - key0 < keys ? r.seen - key0 : keys);
 #pragma unroll 1
-          for (int h = 0; h < L::halves; ++h)
+        for (int h = 0; h < 2; ++h) {                       // half the keys; the tensor core works on the other half
+          wait_bar(s_full + 16 * wg + 8 * h, s_phase & 1, abort_flag, a.status);
+          tc_fence_after();
+          if (!E4M3 && h == 0 && keys < kAttnTile) {                    // what lies behind the last key may be anything: its weight 0 needs a finite value.
+            // (Not before S: only then has this stage's use before last ended, and the parity tells the uses apart.)
+            const uint32_t pos = pos_v(r.t0 + j);
+            wait_bar(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status);
+            uint8_t* v = smem + L::ring + (pos % L::stages) * L::tile_bytes;
+            const int from = keys < 0 ? 0 : keys;
 #pragma unroll 1
-            for (int i = from * 8 + (tid & 127); i < kAttnTile * 8; i += 128) *reinterpret_cast<uint4*>(v + h * kHalfBytes + i * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
-        }
-        if (r.active) {
-          const int see = in_ahead ? keys : (r.seen - key0 < keys ? r.seen - key0 : keys);
-          const bool hide = __any_sync(0xffffffffu, see < kAttnTile);
-          // S is held in registers where there are enough, else read twice.  Two of its four parts are on their way at a time.
-          constexpr int held = E4M3 ? 2 : 4;
-          uint32_t x[held][32];
-          auto fetch = [&](int c) { tc_ld32(t_s + c * 32, x[c % held]); };
-          auto have = [&](int c) {
-            arrived(x[c % held]);
-            if (hide) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[c % held][i] = c * 32 + i < see ? x[c % held][i] : 0xff800000u;
-            }
-          };
-          auto largest = [&](int c, float m0) {
-            const uint32_t (&y)[32] = x[c % held];
-            float m1 = __uint_as_float(y[0]);
-#pragma unroll
-            for (int i = 1; i < 17; i += 2) m1 = max3_nan(m1, __uint_as_float(y[i]), __uint_as_float(y[i + 1]));
-#pragma unroll
-            for (int i = 17; i < 31; i += 2) m0 = max3_nan(m0, __uint_as_float(y[i]), __uint_as_float(y[i + 1]));
-            return max3_nan(m0, m1, __uint_as_float(y[31]));
-          };
-          fetch(0); fetch(1);
-          tc_wait_ld();
-          have(0); have(1);
-          if (held == 4) { fetch(2); fetch(3); }
-          float m_new = largest(0, m), m_other = largest(1, m);
-          if (held == 2) { fetch(2); fetch(3); }
-          tc_wait_ld();
-          have(2); have(3);
-          m_new = max_nan(largest(2, m_new), largest(3, m_other));
-          if (held == 2) { fetch(0); fetch(1); }
-          // The sums keep referring to an older maximum until weights could pass 2^8: fp32 and the weights' type carry that exactly as well.
-          // (A NaN raises too: it then is in the sums.)
-          const bool raise = m_new != m && !((m_new - m) * r.sl2 <= 8.f);
-          if (!any) {
-            m = m_new;
-          } else if (__any_sync(0xffffffffu, raise)) {
-            const float f = raise ? ex2((m - m_new) * r.sl2) : 1.f;
-            if (raise) { m = m_new; l *= f; }
-            if (held == 2) tc_wait_ld();
+            for (int h = 0; h < L::halves; ++h)
 #pragma unroll 1
-            for (int c = 0; c < DP / 16; ++c) {
-              uint32_t o[16];
-              tc_ld16(t_o + c * 16, o);
-              tc_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tc_st16(t_o + c * 16, o);
-            }
-            tc_wait_st();
+              for (int i = from * 8 + (tid & 127); i < kAttnTile * 8; i += 128) *reinterpret_cast<uint4*>(v + h * kHalfBytes + i * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
           }
-          any = true;
-          // no key seen yet: all weights 0; an infinite score: NaN
-          const float shift = m == -CUDART_INF_F ? 0.f : m == CUDART_INF_F ? CUDART_NAN_F : -m * r.sl2;
-          const f32x2 scale2 = pair2(r.sl2, r.sl2), shift2 = pair2(shift, shift);
-          f32x2 sum[2] = {0, 0};
-          if (held == 2) { tc_wait_ld(); have(0); have(1); }
+          if (r.active) {
+            uint32_t x[2][32];
+            tc_ld32(t_s + h * 64, x[0]);
+            tc_ld32(t_s + h * 64 + 32, x[1]);
+            tc_wait_ld();
+            arrived(x[0]); arrived(x[1]);
+            if (__any_sync(0xffffffffu, see < h * 64 + 64)) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t w[16];
+              for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const f32x2 z = fma2(pair2(__uint_as_float(x[c % held][2 * i]), __uint_as_float(x[c % held][2 * i + 1])), scale2, shift2);
-              float p0, p1;
-              if (kPolynomial >> (i & 7) & 1) {
-                ex2_pair(z, p0, p1);
-              } else {
-                unpair2(z, p0, p1);
-                p0 = ex2(p0); p1 = ex2(p1);
+                for (int i = 0; i < 32; ++i) x[c][i] = h * 64 + c * 32 + i < see ? x[c][i] : 0xff800000u;
+            }
+            float top[4] = {m, __uint_as_float(x[0][31]), __uint_as_float(x[1][31]), m};
+#pragma unroll
+            for (int i = 0; i < 31; ++i) {
+              if ((i & 1) == 0 && i + 1 < 31) {
+                top[i & 2 ? 0 : 1] = max3_nan(top[i & 2 ? 0 : 1], __uint_as_float(x[0][i]), __uint_as_float(x[0][i + 1]));
+                top[i & 2 ? 3 : 2] = max3_nan(top[i & 2 ? 3 : 2], __uint_as_float(x[1][i]), __uint_as_float(x[1][i + 1]));
               }
-              sum[i & 1] = add2(sum[i & 1], pair2(p0, p1));
-              w[i] = E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
             }
-            if (held == 2 && c == 1) { fetch(2); fetch(3); tc_wait_ld(); have(2); have(3); }
-            tc_st16(t_s + c * 16, w);
-            if (c == 1) {
+            top[0] = max3_nan(top[0], top[1], __uint_as_float(x[0][30]));
+            top[3] = max3_nan(top[3], top[2], __uint_as_float(x[1][30]));
+            const float m_new = max_nan(top[0], top[3]);
+            // The sums keep referring to an older maximum until weights could pass 2^8: fp32 and the weights' type carry that exactly as well.
+            // (A NaN raises too: it then is in the sums.)
+            const bool raise = r.mine && m_new != m && !((m_new - m) * r.sl2 <= 8.f);
+            if (!any) {
+              m = m_new;
+            } else if (__any_sync(0xffffffffu, raise)) {
+              // O stands still once the product before is through, which comes before the other half's next scores (o_mid: this tile's first half)
+              if (h == 0) wait_bar(s_full + 16 * wg + 8, s_phase & 1, abort_flag, a.status);
+              else wait_bar(o_mid + 8 * wg, s_phase & 1, abort_flag, a.status);
+              tc_fence_after();
+              const float f = raise ? ex2((m - m_new) * r.sl2) : 1.f;
+              if (raise) { m = m_new; l *= f; }
+#pragma unroll 1
+              for (int c = 0; c < DP / 16; ++c) {
+                uint32_t o[16];
+                tc_ld16(t_o + c * 16, o);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tc_st16(t_o + c * 16, o);
+              }
               tc_wait_st();
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(p_half + 8 * wg);
             }
+            any = true;
+            take_turn();
+            // no key seen yet: all weights 0; an infinite score: NaN
+            const float shift = m == -CUDART_INF_F ? 0.f : m == CUDART_INF_F ? CUDART_NAN_F : -m * r.sl2;
+            const f32x2 scale2 = pair2(r.sl2, r.sl2), shift2 = pair2(shift, shift);
+            f32x2 sum[4] = {0, 0, 0, 0};
+            // stage by stage, in place
+#pragma unroll
+            for (int i = 0; i < 64; i += 2) {
+              float z0, z1;
+              unpair2(fma2(pair2(__uint_as_float(x[i >> 5][i & 31]), __uint_as_float(x[i >> 5][(i & 31) + 1])), scale2, shift2), z0, z1);
+              x[i >> 5][i & 31] = __float_as_uint(z0); x[i >> 5][(i & 31) + 1] = __float_as_uint(z1);
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              uint32_t (&y)[32] = x[c];
+              uint32_t w[16];
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                float p0 = __uint_as_float(y[i]), p1 = __uint_as_float(y[i + 1]);
+                if (kPolynomial >> ((i >> 1) & 7) & 1) ex2_pair(pair2(p0, p1), p0, p1);
+                else { p0 = ex2_here(p0); p1 = ex2_here(p1); }
+                y[i] = __float_as_uint(p0); y[i + 1] = __float_as_uint(p1);
+              }
+              if (c == 1) pass_turn();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float p0 = __uint_as_float(y[2 * i]), p1 = __uint_as_float(y[2 * i + 1]);
+                w[i] = E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
+                sum[i & 3] = add2(sum[i & 3], pair2(p0, p1));
+              }
+              tc_st16(t_s + h * 64 + c * 16, w);
+            }
+            float s0, s1;
+            unpair2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
+            l += s0 + s1;
+            tc_wait_st();
+          } else {
+            take_turn();
+            pass_turn();
           }
-          float s0, s1;
-          unpair2(add2(sum[0], sum[1]), s0, s1);
-          l += s0 + s1;
-          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_ready + 16 * wg + 8 * h);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) { if (!r.active) mbar_arrive(p_half + 8 * wg); mbar_arrive(p_ready + 8 * wg); }
+        ++s_phase;
       }
     }
   }
