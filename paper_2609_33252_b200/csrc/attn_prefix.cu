@@ -23,7 +23,6 @@ using namespace ptx;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kItemWarp = 10, kMmaWarp2 = 11, kCodeWarp = 12;     // (kCodeWarp and the next three: e4m3 only)
 constexpr int kItemSlots = 8;                               // items between the warp that walks the schedule and the slowest reader
 constexpr int kMaxShared = 227 * 1024;
-constexpr int kPolynomial = 0;                            // of eight pairs of weights, which go to the multiply-add units
 constexpr int kHalfBytes = kAttnTile * 128;                 // 128 rows of 64 bf16: what a 128-byte swizzled box column is
 
 // Shared memory: Q of two row tiles, the ring of K and V tiles, barriers and the like, the schedule; in an e4m3 cache's kernel the
@@ -250,30 +249,14 @@ __device__ __forceinline__ void unpair2(f32x2 v, float& lo, float& hi) { asm("mo
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { uint32_t r; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
+// (volatile: the order in the source is the order that is wanted)
+__device__ __forceinline__ f32x2 fma2_here(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2_here(f32x2 a, f32x2 b) { f32x2 r; asm volatile("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint32_t pack_bf16_here(float lo, float hi) { uint32_t r; asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { uint32_t r; asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
 
 __device__ __forceinline__ float max3_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-
-// 2^x of a pair on the multiply-add units, which have time while the unit that exponentials go to has none: x = n + f, n the nearest
-// whole number (Cody and Waite's reduction: adding 1.5 * 2^23 rounds and leaves n in the low bits), 2^f by the polynomial of degree 4 with constant 1
-// whose largest relative error on [-1/2, 1/2] is least (2.8e-6; a weight's own rounding is 2^-9 or 2^-12).  x up to 127; -127 and
-// below give exactly 0; NaN does not survive.
-__device__ __forceinline__ void ex2_pair(f32x2 x, float& lo, float& hi) {
-  float a, b;
-  unpair2(x, a, b);
-  x = pair2(fmaxf(a, -127.f), fmaxf(b, -127.f));
-  const f32x2 r = add2(x, pair2(12582912.f, 12582912.f)), n = add2(r, pair2(-12582912.f, -12582912.f)), f = fma2(n, pair2(-1.f, -1.f), x);
-  f32x2 y = fma2(f, pair2(0.009585382416844368f, 0.009585382416844368f), pair2(0.05590662732720375f, 0.05590662732720375f));
-  y = fma2(y, f, pair2(0.24024038016796112f, 0.24024038016796112f));
-  y = fma2(y, f, pair2(0.6931241750717163f, 0.6931241750717163f));
-  y = fma2(y, f, pair2(1.f, 1.f));
-  float r0, r1;
-  unpair2(r, r0, r1);
-  unpair2(y, a, b);
-  lo = __int_as_float(__float_as_int(a) + (__float_as_int(r0) << 23));
-  hi = __int_as_float(__float_as_int(b) + (__float_as_int(r1) << 23));
-}
 
 // What tcgen05.ld brought may be used from here on (the wait before this has seen it arrive).
 __device__ __forceinline__ void arrived(uint32_t (&r)[32]) {
@@ -727,13 +710,15 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         const int step = r.s0 + j;
         const bool in_ahead = step < r.n_ahead;
         const int key0 = (in_ahead ? step : step - r.n_ahead) * kAttnTile, keys = (in_ahead ? r.ahead : r.own) - key0;
-        // Two warps, one of each warpgroup, share a scheduler and its unit for exponentials: left to themselves they fall into step and
-        // want it at the same time, so they take turns.
+        // Two warps, one of each warpgroup, share a scheduler and its unit for exponentials, and fall into step: with heads above 64 they
+        // take turns at it (4096 tokens behind 8192 keys: 983 against 1022 us; heads of 64 lose, 941 against 891, and so do e4m3 caches,
+        // 1127 against 1095, where other warps' work fills the gaps).
+        constexpr bool turns = DP == 128 && !E4M3;
         auto take_turn = [&]() {
-          if (r.dual) wait_bar(my_turn, (e_phase & 1) ^ (wg ^ 1), abort_flag, a.status);
+          if (turns && r.dual) wait_bar(my_turn, (e_phase & 1) ^ (wg ^ 1), abort_flag, a.status);
         };
         auto pass_turn = [&]() {
-          if (!r.dual) return;
+          if (!turns || !r.dual) return;
           ++e_phase;
           if (lane == 0) mbar_arrive(other_turn);
         };
@@ -801,38 +786,40 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
               tc_wait_st();
             }
             any = true;
-            take_turn();
             // no key seen yet: all weights 0; an infinite score: NaN
             const float shift = m == -CUDART_INF_F ? 0.f : m == CUDART_INF_F ? CUDART_NAN_F : -m * r.sl2;
             const f32x2 scale2 = pair2(r.sl2, r.sl2), shift2 = pair2(shift, shift);
             f32x2 sum[4] = {0, 0, 0, 0};
-            // stage by stage, in place
-#pragma unroll
-            for (int i = 0; i < 64; i += 2) {
+            // The unit for exponentials takes 8 cycles a warp for each: what comes before and after them is put between them (a
+            // pair's scaling kAhead pairs ahead, its sum and rounding kBehind pairs behind), in this order, in place.
+            auto scaled = [&](int i) {
               float z0, z1;
-              unpair2(fma2(pair2(__uint_as_float(x[i >> 5][i & 31]), __uint_as_float(x[i >> 5][(i & 31) + 1])), scale2, shift2), z0, z1);
-              x[i >> 5][i & 31] = __float_as_uint(z0); x[i >> 5][(i & 31) + 1] = __float_as_uint(z1);
-            }
+              unpair2(fma2_here(pair2(__uint_as_float(x[i >> 4][2 * i & 31]), __uint_as_float(x[i >> 4][(2 * i & 31) + 1])), scale2, shift2), z0, z1);
+              x[i >> 4][2 * i & 31] = __float_as_uint(z0); x[i >> 4][(2 * i & 31) + 1] = __float_as_uint(z1);
+            };
+            constexpr int kAhead = 4, kBehind = 4;
+            uint32_t w[2][16];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              uint32_t (&y)[32] = x[c];
-              uint32_t w[16];
+            for (int i = 0; i < kAhead; ++i) scaled(i);
+            take_turn();
 #pragma unroll
-              for (int i = 0; i < 32; i += 2) {
-                float p0 = __uint_as_float(y[i]), p1 = __uint_as_float(y[i + 1]);
-                if (kPolynomial >> ((i >> 1) & 7) & 1) ex2_pair(pair2(p0, p1), p0, p1);
-                else { p0 = ex2_here(p0); p1 = ex2_here(p1); }
-                y[i] = __float_as_uint(p0); y[i + 1] = __float_as_uint(p1);
+            for (int i = 0; i < 32 + kBehind; ++i) {
+              if (i + kAhead < 32) scaled(i + kAhead);
+              if (i < 32) {
+                uint32_t &u = x[i >> 4][2 * i & 31], &v = x[i >> 4][(2 * i & 31) + 1];
+                u = __float_as_uint(ex2_here(__uint_as_float(u)));
+                v = __float_as_uint(ex2_here(__uint_as_float(v)));
               }
-              if (c == 1) pass_turn();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const float p0 = __uint_as_float(y[2 * i]), p1 = __uint_as_float(y[2 * i + 1]);
-                w[i] = E4M3 ? pack_f16(p0, p1) : pack_bf16(p0, p1);
-                sum[i & 3] = add2(sum[i & 3], pair2(p0, p1));
+              if (i == 31) pass_turn();
+              if (i >= kBehind) {
+                const int k = i - kBehind;
+                const float p0 = __uint_as_float(x[k >> 4][2 * k & 31]), p1 = __uint_as_float(x[k >> 4][(2 * k & 31) + 1]);
+                w[k >> 4][k & 15] = E4M3 ? pack_f16(p0, p1) : pack_bf16_here(p0, p1);
+                sum[k & 3] = add2_here(sum[k & 3], pair2(p0, p1));
+                if (k == 15) tc_st16(t_s + h * 64, w[0]);
               }
-              tc_st16(t_s + h * 64 + c * 16, w);
             }
+            tc_st16(t_s + h * 64 + 16, w[1]);
             float s0, s1;
             unpair2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
             l += s0 + s1;
