@@ -57,7 +57,7 @@ Carve carve(const cep_attn_config& c) {
   auto take = [&](size_t& f, size_t bytes) { f = o; o = up_to(o + bytes, 256); };
   const size_t rows = (size_t)attn_max_part_rows(c.max_tokens, c.max_seqs, c.max_prefixes, c.n_heads, c.n_kv_heads, kAttnMaxCtas);
   take(w.status, kStWords * 4);
-  take(w.sched, kAttnSchedBytes);
+  take(w.sched, kAttnSchedBytes + kAttnMaxCtas * 4);
   take(w.ml, rows * sizeof(float2));
   take(w.o, rows * attn_padded_dim(c.head_dim) * sizeof(float));
   w.total = o;
@@ -210,7 +210,11 @@ int attn_prefix(cep_attn_plan* p, const cep_attn_batch* b, const void* q, const 
   a.k_scale = p->k_scale; a.v_scale = p->v_scale;
   a.scale_log2 = (float)((double)c.scale * 1.4426950408889634);
   a.part_o = p->part_o; a.part_ml = p->part_ml; a.sched = p->sched; a.status = p->status;
-  const cudaError_t e = launch_attn(a, c.cache_elem == CEP_ELEM_E4M3, p->tm_k, p->tm_v, st);
+  GemmTensorMap maps[4] = {p->tm_k, p->tm_v, {}, {}};
+  int m = make_q_map(&maps[2], a, 1);
+  if (!m) m = make_q_map(&maps[3], a, a.p.tps);
+  if (m) return record_error(CEP_ERR_CUDA, "attn: cuTensorMapEncodeTiled failed (%d)", m);
+  const cudaError_t e = launch_attn(a, c.cache_elem == CEP_ELEM_E4M3, maps, st);
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "attn: a launch failed: %s", cudaGetErrorString(e));
   return leave(p, st, capturing);
 }

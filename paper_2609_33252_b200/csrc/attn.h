@@ -252,11 +252,11 @@ __host__ __device__ inline long long attn_max_part_rows(int max_tokens, int max_
   return 2 * most * Hq + (long long)Hkv * (most / (2 * tps) + max_prefixes) * 2 * tps * Gh + (long long)(n_ctas + 1) * kAttnSplitRows;
 }
 
-// The cost that each CTA gets: equal shares, and no less than two steps, which two warpgroups take at the same time.
+// The cost that each CTA gets: equal shares, and about a step at least.
 __host__ __device__ inline int attn_share(const AttnShape& p, int total) {
   // (fp32 is off by 2^-23 of the sum at most, which is less than one part in 10^4 of a share)
   int share = (int)((float)total * p.per_cta) + 1 + (total >> 21);
-  const int least = 2 * (kAttnTile / 4) * kAttnCostSingle >> p.cost_shift;
+  const int least = (kAttnTile / 4 * kAttnCostSingle + kAttnCostItem / 4) >> p.cost_shift;
   return share > least ? share : least;
 }
 
@@ -291,7 +291,8 @@ struct AttnArgs {
 
 int attn_padded_dim(int D);                  // 64 or 128
 cudaError_t attn_setup();                  // once per plan, with its device current
-cudaError_t launch_attn(const AttnArgs& a, int e4m3, const GemmTensorMap& tm_k, const GemmTensorMap& tm_v, cudaStream_t s);
+cudaError_t launch_attn(const AttnArgs& a, int e4m3, const GemmTensorMap (&maps)[4], cudaStream_t s);       // k, v, q by single tokens, q by row tiles
+int make_q_map(GemmTensorMap* out, const AttnArgs& a, int tokens);         // boxes of `tokens` tokens' query heads of a kv head
 int make_cache_map(GemmTensorMap* out, const void* base, const cep_attn_config& c, const int64_t* stride);    // stride: page, position, head
 
 }  // namespace cep

@@ -12,6 +12,8 @@
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
+#include <algorithm>
+
 #include "attn.h"
 #include "lora_ptx.cuh"
 
@@ -118,7 +120,7 @@ __device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_t
     Pair v{0, 0};
     if (i < n) v = get(i);
     const Pair own = v;
-#pragma unroll 1
+#pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int a = __shfl_up_sync(0xffffffffu, v.a, d);
       const int b = __shfl_up_sync(0xffffffffu, v.b, d);
@@ -128,24 +130,12 @@ __device__ __forceinline__ Pair block_scan(int n, Get get, Put put, Pair* warp_t
     __syncthreads();
     Pair w{0, 0};
     if (lane < n_warps) w = warp_totals[lane];
-    const Pair ahead = carry;
-    Pair mine = ahead;
-#pragma unroll 1
-    for (int d = 16; d; d >>= 1) {                          // sums over the warps before this one, and over all
-      const int a = __shfl_xor_sync(0xffffffffu, w.a, d);
-      const int b = __shfl_xor_sync(0xffffffffu, w.b, d);
-      w.a += a; w.b += b;
-    }
-    carry.a += w.a; carry.b += w.b;
-    Pair x{0, 0};
-    if (lane < warp) x = warp_totals[lane];
-#pragma unroll 1
-    for (int d = 16; d; d >>= 1) {
-      const int a = __shfl_xor_sync(0xffffffffu, x.a, d);
-      const int b = __shfl_xor_sync(0xffffffffu, x.b, d);
-      x.a += a; x.b += b;
-    }
-    mine.a += x.a + v.a - own.a; mine.b += x.b + v.b - own.b;
+    const bool ahead = lane < warp;
+    Pair mine;
+    mine.a = carry.a + __reduce_add_sync(0xffffffffu, ahead ? w.a : 0) + v.a - own.a;
+    mine.b = carry.b + __reduce_add_sync(0xffffffffu, ahead ? w.b : 0) + v.b - own.b;
+    carry.a += __reduce_add_sync(0xffffffffu, w.a);
+    carry.b += __reduce_add_sync(0xffffffffu, w.b);
     if (i < n) put(i, mine);
     __syncthreads();
   }
@@ -242,6 +232,10 @@ __device__ __forceinline__ uint32_t pos_v(uint32_t t) { return 2 * t + 2; }
 // Of an item whose first tile is t0, a warpgroup has all tiles (two row tiles) or those with its parity.
 __device__ __forceinline__ int first_step(uint32_t t0, bool dual, int wg) { return dual ? 0 : (int)((t0 + wg) & 1); }
 
+// The tensor-memory lane of a warpgroup's first row.  Two row tiles: 0.  One with few rows: the second warpgroup's lie half a tile further, as
+// they would otherwise be the work of one scheduler's warps.
+__device__ __forceinline__ int first_row(bool dual, int wg, int rows) { return !dual && wg && rows <= 64 ? 64 : 0; }
+
 // Two fp32 values in one 64-bit register pair: one instruction multiplies and adds both.
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pair2(float lo, float hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
@@ -267,7 +261,8 @@ __device__ __forceinline__ void arrived(uint32_t (&r)[32]) {
 // ---------------------------------------------------------------- the kernel
 template <int DP, bool E4M3>
 __global__ void __launch_bounds__(Layout<DP, E4M3>::threads, 1)
-attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+            const __grid_constant__ CUtensorMap tm_q1, const __grid_constant__ CUtensorMap tm_qn) {
   using L = Layout<DP, E4M3>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -280,6 +275,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   volatile int* first_entity = reinterpret_cast<volatile int*>(smem + L::misc + 456);
   Pair* scratch = reinterpret_cast<Pair*>(smem + L::misc + 512);                       // a block's warps' totals
   const uint32_t ex_turn = bar0 + 768;                                                 // [2][4] a warp of each warpgroup may take its exponentials
+  const uint32_t q_free = bar0 + 832, q_raw = bar0 + 848;
   const Work* work = reinterpret_cast<const Work*>(smem + L::misc + 1024);
   const int words = attn_sched_words(a.p.B, a.p.G), n_codes = L::code_slots(words);
   uint8_t* sched_at = smem + L::codes + n_codes * L::code_bytes;
@@ -290,7 +286,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     for (int i = 0; i < n_codes; ++i) { mbar_init(code_full + 8 * i, 1); mbar_init(code_empty + 8 * i, 4); }
     for (int i = 0; i < 4; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_ready + 8 * i, 4); }
     for (int i = 0; i < 8; ++i) mbar_init(ex_turn + 8 * i, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(o_mid + 8 * i, 1); mbar_init(o_done + 8 * i, 1); mbar_init(q_ready + 8 * i, 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(o_mid + 8 * i, 1); mbar_init(o_done + 8 * i, 1); mbar_init(q_free + 8 * i, 1); mbar_init(q_raw + 8 * i, 1); mbar_init(q_ready + 8 * i, E4M3 ? 4 : 1); }
     // readers of an item: the loading warp, the products of each warpgroup, eight row warps, four decoding warps
     for (int i = 0; i < kItemSlots; ++i) { mbar_init(w_full + 8 * i, 1); mbar_init(w_empty + 8 * i, E4M3 ? 15 : 11); }
     *abort_flag = 0;
@@ -406,41 +402,83 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         while (!mbar_try_wait((E4M3 ? code_full : full) + 8 * (pos % places), (pos / places) & 1) && globaltimer() - t0 < 100000000ull) {}
     }
   } else if (warp == kItemWarp) {
-    // ------------------------------------------------------ the CTA's share of the schedule, item by item
+    // ------------------------------------------------------ the CTA's share of the schedule, item by item, and the items' Q
+    const int x0 = blockIdx.x * s.share, x1 = x0 + s.share;
+    AttnWalk k;
+    k.done = *first_entity < 0;
+    if (!k.done) k = attn_walk_in(p, s, *first_entity, x0);
     if (lane == 0) {
-      const int x0 = blockIdx.x * s.share, x1 = x0 + s.share;
-      AttnWalk k;
-      k.done = *first_entity < 0;
-      if (!k.done) k = attn_walk_in(p, s, *first_entity, x0);
-      Work* out = const_cast<Work*>(work);
-      for (;;) {
-        Work w;
-        w.n = 0;
-        for (; !k.done && k.at < x1 && w.n == 0; attn_walk_next(p, s, &k)) {
-          const AttnItem it = attn_item(p, s, k);
-          const int s0 = attn_steps_before(k, it.n, x0), s1 = attn_steps_before(k, it.n, x1);
-          w.n = s1 - s0; w.s0 = s0;
-          if (w.n == 0) continue;
-          w.head = it.head; w.n_tok = it.n_tok; w.ahead = it.ahead; w.own = it.own; w.n_ahead = it.n_ahead; w.b = it.b; w.g = it.g;
-          w.flags = (it.dual ? kDual : 0) | (attn_is_whole(it, s0, s1) ? kWhole : 0);
-          w.prow = attn_part_row(it, blockIdx.x, s0);
-          if (it.kind == kAttnGroup) {
-            w.lo = s.gfirst[it.g]; w.hi = s.gfirst[it.g + 1];
-            w.tok = s.scum[w.lo] + it.tok; w.seen = 0;
-          } else {
-            w.lo = w.hi = 0;
-            w.tok = s.q0[it.b] + it.tok;
-            w.seen = s.kv[it.b] - (s.q0[it.b + 1] - s.q0[it.b]) + it.tok + 1;
-          }
-        }
-        if (!wait_bar(w_empty + 8 * (turn % kItemSlots), ((turn / kItemSlots) & 1) ^ 1, abort_flag, a.status)) break;
-        out[turn % kItemSlots] = w;
-        mbar_arrive(w_full + 8 * (turn % kItemSlots));
-        ++turn;
-        if (w.n == 0) break;
+      // For the kernel that joins partial results: does this CTA's first item begin in the share before, and use the rows at the cuts?
+      int cut = 0;
+      if (!k.done && k.e >= p.G && x0 > 0 && !attn_has_rows(p, s, k.e - p.G)) {
+        const int n = attn_item(p, s, k).n, before = attn_steps_before(k, n, x0);
+        cut = before > 0 && before < n && attn_steps_before(k, n, x0 - s.share) == 0;
       }
+      static_cast<int32_t*>(a.sched)[words + blockIdx.x] = cut;
+    }
+    Work* out = const_cast<Work*>(work);
+    uint32_t t0 = 0, q_turn[2] = {0, 0};
+    bool alive = true;
+#pragma unroll 1
+    while (alive) {
+      Work w;
+      w.n = 0; w.n_tok = 0; w.flags = 0; w.hi = 0; w.lo = 0; w.tok = 0; w.head = 0;
+#pragma unroll 1
+      for (; !k.done && k.at < x1 && w.n == 0; attn_walk_next(p, s, &k)) {
+        const AttnItem it = attn_item(p, s, k);
+        const int s0 = attn_steps_before(k, it.n, x0), s1 = attn_steps_before(k, it.n, x1);
+        w.n = s1 - s0; w.s0 = s0;
+        if (w.n == 0) continue;
+        w.head = it.head; w.n_tok = it.n_tok; w.ahead = it.ahead; w.own = it.own; w.n_ahead = it.n_ahead; w.b = it.b; w.g = it.g;
+        w.flags = (it.dual ? kDual : 0) | (attn_is_whole(it, s0, s1) ? kWhole : 0);
+        w.prow = attn_part_row(it, blockIdx.x, s0);
+        if (it.kind == kAttnGroup) {
+          w.lo = s.gfirst[it.g]; w.hi = s.gfirst[it.g + 1];
+          w.tok = s.scum[w.lo] + it.tok; w.seen = 0;
+        } else {
+          w.lo = w.hi = 0;
+          w.tok = s.q0[it.b] + it.tok;
+          w.seen = s.kv[it.b] - (s.q0[it.b + 1] - s.q0[it.b]) + it.tok + 1;
+        }
+      }
+      alive = __all_sync(0xffffffffu, wait_bar(w_empty + 8 * (turn % kItemSlots), ((turn / kItemSlots) & 1) ^ 1, abort_flag, a.status));
+      if (!alive) break;
+      if (lane == 0) { out[turn % kItemSlots] = w; mbar_arrive(w_full + 8 * (turn % kItemSlots)); }
+      ++turn;
+      if (w.n == 0) break;
+      // Q of each warpgroup with a part in the item, as soon as the products with its last Q are through.  Rows are tokens x heads, as the
+      // tensor maps' boxes lay them: one box for tokens side by side that fill at least half a row tile, else one for each token.
+#pragma unroll 1
+      for (int wg = 0; wg < 2; ++wg) {
+        const bool dual = w.flags & kDual;
+        if (first_step(t0, dual, wg) >= w.n) continue;
+        const int from = dual ? wg * p.tps : 0, count = max(0, min(dual ? p.tps : w.n_tok, w.n_tok - from));
+        const uint32_t landed = (E4M3 ? q_raw : q_ready) + 8 * wg, dst = sbase + L::q + wg * L::tile_bytes + first_row(dual, wg, w.n_tok * p.Gh) * 128;
+        alive = __all_sync(0xffffffffu, wait_bar(q_free + 8 * wg, (q_turn[wg]++ & 1) ^ 1, abort_flag, a.status));
+        if (!alive) break;
+        const bool box = w.hi == 0 && 2 * count > p.tps;
+        if (lane == 0) mbar_expect_tx(landed, (box ? p.tps : count) * p.Gh * 128 * L::halves);
+        __syncwarp();
+        if (box) {
+          if (lane < L::halves) tma_load_3d(dst + lane * kHalfBytes, &tm_qn, lane * 64, w.head * p.Gh, w.tok + from, landed);
+          continue;
+        }
+#pragma unroll 1
+        for (int i = lane; i < count * L::halves; i += 32) {
+          const int tt = i / L::halves, h = i % L::halves;
+          int token = w.tok + from + tt;
+          if (w.hi > 0) { const int b = sequence_of(s.scum, w.lo, w.hi, token); token = s.q0[b] + (token - s.scum[b]); }
+          tma_load_3d(dst + h * kHalfBytes + tt * p.Gh * 128, &tm_q1, h * 64, w.head * p.Gh, token, landed);
+        }
+      }
+      t0 += w.n;
     }
     __syncwarp();
+    if (!alive) {                                           // copies in flight land before the block's memory is given up
+      const unsigned long long since = globaltimer();
+      for (int wg = 0; wg < 2; ++wg)
+        while (q_turn[wg] && !mbar_try_wait((E4M3 ? q_raw : q_ready) + 8 * wg, (q_turn[wg] - 1) & 1) && globaltimer() - since < 100000000ull) {}
+    }
     if (blockIdx.x == 0) {                                  // the schedule, for the kernel that joins partial results
       int32_t* dst = static_cast<int32_t*>(a.sched);
       const int32_t* src = reinterpret_cast<const int32_t*>(sched_at);
@@ -484,7 +522,10 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             tc_mma_f16(t_s + h * 64, qd + off, kd + off, idesc_s, i > 0);
           }
           tc_commit(s_full + 16 * w + 8 * h);
-          if (h) free_stage(dual, sk);
+          if (h) {
+            free_stage(dual, sk);
+            if (j + step >= n) tc_commit(q_free + 8 * w);
+          }
         };
         auto wait_stage = [&](uint32_t pos) { wait(full + 8 * (pos % L::stages), pos / L::stages); tc_fence_after(); };
         if (j0 < n) {
@@ -535,24 +576,27 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       if (!alive) return;
       const uint8_t* src = smem + L::codes + slot * L::code_bytes;
       uint8_t* dst = smem + L::ring + st * L::tile_bytes;
-      constexpr int per_row = DP / 16, batch = 4;          // 16 codes at a time
-#pragma unroll 1
-      for (int u = 0; u < kAttnTile * per_row / 128; u += batch) {
-        uint4 v[batch];
+      // 16 codes at a time.  Eight neighbouring threads take the left half of one row and the right half of the next (then the other way
+      // round), so that neither their loads nor their stores meet in a bank.
+      constexpr int rounds = kAttnTile * DP / 16 / 128;
+      const int sub = ct >> 2 & 1, row0 = (ct >> 3) * 2 + sub;
+      uint4 v[rounds];
 #pragma unroll
-        for (int i = 0; i < batch; ++i) v[i] = *reinterpret_cast<const uint4*>(src + ((u + i) * 128 + ct) * 16);
+      for (int u = 0; u < rounds; ++u) {
+        const int row = DP == 64 ? u * 32 + (ct >> 2) : (u >> 1) * 32 + row0, c = DP == 64 ? ct & 3 : (ct & 3) + 4 * ((sub + u) & 1);
+        v[u] = *reinterpret_cast<const uint4*>(src + row * DP + c * 16);
+        if (row >= keys) v[u] = make_uint4(0, 0, 0, 0);    // what lies behind the last key may be anything: its weight 0 needs a finite value
+      }
 #pragma unroll
-        for (int i = 0; i < batch; ++i) {
-          const int id = (u + i) * 128 + ct, row = id / per_row, c = id % per_row;
-          if (row >= keys) v[i] = make_uint4(0, 0, 0, 0);  // what lies behind the last key may be anything: its weight 0 needs a finite value
-          uint4 lo, hi;
-          decode4(v[i].x, lo.x, lo.y); decode4(v[i].y, lo.z, lo.w);
-          decode4(v[i].z, hi.x, hi.y); decode4(v[i].w, hi.z, hi.w);
-          uint8_t* at = dst + (c >> 2) * kHalfBytes + row * 128;
-          const int first = (((c & 3) * 2) ^ (row & 7)) << 4, flip = (c & 4) << 2;      // (the other order where c & 4: then the halves' stores share no bank)
-          *reinterpret_cast<uint4*>(at + (first ^ flip)) = flip ? hi : lo;
-          *reinterpret_cast<uint4*>(at + (first ^ 16 ^ flip)) = flip ? lo : hi;
-        }
+      for (int u = 0; u < rounds; ++u) {
+        const int row = DP == 64 ? u * 32 + (ct >> 2) : (u >> 1) * 32 + row0, c = DP == 64 ? ct & 3 : (ct & 3) + 4 * ((sub + u) & 1);
+        uint4 lo, hi;
+        decode4(v[u].x, lo.x, lo.y); decode4(v[u].y, lo.z, lo.w);
+        decode4(v[u].z, hi.x, hi.y); decode4(v[u].w, hi.z, hi.w);
+        uint8_t* at = dst + (c >> 2) * kHalfBytes + row * 128;
+        const int first = (((c & 3) * 2) ^ (row & 7)) << 4;
+        *reinterpret_cast<uint4*>(at + first) = lo;
+        *reinterpret_cast<uint4*>(at + (first ^ 16)) = hi;
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -586,10 +630,11 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;      // this warp's 32 lanes of tensor memory
     const uint32_t t_s = tmem + lanes + wg * 128, t_o = tmem + lanes + 256 + wg * 128;
     const uint32_t my_turn = ex_turn + 32 * wg + 8 * (warp & 3), other_turn = ex_turn + 32 * (wg ^ 1) + 8 * (warp & 3);
-    uint32_t s_phase = 0, o_phase = 0, t0 = 0, e_phase = 0;
+    const uint32_t gh_magic = 65536u / p.Gh + 1;            // x / Gh for x < 128: (x * gh_magic) >> 16
+    uint32_t s_phase = 0, o_phase = 0, t0 = 0, e_phase = 0, q_phase = 0;
     // This thread's row of an item.
-    struct Row { int n, j, s0, n_ahead, ahead, own, seen, head, token; bool dual, whole, mine, active; uint32_t t0; long long prow; float sl2; };
-    // The next item that this warpgroup has a part in: its row of Q goes to shared memory (nothing reads the last item's any more)
+    struct Row { int n, j, s0, n_ahead, ahead, own, seen, kvh, head, token; bool dual, whole, mine, active; uint32_t t0; long long prow; float sl2; };
+    // The next item that this warpgroup has a part in.
     auto next_item = [&](Row& r) -> bool {
       for (;;) {
         const Work& it = take();
@@ -600,11 +645,10 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         if (j >= n) { give_back(); t0 += n; continue; }
         r.n = n; r.j = j; r.t0 = t0; r.dual = dual; r.whole = it.flags & kWhole;
         r.s0 = it.s0; r.n_ahead = it.n_ahead; r.ahead = it.ahead; r.own = it.own;
-        // Two row tiles: the second follows the first.  One: the second warpgroup's rows lie half a tile further, as few rows would
-        // otherwise be the work of one scheduler's warps.
-        const int at = dual ? row : row ^ (wg << 6), row_tok = attn_div(at, p.Gh), row_head = at - row_tok * p.Gh;
+        const int at = row - first_row(dual, wg, it.n_tok * p.Gh);
+        const int row_tok = (int)(((uint32_t)at * gh_magic) >> 16), row_head = at - row_tok * p.Gh;
         const int tt = (dual ? wg * p.tps : 0) + row_tok, kvh = it.head;      // token of the item
-        r.mine = row_tok < p.tps && tt < it.n_tok;
+        r.mine = at >= 0 && row_tok < p.tps && tt < it.n_tok;
         r.token = it.tok + tt;
         r.seen = it.own;
         if (r.mine) {
@@ -615,48 +659,45 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             r.seen = it.seen + tt;
           }
         }
-        r.head = kvh * p.Gh + row_head;
+        r.kvh = kvh; r.head = kvh * p.Gh + row_head;        // (the head of nobody's row is not one)
         // partial rows: those of the item's tokens; where the warpgroups take turns, once for the one with the first tile and once for the other
         r.prow = it.prow + (long long)(tt + (dual ? 0 : j * it.n_tok)) * p.Gh + row_head;
         t0 += n;
         give_back();
         r.active = __any_sync(0xffffffffu, r.mine);
         r.sl2 = a.scale_log2 * (a.k_scale ? a.k_scale[kvh] : 1.f);
-        if (r.mine) {
-          const uint16_t* src = a.q + (long long)r.token * a.q_tok + (long long)r.head * a.q_head;
-          uint8_t* dst = smem + L::q + wg * L::tile_bytes + row * 128;
-          uint4 v[DP / 8];                                  // columns beyond D as zeros (rows of nobody stay as they are: rows do not mix)
-#pragma unroll
-          for (int c = 0; c < DP / 8; ++c) v[c] = c * 8 < a.D ? __ldg(reinterpret_cast<const uint4*>(src + c * 8)) : make_uint4(0, 0, 0, 0);
-          if (E4M3) {
-            // As fp16, times the power of two that brings the row's largest value to 2^14 (exact; what falls below fp16's range then is
-            // 2^-38 of the largest).  The scores are taken back by sl2.
-            uint32_t top = 0;
-#pragma unroll
-            for (int c = 0; c < DP / 8; ++c) {
-              const uint32_t w4[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) top = max(top, max(w4[i] & 0x7fffu, w4[i] >> 16 & 0x7fffu));
-            }
-            const int e = (int)(top >> 7);                  // biased exponent of the largest
-            const int shift = e == 0 || e == 255 ? 0 : min(100, 127 + 14 - e);
-            const float up = __int_as_float((127 + shift) << 23);
-            r.sl2 *= __int_as_float((127 - shift) << 23);
-#pragma unroll
-            for (int c = 0; c < DP / 8; ++c) {
-              auto half2 = [&](uint32_t w2) { return pack_f16(__uint_as_float(w2 << 16) * up, __uint_as_float(w2 & 0xffff0000u) * up); };
-              v[c] = make_uint4(half2(v[c].x), half2(v[c].y), half2(v[c].z), half2(v[c].w));
-            }
-          }
-#pragma unroll
-          for (int c = 0; c < DP / 8; ++c) *reinterpret_cast<uint4*>(dst + (c >> 3) * kHalfBytes + (((c & 7) ^ (row & 7)) << 4)) = v[c];
-        }
-        fence_proxy_async_smem();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_ready + 8 * wg);
         return true;
       }
+    };
+    // e4m3 caches: a row of Q as fp16, times the power of two that brings its largest value to 2^14 (exact; what falls below fp16's range
+    // then is 2^-38 of the largest).  The scores are taken back by sl2.
+    auto convert_q = [&](Row& r) {
+      wait_bar(q_raw + 8 * wg, q_phase++ & 1, abort_flag, a.status);
+      if (r.active) {
+        uint8_t* mine = smem + L::q + wg * L::tile_bytes + row * 128;
+        auto part = [&](int c) { return reinterpret_cast<uint4*>(mine + (c >> 3) * kHalfBytes + (((c & 7) ^ (row & 7)) << 4)); };
+        uint32_t top = 0;
+#pragma unroll 4
+        for (int c = 0; c < DP / 8; ++c) {
+          const uint4 v = *part(c);
+          const uint32_t w4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top = max(top, max(w4[k] & 0x7fffu, w4[k] >> 16 & 0x7fffu));
+        }
+        const int e = (int)(top >> 7);                      // biased exponent of the largest
+        const int shift = e == 0 || e == 255 ? 0 : min(100, 127 + 14 - e);
+        const float up = __int_as_float((127 + shift) << 23);
+        r.sl2 *= __int_as_float((127 - shift) << 23);
+        auto half2 = [&](uint32_t w2) { return pack_f16(__uint_as_float(w2 << 16) * up, __uint_as_float(w2 & 0xffff0000u) * up); };
+#pragma unroll 4
+        for (int c = 0; c < DP / 8; ++c) {
+          const uint4 v = *part(c);
+          *part(c) = make_uint4(half2(v.x), half2(v.y), half2(v.z), half2(v.w));
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_ready + 8 * wg);
     };
     Row r{}, next{};
     float m = 0.f, l = 0.f;                                 // maximum that the sums refer to (unscaled), sum
@@ -668,27 +709,33 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       tc_fence_after();
       if (r.active) {
         const float m2 = m == -CUDART_INF_F ? m : m * r.sl2;
-        const int kvh = r.head / p.Gh;
-        const float inv = l > 0.f ? (a.v_scale ? a.v_scale[kvh] : 1.f) / l : l;        // (a NaN stays)
-        uint16_t* dst = a.out + (long long)r.token * a.out_tok + (long long)r.head * a.out_head;
-        float* part = a.part_o + r.prow * DP;
+        const float inv = l > 0.f ? (a.v_scale ? a.v_scale[r.kvh] : 1.f) / l : l;        // (a NaN stays)
+        // (A row per lane: 32 lines with every access, 4 us for two full row tiles; the other warpgroup works meanwhile.)
+        if (r.whole) {
+          uint16_t* dst = a.out + (long long)r.token * a.out_tok + (long long)r.head * a.out_head;
 #pragma unroll 1
-        for (int c = 0; c < DP / 32; ++c) {
-          uint32_t o[32];
-          tc_ld32(t_o + c * 32, o);
-          tc_wait_ld();
-          if (r.mine && r.whole) {
+          for (int c = 0; c < DP; c += 32) {
+            uint32_t o[32];
+            tc_ld32(t_o + c, o);
+            tc_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              if (c * 32 + i < a.D) {
-                uint32_t w[4];
+            for (int i = 0; i < 32; i += 8) {
+              uint32_t w[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) w[q] = l == 0.f ? 0u : pack_bf16(__uint_as_float(o[i + 2 * q]) * inv, __uint_as_float(o[i + 2 * q + 1]) * inv);
-                *reinterpret_cast<uint4*>(dst + c * 32 + i) = make_uint4(w[0], w[1], w[2], w[3]);
-              }
-          } else if (r.mine) {
+              for (int q = 0; q < 4; ++q) w[q] = l == 0.f ? 0u : pack_bf16(__uint_as_float(o[i + 2 * q]) * inv, __uint_as_float(o[i + 2 * q + 1]) * inv);
+              if (r.mine && c + i < a.D) *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        } else {
+          float* dst = a.part_o + r.prow * DP;
+#pragma unroll 1
+          for (int c = 0; c < DP; c += 32) {
+            uint32_t o[32];
+            tc_ld32(t_o + c, o);
+            tc_wait_ld();
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(part + c * 32 + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            for (int i = 0; i < 32; i += 4)
+              if (r.mine) *reinterpret_cast<uint4*>(dst + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
           }
         }
         if (r.mine && !r.whole) a.part_ml[r.prow] = make_float2(m2, l);
@@ -698,7 +745,8 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     };
 #pragma unroll 1
     for (;;) {
-      const bool more = next_item(next);                    // (its Q arrives while the last item's last product runs)
+      const bool more = next_item(next);
+      if (E4M3 && more) convert_q(next);                    // (while the last item's last product runs)
       if (!first_round) result();
       if (!more) break;
       first_round = false;
@@ -843,61 +891,73 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 }
 
 // ---------------------------------------------------------------- rows whose keys were in several places
-constexpr int kJoinThreads = 256, kJoinBlocks = 4 * 148;
 
-// The partial results of one item for one of its rows, joined into (m, l, o) of a warp; o: this lane's columns 4 lane .. + 3.
-template <int DP>
-__device__ __forceinline__ void join_item(const AttnArgs& a, const AttnSched& s, const AttnWalk& k, const AttnItem& it, int row, float& m, float& l, float4& o) {
+// A row's running (maximum, sum, output), in log2 and unscaled; o: a lane's columns 4 lane .. + 3.
+struct Joined { float m, l; float4 o; };
+
+// Where the partial results of an item are: lane i has the first row of the i-th of a round of 32 (-1: none), for CTAs c0, c0 + 1, ...
+__device__ __forceinline__ long long part_place(const AttnArgs& a, const AttnSched& s, const AttnWalk& k, const AttnItem& it, int c0, int c_hi) {
+  const int lane = threadIdx.x & 31, c = c0 + (lane >> 1);               // a lane for each of a CTA's two results
+  if (c > c_hi) return -1;
+  const int s0 = attn_steps_before(k, it.n, c * s.share), s1 = attn_steps_before(k, it.n, (c + 1) * s.share);
+  return s0 < s1 && (lane & 1) < attn_part_count(it, s0, s1) ? attn_part_row(it, c, s0) + (lane & 1) * it.n_tok * a.p.Gh : -1;
+}
+
+// Joins a round of partial results into `n` (up to N) rows, row0 and those behind it; every lane's loads for all rows go out together.
+template <int DP, int N>
+__device__ __forceinline__ void join_rows(const AttnArgs& a, long long place, int row0, int n, Joined (&j)[N]) {
   const int lane = threadIdx.x & 31;
-  const int c_lo = (int)(k.at / s.share), c_hi = (int)((k.at + k.w - 1) / s.share);
-  for (int c0 = c_lo; c0 <= c_hi; c0 += 16) {               // a lane for each of a CTA's two results
-    const int c = c0 + (lane >> 1);
-    long long at = -1;
-    float2 ml = make_float2(-CUDART_INF_F, 0.f);
-    if (c <= c_hi) {
-      const int s0 = attn_steps_before(k, it.n, c * s.share), s1 = attn_steps_before(k, it.n, (c + 1) * s.share);
-      if (s0 < s1 && (lane & 1) < attn_part_count(it, s0, s1)) {
-        at = attn_part_row(it, c, s0) + (lane & 1) * it.n_tok * a.p.Gh + row;
-        ml = a.part_ml[at];
-      }
-    }
-    float top = ml.x;
+  float2 ml[N];
+  float f[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) ml[i] = place >= 0 && i < n ? a.part_ml[place + row0 + i] : make_float2(-CUDART_INF_F, 0.f);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float top = ml[i].x;
 #pragma unroll
     for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    top = fmaxf(top, m);
-    const float base = top == -CUDART_INF_F ? 0.f : top;
-    const float keep = ex2(m - base);
-    o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep; l *= keep;
-    m = top;
-    const float f = ex2(ml.x - base);
-    float add = ml.y * f;
+    top = fmaxf(top, j[i].m);
+    const float base = top == -CUDART_INF_F ? 0.f : top, keep = ex2(j[i].m - base);
+    j[i].o.x *= keep; j[i].o.y *= keep; j[i].o.z *= keep; j[i].o.w *= keep;
+    j[i].m = top;
+    f[i] = ex2(ml[i].x - base);
+    float add = ml[i].y * f[i];
 #pragma unroll
     for (int d = 16; d; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
-    l += add;
-    unsigned have = __ballot_sync(0xffffffffu, at >= 0);
-    while (have) {
-      const int src = __ffs(have) - 1;
-      have &= have - 1;
-      const long long r = __shfl_sync(0xffffffffu, at, src);
-      const float g = __shfl_sync(0xffffffffu, f, src);
-      if (lane < DP / 4) {
-        const float4 v = *reinterpret_cast<const float4*>(a.part_o + r * DP + lane * 4);
-        o.x += v.x * g; o.y += v.y * g; o.z += v.z * g; o.w += v.w * g;
+    j[i].l = j[i].l * keep + add;
+  }
+  unsigned have = __ballot_sync(0xffffffffu, place >= 0);
+#pragma unroll 2
+  while (have) {
+    const int src = __ffs(have) - 1;
+    have &= have - 1;
+    const long long r = __shfl_sync(0xffffffffu, place, src) + row0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float g = __shfl_sync(0xffffffffu, f[i], src);
+      if (i < n && lane < DP / 4) {
+        const float4 v = *reinterpret_cast<const float4*>(a.part_o + (r + i) * DP + lane * 4);
+        j[i].o.x += v.x * g; j[i].o.y += v.y * g; j[i].o.z += v.z * g; j[i].o.w += v.w * g;
       }
     }
   }
 }
 
 template <int DP>
-__device__ __forceinline__ void write_row(const AttnArgs& a, int token, int head, float m, float l, float4 o) {
+__device__ __forceinline__ void write_row(const AttnArgs& a, int token, int head, int kvh, const Joined& j) {
   const int lane = threadIdx.x & 31;
-  const float inv = l > 0.f ? (a.v_scale ? a.v_scale[head / a.p.Gh] : 1.f) / l : l;
+  const float inv = j.l > 0.f ? (a.v_scale ? a.v_scale[kvh] : 1.f) / j.l : j.l;
   if (lane * 4 < a.D) {
-    const uint2 v = l == 0.f ? make_uint2(0, 0) : make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    const uint2 v = j.l == 0.f ? make_uint2(0, 0) : make_uint2(pack_bf16(j.o.x * inv, j.o.y * inv), pack_bf16(j.o.z * inv, j.o.w * inv));
     *reinterpret_cast<uint2*>(a.out + (long long)token * a.out_tok + (long long)head * a.out_head + lane * 4) = v;
   }
-  if (lane == 0 && a.lse) a.lse[(long long)token * a.lse_tok + head] = (m + __log2f(l)) * 0.6931471805599453f;
+  if (lane == 0 && a.lse) a.lse[(long long)token * a.lse_tok + head] = (j.m + __log2f(j.l)) * 0.6931471805599453f;
 }
+
+// Rows of two kinds.  A token of a sequence with partial rows of its own: its group's prefix and its own keys, or both in one item; a
+// unit of work is up to kJoinRows of its heads that share a kv head.  A longer sequence's item that a cut between two CTAs' shares went
+// through, found at its first cut: a unit is kJoinRows of its rows.
+constexpr int kJoinThreads = 256, kJoinRows = 4;
 
 template <int DP>
 __global__ void __launch_bounds__(kJoinThreads)
@@ -909,65 +969,94 @@ attn_join_kernel(const __grid_constant__ AttnArgs a) {
   {
     int32_t* dst = reinterpret_cast<int32_t*>(join_smem);
     const int32_t* src = static_cast<const int32_t*>(a.sched);
-    for (int i = tid; i < attn_sched_words(p.B, p.G); i += kJoinThreads) dst[i] = src[i];
+#pragma unroll 2
+    for (int i = tid; i < attn_sched_words(p.B, p.G) + p.n_ctas; i += kJoinThreads) dst[i] = src[i];
     __syncthreads();
   }
   AttnSched s = attn_carve(join_smem, p.B, p.G);
+  const int32_t* cuts = reinterpret_cast<const int32_t*>(join_smem) + attn_sched_words(p.B, p.G);
   s.share = attn_share(p, s.cost[p.G + p.B]);
-  // tokens of sequences with partial rows of their own: their group's prefix and their own keys, or both in one item
-  const int n_rows = s.pcum[p.B] * p.Hq;                    // (below 2^31: checked by the plan)
-  for (int u = blockIdx.x * warps + warp; u < n_rows; u += gridDim.x * warps) {
-    const int i = u / p.Hq, head = u - i * p.Hq, b = sequence_of(s.pcum, 0, p.B, i), g = s.group[b], t = i - s.pcum[b];
-    const int kvh = head / p.Gh, rh = head - kvh * p.Gh;
-    float m = -CUDART_INF_F, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int per_head = (p.Gh + kJoinRows - 1) / kJoinRows, per_token = p.Hkv * per_head;
+  const int n_own = s.pcum[p.B] * per_token;                // (below 2^31: checked by the plan)
+  const int per_cut = (2 * p.tps * p.Gh + kJoinRows - 1) / kJoinRows, n_units = n_own + (p.n_ctas - 1) * per_cut;
+#pragma unroll 1
+  for (int u = blockIdx.x * warps + warp; u < n_units; u += gridDim.x * warps) {
+    Joined j[kJoinRows];
+#pragma unroll
+    for (int i = 0; i < kJoinRows; ++i) j[i] = Joined{-CUDART_INF_F, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+    int row0, n, token, kvh, head;                          // rows of the item; first one's token and head
     AttnWalk k;
     k.done = false;
-    k.head = kvh;
-    const bool shares = attn_is_short(p, s, b);
-#pragma unroll 1
-    for (int part = shares ? 0 : 1; part < 2; ++part) {
-      k.e = part ? p.G + b : g;
-      k.x = attn_entity(p, s, k.e);
-      if (k.x.items == 0) continue;                         // (no own keys)
-      const int at = part ? t : s.scum[b] - s.scum[s.gfirst[g]] + t;     // token among the entity's
-      k.r = at / (2 * p.tps);
-      k.w = k.x.a + k.x.slope * (k.r + 1);
-      k.at = s.cost[k.e] + kvh * attn_items_cost(k.x, k.x.items) + attn_items_cost(k.x, k.r);
-      const AttnItem it = attn_item(p, s, k);
-      if (!shares) {                                        // final already?
-        const int c = (int)(k.at / s.share);
-        if (attn_is_whole(it, attn_steps_before(k, it.n, c * s.share), attn_steps_before(k, it.n, (c + 1) * s.share))) { k.done = true; break; }
-      }
-      join_item<DP>(a, s, k, it, (at - k.r * 2 * p.tps) * p.Gh + rh, m, l, o);
+    int part, last, b, g = -1, t = 0;                       // items: 0 the group's, 1 the sequence's
+    if (u < n_own) {
+      const int i = u / per_token, in_token = u - i * per_token;
+      kvh = in_token / per_head;
+      b = sequence_of(s.pcum, 0, p.B, i); g = s.group[b]; t = i - s.pcum[b];
+      const int h0 = (in_token - kvh * per_head) * kJoinRows;
+      n = min(kJoinRows, p.Gh - h0);
+      head = kvh * p.Gh + h0;
+      token = s.q0[b] + t;
+      row0 = h0;                                            // of the token's
+      part = attn_is_short(p, s, b) ? 0 : 1; last = 1;
+    } else {
+      const int cut = (u - n_own) / per_cut;
+      if (!cuts[cut + 1]) continue;
+      k = attn_walk_at(p, s, (cut + 1) * s.share);
+      row0 = (u - n_own - cut * per_cut) * kJoinRows;
+      part = last = 2; kvh = k.head; b = k.e - p.G; n = token = head = 0;
     }
-    if (!k.done) write_row<DP>(a, s.q0[b] + t, head, m, l, o);
-  }
-  // longer sequences' items that a cut between two CTAs' shares went through: found at their first cut
-  for (int c = 1 + blockIdx.x; c < p.n_ctas; c += gridDim.x) {
-    const int x = c * s.share;
-    const AttnWalk k = attn_walk_at(p, s, x);
-    if (k.done) break;
-    const AttnItem it = attn_item(p, s, k);
-    if (it.kind != kAttnJoint || attn_has_rows(p, s, it.b)) continue;
-    const int before = attn_steps_before(k, it.n, x);
-    if (before == 0 || before == it.n || attn_steps_before(k, it.n, x - s.share) > 0) continue;
-    for (int r = warp; r < it.n_tok * p.Gh; r += warps) {
-      float m = -CUDART_INF_F, l = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      join_item<DP>(a, s, k, it, r, m, l, o);
-      const int tt = r / p.Gh;
-      write_row<DP>(a, s.q0[it.b] + it.tok + tt, it.head * p.Gh + (r - tt * p.Gh), m, l, o);
+#pragma unroll 1
+    for (; part <= last; ++part) {
+      int row = row0;
+      if (part < 2) {
+        k.e = part ? p.G + b : g;
+        k.x = attn_entity(p, s, k.e);
+        if (k.x.items == 0) continue;                       // (no own keys)
+        const int at = part ? t : s.scum[b] - s.scum[s.gfirst[g]] + t;   // token among the entity's
+        k.head = kvh;
+        k.r = attn_div(at, 2 * p.tps);
+        k.w = k.x.a + k.x.slope * (k.r + 1);
+        k.at = s.cost[k.e] + kvh * attn_items_cost(k.x, k.x.items) + attn_items_cost(k.x, k.r);
+        row += (at - k.r * 2 * p.tps) * p.Gh;
+      }
+      const AttnItem it = attn_item(p, s, k);
+      const int c_lo = attn_div(k.at, s.share), c_hi = attn_div(k.at + k.w - 1, s.share);
+      if (it.kind == kAttnJoint) {
+        const int first = attn_steps_before(k, it.n, (c_lo + 1) * s.share);
+        if (part == 2) {
+          n = min(kJoinRows, it.n_tok * p.Gh - row0);
+          if (n <= 0) { k.done = true; break; }
+        } else if (attn_is_whole(it, 0, first)) {           // final already
+          k.done = true; break;
+        }
+      }
+#pragma unroll 1
+      for (int c0 = c_lo; c0 <= c_hi; c0 += 16) join_rows<DP>(a, part_place(a, s, k, it, c0, c_hi), row, n, j);
+      if (part == 2) token = s.q0[b] + it.tok;
+    }
+    if (k.done) continue;
+#pragma unroll
+    for (int i = 0; i < kJoinRows; ++i) {
+      if (i >= n) break;
+      const int r = row0 + i, tt = u < n_own ? 0 : attn_div(r, p.Gh);
+      write_row<DP>(a, token + tt, u < n_own ? head + i : kvh * p.Gh + (r - tt * p.Gh), kvh, j[i]);
     }
   }
 }
 
+// A warp per unit up to four blocks per SM, which the host bounds by what the tokens may need: it does not know the lengths.
+int join_blocks(const AttnArgs& a) {
+  const long long per_token = (long long)a.p.Hkv * ((a.p.Gh + kJoinRows - 1) / kJoinRows);
+  const long long units = std::min<long long>(a.p.T, 2ll * a.p.tps * a.p.B) * per_token + (a.p.n_ctas - 1) * (long long)((2 * a.p.tps * a.p.Gh + kJoinRows - 1) / kJoinRows);
+  return (int)std::min<long long>(4 * a.p.n_ctas, (units + kJoinThreads / 32 - 1) / (kJoinThreads / 32));
+}
+
 template <int DP, bool E4M3>
-cudaError_t launch_dim(const AttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t s) {
+cudaError_t launch_dim(const AttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& q1, const CUtensorMap& qn, cudaStream_t s) {
   const int words = attn_sched_words(a.p.B, a.p.G);
-  cudaError_t e = launch_pdl(attn_kernel<DP, E4M3>, dim3(a.p.n_ctas), dim3(Layout<DP, E4M3>::threads), Layout<DP, E4M3>::smem(words), s, 1, a, tk, tv);
+  cudaError_t e = launch_pdl(attn_kernel<DP, E4M3>, dim3(a.p.n_ctas), dim3(Layout<DP, E4M3>::threads), Layout<DP, E4M3>::smem(words), s, 1, a, tk, tv, q1, qn);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attn_join_kernel<DP>, dim3(kJoinBlocks), dim3(kJoinThreads), words * 4, s, 1, a);
+  return launch_pdl(attn_join_kernel<DP>, dim3(join_blocks(a)), dim3(kJoinThreads), (words + a.p.n_ctas) * 4, s, 1, a);
 }
 
 }  // namespace
@@ -982,7 +1071,10 @@ cudaError_t attn_setup() {
   return e;
 }
 
-int make_cache_map(GemmTensorMap* out, const void* base, const cep_attn_config& c, const int64_t* stride) {
+namespace {
+// A tensor map of 16-byte aligned elements in 128-byte swizzled (bf16) or plain (e4m3) boxes; a stride counts where there is a second
+// element along it.
+int encode(GemmTensorMap* out, const void* base, bool e4m3, int rank, const long long* n, const int64_t* stride, const int* box_of) {
   typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   static Encode enc = [] {
@@ -992,26 +1084,39 @@ int make_cache_map(GemmTensorMap* out, const void* base, const cep_attn_config& 
     return ok ? reinterpret_cast<Encode>(p) : nullptr;
   }();
   if (!enc) return -1;
-  const bool e4m3 = c.cache_elem == CEP_ELEM_E4M3;
-  const int elt = e4m3 ? 1 : 2, box_rows = c.page_size < kAttnTile ? c.page_size : kAttnTile;
-  const long long room = (c.head_dim * elt + 15) / 16 * 16;           // (the stride of a single element means nothing)
-  auto bytes = [&](int64_t n, int64_t st) { return (cuuint64_t)(n > 1 ? st * elt : room); };
-  cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
-  cuuint64_t strides[3] = {bytes(c.page_size, stride[1]), bytes(c.n_kv_heads, stride[2]), bytes(c.n_pages, stride[0])};
-  cuuint32_t box[4] = {(cuuint32_t)(e4m3 ? attn_padded_dim(c.head_dim) : 64), (cuuint32_t)box_rows, 1, 1}, es[4] = {1, 1, 1, 1};
-  const CUresult r = enc(reinterpret_cast<CUtensorMap*>(out), e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+  const int elt = e4m3 ? 1 : 2;
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t box[4], es[4] = {1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) { dims[i] = (cuuint64_t)n[i]; box[i] = (cuuint32_t)box_of[i]; }
+  for (int i = 1; i < rank; ++i) strides[i - 1] = (cuuint64_t)(n[i] > 1 ? stride[i] * elt : (n[0] * elt + 15) / 16 * 16);
+  const CUresult r = enc(reinterpret_cast<CUtensorMap*>(out), e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
                          const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                          e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? 0 : -2;
 }
+}  // namespace
 
-cudaError_t launch_attn(const AttnArgs& a, int e4m3, const GemmTensorMap& tm_k, const GemmTensorMap& tm_v, cudaStream_t s) {
-  const CUtensorMap& tk = reinterpret_cast<const CUtensorMap&>(tm_k);
-  const CUtensorMap& tv = reinterpret_cast<const CUtensorMap&>(tm_v);
+int make_cache_map(GemmTensorMap* out, const void* base, const cep_attn_config& c, const int64_t* stride) {
+  const bool e4m3 = c.cache_elem == CEP_ELEM_E4M3;
+  const long long n[4] = {c.head_dim, c.page_size, c.n_kv_heads, c.n_pages};
+  const int64_t st[4] = {1, stride[1], stride[2], stride[0]};
+  const int box[4] = {e4m3 ? attn_padded_dim(c.head_dim) : 64, c.page_size < kAttnTile ? c.page_size : kAttnTile, 1, 1};
+  return encode(out, base, e4m3, 4, n, st, box);
+}
+
+int make_q_map(GemmTensorMap* out, const AttnArgs& a, int tokens) {
+  const long long n[3] = {a.D, a.p.Hq, a.p.T};
+  const int64_t st[3] = {1, a.q_head, a.q_tok};
+  const int box[3] = {64, a.p.Gh, tokens};
+  return encode(out, a.q, false, 3, n, st, box);
+}
+
+cudaError_t launch_attn(const AttnArgs& a, int e4m3, const GemmTensorMap (&maps)[4], cudaStream_t s) {
+  auto map = [&](int i) -> const CUtensorMap& { return reinterpret_cast<const CUtensorMap&>(maps[i]); };
   const bool narrow = attn_padded_dim(a.D) == 64;
-  if (e4m3) return narrow ? launch_dim<64, true>(a, tk, tv, s) : launch_dim<128, true>(a, tk, tv, s);
-  return narrow ? launch_dim<64, false>(a, tk, tv, s) : launch_dim<128, false>(a, tk, tv, s);
+  if (e4m3) return narrow ? launch_dim<64, true>(a, map(0), map(1), map(2), map(3), s) : launch_dim<128, true>(a, map(0), map(1), map(2), map(3), s);
+  return narrow ? launch_dim<64, false>(a, map(0), map(1), map(2), map(3), s) : launch_dim<128, false>(a, map(0), map(1), map(2), map(3), s);
 }
 
 }  // namespace cep
