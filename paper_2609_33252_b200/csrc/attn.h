@@ -25,7 +25,7 @@ constexpr int kAttnMaxSeqs = 1024, kAttnMaxPrefixes = 256;
 constexpr int kAttnMaxCtas = 148;
 constexpr int kAttnSplitRows = 2 * 2 * kAttnTile;                      // partial rows that a CTA's two cut items may need
 // Estimated cost of four keys for one row tile (taken by the warpgroups in turn) and for two, and of an item beside its keys.
-constexpr int kAttnCostSingle = 2, kAttnCostDual = 3, kAttnCostItem = 112;
+constexpr int kAttnCostSingle = 2, kAttnCostDual = 4, kAttnItemSingle = 150, kAttnItemDual = 400;
 
 struct AttnShape {
   int T, B, G;                               // tokens, sequences, groups
@@ -116,10 +116,10 @@ __host__ __device__ inline AttnEntity attn_entity(const AttnShape& p, const Attn
       if (g >= 0) keys += s.glen[g];
     }
   }
-  const int unit = n > p.tps ? kAttnCostDual : kAttnCostSingle;
+  const int unit = n > p.tps ? kAttnCostDual : kAttnCostSingle, fixed = n > p.tps ? kAttnItemDual : kAttnItemSingle;
   AttnEntity x;
   x.items = some ? attn_tiles(p, n) : 0;
-  x.a = (int)((kAttnCostItem + (long long)unit * (keys >> 2)) >> p.cost_shift) + 1;
+  x.a = (int)((fixed + (long long)unit * (keys >> 2)) >> p.cost_shift) + 1;
   x.slope = slope ? unit * 2 * p.tps >> (2 + p.cost_shift) : 0;
   return x;
 }
@@ -256,7 +256,7 @@ __host__ __device__ inline long long attn_max_part_rows(int max_tokens, int max_
 __host__ __device__ inline int attn_share(const AttnShape& p, int total) {
   // (fp32 is off by 2^-23 of the sum at most, which is less than one part in 10^4 of a share)
   int share = (int)((float)total * p.per_cta) + 1 + (total >> 21);
-  const int least = (kAttnTile / 4 * kAttnCostSingle + kAttnCostItem / 4) >> p.cost_shift;
+  const int least = (kAttnTile / 4 * kAttnCostSingle + kAttnItemSingle / 8) >> p.cost_shift;
   return share > least ? share : least;
 }
 
@@ -268,7 +268,7 @@ inline AttnShape attn_shape(int T, int B, int G, int Hq, int Hkv, int causal, lo
   p.tile_magic = (uint32_t)(0x100000000ull / (2 * p.tps) + 1);
   // more than all items can cost: every item with as many keys as the tables hold, and the slope's rounding
   const double items = (double)Hkv * ((double)T / (2 * p.tps) + B + G);
-  const double most = items * (kAttnCostItem + 2 + kAttnCostDual * 0.25 * ((double)own_cap + (double)prefix_cap + T + 4 * p.tps));
+  const double most = items * (kAttnItemDual + 2 + kAttnCostDual * 0.25 * ((double)own_cap + (double)prefix_cap + T + 4 * p.tps));
   while (ldexp(most, -p.cost_shift) + items > 2.0e9) ++p.cost_shift;
   return p;
 }
