@@ -2,8 +2,11 @@
 runs them: the output projection with per-request low-rank adapters, the residual's addition with the norm and the
 expert layer's activation format, the router's logits and selection, the routed experts.
 
-``python -m paper_2609_33252_b200.block [dtype] [tokens]`` runs it on random weights and prints the device time of every
-step (dtype: bf16, fp8 or mxfp4).
+``AttentionBlock`` is what comes before: projection to q, k and v, rotation and the write into a paged cache, attention of
+requests that share a prefix.
+
+``python -m paper_2609_33252_b200.block [dtype] [tokens] [prefix]`` runs it on random weights and prints the device time of every
+step (dtype: bf16, fp8 or mxfp4); with a prefix, the attention block too, requests of 64 tokens behind that many shared keys.
 """
 from __future__ import annotations
 
@@ -85,7 +88,71 @@ class MoEBlock:
         self.layer.close()
 
 
-def main(dtype="mxfp4", tokens=4096):
+class AttentionBlock:
+    """From a layer's normed input to its attention output (what ``MoEBlock`` takes), over the layer's paged cache.
+
+    w_qkv bf16 [(Hq + 2 Hkv) D, H]: rows of all query heads, then the key heads, then the value heads; k_cache, v_cache
+    [pages, page_size, Hkv, D] bf16 or float8_e4m3fn (with k_scale, v_scale fp32 [Hkv]); inv_freq fp32 [R/2].  All are the caller's
+    tensors.  ``run`` may be called on different streams: each call waits for the one before, as the buffers between the
+    steps are shared (who runs ``steps`` orders them).
+    """
+
+    def __init__(self, w_qkv, k_cache, v_cache, n_heads, inv_freq, max_tokens, max_seqs, max_prefixes=1, k_scale=None, v_scale=None, interleaved=False,
+                 max_adapters=0, max_rank=0):
+        Hk, D = k_cache.shape[2:]
+        self.heads = (n_heads, Hk, D)
+        if w_qkv.shape[0] != (n_heads + 2 * Hk) * D:
+            raise cep.CepError(-1, "w_qkv must have (%d + 2 * %d) * %d rows" % (n_heads, Hk, D))
+        self.inv_freq, self.interleaved = inv_freq, interleaved
+        self.projection = cep.LoRAProjection(w_qkv, max_tokens, max_adapters, max_rank)
+        self.attention = cep.PrefixAttention(k_cache, v_cache, n_heads, max_tokens, max_seqs, max_prefixes, k_scale, v_scale)
+        self.qkv = torch.empty(max_tokens, n_heads + 2 * Hk, D, dtype=torch.bfloat16, device=w_qkv.device)
+        self.out = torch.empty(max_tokens, n_heads, D, dtype=torch.bfloat16, device=w_qkv.device)
+        self.done = torch.cuda.Event()                       # the end of the last call
+
+    def steps(self, x, positions, slots, batch, adapter_ids=None, causal=True):
+        """The block as (name, call) pairs.  x bf16 [T,H]; positions int32 [T]; slots int64 [T]; batch: the lengths and page
+        tables of ``PrefixAttention.run`` as a dict, kv_len with the new tokens.  The result is ``out`` [T,Hq,D]."""
+        T, (Hq, Hk, D) = x.shape[0], self.heads
+        qkv, out, att = self.qkv[:T], self.out[:T], self.attention
+        q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
+        return [
+            ("projection to q, k, v", lambda: self.projection.run(x, adapter_ids, qkv.view(T, -1))),
+            ("rotation + cache", lambda: cep.attn_append(k, v, positions, slots, self.inv_freq, att.k_cache, att.v_cache, q=q, q_out=q,
+                                                         interleaved=self.interleaved, k_scale=att.k_scale, v_scale=att.v_scale)),
+            ("attention", lambda: att.run(q, causal=causal, out=out, **batch)),
+        ]
+
+    def run(self, x, positions, slots, batch, adapter_ids=None, causal=True):
+        """Returns the attention output [T, Hq D], a view of the block's buffer (valid until the next call)."""
+        T, (Hq, _, D) = x.shape[0], self.heads
+        stream = torch.cuda.current_stream(x.device)
+        stream.wait_event(self.done)                         # (before the first call: nothing to wait for)
+        if T:                                                # (empty tensors have no address)
+            for _, call in self.steps(x, positions, slots, batch, adapter_ids, causal):
+                call()
+        self.done.record(stream)
+        return self.out[:T].view(T, Hq * D)
+
+    def close(self):
+        self.projection.close()
+        self.attention.close()
+
+
+def _requests(tokens, prefix, page, per_request=64):
+    """Lengths, tables, positions and slots of requests of up to 64 new tokens each behind one prefix; (batch, positions, slots, pages)."""
+    n = [per_request] * (tokens // per_request) + ([tokens % per_request] if tokens % per_request else [])
+    ahead, each = -(-prefix // page), -(-per_request // page)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    first = torch.tensor([0] + n).cumsum(0).tolist()
+    table = [[ahead + b * each + i for i in range(each)] for b in range(len(n))]
+    batch = dict(q_start=i32(first), kv_len=i32(n), page_table=i32(table), prefix_len=i32([prefix]), prefix_pages=i32([list(range(ahead))]))
+    positions = i32([prefix + i for m in n for i in range(m)])
+    slots = torch.tensor([table[b][i // page] * page + i % page for b, m in enumerate(n) for i in range(m)], device="cuda")
+    return batch, positions, slots, ahead + each * len(n)
+
+
+def main(dtype="mxfp4", tokens=4096, prefix=0):
     cfg = wl.scaled(wl.CONFIGS["mid"], T=tokens, chunks=(tokens,), dtype=dtype)
     inp = wl.make_inputs(cfg, device="cuda")
     H, g = cfg.H, torch.Generator(device="cuda").manual_seed(1)
@@ -96,9 +163,19 @@ def main(dtype="mxfp4", tokens=4096):
         block.projection.load_adapter(s, rand(32, H, std=H ** -0.5), rand(H, 32, std=32 ** -0.5), 0.5)
     block.load_experts(inp.w_gate, inp.w_up, inp.w_down, inp.s_gate, inp.s_up, inp.s_down)
     attention, residual = rand(tokens, H), rand(tokens, H)
+    before = None
+    if prefix:
+        heads, kv_heads, dim, page = H // 128, max(1, H // 512), 128, 64
+        batch, positions, slots, pages = _requests(tokens, prefix, page)
+        cache = [rand(pages, page, kv_heads, dim) for _ in range(2)]
+        inv_freq = (10000.0 ** (-torch.arange(0, dim, 2, dtype=torch.float64) / dim)).float().cuda()
+        before = AttentionBlock(rand((heads + 2 * kv_heads) * dim, H, std=H ** -0.5), *cache, heads, inv_freq, tokens, batch["kv_len"].numel())
+        attention = before.out[:tokens].view(tokens, -1)
     adapters = (torch.arange(tokens, device="cuda") * 5 // tokens - 1).to(torch.int32)       # five requests, the first without
     out = torch.empty(tokens, H, dtype=torch.bfloat16, device="cuda")
     steps = block.steps(attention, residual, adapters, out, n_chunks=4)
+    if before:
+        steps = before.steps(rand(tokens, H), positions, slots, batch) + steps
     for _ in range(3):
         for _, call in steps:
             call()
@@ -109,10 +186,13 @@ def main(dtype="mxfp4", tokens=4096):
         m.record()
     torch.cuda.synchronize()
     assert cep.ffn_status(block.layer.plan) == 0 and block.projection.status() == 0
+    assert not before or before.attention.status() == 0
     for (name, _), a, b in zip(steps, marks, marks[1:]):
         print("%-26s %8.1f us" % (name, 1e3 * a.elapsed_time(b)))
     block.close()
+    if before:
+        before.close()
 
 
 if __name__ == "__main__":
-    main(*(sys.argv[1:2] or ["mxfp4"]), *[int(v) for v in sys.argv[2:3]])
+    main(*(sys.argv[1:2] or ["mxfp4"]), *[int(v) for v in sys.argv[2:4]])

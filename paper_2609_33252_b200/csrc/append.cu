@@ -1,20 +1,23 @@
 // New tokens on their way into attention: rotation of q and k by position, k and v to their slots in a paged cache.
 //
 // Per token: sines and cosines of R/2 angles, shared by all heads, then (n_heads + 2 n_kv_heads) heads that are read once and
-// written once; memory is the bound.  A block takes whole tokens.  Each thread asks for its parts of the heads before the
-// angles are computed, so that these cost no time of their own.
+// written once; memory is the bound.  A thread has the same parts of a token's heads for every token that its block comes to, so
+// that all divisions are done once; it asks for them before the angles are computed, which then cost no time of their own.
 //
 // Angles: position * inv_freq reaches 10^6 and more, where fp32 has lost the turn's fraction.  The product with 1/(2 pi) is
 // taken in fp64 (4 instructions a pair, B200 has them at half rate), the whole turns are dropped, and the rest, below half a
 // turn, goes to sincospif.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "cep_common.h"
 
 namespace cep {
 namespace {
 
-constexpr int kAppendThreads = 256, kAppendMaxDim = 1024;
+constexpr int kAppendPerSm = 1024;            // threads, of blocks that come to tokens again (768: 11.1 us where 1536 take 12.4, but 39.5 against 35.5 with small heads)
+constexpr int kAppendMaxThreads = 512, kAppendMaxDim = 1024;
 
 struct AppendArgs {
   const uint16_t *q, *k, *v; uint16_t* q_out;
@@ -27,8 +30,9 @@ struct AppendArgs {
   long long n_slots;
   int T, Hq, Hk, D, R, page_shift;
   int units;                                 // of a head: pairs of vectors
-  int tokens;                                // per block
+  int tokens;                                // that a block takes at a time
   int parts;                                 // blocks that share a token's heads (when there are few tokens)
+  int groups;                                // of blocks, each with every groups-th round of tokens
 };
 
 template <int V> struct Vec;
@@ -63,6 +67,28 @@ __device__ __forceinline__ void put_e4m3(uint8_t* p, const float (&f)[8], float 
   *reinterpret_cast<uint2*>(p) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 
+// Cosines and sines of a token in shared memory: eight threads read eight neighbouring angles each, two 16-byte chunks at a time, which
+// the swizzle keeps apart (angles as pairs of cosine and sine met four to a bank: the kernel waited for them).
+__device__ __forceinline__ int angle_room(int half) { return (half + 7) / 8 * 8; }
+__device__ __forceinline__ int angle_at(int i) { return (((i >> 2) ^ (i >> 5 & 1)) << 2) + (i & 3); }
+__device__ __forceinline__ void put_turn(float* cosines, int room, int i, int position, float inv_freq) {
+  const double turn = (double)position * ((double)inv_freq * 0.15915494309189533577);
+  float s, c;
+  sincospif((float)(2.0 * (turn - rint(turn))), &s, &c);
+  cosines[angle_at(i)] = c;
+  cosines[room + angle_at(i)] = s;
+}
+template <int V> __device__ __forceinline__ void get_turns(const float* p, int i, float (&f)[V]) {
+  if (V == 8) {
+    const float4 a = *reinterpret_cast<const float4*>(p + angle_at(i)), b = *reinterpret_cast<const float4*>(p + angle_at(i + 4));
+    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = v[j];
+  } else {
+    f[0] = p[angle_at(i)];
+  }
+}
+
 // A unit of a head: two vectors of V columns.  Rotated columns: the vectors that turn with one another (halves), or 2V
 // neighbouring columns (interleaved); behind them, and in v, 2V neighbouring columns that are copied.
 struct Place { int head, first, second, angle; };          // column of each vector (second < 0: none), first angle (-1: copied)
@@ -85,110 +111,120 @@ __device__ __forceinline__ Place place(const AppendArgs& a, int unit, int rotate
 }
 
 template <int V, bool INTERLEAVED, bool E4M3, int UNROLL>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendArgs a) {
-  extern __shared__ float2 turns[];                        // [tokens][R/2] cosine, sine
+__global__ void __launch_bounds__(kAppendMaxThreads) append_kernel(const __grid_constant__ AppendArgs a) {
+  extern __shared__ __align__(16) float turns[];                        // [2][tokens][2][R/2 rounded up] cosines, sines
   typedef typename Vec<V>::T T;
   pdl_enter();
-  const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts;
-  const int t0 = group * a.tokens, n_tok = min(a.tokens, a.T - t0), half = a.R / 2;
-  const int per_token = (a.Hq + 2 * a.Hk) * a.units, n_units = n_tok * per_token;
-  const int tid = threadIdx.x, step = a.parts * kAppendThreads;
-  bool ready = false;
-  for (int base = part * kAppendThreads + tid; base < n_units || !ready; base += UNROLL * step) {
-    T x[UNROLL], y[UNROLL];
+  const int group = blockIdx.x / a.parts, part = blockIdx.x - group * a.parts, half = a.R / 2, room = angle_room(half);
+  const int per_token = (a.Hq + 2 * a.Hk) * a.units, n_units = a.tokens * per_token;
+  const int tid = threadIdx.x, threads = blockDim.x, step = a.parts * threads;
+  int buffer = 0;
+#pragma unroll 1
+  for (int base = part * threads; base < n_units; base += UNROLL * step) {
+    // this thread's parts: columns, head, which of the tokens at a time; its tensors' base and strides
     Place pl[UNROLL];
     int tok[UNROLL];
     const uint16_t* src[UNROLL];
+    long long src_tok[UNROLL];
 #pragma unroll
     for (int i = 0; i < UNROLL; ++i) {
-      const int u = base + i * step;
-      pl[i].first = -1;
+      const int u = base + i * step + tid;
+      pl[i].first = -1; tok[i] = 0; src[i] = nullptr; src_tok[i] = 0;
       if (u >= n_units) continue;
       tok[i] = u / per_token;
-      const int in_token = u - tok[i] * per_token, vs = (a.Hq + a.Hk) * a.units;
-      pl[i] = place<V, INTERLEAVED>(a, in_token, in_token < vs ? a.R : 0);
+      const int in_token = u - tok[i] * per_token;
+      pl[i] = place<V, INTERLEAVED>(a, in_token, in_token < (a.Hq + a.Hk) * a.units ? a.R : 0);
       if (pl[i].first < 0) continue;
-      const long long t = t0 + tok[i];
       const int h = pl[i].head;
-      src[i] = h < a.Hq ? a.q + t * a.q_tok + h * a.q_head
-             : h < a.Hq + a.Hk ? a.k + t * a.k_tok + (h - a.Hq) * a.k_head : a.v + t * a.v_tok + (h - a.Hq - a.Hk) * a.v_head;
-      x[i] = *reinterpret_cast<const T*>(src[i] + pl[i].first);
-      if (pl[i].second >= 0) y[i] = *reinterpret_cast<const T*>(src[i] + pl[i].second);
+      src[i] = h < a.Hq ? a.q + h * a.q_head : h < a.Hq + a.Hk ? a.k + (h - a.Hq) * a.k_head : a.v + (h - a.Hq - a.Hk) * a.v_head;
+      src_tok[i] = h < a.Hq ? a.q_tok : h < a.Hq + a.Hk ? a.k_tok : a.v_tok;
     }
-    if (!ready) {                                          // (every thread comes here once)
-      for (int i = tid; i < n_tok * half; i += kAppendThreads) {
+#pragma unroll 1
+    for (long long t0 = (long long)group * a.tokens; t0 < a.T; t0 += (long long)a.groups * a.tokens) {
+      const int n_tok = (int)min((long long)a.tokens, a.T - t0);
+      T x[UNROLL], y[UNROLL];
+      long long slot[UNROLL];
+#pragma unroll
+      for (int i = 0; i < UNROLL; ++i) {
+        if (pl[i].first < 0 || tok[i] >= n_tok) continue;
+        const uint16_t* from = src[i] + (t0 + tok[i]) * src_tok[i];
+        x[i] = *reinterpret_cast<const T*>(from + pl[i].first);
+        if (pl[i].second >= 0) y[i] = *reinterpret_cast<const T*>(from + pl[i].second);
+        slot[i] = pl[i].head < a.Hq ? 0 : a.slots[t0 + tok[i]];
+      }
+      float* cs_of = turns + buffer * a.tokens * 2 * room;
+      buffer ^= 1;                                         // (the other one may still be read)
+      for (int i = tid; i < n_tok * half; i += threads) {
         const int t = i / half, f = i - t * half;
-        const double turn = (double)a.positions[t0 + t] * ((double)a.inv_freq[f] * 0.15915494309189533577);
-        float2 cs;
-        sincospif((float)(2.0 * (turn - rint(turn))), &cs.y, &cs.x);
-        turns[i] = cs;
+        put_turn(cs_of + t * 2 * room, room, f, a.positions[t0 + t], a.inv_freq[f]);
       }
       __syncthreads();
-      ready = true;
-    }
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
-      if (pl[i].first < 0) continue;
-      float f[V], g[V];
-      unpack(x[i], f);
-      if (pl[i].second >= 0) unpack(y[i], g);
-      if (pl[i].angle >= 0) {
-        const float2* cs = turns + tok[i] * half + pl[i].angle;
-        if (INTERLEAVED && V > 1) {
+      for (int i = 0; i < UNROLL; ++i) {
+        if (pl[i].first < 0 || tok[i] >= n_tok) continue;
+        float f[V], g[V];
+        unpack(x[i], f);
+        if (pl[i].second >= 0) unpack(y[i], g);
+        if (pl[i].angle >= 0) {
+          float co[V], si[V];
+          get_turns<V>(cs_of + tok[i] * 2 * room, pl[i].angle, co);
+          get_turns<V>(cs_of + tok[i] * 2 * room + room, pl[i].angle, si);
+          if (INTERLEAVED && V > 1) {
 #pragma unroll
-          for (int j = 0; j < V; j += 2) {
-            const float2 c0 = cs[j / 2], c1 = cs[V / 2 + j / 2];
-            const float p0 = f[j], p1 = f[(j + 1) % V], r0 = g[j], r1 = g[(j + 1) % V];
-            f[j] = p0 * c0.x - p1 * c0.y; f[(j + 1) % V] = p0 * c0.y + p1 * c0.x;
-            g[j] = r0 * c1.x - r1 * c1.y; g[(j + 1) % V] = r0 * c1.y + r1 * c1.x;
-          }
-        } else {
+            for (int j = 0; j < V; j += 2) {
+              const float c0 = co[j / 2], s0 = si[j / 2], c1 = co[V / 2 + j / 2], s1 = si[V / 2 + j / 2];
+              const float p0 = f[j], p1 = f[(j + 1) % V], r0 = g[j], r1 = g[(j + 1) % V];
+              f[j] = p0 * c0 - p1 * s0; f[(j + 1) % V] = p0 * s0 + p1 * c0;
+              g[j] = r0 * c1 - r1 * s1; g[(j + 1) % V] = r0 * s1 + r1 * c1;
+            }
+          } else {
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            const float2 c = cs[j];
-            const float p0 = f[j], p1 = g[j];
-            f[j] = p0 * c.x - p1 * c.y; g[j] = p0 * c.y + p1 * c.x;
+            for (int j = 0; j < V; ++j) {
+              const float p0 = f[j], p1 = g[j];
+              f[j] = p0 * co[j] - p1 * si[j]; g[j] = p0 * si[j] + p1 * co[j];
+            }
           }
         }
-      }
-      const long long t = t0 + tok[i];
-      int h = pl[i].head;
-      if (h < a.Hq) {
-        uint16_t* dst = a.q_out + t * a.qo_tok + h * a.qo_head;
-        put_bf16(dst + pl[i].first, f);
-        if (pl[i].second >= 0) put_bf16(dst + pl[i].second, g);
-        continue;
-      }
-      const long long slot = a.slots[t];
-      if (slot < 0 || slot >= a.n_slots) {
-        if (slot != -1 && a.status) *a.status = 1;
-        continue;
-      }
-      h -= a.Hq;
-      const bool is_k = h < a.Hk;
-      if (!is_k) h -= a.Hk;
-      const long long page = slot >> a.page_shift, pos = slot & ((1 << a.page_shift) - 1);
-      const long long at = is_k ? page * a.kc[0] + pos * a.kc[1] + h * a.kc[2] : page * a.vc[0] + pos * a.vc[1] + h * a.vc[2];
-      uint8_t* cache = is_k ? a.k_cache : a.v_cache;
-      if (E4M3) {
-        const float* scale = is_k ? a.k_scale : a.v_scale;
-        const float s = scale ? scale[h] : 1.f;
-        put_e4m3(cache + at + pl[i].first, f, s);
-        if (pl[i].second >= 0) put_e4m3(cache + at + pl[i].second, g, s);
-      } else {
-        uint16_t* dst = reinterpret_cast<uint16_t*>(cache) + at;
-        put_bf16(dst + pl[i].first, f);
-        if (pl[i].second >= 0) put_bf16(dst + pl[i].second, g);
+        int h = pl[i].head;
+        if (h < a.Hq) {
+          uint16_t* dst = a.q_out + (t0 + tok[i]) * a.qo_tok + h * a.qo_head;
+          put_bf16(dst + pl[i].first, f);
+          if (pl[i].second >= 0) put_bf16(dst + pl[i].second, g);
+          continue;
+        }
+        if (slot[i] < 0 || slot[i] >= a.n_slots) {
+          if (slot[i] != -1 && a.status) *a.status = 1;
+          continue;
+        }
+        h -= a.Hq;
+        const bool is_k = h < a.Hk;
+        if (!is_k) h -= a.Hk;
+        const long long page = slot[i] >> a.page_shift, pos = slot[i] & ((1 << a.page_shift) - 1);
+        const long long at = is_k ? page * a.kc[0] + pos * a.kc[1] + h * a.kc[2] : page * a.vc[0] + pos * a.vc[1] + h * a.vc[2];
+        uint8_t* cache = is_k ? a.k_cache : a.v_cache;
+        if (E4M3) {
+          const float* scale = is_k ? a.k_scale : a.v_scale;
+          const float s = scale ? scale[h] : 1.f;
+          put_e4m3(cache + at + pl[i].first, f, s);
+          if (pl[i].second >= 0) put_e4m3(cache + at + pl[i].second, g, s);
+        } else {
+          uint16_t* dst = reinterpret_cast<uint16_t*>(cache) + at;
+          put_bf16(dst + pl[i].first, f);
+          if (pl[i].second >= 0) put_bf16(dst + pl[i].second, g);
+        }
       }
     }
   }
 }
 
+constexpr int unroll_of(int v) { return v == 8 ? 3 : 4; }
+
 template <int V, bool INTERLEAVED>
-cudaError_t launch(const AppendArgs& a, bool e4m3, int blocks, size_t smem, cudaStream_t s) {
-  constexpr int U = V == 8 ? 3 : 2;
-  if (e4m3) return launch_pdl(append_kernel<V, INTERLEAVED, true, U>, dim3(blocks), dim3(kAppendThreads), smem, s, 1, a);
-  return launch_pdl(append_kernel<V, INTERLEAVED, false, U>, dim3(blocks), dim3(kAppendThreads), smem, s, 1, a);
+cudaError_t launch(const AppendArgs& a, bool e4m3, int threads, size_t smem, cudaStream_t s) {
+  constexpr int U = unroll_of(V);
+  const dim3 grid(a.groups * a.parts), block(threads);
+  if (e4m3) return launch_pdl(append_kernel<V, INTERLEAVED, true, U>, grid, block, smem, s, 1, a);
+  return launch_pdl(append_kernel<V, INTERLEAVED, false, U>, grid, block, smem, s, 1, a);
 }
 
 bool on(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -250,20 +286,25 @@ extern "C" int attn_append(const cep_append_desc* d, const void* q, const void* 
   a.units = (a.R / (2 * V)) + (a.D - a.R + 2 * V - 1) / (2 * V);
   const int v_units = (a.D + 2 * V - 1) / (2 * V);
   if (v_units > a.units) a.units = v_units;
-  const int per_token = (a.Hq + 2 * a.Hk) * a.units, unroll = wide ? 3 : 2;
-  // Few tokens: a token's heads are shared by as many blocks as can have a thread's worth of loads each.  Many: as many
-  // tokens per block as keep all its threads loading, and the device full.
+  const int per_token = (a.Hq + 2 * a.Hk) * a.units, unroll = unroll_of(V);
+  auto warps = [](int n) { return (n + 31) / 32 * 32; };
+  // Few tokens: a token's heads are shared by blocks whose threads have a part each.  Many: as many tokens at a time as give 256 threads
+  // their parts, and blocks that come to tokens again and again, up to what the device holds.
+  int threads;
   a.tokens = 1; a.parts = 1;
-  const int passes = (per_token + kAppendThreads * unroll - 1) / (kAppendThreads * unroll);
-  if (a.T < 2 * 148 && passes > 0) a.parts = (per_token + kAppendThreads - 1) / kAppendThreads;
-  else
-    while (a.tokens < 16 && a.tokens * 2 * per_token <= kAppendThreads * unroll && a.T / (a.tokens * 2) >= 4 * 148) a.tokens *= 2;
-  const long long blocks = ((long long)a.T + a.tokens - 1) / a.tokens * a.parts;
-  if (blocks > 0x7fffffffll) return record_error(CEP_ERR_UNSUPPORTED, "append: too many tokens");
-  const size_t smem = (size_t)a.tokens * (a.R / 2) * sizeof(float2);
+  if (a.T < 2 * 148) {
+    threads = std::min(256, warps(per_token));
+    a.parts = (per_token + threads - 1) / threads;
+  } else {
+    while (a.tokens < 16 && a.tokens * 2 * per_token <= 256 * unroll) a.tokens *= 2;
+    threads = std::min(kAppendMaxThreads, warps((a.tokens * per_token + unroll - 1) / unroll));
+  }
+  a.groups = std::min((a.T + a.tokens - 1) / a.tokens, 148 * std::max(1, kAppendPerSm / threads));
+  if (a.parts > 1) a.groups = a.T;
+  const size_t smem = 2 * (size_t)a.tokens * 2 * ((a.R / 2 + 7) / 8 * 8) * sizeof(float);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = wide ? (d->interleaved ? launch<8, true>(a, e4m3, (int)blocks, smem, s) : launch<8, false>(a, e4m3, (int)blocks, smem, s))
-                             : (d->interleaved ? launch<1, true>(a, e4m3, (int)blocks, smem, s) : launch<1, false>(a, e4m3, (int)blocks, smem, s));
+  const cudaError_t e = wide ? (d->interleaved ? launch<8, true>(a, e4m3, threads, smem, s) : launch<8, false>(a, e4m3, threads, smem, s))
+                             : (d->interleaved ? launch<1, true>(a, e4m3, threads, smem, s) : launch<1, false>(a, e4m3, threads, smem, s));
   if (e != cudaSuccess) return record_error(CEP_ERR_CUDA, "append launch failed: %s", cudaGetErrorString(e));
   return CEP_OK;
 }
