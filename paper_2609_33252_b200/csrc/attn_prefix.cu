@@ -273,6 +273,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::misc + 448);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::misc + 452);
   volatile int* first_entity = reinterpret_cast<volatile int*>(smem + L::misc + 456);
+  const uint32_t loaded = bar0 + 460;                                                  // ring places whose copies have been asked for
   Pair* scratch = reinterpret_cast<Pair*>(smem + L::misc + 512);                       // a block's warps' totals
   const uint32_t ex_turn = bar0 + 768;                                                 // [2][4] a warp of each warpgroup may take its exponentials
   const uint32_t q_free = bar0 + 832, q_raw = bar0 + 848;
@@ -290,6 +291,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     // readers of an item: the loading warp, the products of each warpgroup, eight row warps, four decoding warps
     for (int i = 0; i < kItemSlots; ++i) { mbar_init(w_full + 8 * i, 1); mbar_init(w_empty + 8 * i, E4M3 ? 15 : 11); }
     *abort_flag = 0;
+    *reinterpret_cast<volatile uint32_t*>(smem + L::misc + 460) = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
@@ -307,6 +309,26 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
   AttnSched s = attn_carve(sched_at, p.B, p.G);
   build_schedule(a, s, scratch, first_entity);
 
+  // A stage of the ring has landed.  The barrier's parity tells two uses apart, not three: where the use before this one was the other
+  // warpgroup's, it may not even have landed yet.  Once the copies of `pos` are asked for it has, and has been freed.  (Decoded codes
+  // land in the order of their places: who has seen a later one has seen it.)  seen: places known to be asked for.
+  auto wait_ring = [&](uint32_t pos, uint32_t& seen) -> bool {
+    if (!E4M3 && seen <= pos) {
+      uint32_t spin = 0;
+      unsigned long long since = 0;
+#pragma unroll 1
+      for (;;) {
+        asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(seen) : "r"(loaded) : "memory");
+        if (seen > pos) break;
+        if ((++spin & 255u) != 0u) continue;
+        const unsigned long long now = globaltimer();
+        if (since == 0) since = now;
+        if (now - since > kWaitLimitNs) { *abort_flag = 1; atomicExch(&a.status[kStTimeout], 1); }
+        if (*abort_flag) return false;
+      }
+    }
+    return wait_bar(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status);
+  };
   // the next item; every reader gives it back after its last look
   uint32_t turn = 0;
   auto take = [&]() -> const Work& {
@@ -369,6 +391,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
         }
       }
       __syncwarp();
+      if (!E4M3 && lane == 0) asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(loaded), "r"(pos + 1) : "memory");
     };
     auto next_tile = [&]() -> bool {                        // moves on to the next tile, if there is one
       if (++j < it.n) return true;
@@ -495,7 +518,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       const int w = warp == kMmaWarp2;
       const uint32_t t_s = tmem + w * 128, t_o = tmem + 256 + w * 128;
       const uint64_t qd = make_smem_desc(sbase + L::q + w * L::tile_bytes);
-      uint32_t t0 = 0, q_phase = 0, p_phase = 0;
+      uint32_t t0 = 0, q_phase = 0, p_phase = 0, seen = 0;
       bool alive = true;
       auto wait = [&](uint32_t bar, uint32_t parity) { alive = alive && wait_bar(bar, parity & 1, abort_flag, a.status); };
       // A stage is free when both threads say so; a tile of one warpgroup is none of the other's business.
@@ -527,7 +550,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             if (j + step >= n) tc_commit(q_free + 8 * w);
           }
         };
-        auto wait_stage = [&](uint32_t pos) { wait(full + 8 * (pos % L::stages), pos / L::stages); tc_fence_after(); };
+        auto wait_stage = [&](uint32_t pos) { alive = alive && wait_ring(pos, seen); tc_fence_after(); };
         if (j0 < n) {
           wait(q_ready + 8 * w, q_phase++);
           wait_stage(pos_k(t0 + j0));
@@ -776,9 +799,9 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
           wait_bar(s_full + 16 * wg + 8 * h, s_phase & 1, abort_flag, a.status);
           tc_fence_after();
           if (!E4M3 && h == 0 && keys < kAttnTile) {                    // what lies behind the last key may be anything: its weight 0 needs a finite value.
-            // (Not before S: only then has this stage's use before last ended, and the parity tells the uses apart.)
             const uint32_t pos = pos_v(r.t0 + j);
-            wait_bar(full + 8 * (pos % L::stages), (pos / L::stages) & 1, abort_flag, a.status);
+            uint32_t seen = 0;
+            wait_ring(pos, seen);
             uint8_t* v = smem + L::ring + (pos % L::stages) * L::tile_bytes;
             const int from = keys < 0 ? 0 : keys;
 #pragma unroll 1
