@@ -15,7 +15,7 @@ struct cep_attn_plan {
   int device, n_ctas;
   GemmTensorMap tm_k, tm_v;
   const float *k_scale, *v_scale;
-  int32_t* status; void* sched; float* part_o; float2* part_ml;
+  int32_t* status; void* records; float* part_o; float2* part_ml;
   // The plan's last enqueued work.  Work on another stream waits for it: the workspace is shared.
   cudaEvent_t last; unsigned long long last_stream; bool have_last;    // (by id: a handle can come back as another stream's)
 };
@@ -50,14 +50,14 @@ int check_config(const cep_attn_config* c) {
   return CEP_OK;
 }
 
-struct Carve { size_t status, sched, ml, o, total; };
+struct Carve { size_t status, records, ml, o, total; };
 Carve carve(const cep_attn_config& c) {
   Carve w{};
   size_t o = 0;
   auto take = [&](size_t& f, size_t bytes) { f = o; o = up_to(o + bytes, 256); };
   const size_t rows = (size_t)attn_max_part_rows(c.max_tokens, c.max_seqs, c.max_prefixes, c.n_heads, c.n_kv_heads, kAttnMaxCtas);
   take(w.status, kStWords * 4);
-  take(w.sched, kAttnSchedBytes + kAttnMaxCtas * 4);
+  take(w.records, attn_record_bytes(c.max_seqs, c.max_prefixes, attn_most_own(c.max_tokens, c.max_seqs, c.n_heads, c.n_kv_heads)));
   take(w.ml, rows * sizeof(float2));
   take(w.o, rows * attn_padded_dim(c.head_dim) * sizeof(float));
   w.total = o;
@@ -118,7 +118,7 @@ int attn_plan(const cep_attn_config* cfg, const void* k_cache, const void* v_cac
   p->cfg = *cfg; p->k_scale = k_scale; p->v_scale = v_scale;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p->status = reinterpret_cast<int32_t*>(ws + w.status);
-  p->sched = ws + w.sched;
+  p->records = ws + w.records;
   p->part_ml = reinterpret_cast<float2*>(ws + w.ml);
   p->part_o = reinterpret_cast<float*>(ws + w.o);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -209,7 +209,7 @@ int attn_prefix(cep_attn_plan* p, const cep_attn_batch* b, const void* q, const 
   a.lse = lse; a.lse_tok = b->lse_token_stride;
   a.k_scale = p->k_scale; a.v_scale = p->v_scale;
   a.scale_log2 = (float)((double)c.scale * 1.4426950408889634);
-  a.part_o = p->part_o; a.part_ml = p->part_ml; a.sched = p->sched; a.status = p->status;
+  a.part_o = p->part_o; a.part_ml = p->part_ml; a.records = p->records; a.status = p->status;
   GemmTensorMap maps[4] = {p->tm_k, p->tm_v, {}, {}};
   int m = make_q_map(&maps[2], a, 1);
   if (!m) m = make_q_map(&maps[3], a, a.p.tps);

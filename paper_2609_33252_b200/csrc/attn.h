@@ -70,6 +70,8 @@ __host__ __device__ inline AttnSched attn_carve(void* base, int B, int G) {
 }
 __host__ __device__ constexpr int attn_sched_words(int B, int G) { return G + B + 1 + 4 * B + 3 + 3 * G + 2 + (B + 1) / 2; }      // 4-byte words
 constexpr int kAttnSchedBytes = attn_sched_words(kAttnMaxSeqs, kAttnMaxPrefixes) * 4;
+// Records of the joining kernel: a head, 48 bytes per CTA, group and sequence, 4 per token of a sequence of up to two row tiles.
+inline size_t attn_record_bytes(int max_seqs, int max_prefixes, long long tokens) { return 16 + 48ull * (kAttnMaxCtas + max_prefixes + max_seqs) + 4ull * tokens; }
 
 __host__ __device__ inline int attn_key_tiles(int keys) { return (keys + kAttnTile - 1) / kAttnTile; }
 
@@ -245,10 +247,14 @@ __host__ __device__ inline int attn_part_count(const AttnItem& it, int s0, int s
 __host__ __device__ inline bool attn_is_whole(const AttnItem& it, int s0, int s1) {
   return it.kind == kAttnJoint && s1 - s0 == it.n && attn_part_count(it, s0, s1) == 1;
 }
+// Tokens of sequences with partial rows of their own, at most.
+__host__ __device__ inline long long attn_most_own(int max_tokens, int max_seqs, int Hq, int Hkv) {
+  const long long most = (long long)max_seqs * 2 * (kAttnTile / (Hq / Hkv));
+  return most < max_tokens ? most : max_tokens;
+}
 __host__ __device__ inline long long attn_max_part_rows(int max_tokens, int max_seqs, int max_prefixes, int Hq, int Hkv, int n_ctas) {
   const int Gh = Hq / Hkv, tps = kAttnTile / Gh;
-  long long most = (long long)max_seqs * 2 * tps;                      // tokens of sequences with rows of their own
-  if (most > max_tokens) most = max_tokens;
+  const long long most = attn_most_own(max_tokens, max_seqs, Hq, Hkv);
   return 2 * most * Hq + (long long)Hkv * (most / (2 * tps) + max_prefixes) * 2 * tps * Gh + (long long)(n_ctas + 1) * kAttnSplitRows;
 }
 
@@ -285,7 +291,7 @@ struct AttnArgs {
   float scale_log2;                          // softmax scale * log2(e)
   float* part_o;                             // [rows][padded D]
   float2* part_ml;                           // [rows] maximum (in log2), sum
-  void* sched;                               // kAttnSchedBytes: the schedule as the merge kernel reads it
+  void* records;                             // attn_record_bytes: what the joining kernel needs of the schedule
   int32_t* status;
 };
 

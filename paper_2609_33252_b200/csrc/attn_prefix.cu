@@ -211,6 +211,60 @@ __device__ __forceinline__ int sequence_of(const int32_t* before, int lo, int hi
   return lo;
 }
 
+// ---------------------------------------------------------------- records for the kernel that joins partial results
+// Where the partial results of an item are.
+struct JoinPart {
+  long long rows;                            // first partial row
+  int32_t at, w, n, n_tok, dual, joint;      // its place and length on the cost axis, steps, tokens; two row tiles; prefix and own keys in one
+};
+struct alignas(16) JoinSeq {                 // a sequence with partial rows of its own: its (only) item of kv head 0
+  JoinPart part;                             // n = 0: no own keys
+  int32_t q0, first, g, in_group;            // first token; first among those of such sequences; group (-1: shares nothing); first among the group's short ones
+};
+struct alignas(16) JoinGroup { JoinPart part; int32_t items, n_short, pad[2]; };       // item 0 of kv head 0; items per kv head; tokens
+struct alignas(16) JoinCut { JoinPart part; int32_t token, head, pad[2]; };            // part.n = 0: no item to join at the start of this CTA's share
+struct JoinRecords { int32_t* head; JoinSeq* seq; JoinGroup* group; JoinCut* cut; int32_t* seq_of; };    // head: share, tokens
+static_assert(sizeof(JoinPart) == 32 && sizeof(JoinSeq) == 48 && sizeof(JoinGroup) == 48 && sizeof(JoinCut) == 48, "");
+__device__ __forceinline__ JoinRecords records_of(const AttnArgs& a) {
+  JoinRecords r;
+  uint8_t* p = static_cast<uint8_t*>(a.records);
+  r.head = reinterpret_cast<int32_t*>(p); p += 16;
+  r.cut = reinterpret_cast<JoinCut*>(p); p += kAttnMaxCtas * sizeof(JoinCut);
+  r.group = reinterpret_cast<JoinGroup*>(p); p += a.p.G * sizeof(JoinGroup);
+  r.seq = reinterpret_cast<JoinSeq*>(p); p += a.p.B * sizeof(JoinSeq);
+  r.seq_of = reinterpret_cast<int32_t*>(p);
+  return r;
+}
+// By a warp of every CTA that has nothing else to do by then; each writes its part.
+__device__ __forceinline__ void write_records(const AttnArgs& a, const AttnSched& s, const JoinPart& cut, int cut_token, int cut_head) {
+  const AttnShape& p = a.p;
+  const JoinRecords r = records_of(a);
+  const int lane = threadIdx.x & 31, worker = blockIdx.x * 32 + lane, workers = gridDim.x * 32;
+  if (lane == 0) r.cut[blockIdx.x] = JoinCut{cut, cut_token, cut_head, {0, 0}};
+  if (worker == 0) { r.head[0] = s.share; r.head[1] = s.pcum[p.B]; }
+#pragma unroll 1
+  for (int e = worker; e < p.G + p.B; e += workers) {
+    AttnWalk k;
+    k.done = false; k.e = e; k.head = 0; k.r = 0; k.at = s.cost[e];
+    k.x = attn_entity(p, s, e);
+    k.w = k.x.a + k.x.slope;
+    JoinPart part{};
+    if (k.x.items > 0) {
+      const AttnItem it = attn_item(p, s, k);
+      part = JoinPart{it.rows, k.at, k.w, it.n, it.n_tok, it.dual, it.kind == kAttnJoint};
+    }
+    if (e < p.G) {
+      r.group[e] = JoinGroup{part, k.x.items, s.scum[s.gfirst[e + 1]] - s.scum[s.gfirst[e]], {0, 0}};
+    } else {
+      const int b = e - p.G, g = attn_is_short(p, s, b) ? s.group[b] : -1;
+      r.seq[b] = JoinSeq{part, s.q0[b], s.pcum[b], g, g >= 0 ? s.scum[b] - s.scum[s.gfirst[g]] : 0};
+    }
+  }
+  // tokens of sequences with partial rows of their own -> their sequence
+#pragma unroll 1
+  for (int i = worker; i < s.pcum[p.B]; i += workers) r.seq_of[i] = sequence_of(s.pcum, 0, p.B, i);
+}
+
 // What a CTA has of an item, as the warp that walks the schedule hands it to the others.
 struct alignas(16) Work {
   int32_t n, s0;                             // steps (0: no more items), the first of them
@@ -430,15 +484,6 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
     AttnWalk k;
     k.done = *first_entity < 0;
     if (!k.done) k = attn_walk_in(p, s, *first_entity, x0);
-    if (lane == 0) {
-      // For the kernel that joins partial results: does this CTA's first item begin in the share before, and use the rows at the cuts?
-      int cut = 0;
-      if (!k.done && k.e >= p.G && x0 > 0 && !attn_has_rows(p, s, k.e - p.G)) {
-        const int n = attn_item(p, s, k).n, before = attn_steps_before(k, n, x0);
-        cut = before > 0 && before < n && attn_steps_before(k, n, x0 - s.share) == 0;
-      }
-      static_cast<int32_t*>(a.sched)[words + blockIdx.x] = cut;
-    }
     Work* out = const_cast<Work*>(work);
     uint32_t t0 = 0, q_turn[2] = {0, 0};
     bool alive = true;
@@ -502,12 +547,20 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       for (int wg = 0; wg < 2; ++wg)
         while (q_turn[wg] && !mbar_try_wait((E4M3 ? q_raw : q_ready) + 8 * wg, (q_turn[wg] - 1) & 1) && globaltimer() - since < 100000000ull) {}
     }
-    if (blockIdx.x == 0) {                                  // the schedule, for the kernel that joins partial results
-      int32_t* dst = static_cast<int32_t*>(a.sched);
-      const int32_t* src = reinterpret_cast<const int32_t*>(sched_at);
-#pragma unroll 1
-      for (int i = lane; i < words; i += 32) dst[i] = src[i];
+    // For the kernel that joins partial results: does this CTA's first item begin in the share before, and use the rows at the cuts?
+    JoinPart cut{};
+    k.done = *first_entity < 0;
+    if (!k.done) k = attn_walk_in(p, s, *first_entity, x0);
+    int cut_token = 0, cut_head = 0;
+    if (!k.done && k.e >= p.G && x0 > 0 && !attn_has_rows(p, s, k.e - p.G)) {
+      const AttnItem it = attn_item(p, s, k);
+      const int before = attn_steps_before(k, it.n, x0);
+      if (before > 0 && before < it.n && attn_steps_before(k, it.n, x0 - s.share) == 0) {
+        cut = JoinPart{it.rows, k.at, k.w, it.n, it.n_tok, it.dual, 1};
+        cut_token = s.q0[it.b] + it.tok; cut_head = it.head;
+      }
     }
+    write_records(a, s, cut, cut_token, cut_head);
   } else if (warp == kMmaWarp || warp == kMmaWarp2) {
     // ------------------------------------------------------ tensor core: one thread for each warpgroup's products
     // (Elected, not picked by its number: the compiler then knows that one thread issues, and a product of 128 x 128 x 16 takes its 64
@@ -918,12 +971,16 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
 // A row's running (maximum, sum, output), in log2 and unscaled; o: a lane's columns 4 lane .. + 3.
 struct Joined { float m, l; float4 o; };
 
-// Where the partial results of an item are: lane i has the first row of the i-th of a round of 32 (-1: none), for CTAs c0, c0 + 1, ...
-__device__ __forceinline__ long long part_place(const AttnArgs& a, const AttnSched& s, const AttnWalk& k, const AttnItem& it, int c0, int c_hi) {
-  const int lane = threadIdx.x & 31, c = c0 + (lane >> 1);               // a lane for each of a CTA's two results
+// Lane i has the first row of the i-th partial result of a round of 32 (-1: none), two for each CTA from c0 on.
+__device__ __forceinline__ long long part_place(const AttnArgs& a, int share, const JoinPart& j, int c0, int c_hi) {
+  const int lane = threadIdx.x & 31, c = c0 + (lane >> 1);
   if (c > c_hi) return -1;
-  const int s0 = attn_steps_before(k, it.n, c * s.share), s1 = attn_steps_before(k, it.n, (c + 1) * s.share);
-  return s0 < s1 && (lane & 1) < attn_part_count(it, s0, s1) ? attn_part_row(it, c, s0) + (lane & 1) * it.n_tok * a.p.Gh : -1;
+  AttnWalk k;
+  k.at = j.at; k.w = j.w;
+  AttnItem it;
+  it.rows = j.rows; it.dual = j.dual;
+  const int s0 = attn_steps_before(k, j.n, c * share), s1 = attn_steps_before(k, j.n, (c + 1) * share);
+  return s0 < s1 && (lane & 1) < attn_part_count(it, s0, s1) ? attn_part_row(it, c, s0) + (lane & 1) * j.n_tok * a.p.Gh : -1;
 }
 
 // Joins a round of partial results into `n` (up to N) rows, row0 and those behind it; every lane's loads for all rows go out together.
@@ -950,7 +1007,7 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, long long place, in
     j[i].l = j[i].l * keep + add;
   }
   unsigned have = __ballot_sync(0xffffffffu, place >= 0);
-#pragma unroll 2
+#pragma unroll 4
   while (have) {
     const int src = __ffs(have) - 1;
     have &= have - 1;
@@ -983,86 +1040,80 @@ __device__ __forceinline__ void write_row(const AttnArgs& a, int token, int head
 constexpr int kJoinThreads = 256, kJoinRows = 4;
 
 template <int DP>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads, 2)
 attn_join_kernel(const __grid_constant__ AttnArgs a) {
-  extern __shared__ uint8_t join_smem[];
   pdl_enter();
   const AttnShape& p = a.p;
   const int tid = threadIdx.x, warp = tid >> 5, warps = kJoinThreads / 32;
-  {
-    int32_t* dst = reinterpret_cast<int32_t*>(join_smem);
-    const int32_t* src = static_cast<const int32_t*>(a.sched);
-#pragma unroll 2
-    for (int i = tid; i < attn_sched_words(p.B, p.G) + p.n_ctas; i += kJoinThreads) dst[i] = src[i];
-    __syncthreads();
-  }
-  AttnSched s = attn_carve(join_smem, p.B, p.G);
-  const int32_t* cuts = reinterpret_cast<const int32_t*>(join_smem) + attn_sched_words(p.B, p.G);
-  s.share = attn_share(p, s.cost[p.G + p.B]);
+  const JoinRecords rec = records_of(a);
+  const int share = rec.head[0], tokens = rec.head[1];
   const int per_head = (p.Gh + kJoinRows - 1) / kJoinRows, per_token = p.Hkv * per_head;
-  const int n_own = s.pcum[p.B] * per_token;                // (below 2^31: checked by the plan)
-  const int per_cut = (2 * p.tps * p.Gh + kJoinRows - 1) / kJoinRows, n_units = n_own + (p.n_ctas - 1) * per_cut;
+  const int n_own = tokens * per_token;                     // (below 2^31: checked by the plan)
+  const int tile = 2 * p.tps, per_cut = (tile * p.Gh + kJoinRows - 1) / kJoinRows;
+  const int n_units = n_own + (p.T > tile ? (p.n_ctas - 1) * per_cut : 0);
 #pragma unroll 1
   for (int u = blockIdx.x * warps + warp; u < n_units; u += gridDim.x * warps) {
     Joined j[kJoinRows];
 #pragma unroll
     for (int i = 0; i < kJoinRows; ++i) j[i] = Joined{-CUDART_INF_F, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
-    int row0, n, token, kvh, head;                          // rows of the item; first one's token and head
-    AttnWalk k;
-    k.done = false;
-    int part, last, b, g = -1, t = 0;                       // items: 0 the group's, 1 the sequence's
-    if (u < n_own) {
+    const bool own = u < n_own;
+    int row0, n, token, kvh, head = 0;                      // row of the token (of the cut item); rows; token of row 0; its head
+    JoinPart part, ahead;
+    int rows_ahead = 0;                                     // rows of the group's item before row 0's
+    ahead.n = 0;
+    if (own) {
       const int i = u / per_token, in_token = u - i * per_token;
+      const JoinSeq q = rec.seq[rec.seq_of[i]];
       kvh = in_token / per_head;
-      b = sequence_of(s.pcum, 0, p.B, i); g = s.group[b]; t = i - s.pcum[b];
-      const int h0 = (in_token - kvh * per_head) * kJoinRows;
-      n = min(kJoinRows, p.Gh - h0);
-      head = kvh * p.Gh + h0;
-      token = s.q0[b] + t;
-      row0 = h0;                                            // of the token's
-      part = attn_is_short(p, s, b) ? 0 : 1; last = 1;
+      row0 = (in_token - kvh * per_head) * kJoinRows;
+      n = min(kJoinRows, p.Gh - row0);
+      head = kvh * p.Gh + row0;
+      const int t = i - q.first;
+      token = q.q0 + t;
+      part = q.part;
+      part.at += kvh * part.w;
+      part.rows += 2ll * kvh * part.n_tok * p.Gh;
+      row0 += t * p.Gh;
+      if (q.g >= 0) {
+        const JoinGroup g = rec.group[q.g];
+        const int in_group = q.in_group + t, r = attn_div(in_group, tile);
+        ahead = g.part;
+        ahead.at += (kvh * g.items + r) * ahead.w;
+        ahead.rows += (long long)(kvh * g.items + r) * tile * p.Gh;
+        ahead.n_tok = min(tile, g.n_short - r * tile);
+        rows_ahead = (in_group - r * tile - t) * p.Gh;
+      }
     } else {
       const int cut = (u - n_own) / per_cut;
-      if (!cuts[cut + 1]) continue;
-      k = attn_walk_at(p, s, (cut + 1) * s.share);
       row0 = (u - n_own - cut * per_cut) * kJoinRows;
-      part = last = 2; kvh = k.head; b = k.e - p.G; n = token = head = 0;
+      const JoinCut c = rec.cut[cut + 1];
+      part = c.part;
+      n = min(kJoinRows, part.n_tok * p.Gh - row0);
+      token = c.token; kvh = c.head;
+      if (part.n == 0 || n <= 0) continue;
     }
+    bool final = false;
 #pragma unroll 1
-    for (; part <= last; ++part) {
-      int row = row0;
-      if (part < 2) {
-        k.e = part ? p.G + b : g;
-        k.x = attn_entity(p, s, k.e);
-        if (k.x.items == 0) continue;                       // (no own keys)
-        const int at = part ? t : s.scum[b] - s.scum[s.gfirst[g]] + t;   // token among the entity's
-        k.head = kvh;
-        k.r = attn_div(at, 2 * p.tps);
-        k.w = k.x.a + k.x.slope * (k.r + 1);
-        k.at = s.cost[k.e] + kvh * attn_items_cost(k.x, k.x.items) + attn_items_cost(k.x, k.r);
-        row += (at - k.r * 2 * p.tps) * p.Gh;
+    for (int side = 0; side < 2; ++side) {
+      const JoinPart x = side ? part : ahead;
+      if (x.n == 0) continue;
+      const int c_lo = x.at / share, c_hi = (x.at + x.w - 1) / share;
+      if (own && x.joint) {                                 // all in one part, which wrote the rows themselves?
+        AttnWalk k;
+        k.at = x.at; k.w = x.w;
+        final = attn_steps_before(k, x.n, (c_lo + 1) * share) == x.n && (x.dual || x.n == 1);
+        if (final) break;
       }
-      const AttnItem it = attn_item(p, s, k);
-      const int c_lo = attn_div(k.at, s.share), c_hi = attn_div(k.at + k.w - 1, s.share);
-      if (it.kind == kAttnJoint) {
-        const int first = attn_steps_before(k, it.n, (c_lo + 1) * s.share);
-        if (part == 2) {
-          n = min(kJoinRows, it.n_tok * p.Gh - row0);
-          if (n <= 0) { k.done = true; break; }
-        } else if (attn_is_whole(it, 0, first)) {           // final already
-          k.done = true; break;
-        }
-      }
+      const int row = row0 + (side ? 0 : rows_ahead);
 #pragma unroll 1
-      for (int c0 = c_lo; c0 <= c_hi; c0 += 16) join_rows<DP>(a, part_place(a, s, k, it, c0, c_hi), row, n, j);
-      if (part == 2) token = s.q0[b] + it.tok;
+      for (int c0 = c_lo; c0 <= c_hi; c0 += 16) join_rows<DP>(a, part_place(a, share, x, c0, c_hi), row, n, j);
     }
-    if (k.done) continue;
+    if (final) continue;
 #pragma unroll
     for (int i = 0; i < kJoinRows; ++i) {
       if (i >= n) break;
-      const int r = row0 + i, tt = u < n_own ? 0 : attn_div(r, p.Gh);
-      write_row<DP>(a, token + tt, u < n_own ? head + i : kvh * p.Gh + (r - tt * p.Gh), kvh, j[i]);
+      const int r = row0 + i, tt = own ? 0 : attn_div(r, p.Gh);
+      write_row<DP>(a, token + tt, own ? head + i : kvh * p.Gh + (r - tt * p.Gh), kvh, j[i]);
     }
   }
 }
@@ -1079,7 +1130,7 @@ cudaError_t launch_dim(const AttnArgs& a, const CUtensorMap& tk, const CUtensorM
   const int words = attn_sched_words(a.p.B, a.p.G);
   cudaError_t e = launch_pdl(attn_kernel<DP, E4M3>, dim3(a.p.n_ctas), dim3(Layout<DP, E4M3>::threads), Layout<DP, E4M3>::smem(words), s, 1, a, tk, tv, q1, qn);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attn_join_kernel<DP>, dim3(join_blocks(a)), dim3(kJoinThreads), (words + a.p.n_ctas) * 4, s, 1, a);
+  return launch_pdl(attn_join_kernel<DP>, dim3(join_blocks(a)), dim3(kJoinThreads), 0, s, 1, a);
 }
 
 }  // namespace
