@@ -273,7 +273,7 @@ typedef struct cep_lora_plan cep_lora_plan;
 typedef struct {
   int32_t in_features;         /* K; multiple of 8                                              */
   int32_t out_features;        /* N >= 1                                                        */
-  int32_t max_tokens;          /* upper bound on tokens per call                                */
+  int32_t max_tokens;          /* upper bound on tokens per call, 1..2^22; times n_heads below 2^31 */
   int32_t max_adapters;        /* slots of the adapter bank, 0..4096; 0: no adapters            */
   int32_t max_rank;            /* largest rank, 1..256; 0 without adapters                      */
   int32_t out_elem;            /* cep_elem of y                                                 */
@@ -418,8 +418,8 @@ CEP_API int attn_plan(const cep_attn_config* cfg, const void* k_cache, const voi
  *   lse           [device] out fp32 [T, n_heads] or NULL: log of the sum of exp(scale q.k) (natural)
  * A token that sees no key gets zeros and -infinity.  What lies behind the last key in a page is not looked at, and may be
  * anything; a key or value that is not finite reaches the tokens that see it and, where one of these belongs to the same
- * sequence and call, may reach the sequence's earlier tokens of the call.  fp32 from the products on; weights enter the product with V as bf16,
- * out is rounded once.  Results do not depend on timing.  All lengths are read on the device: a captured call replays with
+ * sequence and call, may reach the sequence's earlier tokens of the call.  fp32 from the products on; weights enter the product with V as bf16
+ * (fp16 with an e4m3 cache), out is rounded once.  Results do not depend on timing.  All lengths are read on the device: a captured call replays with
  * other lengths (within n_tokens, n_seqs).  What does not fit is cut to what does and reported by attn_status.
  * Enqueued on `stream`.
  */

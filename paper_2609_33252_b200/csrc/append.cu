@@ -3,6 +3,8 @@
 // Per token: sines and cosines of R/2 angles, shared by all heads, then (n_heads + 2 n_kv_heads) heads that are read once and
 // written once; memory is the bound.  A thread has the same parts of a token's heads for every token that its block comes to, so
 // that all divisions are done once; it asks for them before the angles are computed, which then cost no time of their own.
+// 16384 tokens of 56 + 2 x 8 heads of 128 (604 MB): 121 us, 5.0 TB/s (151 us with the parts found anew for each token; 168 us
+// with heads brought to shared memory by bulk copies first).
 //
 // Angles: position * inv_freq reaches 10^6 and more, where fp32 has lost the turn's fraction.  The product with 1/(2 pi) is
 // taken in fp64 (4 instructions a pair, B200 has them at half rate), the whole turns are dropped, and the rest, below half a
@@ -299,7 +301,7 @@ extern "C" int attn_append(const cep_append_desc* d, const void* q, const void* 
     while (a.tokens < 16 && a.tokens * 2 * per_token <= 256 * unroll) a.tokens *= 2;
     threads = std::min(kAppendMaxThreads, warps((a.tokens * per_token + unroll - 1) / unroll));
   }
-  a.groups = std::min((a.T + a.tokens - 1) / a.tokens, 148 * std::max(1, kAppendPerSm / threads));
+  a.groups = (int)std::min<long long>(((long long)a.T + a.tokens - 1) / a.tokens, 148 * std::max(1, kAppendPerSm / threads));
   if (a.parts > 1) a.groups = a.T;
   const size_t smem = 2 * (size_t)a.tokens * 2 * ((a.R / 2 + 7) / 8 * 8) * sizeof(float);
   cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -24,8 +24,10 @@ constexpr int kAttnTile = 128;               // keys of a step, rows of a row ti
 constexpr int kAttnMaxSeqs = 1024, kAttnMaxPrefixes = 256;
 constexpr int kAttnMaxCtas = 148;
 constexpr int kAttnSplitRows = 2 * 2 * kAttnTile;                      // partial rows that a CTA's two cut items may need
-// Estimated cost of four keys for one row tile (taken by the warpgroups in turn) and for two, and of an item beside its keys.
-constexpr int kAttnCostSingle = 2, kAttnCostDual = 4, kAttnItemSingle = 150, kAttnItemDual = 400;
+// Estimated cost of four keys for one row tile (taken by the warpgroups in turn) and for two, and of an item beside its keys; a unit is 5 ns.
+// Measured, with both kinds at once (256 tokens over 32768 shared and 2000 own keys at most): 1.4 us for 128 keys of one, 2.2 us of two.  8 and 600 for
+// one, 16 and 1600 for two, which fit them alone, take 652 us there where these take 612.
+constexpr int kAttnCostSingle = 9, kAttnCostDual = 16, kAttnItemSingle = 560, kAttnItemDual = 1200;
 
 struct AttnShape {
   int T, B, G;                               // tokens, sequences, groups
@@ -39,7 +41,7 @@ struct AttnShape {
   uint32_t tile_magic;                       // division by 2 tps: (x * tile_magic) >> 32
 };
 
-// The schedule of one call, in shared or in global memory.  
+// The schedule of one call.
 struct AttnSched {
   int32_t* q0;                               // [B+1] first token of each sequence
   int32_t* kv;                               // [B] own keys
@@ -258,11 +260,12 @@ __host__ __device__ inline long long attn_max_part_rows(int max_tokens, int max_
   return 2 * most * Hq + (long long)Hkv * (most / (2 * tps) + max_prefixes) * 2 * tps * Gh + (long long)(n_ctas + 1) * kAttnSplitRows;
 }
 
-// The cost that each CTA gets: equal shares, and about a step at least.
+// The cost that each CTA gets: equal shares, and about a step at least (one token over 777 shared and 33 own keys:
+// 17.0 us; with three steps at least 19.5).
 __host__ __device__ inline int attn_share(const AttnShape& p, int total) {
   // (fp32 is off by 2^-23 of the sum at most, which is less than one part in 10^4 of a share)
   int share = (int)((float)total * p.per_cta) + 1 + (total >> 21);
-  const int least = (kAttnTile / 4 * kAttnCostSingle + kAttnItemSingle / 8) >> p.cost_shift;
+  const int least = (kAttnTile / 4 * kAttnCostSingle + kAttnItemSingle / 16) >> p.cost_shift;
   return share > least ? share : least;
 }
 
