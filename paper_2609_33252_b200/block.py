@@ -94,7 +94,7 @@ class AttentionBlock:
     w_qkv bf16 [(Hq + 2 Hkv) D, H]: rows of all query heads, then the key heads, then the value heads; k_cache, v_cache
     [pages, page_size, Hkv, D] bf16 or float8_e4m3fn (with k_scale, v_scale fp32 [Hkv]); inv_freq fp32 [R/2].  All are the caller's
     tensors.  ``run`` may be called on different streams: each call waits for the one before, as the buffers between the
-    steps are shared (who runs ``steps`` orders them).
+    steps are shared (who runs ``steps`` orders them, and who captures ``run`` into a graph its replays).
     """
 
     def __init__(self, w_qkv, k_cache, v_cache, n_heads, inv_freq, max_tokens, max_seqs, max_prefixes=1, k_scale=None, v_scale=None, interleaved=False,
@@ -114,6 +114,8 @@ class AttentionBlock:
         """The block as (name, call) pairs.  x bf16 [T,H]; positions int32 [T]; slots int64 [T]; batch: the lengths and page
         tables of ``PrefixAttention.run`` as a dict, kv_len with the new tokens.  The result is ``out`` [T,Hq,D]."""
         T, (Hq, Hk, D) = x.shape[0], self.heads
+        if T > self.out.shape[0]:
+            raise cep.CepError(-4, "%d tokens, the block was made for %d" % (T, self.out.shape[0]))
         qkv, out, att = self.qkv[:T], self.out[:T], self.attention
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hk], qkv[:, Hq + Hk:]
         return [
@@ -127,11 +129,14 @@ class AttentionBlock:
         """Returns the attention output [T, Hq D], a view of the block's buffer (valid until the next call)."""
         T, (Hq, _, D) = x.shape[0], self.heads
         stream = torch.cuda.current_stream(x.device)
-        stream.wait_event(self.done)                         # (before the first call: nothing to wait for)
+        capturing = torch.cuda.is_current_stream_capturing()            # (a graph cannot wait for what is not in it)
+        if not capturing:
+            stream.wait_event(self.done)                     # (before the first call: nothing to wait for)
         if T:                                                # (empty tensors have no address)
             for _, call in self.steps(x, positions, slots, batch, adapter_ids, causal):
                 call()
-        self.done.record(stream)
+        if not capturing:
+            self.done.record(stream)
         return self.out[:T].view(T, Hq * D)
 
     def close(self):

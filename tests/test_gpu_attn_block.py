@@ -146,3 +146,34 @@ def test_a_projection_of_the_wrong_height_is_refused():
     kv = torch.zeros(2, PAGE, 2, D, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(cep.CepError, match="rows"):
         AttentionBlock(rand((9 * D, 64), 1), kv, kv.clone(), 6, torch.rand(32, device="cuda"), 8, 1)
+
+
+def test_a_captured_block_replays_between_eager_calls():
+    kv = [torch.zeros(8, PAGE, 2, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    att = AttentionBlock(rand((10 * D, 128), 1, 128 ** -0.5), *kv, 6, torch.rand(D // 2, device="cuda"), 8, 4)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    x, positions, slots = rand((4, 128), 2), i32([0, 1, 2, 0]), torch.tensor([0, 1, 2, PAGE], device="cuda")
+    batch = dict(q_start=i32([0, 3, 4]), kv_len=i32([3, 1]), page_table=i32([[0], [1]]))
+    want = att.run(x, positions, slots, batch).clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = att.run(x, positions, slots, batch)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want)
+        assert torch.equal(att.run(x, positions, slots, batch), want)
+    torch.cuda.synchronize()
+    assert att.attention.status() == 0
+    del graph
+    att.close()
+
+
+def test_more_tokens_than_the_block_was_made_for_are_refused():
+    kv = [torch.zeros(2, PAGE, 2, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    att = AttentionBlock(rand((10 * D, 64), 1), *kv, 6, torch.rand(32, device="cuda"), 8, 1)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    for T in (9, 16):
+        with pytest.raises(cep.CepError, match="made for 8"):
+            att.run(rand((T, 64), 2), i32([0] * T), torch.zeros(T, dtype=torch.int64, device="cuda"), dict(q_start=i32([0, T]), kv_len=i32([T]), page_table=i32([[0]])))
+    att.close()

@@ -277,3 +277,14 @@ def test_outputs_and_inputs_with_strides():
     table[:, :n] = b.meta["page_table"]
     q = torch.stack([b.q] * 3, dim=1)                                # tokens three apart
     assert torch.equal(b.layer.run(q[:, 1], **dict(b.meta, page_table=table[:, :n])), want)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("page", [16, 128])
+def test_long_and_short_requests_side_by_side(page, e4m3):
+    """Items of one tile between items of many: the warpgroups' turns, the ring's places and the items' queue in every order."""
+    for seed in range(6):
+        g = torch.Generator().manual_seed(seed)
+        q_len = [[1, 1, 2, 40, 1, 300][int(i)] for i in torch.randint(0, 6, (24,), generator=g)]
+        kv_len = [n + [0, 3, 130, 1500][int(i)] for n, i in zip(q_len, torch.randint(0, 4, (24,), generator=g))]
+        Batch(q_len, kv_len, 8, 2, 128, page=page, prefix=[257], e4m3=e4m3).check(causal=bool(seed & 1))
