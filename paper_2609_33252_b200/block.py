@@ -104,11 +104,13 @@ class AttentionBlock:
         if w_qkv.shape[0] != (n_heads + 2 * Hk) * D:
             raise cep.CepError(-1, "w_qkv must have (%d + 2 * %d) * %d rows" % (n_heads, Hk, D))
         self.inv_freq, self.interleaved = inv_freq, interleaved
+        self.bad_slots = torch.zeros(1, dtype=torch.int32, device=w_qkv.device)      # set by the write into the cache
         self.projection = cep.LoRAProjection(w_qkv, max_tokens, max_adapters, max_rank)
         self.attention = cep.PrefixAttention(k_cache, v_cache, n_heads, max_tokens, max_seqs, max_prefixes, k_scale, v_scale)
         self.qkv = torch.empty(max_tokens, n_heads + 2 * Hk, D, dtype=torch.bfloat16, device=w_qkv.device)
         self.out = torch.empty(max_tokens, n_heads, D, dtype=torch.bfloat16, device=w_qkv.device)
         self.done = torch.cuda.Event()                       # the end of the last call
+        self.done.record(torch.cuda.current_stream(w_qkv.device))    # (before the first: of the clearing above)
 
     def steps(self, x, positions, slots, batch, adapter_ids=None, causal=True):
         """The block as (name, call) pairs.  x bf16 [T,H]; positions int32 [T]; slots int64 [T]; batch: the lengths and page
@@ -121,7 +123,8 @@ class AttentionBlock:
         return [
             ("projection to q, k, v", lambda: self.projection.run(x, adapter_ids, qkv.view(T, -1))),
             ("rotation + cache", lambda: cep.attn_append(k, v, positions, slots, self.inv_freq, att.k_cache, att.v_cache, q=q, q_out=q,
-                                                         interleaved=self.interleaved, k_scale=att.k_scale, v_scale=att.v_scale)),
+                                                         interleaved=self.interleaved, k_scale=att.k_scale, v_scale=att.v_scale,
+                                                         status=self.bad_slots)),
             ("attention", lambda: att.run(q, causal=causal, out=out, **batch)),
         ]
 
@@ -131,13 +134,25 @@ class AttentionBlock:
         stream = torch.cuda.current_stream(x.device)
         capturing = torch.cuda.is_current_stream_capturing()            # (a graph cannot wait for what is not in it)
         if not capturing:
-            stream.wait_event(self.done)                     # (before the first call: nothing to wait for)
+            stream.wait_event(self.done)
         if T:                                                # (empty tensors have no address)
             for _, call in self.steps(x, positions, slots, batch, adapter_ids, causal):
                 call()
         if not capturing:
             self.done.record(stream)
         return self.out[:T].view(T, Hq * D)
+
+    def status(self) -> int:
+        """Waits for the block's work and returns what its steps reported since the last call: 0, or the projection's status, the
+        attention's, or -6 (CEP_ERR_BAD_ROUTING) where a slot other than -1 lay outside the cache, whose token's key and value were not
+        written; the first of them, and all are cleared.  (Replays of a graph are the caller's to wait for.)"""
+        codes = [self.projection.status(), self.attention.status()]
+        self.done.synchronize()
+        if int(self.bad_slots):
+            self.bad_slots.zero_()
+            torch.cuda.current_stream(self.bad_slots.device).synchronize()           # (the next call may come on another stream)
+            codes.append(-6)
+        return next((c for c in codes if c), 0)
 
     def close(self):
         self.projection.close()
@@ -191,7 +206,7 @@ def main(dtype="mxfp4", tokens=4096, prefix=0):
         m.record()
     torch.cuda.synchronize()
     assert cep.ffn_status(block.layer.plan) == 0 and block.projection.status() == 0
-    assert not before or before.attention.status() == 0
+    assert not before or before.status() == 0
     for (name, _), a, b in zip(steps, marks, marks[1:]):
         print("%-26s %8.1f us" % (name, 1e3 * a.elapsed_time(b)))
     block.close()
