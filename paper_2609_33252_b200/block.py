@@ -77,9 +77,11 @@ class MoEBlock:
             return out
         stream = torch.cuda.current_stream(attention.device)
         stream.wait_event(self.done)                         # (before the first call: nothing to wait for)
-        for _, call in self.steps(attention, residual, adapter_ids, out, n_chunks):
-            call()
-        self.done.record(stream)
+        try:
+            for _, call in self.steps(attention, residual, adapter_ids, out, n_chunks):
+                call()
+        finally:                                             # (a step that is refused leaves those before it at work)
+            self.done.record(stream)
         return out
 
     def close(self):
@@ -135,11 +137,13 @@ class AttentionBlock:
         capturing = torch.cuda.is_current_stream_capturing()            # (a graph cannot wait for what is not in it)
         if not capturing:
             stream.wait_event(self.done)
-        if T:                                                # (empty tensors have no address)
-            for _, call in self.steps(x, positions, slots, batch, adapter_ids, causal):
-                call()
-        if not capturing:
-            self.done.record(stream)
+        try:
+            if T:                                            # (empty tensors have no address)
+                for _, call in self.steps(x, positions, slots, batch, adapter_ids, causal):
+                    call()
+        finally:                                             # (a step that is refused leaves those before it at work)
+            if not capturing:
+                self.done.record(stream)
         return self.out[:T].view(T, Hq * D)
 
     def status(self) -> int:

@@ -81,3 +81,24 @@ def test_the_first_report_is_returned_and_all_are_cleared(fake, codes, slot, wan
     fake.appended[0]["status"].fill_(slot)
     assert block.status() == want
     assert block.status() == 0
+
+
+def test_what_a_refused_call_has_started_is_waited_for(fake):
+    # the next call may come on another stream: it would write the buffers that the steps before the refusal still use
+    block = make()
+    fake.log.clear()
+    fake.fail = "attention"
+    with pytest.raises(blocks.cep.CepError):
+        run(block)
+    assert fake.log == ["wait", "projection", "append", "done"]
+
+
+def test_what_a_refused_call_of_the_expert_block_has_started_is_waited_for(fake):
+    def refuse():
+        raise blocks.cep.CepError(-1, "refused")
+    block = object.__new__(blocks.MoEBlock)
+    block.H, block.done = H, torch.cuda.Event()
+    block.steps = lambda *a: [("first", lambda: fake.log.append("first")), ("second", refuse)]
+    with pytest.raises(blocks.cep.CepError):
+        block.run(torch.zeros(3, H), torch.zeros(3, H))
+    assert fake.log == ["wait", "first", "done"]
