@@ -414,7 +414,7 @@ CEP_API int attn_plan(const cep_attn_config* cfg, const void* k_cache, const voi
  *                 prefix_start[G] have no prefix.  NULL: one group of all sequences (G <= 1)
  *   prefix_len    [device] int32 [G] keys of each group's prefix
  *   prefix_pages  [device] int32 [G, prefix_width]
- *   out           [device] out bf16 [T, n_heads, D]; may not overlap q
+ *   out           [device] out bf16 [T, n_heads, D]; may not overlap q (CEP_ERR_ARG; in one buffer with q it has q's token stride)
  *   lse           [device] out fp32 [T, n_heads] or NULL: log of the sum of exp(scale q.k) (natural)
  * A token that sees no key gets zeros and -infinity.  What lies behind the last key in a page is not looked at, and may be
  * anything; a key or value that is not finite reaches the tokens that see it and, where one of these belongs to the same

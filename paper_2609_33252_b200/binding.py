@@ -841,7 +841,7 @@ class PrefixAttention:
     def run(self, q, q_start, kv_len, page_table, prefix_start=None, prefix_len=None, prefix_pages=None, causal=True, out=None, lse=None, stream=None):
         """q bf16 [T,Hq,D] (heads may be strided), q_start int32 [B+1], kv_len int32 [B], page_table int32 [B,W]; prefixes: prefix_len
         int32 [G], prefix_pages int32 [G,Wp], prefix_start int32 [G+1] first sequence of each group (None: one group of all).  Returns out
-        [T,Hq,D] (allocated if not given); lse fp32 [T,Hq] is filled if given.  Tensors are recorded on a `stream` that is given."""
+        [T,Hq,D] (allocated if not given; it may not overlap q); lse fp32 [T,Hq] is filled if given.  Tensors are recorded on a `stream` that is given."""
         torch = _torch()
         dev, i32 = self.device_index, torch.int32
         T = q.shape[0]

@@ -188,6 +188,10 @@ int attn_prefix(cep_attn_plan* p, const cep_attn_batch* b, const void* q, const 
   for (int i = 0; i < 4; ++i)
     if (count[i] > 1 && (strides[i] < c.head_dim || strides[i] % 8)) return record_error(CEP_ERR_ARG, "attn: heads of q and out must lie multiples of 16 bytes and at least head_dim apart");
   if (!on(q, 16) || !on(out, 16)) return record_error(CEP_ERR_ARG, "attn: q and out must start on 16 bytes");
+  // a block writes rows of out while another still reads q
+  if (rows_meet(head_rows(q, b->n_tokens, c.n_heads, b->q_token_stride, b->q_head_stride, c.head_dim),
+                head_rows(out, b->n_tokens, c.n_heads, b->out_token_stride, b->out_head_stride, c.head_dim)))
+    return record_error(CEP_ERR_ARG, "attn: out overlaps q");
   if (lse && b->n_tokens > 1 && b->lse_token_stride < c.n_heads) return record_error(CEP_ERR_ARG, "attn: rows of lse lie less than n_heads apart");
   for (const void* i : {(const void*)q_start, (const void*)kv_len, (const void*)page_table, (const void*)prefix_start, (const void*)prefix_len, (const void*)prefix_pages, (const void*)lse})
     if (!on(i, 4)) return record_error(CEP_ERR_ARG, "attn: a pointer is not aligned to its element type");

@@ -36,6 +36,39 @@ static_assert(3 * (kLeastTmemBlock + kBlockShared) > kSmShared, "three blocks wo
 // Sets the calling thread's plan-less error string (cep_last_error(NULL)) and returns `code`.
 int record_error(int code, const char* fmt, ...);
 
+// The heads of a [tokens, heads, width] tensor in memory: bytes, strides between tokens and heads (which count where there is a second one).
+struct HeadRows {
+  uintptr_t at;
+  int64_t tokens, heads, token_stride, head_stride, width;
+};
+inline HeadRows head_rows(const void* p, int64_t tokens, int64_t heads, int64_t token_stride, int64_t head_stride, int64_t dim) {   // of 16-bit elements
+  const bool one_run = heads <= 1 || head_stride == dim;             // of all heads
+  return {reinterpret_cast<uintptr_t>(p), tokens, one_run ? heads > 0 : heads, tokens > 1 ? 2 * token_stride : 0, one_run ? 0 : 2 * head_stride,
+          2 * dim * (one_run ? heads : 1)};
+}
+// Whether two tensors share bytes.  Views of one buffer have its token stride and are told apart exactly; where the strides differ, those whose
+// addresses interleave count as sharing.
+inline bool rows_meet(const HeadRows& a, const HeadRows& b) {
+  if (a.tokens <= 0 || b.tokens <= 0 || a.heads <= 0 || b.heads <= 0) return false;
+  auto span = [](const HeadRows& r) { return (r.tokens - 1) * r.token_stride + (r.heads - 1) * r.head_stride + r.width; };
+  const int64_t d = (int64_t)(b.at - a.at);
+  if (d >= span(a) || -d >= span(b)) return false;
+  if (a.tokens > 1 && b.tokens > 1 && a.token_stride != b.token_stride) return true;
+  const int64_t s = a.token_stride > b.token_stride ? a.token_stride : b.token_stride;
+  for (int64_t i = 0; i < a.heads; ++i)
+    for (int64_t j = 0; j < b.heads; ++j) {
+      const int64_t c = d + j * b.head_stride - i * a.head_stride;   // b's token k later (or earlier) begins c + k s behind a's head
+      int64_t k = 1 - a.tokens;
+      if (s > 0) {
+        const int64_t x = -b.width - c;                              // the first k with c + k s > -b.width
+        const int64_t first = (x >= 0 ? x / s : -((-x + s - 1) / s)) + 1;
+        if (first > k) k = first;
+      }
+      if (k < b.tokens && c + k * s < a.width && c + k * s > -b.width) return true;
+    }
+  return false;
+}
+
 // Device status word layout (int32 each).
 enum StatusWord { kStBadRouting = 0, kStTimeout = 1, kStBoundsViolation = 2, kStDetail = 3, kStWords = 8 };
 

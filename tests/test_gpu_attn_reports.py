@@ -5,7 +5,7 @@ import torch
 import paper_2609_33252_b200 as cep
 from paper_2609_33252_b200.block import AttentionBlock
 
-from test_gpu_attn import rand
+from test_gpu_attn import Batch, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +42,26 @@ def test_a_block_reports_slots_outside_the_cache(e4m3):
     assert att.status() == -4 and att.status() == 0
     assert torch.equal(run([0, 1, 2, page]), want)
     att.close()
+
+
+def test_an_output_that_overlaps_the_queries_is_refused():
+    b = Batch([1, 30, 300, 2], [50, 30, 400, 2], 6, 2, 64, prefix=[200])
+    want = b.check()
+    T, meta = b.T, b.meta
+    store = torch.zeros(T + 1, 13, 64, dtype=torch.bfloat16, device="cuda")
+    store[:T, :6] = b.q
+    q = store[:T, :6]
+    turned = torch.zeros(6, 2 * T, 64, dtype=torch.bfloat16, device="cuda").transpose(0, 1)      # heads outside
+    turned[:T] = b.q
+    for x, out in ((b.q, b.q), (q, q), (q, store[:T, 5:11]), (q, store[1:, :6]), (q, store[1:, 3:9]), (turned[:T], turned[:T]), (turned[:T], turned[T - 1:2 * T - 1]),
+                   (q, store.view(-1)[64:64 * (6 * T + 1)].view(T, 6, 64))):
+        before = store.clone(), turned.clone()
+        with pytest.raises(cep.CepError, match="overlaps"):
+            b.layer.run(x, out=out, **meta)
+        assert torch.equal(store, before[0]) and torch.equal(turned, before[1])
+    # other columns, rows or heads of one buffer
+    for x, out in ((q, store[:T, 6:12]), (q, store[:T, 7:13]), (turned[:T], turned[T:])):
+        assert torch.equal(b.layer.run(x, out=out, **meta), want) and torch.equal(x, b.q)
+    both = torch.stack((b.q, torch.zeros_like(b.q)), dim=2).view(T, 12, 64)                      # every other head
+    assert torch.equal(b.layer.run(both[:, ::2], out=both[:, 1::2], **meta), want) and torch.equal(both[:, ::2], b.q)
+    assert b.layer.status() == 0
