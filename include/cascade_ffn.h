@@ -343,7 +343,8 @@ typedef struct {
  *   positions     [device] int32 [T]
  *   slots         [device] int64 [T] page * page_size + position in the page; -1: k and v of the token are not written
  *   inv_freq      [device] fp32 [R/2]
- *   q_out         [device] out bf16 [T, n_heads, D]; may be q itself
+ *   q_out         [device] out bf16 [T, n_heads, D]; may be q itself, but not overlap k, v or a part of q (in one buffer with them it has
+ *                 their token stride)
  *   k_cache, v_cache  [device] bf16 or e4m3 [n_pages, page_size, n_kv_heads, D]; nothing but the slots is written
  *   k_scale, v_scale  [device] fp32 [n_kv_heads] or NULL (all ones): codes are x / scale, to nearest even, saturating
  *                 (CEP_ELEM_E4M3 only)

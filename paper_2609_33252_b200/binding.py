@@ -425,7 +425,7 @@ def attn_append(k, v, positions, slots, inv_freq, k_cache, v_cache, q=None, q_ou
     k, v bf16 [T,Hkv,D]; q bf16 [T,Hq,D] or None; positions int32 [T]; slots int64 [T] (-1: not written); inv_freq fp32 [R/2];
     k_cache, v_cache bf16 or float8_e4m3fn [pages, page_size, Hkv, D], any strides with contiguous heads; k_scale, v_scale fp32 [Hkv]
     (e4m3); status int32 [1], set to 1 where a slot lies outside the cache.  Returns the rotated q in q_out (allocated if not given;
-    may be q).  Tensors are recorded on a `stream` that is given."""
+    may be q, but not overlap k, v or a part of q).  Tensors are recorded on a `stream` that is given."""
     torch = _torch_module or _torch()
     dev = torch._C._cuda_getDevice()
     bf16 = torch.bfloat16

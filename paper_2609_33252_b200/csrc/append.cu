@@ -272,6 +272,13 @@ extern "C" int attn_append(const cep_append_desc* d, const void* q, const void* 
       if (s.n[i] > 1) { strides = strides && s.st[i] >= D; wide = wide && s.st[i] * s.bytes % s.vec == 0; }    // (of a single element it means nothing)
   }
   if (!strides) return record_error(CEP_ERR_ARG, "append: a stride is smaller than head_dim");
+  // a rotated head is written by the thread that has read it, others may be read later
+  const HeadRows q_new = head_rows(q_out, T, d->n_heads, d->q_out_token_stride, d->q_out_head_stride, D);
+  const bool in_place = q == q_out && (T == 1 || d->q_token_stride == d->q_out_token_stride) && (d->n_heads == 1 || d->q_head_stride == d->q_out_head_stride);
+  if ((!in_place && rows_meet(head_rows(q, T, d->n_heads, d->q_token_stride, d->q_head_stride, D), q_new)) ||
+      rows_meet(head_rows(k, T, d->n_kv_heads, d->k_token_stride, d->k_head_stride, D), q_new) ||
+      rows_meet(head_rows(v, T, d->n_kv_heads, d->v_token_stride, d->v_head_stride, D), q_new))
+    return record_error(CEP_ERR_ARG, "append: q_out overlaps k, v or a part of q");
   if (!aligned || !on(positions, 4) || !on(slots, 8) || !on(inv_freq, 4) || !on(k_scale, 4) || !on(v_scale, 4) || !on(status, 4))
     return record_error(CEP_ERR_ARG, "append: a pointer is not aligned to its element type");
   AppendArgs a{};
