@@ -420,7 +420,7 @@ CEP_API int attn_plan(const cep_attn_config* cfg, const void* k_cache, const voi
  * A token that sees no key gets zeros and -infinity.  What lies behind the last key in a page is not looked at, and may be
  * anything; a key or value that is not finite reaches the tokens that see it and, where one of these belongs to the same
  * sequence and call, may reach the sequence's earlier tokens of the call.  fp32 from the products on; weights enter the product with V as bf16
- * (fp16 with an e4m3 cache), out is rounded once.  Results do not depend on timing.  All lengths are read on the device: a captured call replays with
+ * (with an e4m3 cache as fp16, where a weight below 2^-21 of a row's largest may be off by 2^-32 of that), out is rounded once.  Results do not depend on timing.  All lengths are read on the device: a captured call replays with
  * other lengths (within n_tokens, n_seqs).  What does not fit is cut to what does and reported by attn_status.
  * Enqueued on `stream`.
  */

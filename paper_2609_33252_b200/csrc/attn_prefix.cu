@@ -278,6 +278,12 @@ struct alignas(16) Work {
 static_assert(sizeof(Work) == 64, "");
 enum { kDual = 1, kWhole = 2 };
 
+// Weights are fp32 in the sums and enter the product with V in the 16 bits that its operands have: bf16 with V's own bf16 (2^-8 of a weight at most;
+// its exponents are fp32's), fp16 with decoded codes (2^-11).  fp16 ends at 2^-24, which a row with one strong key reaches, so its weights
+// are all multiplied by 2^kLift: with maxima that lag by 2^8 at most they stay below 2^15, and those from 2^-21 of the
+// largest on keep all of their bits, from 2^-32 on some.  (Without: 2^-14 and 2^-25.)
+constexpr float kLift = 7.f;
+
 // The CTA's key tiles are numbered through, t = 0, 1, ...  Places in the ring, in the order in which the tensor core needs them:
 // K0 K1 V0 K2 V1 K3 V2 ...
 __device__ __forceinline__ uint32_t pos_k(uint32_t t) { return t ? 2 * t - 1 : 0; }
@@ -300,6 +306,7 @@ __device__ __forceinline__ f32x2 fma2_here(f32x2 a, f32x2 b, f32x2 c) { f32x2 r;
 __device__ __forceinline__ f32x2 add2_here(f32x2 a, f32x2 b) { f32x2 r; asm volatile("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ uint32_t pack_bf16_here(float lo, float hi) { uint32_t r; asm volatile("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { uint32_t r; asm volatile("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
+__device__ __forceinline__ uint32_t pack_f16_finite(float lo, float hi) { uint32_t r; asm volatile("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo)); return r; }
 
 __device__ __forceinline__ float max3_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
@@ -782,7 +789,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
       ++o_phase;
       tc_fence_after();
       if (r.active) {
-        const float m2 = m == -CUDART_INF_F ? m : m * r.sl2;
+        const float m2 = m == -CUDART_INF_F ? m : E4M3 ? m * r.sl2 - kLift : m * r.sl2;
         const float inv = l > 0.f ? (a.v_scale ? a.v_scale[r.kvh] : 1.f) / l : l;        // (a NaN stays)
         // (A row per lane: 32 lines with every access, 4 us for two full row tiles; the other warpgroup works meanwhile.)
         if (r.whole) {
@@ -909,7 +916,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
             }
             any = true;
             // no key seen yet: all weights 0; an infinite score: NaN
-            const float shift = m == -CUDART_INF_F ? 0.f : m == CUDART_INF_F ? CUDART_NAN_F : -m * r.sl2;
+            const float shift = m == -CUDART_INF_F ? 0.f : m == CUDART_INF_F ? CUDART_NAN_F : E4M3 ? kLift - m * r.sl2 : -m * r.sl2;
             const f32x2 scale2 = pair2(r.sl2, r.sl2), shift2 = pair2(shift, shift);
             f32x2 sum[4] = {0, 0, 0, 0};
             // The unit for exponentials takes 8 cycles a warp for each: what comes before and after them is put between them (a
@@ -936,7 +943,7 @@ attn_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensor
               if (i >= kBehind) {
                 const int k = i - kBehind;
                 const float p0 = __uint_as_float(x[k >> 4][2 * k & 31]), p1 = __uint_as_float(x[k >> 4][(2 * k & 31) + 1]);
-                w[k >> 4][k & 15] = E4M3 ? pack_f16(p0, p1) : pack_bf16_here(p0, p1);
+                w[k >> 4][k & 15] = E4M3 ? pack_f16_finite(p0, p1) : pack_bf16_here(p0, p1);
                 sum[k & 3] = add2_here(sum[k & 3], pair2(p0, p1));
                 if (k == 15) tc_st16(t_s + h * 64, w[0]);
               }
