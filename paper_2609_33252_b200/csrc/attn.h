@@ -101,8 +101,10 @@ __host__ __device__ inline bool attn_is_short(const AttnShape& p, const AttnSche
 // Sequences of up to two row tiles have partial rows of their own; longer ones use those of the CTAs whose cut goes through them.
 __host__ __device__ inline bool attn_has_rows(const AttnShape& p, const AttnSched& s, int b) { return s.q0[b + 1] - s.q0[b] <= 2 * p.tps; }
 
-// An entity's items per kv head, and what item r (0-based) of them costs: a + slope * (r + 1).
-struct AttnEntity { int items, a, slope; };
+// An entity's items per kv head, and what the first r of them cost: r a + (slope r (r + 1) / 2 >> shift), as item r sees slope more than the one before.
+// (The slope is not shifted by itself: with few tokens per row tile, and a shift for wide page tables, nothing would be left of it, and the last
+// items of a long prompt would count as much as the first.)
+struct AttnEntity { int items, a, slope, shift; };
 __host__ __device__ inline AttnEntity attn_entity(const AttnShape& p, const AttnSched& s, int e) {
   int n, keys, slope = 0;
   bool some = true;
@@ -124,10 +126,12 @@ __host__ __device__ inline AttnEntity attn_entity(const AttnShape& p, const Attn
   AttnEntity x;
   x.items = some ? attn_tiles(p, n) : 0;
   x.a = (int)((fixed + (long long)unit * (keys >> 2)) >> p.cost_shift) + 1;
-  x.slope = slope ? unit * 2 * p.tps >> (2 + p.cost_shift) : 0;
+  x.slope = slope ? unit * 2 * p.tps >> 2 : 0;
+  x.shift = p.cost_shift;
   return x;
 }
-__host__ __device__ inline int attn_items_cost(const AttnEntity& x, int r) { return r * x.a + (x.slope ? x.slope * (int)(((long long)r * (r + 1)) >> 1) : 0); }
+__host__ __device__ inline int attn_items_cost(const AttnEntity& x, int r) { return r * x.a + (x.slope ? (int)(x.slope * ((long long)r * (r + 1) >> 1) >> x.shift) : 0); }
+__host__ __device__ inline int attn_item_cost(const AttnEntity& x, int r) { return x.slope ? attn_items_cost(x, r + 1) - attn_items_cost(x, r) : x.a; }
 
 // Where a CTA's walk over its items stands.
 struct AttnWalk {
@@ -149,15 +153,15 @@ __host__ __device__ inline AttnWalk attn_walk_in(const AttnShape& p, const AttnS
   if (k.x.slope == 0) {
     r = attn_div(rest, k.x.a);
   } else {                                   // the root of slope r^2 / 2 + (a + slope / 2) r = rest, put right by the sums themselves
-    const float h = (float)k.x.a / (float)k.x.slope + 0.5f;
-    r = (int)(sqrtf(h * h + 2.f * (float)rest / (float)k.x.slope) - h);
+    const float slope = (float)k.x.slope / (float)(1u << k.x.shift), h = (float)k.x.a / slope + 0.5f, x2 = 2.f * (float)rest / slope;
+    r = (int)(x2 / (sqrtf(h * h + x2) + h));
     if (r > k.x.items - 1) r = k.x.items - 1;
     while (r > 0 && attn_items_cost(k.x, r) > rest) --r;
     while (attn_items_cost(k.x, r + 1) <= rest) ++r;
   }
   k.r = r;
   k.at = x - (rest - attn_items_cost(k.x, r));
-  k.w = k.x.a + k.x.slope * (r + 1);
+  k.w = attn_item_cost(k.x, r);
   return k;
 }
 __host__ __device__ inline AttnWalk attn_walk_at(const AttnShape& p, const AttnSched& s, int x) {
@@ -183,7 +187,7 @@ __host__ __device__ inline void attn_walk_next(const AttnShape& p, const AttnSch
       k->x = attn_entity(p, s, k->e);
     }
   }
-  k->w = k->x.a + k->x.slope * (k->r + 1);
+  k->w = attn_item_cost(k->x, k->r);
 }
 
 enum AttnKind { kAttnGroup = 0, kAttnOwn = 1, kAttnJoint = 2 };
