@@ -94,13 +94,13 @@ class AttentionBlock:
     """From a layer's normed input to its attention output (what ``MoEBlock`` takes), over the layer's paged cache.
 
     w_qkv bf16 [(Hq + 2 Hkv) D, H]: rows of all query heads, then the key heads, then the value heads; k_cache, v_cache
-    [pages, page_size, Hkv, D] bf16 or float8_e4m3fn (with k_scale, v_scale fp32 [Hkv]); inv_freq fp32 [R/2].  All are the caller's
-    tensors.  ``run`` may be called on different streams: each call waits for the one before, as the buffers between the
+    [pages, page_size, Hkv, D] bf16 or float8_e4m3fn (with k_scale, v_scale fp32 [Hkv]); inv_freq fp32 [R/2]; scale of the scores, 1/sqrt(D)
+    by default.  All are the caller's tensors.  ``run`` may be called on different streams: each call waits for the one before, as the buffers between the
     steps are shared (who runs ``steps`` orders them, and who captures ``run`` into a graph its replays).
     """
 
     def __init__(self, w_qkv, k_cache, v_cache, n_heads, inv_freq, max_tokens, max_seqs, max_prefixes=1, k_scale=None, v_scale=None, interleaved=False,
-                 max_adapters=0, max_rank=0):
+                 max_adapters=0, max_rank=0, scale=None):
         Hk, D = k_cache.shape[2:]
         self.heads = (n_heads, Hk, D)
         if w_qkv.shape[0] != (n_heads + 2 * Hk) * D:
@@ -108,7 +108,7 @@ class AttentionBlock:
         self.inv_freq, self.interleaved = inv_freq, interleaved
         self.bad_slots = torch.zeros(1, dtype=torch.int32, device=w_qkv.device)      # set by the write into the cache
         self.projection = cep.LoRAProjection(w_qkv, max_tokens, max_adapters, max_rank)
-        self.attention = cep.PrefixAttention(k_cache, v_cache, n_heads, max_tokens, max_seqs, max_prefixes, k_scale, v_scale)
+        self.attention = cep.PrefixAttention(k_cache, v_cache, n_heads, max_tokens, max_seqs, max_prefixes, k_scale, v_scale, scale)
         self.qkv = torch.empty(max_tokens, n_heads + 2 * Hk, D, dtype=torch.bfloat16, device=w_qkv.device)
         self.out = torch.empty(max_tokens, n_heads, D, dtype=torch.bfloat16, device=w_qkv.device)
         self.done = torch.cuda.Event()                       # the end of the last call

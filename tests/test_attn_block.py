@@ -102,3 +102,10 @@ def test_what_a_refused_call_of_the_expert_block_has_started_is_waited_for(fake)
     with pytest.raises(blocks.cep.CepError):
         block.run(torch.zeros(3, H), torch.zeros(3, H))
     assert fake.log == ["wait", "first", "done"]
+
+
+@pytest.mark.parametrize("kw,want", [({}, None), (dict(scale=0.03), 0.03)])
+def test_the_scale_of_the_scores_reaches_the_attention(fake, kw, want):
+    make(**kw)
+    (name, args, options), = [m for m in fake.made if m[0] == "attention"]
+    assert options == {} and args[8] == want                         # k_cache, v_cache, heads, tokens, seqs, prefixes, two scales, scale

@@ -65,3 +65,21 @@ def test_an_output_that_overlaps_the_queries_is_refused():
     both = torch.stack((b.q, torch.zeros_like(b.q)), dim=2).view(T, 12, 64)                      # every other head
     assert torch.equal(b.layer.run(both[:, ::2], out=both[:, 1::2], **meta), want) and torch.equal(both[:, ::2], b.q)
     assert b.layer.status() == 0
+
+
+def test_a_block_with_a_scale_of_its_own():
+    D = 64
+    kv = [torch.zeros(4, 16, 2, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    w, inv_freq = rand((10 * D, 128), 1, 128 ** -0.5), torch.rand(D // 2, device="cuda")
+    x, positions, slots = rand((4, 128), 2), i32([0, 1, 2, 3]), torch.arange(4, device="cuda")
+    batch = dict(q_start=i32([0, 4]), kv_len=i32([4]), page_table=i32([[0]]))
+    outs = []
+    for kw in ({}, dict(scale=D ** -0.5), dict(scale=0.7)):
+        att = AttentionBlock(w, *kv, 6, inv_freq, 8, 1, **kw)
+        outs.append(att.run(x, positions, slots, batch).clone())
+        layer = cep.PrefixAttention(*kv, 6, 8, 1, **kw)
+        assert torch.equal(layer.run(att.qkv[:4, :6], **batch).view(4, -1), outs[-1])
+        assert att.status() == 0 and layer.status() == 0
+        att.close()
+        layer.close()
+    assert torch.equal(outs[0], outs[1]) and not torch.equal(outs[0], outs[2])
