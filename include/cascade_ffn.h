@@ -273,7 +273,7 @@ typedef struct cep_lora_plan cep_lora_plan;
 typedef struct {
   int32_t in_features;         /* K; multiple of 8                                              */
   int32_t out_features;        /* N >= 1                                                        */
-  int32_t max_tokens;          /* upper bound on tokens per call, 1..2^22; times n_heads below 2^31 */
+  int32_t max_tokens;          /* upper bound on tokens per call                                */
   int32_t max_adapters;        /* slots of the adapter bank, 0..4096; 0: no adapters            */
   int32_t max_rank;            /* largest rank, 1..256; 0 without adapters                      */
   int32_t out_elem;            /* cep_elem of y                                                 */
@@ -373,7 +373,7 @@ typedef struct {
   int32_t page_size;           /* 16, 32, 64, 128 or 256                                        */
   int32_t n_pages;
   int32_t cache_elem;          /* CEP_ELEM_BF16 or CEP_ELEM_E4M3                                */
-  int32_t max_tokens;          /* upper bound on tokens per call                                */
+  int32_t max_tokens;          /* upper bound on tokens per call, 1..2^22; times n_heads below 2^31 */
   int32_t max_seqs;            /* on sequences, 1..1024                                         */
   int32_t max_prefixes;        /* on groups, 0..256                                             */
   float scale;                 /* > 0                                                           */
@@ -391,14 +391,21 @@ typedef struct {
   int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride, lse_token_stride;
 } cep_attn_batch;
 
-/* Bytes of device workspace.  [host] out. */
+/*
+ * Bytes of device workspace.  [host] out.  Nearly all of it is room for partial results, 4 D' + 8 bytes a row (D' = 64 or 128):
+ *   2 m n_heads + n_kv_heads (m / 2t + max_prefixes) 2t g + 149 * 512 rows,   g = n_heads / n_kv_heads, t = 128 / g (rounded down),
+ *   m = min(max_tokens, 2 t max_seqs), the tokens of sequences of up to 2 t tokens; longer ones need none of their own
+ * 56 heads, 8 kv heads of 128: 66 MB for 256 tokens of 256 sequences, 759 MB for 8192 of 256, 1475 MB for 16384 of 512, 119 MB for
+ * 16384 of 24.
+ */
 CEP_API int attn_plan_workspace_bytes(const cep_attn_config* cfg, size_t* bytes);
 
 /*
  * `k_cache`, `v_cache` [device] [n_pages, page_size, n_kv_heads, D], 16-byte aligned; `k_scale`, `v_scale` [device] fp32
  * [n_kv_heads], positive, or NULL (all ones): a key is its stored value times its head's scale.  `workspace` [device], 256-byte
- * aligned.  All stay owned by the caller and must outlive the plan.  Must be called with the target device current (memory of
- * another device is refused); clears the status word on `stream`, which may not be under capture (CEP_ERR_STATE).  A plan is
+ * aligned, this plan's alone (its status word lies in it).  All stay owned by the caller and must outlive the plan.  Must be called with the
+ * target device current (memory of another device is refused); clears the status word on `stream`, which may not be under capture
+ * (CEP_ERR_STATE).  A plan is
  * not thread-safe.  Its calls may go to different streams: each waits for the plan's previous work (inside a stream capture
  * the caller orders; graphs of one plan share its workspace and may not run at the same time).
  */

@@ -3,8 +3,10 @@
 // Per token: sines and cosines of R/2 angles, shared by all heads, then (n_heads + 2 n_kv_heads) heads that are read once and
 // written once; memory is the bound.  A thread has the same parts of a token's heads for every token that its block comes to, so
 // that all divisions are done once; it asks for them before the angles are computed, which then cost no time of their own.
-// 16384 tokens of 56 + 2 x 8 heads of 128 (604 MB): 121 us, 5.0 TB/s (151 us with the parts found anew for each token; 168 us
-// with heads brought to shared memory by bulk copies first).
+// 16384 tokens of 56 + 2 x 8 heads of 128 (604 MB): 135 us, 4.5 TB/s (151 us with the parts found anew for each token, which is better
+// for 1531 tokens of 36 heads of 80: 6.1 against 7.6 us).  Few warps bound it: 107 to 111 registers let an SM hold two blocks, 12 to 16 warps,
+// which spend a third of their time at the barrier behind the angles.
+// Heads that cannot be taken 16 bytes at a time go element by element: the same 16384 tokens 550 us.
 //
 // Angles: position * inv_freq reaches 10^6 and more, where fp32 has lost the turn's fraction.  The product with 1/(2 pi) is
 // taken in fp64 (4 instructions a pair, B200 has them at half rate), the whole turns are dropped, and the rest, below half a
@@ -18,7 +20,9 @@
 namespace cep {
 namespace {
 
-constexpr int kAppendPerSm = 1024;            // threads, of blocks that come to tokens again (768: 11.1 us where 1536 take 12.4, but 39.5 against 35.5 with small heads)
+// Threads per SM that the blocks which come to tokens again are counted for (768: 11.1 us where 1536 take 12.4, but 39.5 against 35.5 with small
+// heads).  Registers let about 576 run at a time: the rest of the blocks start when the first have ended.
+constexpr int kAppendPerSm = 1024;
 constexpr int kAppendMaxThreads = 512, kAppendMaxDim = 1024;
 
 struct AppendArgs {
@@ -298,7 +302,7 @@ extern "C" int attn_append(const cep_append_desc* d, const void* q, const void* 
   const int per_token = (a.Hq + 2 * a.Hk) * a.units, unroll = unroll_of(V);
   auto warps = [](int n) { return (n + 31) / 32 * 32; };
   // Few tokens: a token's heads are shared by blocks whose threads have a part each.  Many: as many tokens at a time as give 256 threads
-  // their parts, and blocks that come to tokens again and again, up to what the device holds.
+  // their parts, and blocks that come to tokens again and again, up to kAppendPerSm threads an SM.
   int threads;
   a.tokens = 1; a.parts = 1;
   if (a.T < 2 * 148) {

@@ -25,8 +25,12 @@ constexpr int kAttnMaxSeqs = 1024, kAttnMaxPrefixes = 256;
 constexpr int kAttnMaxCtas = 148;
 constexpr int kAttnSplitRows = 2 * 2 * kAttnTile;                      // partial rows that a CTA's two cut items may need
 // Estimated cost of four keys for one row tile (taken by the warpgroups in turn) and for two, and of an item beside its keys; a unit is 5 ns.
-// Measured, with both kinds at once (256 tokens over 32768 shared and 2000 own keys at most): 1.4 us for 128 keys of one, 2.2 us of two.  8 and 600 for
-// one, 16 and 1600 for two, which fit them alone, take 652 us there where these take 612.
+// So 128 keys count 1.44 us for one and 2.56 for two, an item 2.8 and 6 us beside them.  8 and 600 for one, 16 and 1600 for two fit each kind alone;
+// what counts is the ratio of both kinds where they run side by side.  These, those, and these with 14 in the place of 16, us:
+//   256 tokens over 32768 shared, up to 4096 own keys   707   760   749      4096 tokens, prompts and decoding over 8192 shared  1284  1340  1320
+//    64 over 8192, up to 2000                            80    81    85      the same over 2048, 16 heads, 4 kv heads             142   141   138
+//    96 over 16384, up to 1000                          129   124   124      256 over 4096, up to 512                             141   142   143
+//   128 over 5000, up to 1500, e4m3                     160   154   164      48 x 1..8 over 8192, up to 2000                       64    64    65
 constexpr int kAttnCostSingle = 9, kAttnCostDual = 16, kAttnItemSingle = 560, kAttnItemDual = 1200;
 
 struct AttnShape {
